@@ -380,6 +380,53 @@ int lemo_scatter_grad(const void* G, int64_t ldg, const int32_t* kept_idx, int64
                       int64_t lddx, int64_t S, int32_t C, lemo_dtype_t g_dt, lemo_dtype_t dx_dt,
                       int32_t mode, void* stream);
 
+/*
+ * What stands between two blocks of a layer, on the kept rows in place: the norm of a block's result, its gate, the scaled
+ * add into the residual stream (the in-place add of Sec. 4.4), and the norm that the next block reads:
+ *
+ *     u = post(Y[m])     R[kept_idx[m]] = residual_scale * R[kept_idx[m]] + block_scale * g_m * u     N[m] = next(R[kept_idx[m]])
+ *
+ *   post, next: LEMO_NORM_NONE   the row as it is (next: N is not written and may be NULL)
+ *               LEMO_NORM_RMS    x / sqrt(mean(x^2) + eps) * w + b
+ *               LEMO_NORM_LAYER  (x - mean) / sqrt(mean((x - mean)^2) + eps) * w + b
+ *   w_post, b_post, w_next, b_next  [C] of dtype dt, or NULL for ones / zeros; not read where their norm is NONE.
+ *   Y [M, C] row stride ldy, the block's result, or NULL: then R is only read, and next must be a norm (the norm before a
+ *     layer's first block).
+ *   gate [M, C] row stride ld_gate, or with ld_gate 0 one row [C] for all, or NULL for ones.  g is the gate's value, with
+ *     LEMO_GATE_SIGMOID its logistic function.
+ *   R [S, C] row stride ldr, read and written at the rows kept_idx names (NULL: rows 0..M-1).  Each row at most once (not
+ *     checked); other rows are not touched.  A value outside [0, S) drops the row: its N and stats are zeros.
+ *   N [M, C] row stride ldn.  The second norm is that of the row as it is stored, so that this call and a call with Y = NULL
+ *     behind it give the same bits.
+ *   stats [M, 4] float, 16-byte aligned, or NULL: mean and 1 / deviation of post, then of next (0 where a norm is NONE; the mean
+ *     is 0 for RMS); what the gradient takes.
+ *
+ * lemo_norm_residual_grad: from dN = the gradient of N and dR = that of the new residual rows, in place,
+ *     dr = dR[kept_idx[m]] + next'(dN[m])      dR[kept_idx[m]] = residual_scale * dr
+ *     dgate = block_scale * u * dr (times the slope of the logistic function)       dY = post'(block_scale * g * dr)
+ *     dw_*, db_* [C] float: gradients of weights and biases, sums over the rows;  dgate_sum [C] float: sum of dgate over the
+ *     rows, the gradient of a shared gate (ld_gate 0; then dgate must be NULL).
+ *   R, Y, gate, stats: as the forward call left or took them.  Every result but dR may be NULL.  dN and R are not read where next
+ *   is NONE.  M == 0 writes zeros to the sums.  dY [M, C] and dgate [M, C] are zeros for dropped rows.
+ *   workspace: lemo_norm_residual_grad_workspace_bytes(M, C) bytes, 256-byte aligned; not needed if none of the sums is asked for.
+ *
+ * binary32 arithmetic; one rounding at every store; no atomics: the same bits on every run.  N may be Y, dY may be dN, dgate may be
+ * gate (same base and row stride); otherwise results overlap neither operands nor each other.
+ * Supported: C % 8 == 0 (bf16) / % 4 (fp32), C <= 16384; operands, weights and strides follow the 16-byte rule.
+ */
+enum { LEMO_NORM_NONE = 0, LEMO_NORM_RMS = 1, LEMO_NORM_LAYER = 2 };
+enum { LEMO_GATE_SIGMOID = 1u };
+int lemo_norm_residual(const void* Y, int64_t ldy, const void* gate, int64_t ld_gate, void* R, int64_t ldr, int64_t S, const int32_t* kept_idx,
+                       int64_t M, const void* w_post, const void* b_post, int32_t post, const void* w_next, const void* b_next, int32_t next,
+                       float eps, float residual_scale, float block_scale, void* N, int64_t ldn, float* stats, int32_t C, lemo_dtype_t dt,
+                       uint32_t flags, void* stream);
+int lemo_norm_residual_grad_workspace_bytes(int64_t M, int32_t C, size_t* bytes);
+int lemo_norm_residual_grad(const void* dN, int64_t lddn, void* dR, int64_t lddr, int64_t S, const void* R, int64_t ldr, const void* Y, int64_t ldy,
+                            const void* gate, int64_t ld_gate, const int32_t* kept_idx, int64_t M, const void* w_post, const void* b_post,
+                            int32_t post, const void* w_next, int32_t next, float residual_scale, float block_scale, const float* stats, void* dY,
+                            int64_t lddy, void* dgate, int64_t ld_dgate, float* dw_post, float* db_post, float* dw_next, float* db_next,
+                            float* dgate_sum, int32_t C, lemo_dtype_t dt, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

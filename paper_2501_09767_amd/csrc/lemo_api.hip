@@ -2,6 +2,7 @@
 #include <cmath>
 #include <mutex>
 
+#include "api_checks.hpp"
 #include "lemo_common.hpp"
 
 using namespace lemo;
@@ -16,11 +17,6 @@ constexpr long long LEMO_STATIC_MAX_HS = 1ll << 20;
 static __device__ __align__(256) unsigned char scratch[3 * LEMO_STATIC_MAX_HS * sizeof(float)];
 
 namespace {
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline bool valid_dtype(int dt) { return dt == LEMO_F32 || dt == LEMO_BF16; }
-inline int elems_per_16B(int dt) { return dt == LEMO_BF16 ? 8 : 4; }
-inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // device address of the current device's copy of `scratch`, looked up once per device
 constexpr int MAX_DEVICES = 64;
@@ -119,8 +115,6 @@ static int check_qk(const void* Q, const void* K, int64_t S, int32_t H, int32_t 
     p.flags = flags;
     return LEMO_OK;
 }
-
-static inline int hip_rc(int e) { return e == 0 ? LEMO_OK : LEMO_ERR_HIP; }
 
 int lemo_score_rowstats(const void* Q, const void* K, int64_t S, int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt,
                         int64_t q_tok_stride, int64_t q_head_stride, int64_t k_tok_stride, int64_t k_head_stride,

@@ -13,7 +13,7 @@ import importlib.machinery
 import importlib.util
 import os
 import warnings
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -30,7 +30,8 @@ EXPORTS = ("lemo_strerror", "lemo_keep_k", "lemo_kept_count", "lemo_score_worksp
            "lemo_select_topk", "lemo_head_mean_select_topk", "lemo_launch_floor", "lemo_probe_sweep_issue_mix", "lemo_gather_gemm", "lemo_gather_gemm_add", "lemo_scatter_grad",
            "lemo_score_blocks_workspace_bytes", "lemo_score_blocks", "lemo_threshold_init", "lemo_select_threshold",
            "lemo_kept_attention_workspace_bytes", "lemo_kept_attention",
-           "lemo_gather_gemm_dw_workspace_bytes", "lemo_gather_gemm_dw", "lemo_gather_gemm_dx")
+           "lemo_gather_gemm_dw_workspace_bytes", "lemo_gather_gemm_dw", "lemo_gather_gemm_dx",
+           "lemo_norm_residual", "lemo_norm_residual_grad_workspace_bytes", "lemo_norm_residual_grad")
 
 
 class LemoError(RuntimeError):
@@ -98,6 +99,14 @@ def _load() -> ctypes.CDLL:
     lib.lemo_gather_gemm_add.argtypes = [vp, i64, i64, vp, i64, vp, i64, vp, vp, i64, i64, vp, i32, i32, ctypes.c_int, vp]
     lib.lemo_scatter_grad.restype = ctypes.c_int
     lib.lemo_scatter_grad.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, ctypes.c_int, ctypes.c_int, i32, vp]
+    lib.lemo_norm_residual.restype = ctypes.c_int
+    lib.lemo_norm_residual.argtypes = [vp, i64, vp, i64, vp, i64, i64, vp, i64, vp, vp, i32, vp, vp, i32, f32, f32, f32, vp, i64, vp, i32, ctypes.c_int,
+                                       u32, vp]
+    lib.lemo_norm_residual_grad_workspace_bytes.restype = ctypes.c_int
+    lib.lemo_norm_residual_grad_workspace_bytes.argtypes = [i64, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.lemo_norm_residual_grad.restype = ctypes.c_int
+    lib.lemo_norm_residual_grad.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, i32, f32, f32, vp, vp, i64, vp, i64,
+                                            vp, vp, vp, vp, vp, i32, ctypes.c_int, u32, vp, ctypes.c_size_t, vp]
     return lib
 
 
@@ -596,3 +605,127 @@ def lemo_scatter_grad(G: torch.Tensor, kept_idx: torch.Tensor, dX: torch.Tensor,
     _check(_lib.lemo_scatter_grad(_ptr(G), G.stride(0) if M > 0 else C, _ptr(kept_idx), M, _ptr(dX), dX.stride(0),
                                   dX.shape[0], C, _dt(G), _dt(dX), int(mode), _stream()), "lemo_scatter_grad")
     return dX
+
+
+# --------------------------------------------------------------------------------- norms around a block
+
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+GATE_SIGMOID = 1
+
+
+class NormGrads(NamedTuple):
+    """What lemo_norm_residual_grad returns beside dR: None where there is nothing to take a gradient of."""
+    dY: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]      # [M,C], or [C] float32 for a gate that all rows share
+    dw_post: Optional[torch.Tensor]    # [C] float32, like the three below
+    db_post: Optional[torch.Tensor]
+    dw_next: Optional[torch.Tensor]
+    db_next: Optional[torch.Tensor]
+
+
+def _here(*ts):
+    """Tensors of a call: on the device that is current, whose stream the call goes to."""
+    _dev(*ts)
+    for t in ts:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError("tensors must live on the current device")
+
+
+def _index(t: Optional[torch.Tensor], M: int, name: str):
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (M,) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous int32 [M]")
+
+
+def _rows_of(t: Optional[torch.Tensor], M: int, C: int, dtype, name: str) -> int:
+    """Row stride of an [M,C] operand that may be missing."""
+    if t is None:
+        return C
+    if t.dim() != 2 or tuple(t.shape) != (M, C) or t.dtype != dtype or (t.stride(1) != 1 and C > 1 and M > 0):
+        raise ValueError(f"{name} must be [{M},{C}] of the residual's dtype, rows contiguous")
+    return t.stride(0) if M > 1 else C
+
+
+def _channels(t: Optional[torch.Tensor], C: int, dtype, name: str):
+    if t is not None and (tuple(t.shape) != (C,) or t.dtype != dtype or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous [{C}] of {dtype}")
+
+
+def _norm_args(Y, R, kept_idx, gate, w_post, b_post, w_next, b_next):
+    """Sizes and strides shared by the norm calls: M, S, C, ldy, ld_gate, ldr."""
+    if R.dim() != 2 or (R.stride(1) != 1 and R.shape[1] > 1):
+        raise ValueError("R must be [S,C], rows contiguous")
+    _dt(R)
+    S, C = R.shape
+    M = Y.shape[0] if Y is not None and Y.dim() == 2 else kept_idx.numel() if kept_idx is not None else S
+    _index(kept_idx, M, "kept_idx")
+    ld_gate = 0
+    if gate is not None and gate.dim() == 1:
+        _channels(gate, C, R.dtype, "gate")
+    else:
+        ld_gate = _rows_of(gate, M, C, R.dtype, "gate")
+    for name, t in (("w_post", w_post), ("b_post", b_post), ("w_next", w_next), ("b_next", b_next)):
+        _channels(t, C, R.dtype, name)
+    return M, S, C, _rows_of(Y, M, C, R.dtype, "Y"), ld_gate, R.stride(0) if S > 1 else C
+
+
+def lemo_norm_residual(Y: Optional[torch.Tensor], R: torch.Tensor, kept_idx: Optional[torch.Tensor] = None, *, gate: Optional[torch.Tensor] = None,
+                       post: int = NORM_NONE, next: int = NORM_RMS, w_post: Optional[torch.Tensor] = None, b_post: Optional[torch.Tensor] = None,
+                       w_next: Optional[torch.Tensor] = None, b_next: Optional[torch.Tensor] = None, eps: float = 1e-5, residual_scale: float = 1.0,
+                       block_scale: float = 1.0, flags: int = 0, N: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None):
+    """In place: R[kept_idx] = residual_scale * R[kept_idx] + block_scale * gate * post(Y) -> (N = next(R[kept_idx]) [M,C] or None,
+    stats [M,4] float32).  Y [M,C] or None, R [S,C], gate [M,C] or one row [C]."""
+    _here(Y, R, kept_idx, gate, w_post, b_post, w_next, b_next, N, stats)
+    M, S, C, ldy, ldg, ldr = _norm_args(Y, R, kept_idx, gate, w_post, b_post, w_next, b_next)
+    if N is None and next != NORM_NONE:
+        N = torch.empty((M, C), dtype=R.dtype, device=R.device)
+    ldn = _rows_of(N, M, C, R.dtype, "N")
+    if stats is None:
+        stats = torch.empty((M, 4), dtype=torch.float32, device=R.device)
+    elif stats.dtype != torch.float32 or tuple(stats.shape) != (M, 4) or not stats.is_contiguous():
+        raise ValueError("stats must be contiguous float32 [M,4]")
+    _check(_lib.lemo_norm_residual(_ptr(Y), ldy, _ptr(gate), ldg, _ptr(R), ldr, S, _ptr(kept_idx), M, _ptr(w_post), _ptr(b_post), int(post),
+                                   _ptr(w_next), _ptr(b_next), int(next), float(eps), float(residual_scale), float(block_scale), _ptr(N), ldn,
+                                   _ptr(stats), C, _dt(R), int(flags), _stream()), "lemo_norm_residual")
+    return N, stats
+
+
+def lemo_norm_residual_grad_workspace_bytes(M: int, C: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.lemo_norm_residual_grad_workspace_bytes(M, C, ctypes.byref(n)), "lemo_norm_residual_grad_workspace_bytes")
+    return int(n.value)
+
+
+def lemo_norm_residual_grad(dN: Optional[torch.Tensor], dR: torch.Tensor, R: torch.Tensor, Y: Optional[torch.Tensor], kept_idx: Optional[torch.Tensor],
+                            stats: torch.Tensor, *, gate: Optional[torch.Tensor] = None, post: int = NORM_NONE, next: int = NORM_RMS,
+                            w_post: Optional[torch.Tensor] = None, b_post: Optional[torch.Tensor] = None, w_next: Optional[torch.Tensor] = None,
+                            residual_scale: float = 1.0, block_scale: float = 1.0, flags: int = 0, workspace: Optional[torch.Tensor] = None) -> NormGrads:
+    """Gradients of lemo_norm_residual: dR [S,C] (of the new residual rows) becomes that of the old ones in place; returns the others.
+    R, Y, gate, stats as the forward call left or took them."""
+    _here(dN, dR, R, Y, kept_idx, stats, gate, w_post, b_post, w_next, workspace)
+    M, S, C, ldy, ldg, ldr = _norm_args(Y, R, kept_idx, gate, w_post, b_post, w_next, None)
+    if tuple(dR.shape) != (S, C) or dR.dtype != R.dtype or (dR.stride(1) != 1 and C > 1):
+        raise ValueError("dR must be [S,C] of the residual's dtype, rows contiguous")
+    if stats.dtype != torch.float32 or tuple(stats.shape) != (M, 4) or not stats.is_contiguous():
+        raise ValueError("stats must be contiguous float32 [M,4]")
+    lddn = _rows_of(dN, M, C, R.dtype, "dN")
+
+    def rows():
+        return torch.empty((M, C), dtype=R.dtype, device=R.device)
+
+    def sums(wanted):
+        return torch.empty(C, dtype=torch.float32, device=R.device) if wanted else None
+
+    shared = gate is not None and gate.dim() == 1
+    dY = rows() if Y is not None else None
+    dgate = rows() if gate is not None and not shared else None
+    dgate_sum = sums(shared)
+    dw_post, db_post = sums(post != NORM_NONE), sums(post != NORM_NONE and (b_post is not None or post == NORM_LAYER))
+    dw_next, db_next = sums(next != NORM_NONE), sums(next != NORM_NONE)
+    if workspace is None:
+        workspace = torch.empty(lemo_norm_residual_grad_workspace_bytes(M, C), dtype=torch.uint8, device=R.device)
+    _check(_lib.lemo_norm_residual_grad(_ptr(dN), lddn, _ptr(dR), dR.stride(0) if S > 1 else C, S, _ptr(R), ldr, _ptr(Y), ldy, _ptr(gate), ldg,
+                                        _ptr(kept_idx), M, _ptr(w_post), _ptr(b_post), int(post), _ptr(w_next), int(next), float(residual_scale),
+                                        float(block_scale), _ptr(stats), _ptr(dY), C, _ptr(dgate), C, _ptr(dw_post), _ptr(db_post), _ptr(dw_next),
+                                        _ptr(db_next), _ptr(dgate_sum), C, _dt(R), int(flags), _ptr(workspace),
+                                        workspace.numel() * workspace.element_size(), _stream()), "lemo_norm_residual_grad")
+    return NormGrads(dY, dgate_sum if shared else dgate, dw_post, db_post, dw_next, db_next)
