@@ -427,6 +427,74 @@ int lemo_norm_residual_grad(const void* dN, int64_t lddn, void* dR, int64_t lddr
                             int64_t lddy, void* dgate, int64_t ld_dgate, float* dw_post, float* db_post, float* dw_next, float* db_next,
                             float* dgate_sum, int32_t C, lemo_dtype_t dt, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Attention over key blocks that a cheap score selects for each query (the criterion of Sec. 4.2 taken block by block, with a list
+ * for every query in the place of one kept list).  Keys are cut into blocks of b tokens, nb = ceil(S_k / b), the last one may be
+ * shorter; queries into blocks of bq tokens, n_qb = ceil(S_q / bq), each with a list of key blocks for every KV head g = floor(h * H_kv /
+ * H) -- bq = 1 gives every query a list of its own.  Query i stands at position q_start + i, key j at position j.
+ *
+ *   lemo_block_means     means[n, g, :] = mean of K[j, g, :] over the keys of block n                  [nb, H_kv, d] float
+ *   lemo_select_blocks   s[m, g, n] = sum over the queries i of block m and the heads h of g of <Q[i, h], means[n, g]>;
+ *                        blocks[m, g, :] = the T blocks of highest s, ties to the LOWER index (-0.0 ties +0.0), in ascending
+ *                        order, -1 behind them.  LEMO_CAUSAL: blocks that begin behind the last query of m are left out, and those that
+ *                        hold a position of a query of m are always listed (LEMO_ERR_SHAPE if T has no room for them; their means
+ *                        are not read).  Sums and comparisons in 64 bits.  Scores that are not numbers give lists that are
+ *                        unspecified but in range.
+ *   lemo_block_attention O[i, h, :] = sum_j softmax_j( scale * <Q[i, h], K[j, g]> ) V[j, g, :] over the keys j of the blocks that
+ *                        i's list names (LEMO_CAUSAL: j <= q_start + i).  An entry of a list counts if it lies in [0, nb) and
+ *                        above every such entry before it; others are passed over, so that no key counts twice.  A query that
+ *                        sees no key gets zeros, and -infinity in lse2.
+ *   lemo_block_attention_grad   dQ, dK, dV of that from dO; O and lse2 as the forward call left them.
+ *
+ *   Q [S_q,H,d], K and V [S_k,H_kv,d], O and dO [S_q,H,d]: element strides, d contiguous, 16-byte rule, token strides below 2^22
+ *   elements.  blocks [n_qb, H_kv, T] int32.  scale <= 0 selects 1/sqrt(d).  lse2 [H, S_q] float, base-2 logarithm of the sum
+ *   of a query's exponentials, or NULL (forward).  dQ [S_q,H,d], dK and dV [S_k,H_kv,d] contiguous, written in full: keys that no
+ *   list names get zeros.
+ *   workspace: lemo_block_attention_workspace_bytes() (may be 0: then NULL will do), lemo_block_attention_grad_workspace_bytes()
+ *   bytes, 256-byte aligned.
+ *
+ * Single tokens of a batch of B sequences, each with its keys and values in a cache of S_max tokens (sequence stride, 64-bit) and its
+ * length on the device: the newest token, position lengths[s] - 1, attends its list.  Lengths outside [0, S_max] are taken as the
+ * nearer end; a sequence of length 0 gets an empty list and zeros.  What lies in the cache behind a sequence is not used.
+ *   lemo_block_means_step       means [B, ceil(S_max / b), H_kv, d]: writes the mean of the block that the newest token has filled, if
+ *                               lengths[s] is a multiple of b; a block's mean is there when a later token first scores it
+ *   lemo_select_blocks_step     Q [B,H,d] -> blocks [B, H_kv, T], as with LEMO_CAUSAL
+ *   lemo_block_attention_step   O [B,H,d]
+ *
+ * Probabilities (and in the gradient dS) are rounded to bf16 for the products that follow; sums in binary32; one rounding at the store.
+ * dK and dV sum over the heads of a group before they are rounded.  No atomics on results: the same bits on every run.  Values that are
+ * not finite in K or V at a key behind a query spoil the query's result only if the key lies in the same 32 keys (counted from its
+ * block's start) as one that the query, or one of the 31 rows beside it, sees.
+ * Supported: d in {64, 128}; b % 32 == 0; H % H_kv == 0; T * b <= 131072; S_q, S_k below 2^31 - 4096; the choice and the gradient:
+ * nb <= 16384; means and choice LEMO_F32 and LEMO_BF16, attention LEMO_BF16; the gradient: Q and dO each spanning less than 4 GiB - 4096.
+ * Results overlap neither operands nor each other.
+ */
+int lemo_block_means(const void* K, int64_t S, int32_t H_kv, int32_t d, lemo_dtype_t dt, int64_t k_tok_stride, int64_t k_head_stride, int32_t b, float* means,
+                     void* stream);
+int lemo_select_blocks(const void* Q, int64_t S_q, int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt, int64_t q_tok_stride, int64_t q_head_stride,
+                       const float* means, int64_t S_k, int64_t q_start, int32_t b, int32_t bq, int32_t T, uint32_t flags, int32_t* blocks, void* stream);
+int lemo_block_attention_workspace_bytes(int64_t S_q, int32_t H, int32_t H_kv, int32_t d, int32_t T, int32_t b, int32_t bq, size_t* bytes);
+int lemo_block_attention(const void* Q, const void* K, const void* V, int64_t S_q, int64_t S_k, int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt,
+                         int64_t q_tok_stride, int64_t q_head_stride, int64_t k_tok_stride, int64_t k_head_stride, int64_t v_tok_stride,
+                         int64_t v_head_stride, const int32_t* blocks, int32_t T, int32_t b, int32_t bq, int64_t q_start, float scale, uint32_t flags,
+                         void* O, int64_t o_tok_stride, int64_t o_head_stride, float* lse2, void* workspace, size_t workspace_bytes, void* stream);
+int lemo_block_attention_grad_workspace_bytes(int64_t S_q, int64_t S_k, int32_t H, int32_t H_kv, int32_t d, int32_t T, int32_t b, int32_t bq, size_t* bytes);
+int lemo_block_attention_grad(const void* dO, const void* Q, const void* K, const void* V, const void* O, const float* lse2, int64_t S_q, int64_t S_k,
+                              int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt, int64_t do_tok_stride, int64_t do_head_stride, int64_t q_tok_stride,
+                              int64_t q_head_stride, int64_t k_tok_stride, int64_t k_head_stride, int64_t v_tok_stride, int64_t v_head_stride,
+                              int64_t o_tok_stride, int64_t o_head_stride, const int32_t* blocks, int32_t T, int32_t b, int32_t bq, int64_t q_start,
+                              float scale, uint32_t flags, void* dQ, void* dK, void* dV, void* workspace, size_t workspace_bytes, void* stream);
+int lemo_block_means_step(const void* K, int32_t B, int64_t S_max, int32_t H_kv, int32_t d, lemo_dtype_t dt, int64_t k_seq_stride, int64_t k_tok_stride,
+                          int64_t k_head_stride, const int32_t* lengths, int32_t b, float* means, void* stream);
+int lemo_select_blocks_step(const void* Q, int32_t B, int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt, int64_t q_tok_stride, int64_t q_head_stride,
+                            const float* means, int64_t S_max, const int32_t* lengths, int32_t b, int32_t T, int32_t* blocks, void* stream);
+int lemo_block_attention_step_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t d, int32_t T, int32_t b, size_t* bytes);
+int lemo_block_attention_step(const void* Q, const void* K, const void* V, int32_t B, int64_t S_max, int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt,
+                              int64_t q_tok_stride, int64_t q_head_stride, int64_t k_seq_stride, int64_t k_tok_stride, int64_t k_head_stride,
+                              int64_t v_seq_stride, int64_t v_tok_stride, int64_t v_head_stride, const int32_t* lengths, const int32_t* blocks, int32_t T,
+                              int32_t b, float scale, void* O, int64_t o_tok_stride, int64_t o_head_stride, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,146 @@
+// Attention over listed key blocks: parameter blocks, the launchers, and what the forward and the gradient kernels share.
+#pragma once
+#include "lemo_common.hpp"
+
+namespace lemo {
+
+// A list names key blocks for the rows of one query block: R = bq * G rows of the G query heads that read one key head, row r being
+// query r / G of the block in head r % G of the group.  Work on a list is cut into tiles of rows; keys come in subtiles of 32.
+struct BlockAttnParams {
+    const uint16_t *Q, *K, *V;
+    uint16_t* O;
+    float* lse2;         // [H, S_q] or null
+    const int* blocks;   // [n_qb, H_kv, T]
+    const int* lengths;  // single tokens: [n_qb] keys of every sequence, or null
+    float* parts;        // where a list is shared by several workgroups: their results, see PART_ROW
+    int S_q, S_k, H, H_kv, G, T, b, bq, n_qb;
+    int R, n_rt, n_parts;  // rows of a query block, tiles of them, shares of a list
+    long long q_start;
+    long long q_ts, q_hs, k_ts, k_hs, k_ss, v_ts, v_hs, v_ss, o_ts, o_hs;  // element strides: token, head, sequence
+    float c2;
+    unsigned flags;
+    HeadOrder order;
+};
+
+struct BlockGradParams {
+    BlockAttnParams a;   // (O: the forward result, read only; lse2: likewise)
+    const uint16_t* dO;
+    long long do_ts, do_hs;
+    uint16_t *dQ, *dK, *dV;  // contiguous
+    float scale;
+    float* delta;        // [H, S_q]: sum over a row of dO O
+    unsigned* bits;      // [H_kv][words][nb]: bit i of word w: query block 32 w + i lists key block n
+    int* counts;         // [H_kv * nb] query blocks that list a key block
+    int* first;          // [H_kv * nb] where their list starts in `lists`
+    int* lists;          // query blocks, ascending, key block by key block
+    int* slots;          // [H_kv * nb] first partial result of a key block that is shared, or -1
+    int2* items;         // (key block, share) in order of launch
+    int* totals;         // [0]: items
+    float* partial;      // [slot][2][b][d]
+    int nb, words, share;  // share: query blocks that a workgroup takes of a list
+    int max_items;
+};
+
+struct BlockGradLayout { size_t delta, bits, counts, first, lists, slots, items, totals, partial, bytes; int share, max_items; };
+
+constexpr int MAX_LISTED_SUBTILES = 4096;  // subtiles of 32 keys that a list may name: they stand in LDS, 16 KB
+constexpr int MAX_LISTED_BLOCKS = 16384;   // key blocks that a choice is made from: their scores stand in LDS, 128 KB
+
+int block_attention_parts(long long tiles, long long subtiles);
+int block_attention_tile_rows(int R);
+int launch_block_attention(BlockAttnParams p, int d, hipStream_t st);
+BlockGradLayout block_grad_layout(long long S_q, long long S_k, int H, int H_kv, int d, int T, int b, int bq);
+int launch_block_attention_grad(BlockGradParams p, int d, hipStream_t st);
+
+struct BlockSelectParams {
+    const void* Q;
+    const float* means;   // [sequences][nb][H_kv][d]
+    const int* lengths;   // single tokens, or null
+    int* blocks;          // [n_qb, H_kv, T]
+    int S_q, S_k, H, H_kv, G, d, T, b, bq, n_qb, nb;
+    long long q_start, q_ts, q_hs, means_ss;
+    unsigned flags;
+};
+int launch_block_means(const void* K, long long S, int H_kv, int d, lemo_dtype_t dt, long long k_ts, long long k_hs, int b, float* means, hipStream_t st);
+int launch_block_means_step(const void* K, const int* lengths, int B, long long S_max, int H_kv, int d, lemo_dtype_t dt, long long k_ss, long long k_ts,
+                            long long k_hs, int b, float* means, int nb, hipStream_t st);
+int launch_select_blocks(const BlockSelectParams& p, lemo_dtype_t dt, hipStream_t st);
+
+#ifdef __HIPCC__
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+// A tile of head rows in LDS: rows of 16-byte pieces without padding, piece p of row r at position p ^ swz(r).  16 consecutive rows then
+// have any one piece in 16 different bank groups (row fragments), and so have 4 consecutive rows any two neighbouring pieces
+// (transposing reads): both kinds of read are free of conflicts.
+template <int D> struct HeadTile {
+    static constexpr int ROWB = D * 2, PIECES = D / 8, CHUNKS = D / 16, COLS = D / 32;
+    __device__ static constexpr int swz(int r) { return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3); }
+    // this lane's 16 bytes of chunk c of row l32 of a subtile (an MFMA operand that has the subtile's rows as its own)
+    __device__ static u32x4 row_fragment(const char* sub, int c, int lane) {
+        const int r = lane & 31;
+        return *reinterpret_cast<const u32x4*>(sub + r * ROWB + (((2 * c + (lane >> 5)) ^ swz(r)) << 4));
+    }
+    // operand that has columns 32 col + l32 as its rows and, as its contraction, rows 16 c + 4 half + {0..3} and 16 c + 8 + 4 half + {0..3}
+    // of the subtile: the rows that registers 8 c .. 8 c + 7 of an accumulator belong to
+    __device__ static u32x4 column_fragment(const char* sub, int col, int c, int lane) {
+        const int half = lane >> 5, l32 = lane & 31, r = 16 * c + 4 * half + ((l32 & 15) >> 2);
+        const int piece = col * 4 + (l32 >> 4) * 2 + ((l32 & 3) >> 1), low = (l32 & 1) * 8;
+        const char* at0 = sub + r * ROWB + ((piece ^ swz(r)) << 4) + low;
+        const char* at1 = sub + (r + 8) * ROWB + ((piece ^ swz(r + 8)) << 4) + low;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at0));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at1));
+        const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+        return u32x4{l2.x, l2.y, h2.x, h2.y};
+    }
+};
+
+// The list of a query block as the rule for it says: an entry counts if it names a block, [0, nb), and lies above every such entry
+// before it.  One wave; `take(entry, counts)` is called for 64 entries at a time, by all lanes.
+template <typename F> __device__ __forceinline__ void walk_list(const int* list, int T, int nb, int lane, F&& take) {
+    int top = -1;  // highest block so far
+    for (int e0 = 0; e0 < T; e0 += 64) {
+        const int raw = e0 + lane < T ? list[e0 + lane] : -1, n = raw >= 0 && raw < nb ? raw : -1;
+        int high = n;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const int other = __shfl_up(high, s);
+            if (lane >= s) high = max(high, other);
+        }
+        const int before = __shfl_up(high, 1);
+        take(n, n > max(top, lane > 0 ? before : -1));
+        top = max(top, __shfl(high, 63));
+    }
+}
+
+// The subtiles of a list up to key `limit`, as first keys in `keys` (LDS); returns how many.  One wave.
+__device__ __forceinline__ int list_subtiles(const int* list, int T, int b, int nb, int limit, int* keys, int lane) {
+    int count = 0;
+    const int most = b / 32;
+    walk_list(list, T, nb, lane, [&](int n, bool counts) {
+        const int first = n * b;
+        const int mine = counts && first <= limit ? min(most, (limit - first) / 32 + 1) : 0;
+        int sum = mine;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const int other = __shfl_up(sum, s);
+            if (lane >= s) sum += other;
+        }
+        const int at = count + sum - mine;
+        for (int i = 0; i < mine; ++i) keys[at + i] = first + 32 * i;
+        count += __shfl(sum, 63);
+    });
+    return count;
+}
+
+// before a barrier that hands a stage over: this wave's LDS-direct loads have landed, its LDS reads have returned
+__device__ __forceinline__ void settle_stage() {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    __builtin_amdgcn_s_waitcnt(LGKMCNT0);
+}
+__device__ __forceinline__ float half_waves_max(float v) {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+#endif
+
+}  // namespace lemo

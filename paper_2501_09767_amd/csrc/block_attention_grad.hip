@@ -1,0 +1,553 @@
+// Gradients of the attention over listed key blocks (lemo_block_attention_grad).
+//
+//   P = 2^(c2 <q,k> - lse2[q])      delta = <dO, O> of a row      dS = P (<dO, v> - delta)
+//   dQ = scale dS K      dK = scale dS^T Q      dV = P^T dO        sums over what the lists pair, keys of a group shared by its heads
+//
+// Two passes without atomics, so that the same bits come on every run.  The first goes by query blocks, as the forward pass does, and
+// leaves dQ and delta.  The second goes by key blocks: a key block's queries are those whose lists name it, which are turned
+// round first -- a bit for every (query block, key block), counted, laid out as lists of ascending query blocks, and cut into items
+// of at most `share` query blocks, since a popular block may be on every list.  The parts of a block that was cut are added in
+// order.  Each pass forms its logits and probabilities again: 7 products for the 5 of the definition, which costs less than writing and
+// reading dS (2 bytes a pair) would.
+#include "block_attention.hpp"
+
+namespace lemo {
+
+constexpr int BG_STAGE = 4;  // subtiles of 32 of a stage
+
+// ---- by query blocks: dQ, delta -----------------------------------------------------------------------
+
+template <int D, int WAVES> struct DqGeo {
+    using Tile = HeadTile<D>;
+    static constexpr int SUB = 32 * Tile::ROWB, STAGE = 2 * BG_STAGE * SUB;
+    static constexpr int PITCH = D + 4, JOIN = WAVES * 32 * PITCH * 4;
+    static constexpr int LIST = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
+    static constexpr int lds(int subtiles) { return LIST + subtiles * 4; }
+};
+
+template <int D, int WAVES, int KS>
+__global__ __launch_bounds__(WAVES * 64, 1) void block_dq_kernel(BlockGradParams gp) {
+    const BlockAttnParams& p = gp.a;
+    using Geo = DqGeo<D, WAVES>;
+    using Tile = HeadTile<D>;
+    constexpr int ROWS = WAVES / KS * 32;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    __shared__ int listed;
+    int* const keys = reinterpret_cast<int*>(smem + Geo::LIST);
+
+    int g, rank;
+    decode_block(p.order, p.H_kv, p.n_qb * p.n_rt, g, rank);
+    const int rt = rank % p.n_rt, qb = rank / p.n_rt;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool causal = (p.flags & LEMO_CAUSAL) != 0;
+    const int S = p.S_k;
+    const long long pos0 = p.q_start + (long long)qb * p.bq;
+    const int rows = min(p.bq, p.S_q - qb * p.bq) * p.G, row_end = min(rows, (rt + 1) * ROWS);
+    auto limit_of = [&](int row) { return causal ? (int)min(pos0 + row / p.G, (long long)S - 1) : S - 1; };
+
+    if (wave == 0) {
+        const int n = rt * ROWS < rows ? list_subtiles(p.blocks + ((long long)qb * p.H_kv + g) * p.T, p.T, p.b, gp.nb, limit_of(row_end - 1), keys, lane) : 0;
+        if (lane == 0) listed = n;
+    }
+    __syncthreads();
+    const int n_sub = listed, n_stage = (n_sub + BG_STAGE - 1) / BG_STAGE;
+
+    const int row0 = rt * ROWS + wave / KS * 32, row = row0 + l32;
+    const bool live = row < rows;
+    const int lim = live ? limit_of(row) : -1;
+    const int clean = row0 < rows ? limit_of(row0) : -1, reach = row0 < rows ? limit_of(min(row0 + 31, rows - 1)) : -1;
+    const long long i_row = (long long)qb * p.bq + row / p.G;
+    const int h_row = g * p.G + row % p.G;
+    u32x4 qf[Tile::CHUNKS], dof[Tile::CHUNKS];
+    float delta = 0.f, lse = INFINITY;  // a row that is not there, or saw no key: probabilities 0
+#pragma unroll
+    for (int c = 0; c < Tile::CHUNKS; ++c) qf[c] = dof[c] = u32x4{0u, 0u, 0u, 0u};
+    if (live) {
+        const char* const q = reinterpret_cast<const char*>(p.Q + i_row * p.q_ts + h_row * p.q_hs);
+        const char* const o = reinterpret_cast<const char*>(p.O + i_row * p.o_ts + h_row * p.o_hs);
+        const char* const d = reinterpret_cast<const char*>(gp.dO + i_row * gp.do_ts + h_row * gp.do_hs);
+#pragma unroll
+        for (int c = 0; c < Tile::CHUNKS; ++c) {
+            qf[c] = *reinterpret_cast<const u32x4*>(q + c * 32 + half * 16);
+            dof[c] = *reinterpret_cast<const u32x4*>(d + c * 32 + half * 16);
+            const u32x4 of = *reinterpret_cast<const u32x4*>(o + c * 32 + half * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                delta = fmaf(bf16lo_to_f32(of[e]), bf16lo_to_f32(dof[c][e]), fmaf(bf16hi_to_f32(of[e]), bf16hi_to_f32(dof[c][e]), delta));
+        }
+        const float stored = p.lse2[(long long)h_row * p.S_q + i_row];
+        lse = stored == -INFINITY ? INFINITY : stored;
+    }
+    delta += __shfl_xor(delta, 32);
+    if (live && half == 0 && wave % KS == 0) gp.delta[(long long)h_row * p.S_q + i_row] = delta;
+
+    const char* const kbase = reinterpret_cast<const char*>(p.K + (long long)g * p.k_hs);
+    const char* const vbase = reinterpret_cast<const char*>(p.V + (long long)g * p.v_hs);
+    constexpr int RPI = 1024 / Tile::ROWB, PER_SUB = 32 / RPI, LOADS = 2 * BG_STAGE * PER_SUB / WAVES;
+    const int in_row = lane / Tile::PIECES, pos = lane % Tile::PIECES;
+    auto load_stage = [&](int t, int buf) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int unit = i * WAVES + wave, which = unit / PER_SUB, part = unit % PER_SUB;
+            const bool v = which >= BG_STAGE;
+            const int s = t * BG_STAGE + which % BG_STAGE;
+            const int key = s < n_sub ? __builtin_amdgcn_readfirstlane(keys[s]) : S;
+            const long long pitch = (v ? p.v_ts : p.k_ts) * 2;
+            const u32x4 rsrc = raw_rsrc((v ? vbase : kbase) + (long long)min(key, S) * pitch, key < S ? (long long)(S - 1 - key) * pitch + Tile::ROWB : 0);
+            const int r = part * RPI + in_row;
+            lds_direct_b128(rsrc, lds_offset_of(smem) + buf * Geo::STAGE + which * Geo::SUB + part * 1024, r * (int)pitch + ((pos ^ Tile::swz(r)) << 4));
+        }
+    };
+    f32x16 dq[Tile::COLS];
+#pragma unroll
+    for (int c = 0; c < Tile::COLS; ++c) dq[c] = f32x16{0};
+    if (n_stage > 0) {
+        load_stage(0, 0);
+        settle_stage();
+    }
+    for (int t = 0; t < n_stage; ++t) {
+        __syncthreads();
+        if (t + 1 < n_stage) load_stage(t + 1, (t + 1) & 1);
+        const char* const sk = smem + (t & 1) * Geo::STAGE;
+#pragma unroll 1
+        for (int j = wave % KS; j < BG_STAGE; j += KS) {
+            if (t * BG_STAGE + j >= n_sub) break;
+            const int key = __builtin_amdgcn_readfirstlane(keys[t * BG_STAGE + j]);
+            if (key > reach) continue;
+            const char* const ks = sk + j * Geo::SUB;
+            const char* const vs = ks + BG_STAGE * Geo::SUB;
+            f32x16 acc = {0}, dp = {0};
+#pragma unroll
+            for (int c = 0; c < Tile::CHUNKS; ++c) {
+                mma_chunk<bf16_t>(acc, Tile::row_fragment(ks, c, lane), qf[c]);  // [key][row]
+                mma_chunk<bf16_t>(dp, Tile::row_fragment(vs, c, lane), dof[c]);
+            }
+            float ds[16];
+            const bool masked = key + 31 > clean;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                float x = fmaf(acc[r], p.c2, -lse);
+                if (masked) x = key + acc_row(r, lane) <= lim ? x : -INFINITY;
+                ds[r] = __builtin_amdgcn_exp2f(x) * (dp[r] - delta);
+            }
+            u32x4 pb[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                pb[c] = u32x4{pack_bf16x2_hw(ds[8 * c + 0], ds[8 * c + 1]), pack_bf16x2_hw(ds[8 * c + 2], ds[8 * c + 3]),
+                              pack_bf16x2_hw(ds[8 * c + 4], ds[8 * c + 5]), pack_bf16x2_hw(ds[8 * c + 6], ds[8 * c + 7])};
+#pragma unroll
+            for (int col = 0; col < Tile::COLS; ++col)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) mma_chunk<bf16_t>(dq[col], Tile::column_fragment(ks, col, c, lane), pb[c]);  // [head column][row]
+        }
+        settle_stage();
+    }
+    // the waves that share rows add in LDS, in wave order
+    __syncthreads();
+    constexpr int LPR = D / 8;
+    const int first = wave - wave % KS;
+    float* const sums = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int col = 0; col < Tile::COLS; ++col)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<f32x4*>(sums + (wave * 32 + l32) * Geo::PITCH + col * 32 + q * 8 + half * 4) =
+                f32x4{dq[col][q * 4], dq[col][q * 4 + 1], dq[col][q * 4 + 2], dq[col][q * 4 + 3]};
+    __syncthreads();
+    const int c0 = lane % LPR * 8;
+#pragma unroll
+    for (int r = 0; r < 32 / KS; r += 64 / LPR) {
+        const int in = wave % KS * (32 / KS) + r + lane / LPR, out = row0 + in;
+        if (out >= rows) continue;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < KS; ++w) {
+            const float* at = sums + ((first + w) * 32 + in) * Geo::PITCH + c0;
+            const f32x4 lo = *reinterpret_cast<const f32x4*>(at), hi = *reinterpret_cast<const f32x4*>(at + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[e] += lo[e]; v[e + 4] += hi[e]; }
+        }
+        u32x4 piece;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) piece[e] = pack_bf16x2_hw(v[2 * e] * gp.scale, v[2 * e + 1] * gp.scale);
+        *reinterpret_cast<u32x4*>(gp.dQ + (((long long)qb * p.bq + out / p.G) * p.H + g * p.G + out % p.G) * D + c0) = piece;
+    }
+}
+
+// ---- the lists turned round ---------------------------------------------------------------------------
+
+// A workgroup: 32 query blocks of one group; its four waves walk eight lists each and leave the blocks' bits in LDS.
+__global__ __launch_bounds__(256) void block_bits_kernel(BlockGradParams gp) {
+    const BlockAttnParams& p = gp.a;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    unsigned* const bits = reinterpret_cast<unsigned*>(smem);
+    const int w = blockIdx.x, g = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int n = threadIdx.x; n < gp.nb; n += 256) bits[n] = 0;
+    __syncthreads();
+    for (int i = wave; i < 32; i += 4) {
+        const int qb = w * 32 + i;
+        if (qb >= p.n_qb) break;
+        const long long last = p.q_start + min((long long)(qb + 1) * p.bq, (long long)p.S_q) - 1;
+        walk_list(p.blocks + ((long long)qb * p.H_kv + g) * p.T, p.T, gp.nb, lane, [&](int n, bool counts) {
+            if (counts && (!(p.flags & LEMO_CAUSAL) || (long long)n * p.b <= last)) atomicOr(bits + n, 1u << i);
+        });
+    }
+    __syncthreads();
+    for (int n = threadIdx.x; n < gp.nb; n += 256) gp.bits[((long long)g * gp.words + w) * gp.nb + n] = bits[n];
+}
+
+__global__ __launch_bounds__(64) void block_count_kernel(BlockGradParams gp) {
+    const int n = blockIdx.x * 64 + threadIdx.x, g = blockIdx.y;
+    if (n >= gp.nb) return;
+    int count = 0;
+#pragma unroll 8
+    for (int w = 0; w < gp.words; ++w) count += __popc(gp.bits[((long long)g * gp.words + w) * gp.nb + n]);
+    gp.counts[g * gp.nb + n] = count;
+}
+
+// One workgroup: where every key block's list, items and partial results start.
+__global__ __launch_bounds__(1024) void block_layout_kernel(BlockGradParams gp) {
+    __shared__ int sums[3][16];
+    const int total = gp.a.H_kv * gp.nb, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int base[3] = {0, 0, 0};
+    for (int n0 = 0; n0 < total; n0 += 1024) {
+        const int n = n0 + (int)threadIdx.x;
+        const int count = n < total ? gp.counts[n] : 0;
+        const int items = n < total ? max(1, (count + gp.share - 1) / gp.share) : 0;
+        const int mine[3] = {count, items, items > 1 ? items : 0};
+        int sum[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            sum[k] = mine[k];
+#pragma unroll
+            for (int s = 1; s < 64; s <<= 1) {
+                const int other = __shfl_up(sum[k], s);
+                if (lane >= s) sum[k] += other;
+            }
+            if (lane == 63) sums[k][wave] = sum[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            int all = 0;
+            for (int v = 0; v < 16; ++v) {
+                if (v < wave) sum[k] += sums[k][v];
+                all += sums[k][v];
+            }
+            sum[k] += base[k] - mine[k];
+            base[k] += all;
+        }
+        __syncthreads();
+        if (n < total) {
+            gp.first[n] = sum[0];
+            gp.slots[n] = items > 1 ? sum[2] : -1;
+            for (int i = 0; i < items; ++i) gp.items[sum[1] + i] = make_int2(n, i);
+        }
+    }
+    if (threadIdx.x == 0) gp.totals[0] = base[1];
+}
+
+__global__ __launch_bounds__(64) void block_lists_kernel(BlockGradParams gp) {
+    const int n = blockIdx.x * 64 + threadIdx.x, g = blockIdx.y;
+    if (n >= gp.nb) return;
+    int* out = gp.lists + gp.first[g * gp.nb + n];
+    for (int w = 0; w < gp.words; ++w) {
+        unsigned set = gp.bits[((long long)g * gp.words + w) * gp.nb + n];
+        while (set) {
+            *out++ = w * 32 + __ffs(set) - 1;
+            set &= set - 1;
+        }
+    }
+}
+
+// ---- by key blocks: dK, dV ----------------------------------------------------------------------------
+
+// KW waves hold 32 keys each, and 4 / KW waves share keys and take the row subtiles of a stage in turn.
+struct RowInfo { unsigned q, d; float lse, delta; int pos; };  // byte offsets of a row in Q and dO, its statistics, its position
+
+template <int D> struct DkvGeo {
+    using Tile = HeadTile<D>;
+    static constexpr int SUB = 32 * Tile::ROWB, STAGE = 2 * BG_STAGE * SUB, ROWS = BG_STAGE * 32;
+    static constexpr int PITCH = D + 4, JOIN = 4 * 32 * PITCH * 4;
+    static constexpr int TABLE = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;  // three tables of rows stand behind the stages
+    static constexpr int LDS = TABLE + 3 * ROWS * 5 * 4;
+};
+
+template <int D, int KW>
+__global__ __launch_bounds__(256, 1) void block_dkv_kernel(BlockGradParams gp) {
+    const BlockAttnParams& p = gp.a;
+    using Geo = DkvGeo<D>;
+    using Tile = HeadTile<D>;
+    constexpr int SHARES = 4 / KW, ROWS = Geo::ROWS;
+    if ((int)blockIdx.x >= gp.totals[0]) return;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    // tables: [ring of 3][ROWS] of each field
+    unsigned* const t_q = reinterpret_cast<unsigned*>(smem + Geo::TABLE);
+    unsigned* const t_d = t_q + 3 * ROWS;
+    float* const t_lse = reinterpret_cast<float*>(t_d + 3 * ROWS);
+    float* const t_delta = t_lse + 3 * ROWS;
+    int* const t_pos = reinterpret_cast<int*>(t_delta + 3 * ROWS);
+
+    const int2 item = gp.items[blockIdx.x];
+    const int g = item.x / gp.nb, n = item.x % gp.nb;
+    const int* const list = gp.lists + gp.first[item.x] + item.y * gp.share;
+    const int in_list = min(gp.share, gp.counts[item.x] - item.y * gp.share);  // query blocks of the item
+    const int n_rows = max(in_list, 0) * p.R, n_stage = (n_rows + ROWS - 1) / ROWS;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool causal = (p.flags & LEMO_CAUSAL) != 0;
+    const int key0 = n * p.b + (blockIdx.y * KW + wave % KW) * 32, key = key0 + l32;
+    const int share = wave / KW;
+
+    u32x4 kf[Tile::CHUNKS], vf[Tile::CHUNKS];
+#pragma unroll
+    for (int c = 0; c < Tile::CHUNKS; ++c) kf[c] = vf[c] = u32x4{0u, 0u, 0u, 0u};
+    if (key < p.S_k) {
+        const char* const k = reinterpret_cast<const char*>(p.K + key * p.k_ts + g * p.k_hs);
+        const char* const v = reinterpret_cast<const char*>(p.V + key * p.v_ts + g * p.v_hs);
+#pragma unroll
+        for (int c = 0; c < Tile::CHUNKS; ++c) {
+            kf[c] = *reinterpret_cast<const u32x4*>(k + c * 32 + half * 16);
+            vf[c] = *reinterpret_cast<const u32x4*>(v + c * 32 + half * 16);
+        }
+    }
+
+    // rows of a stage: row v of the item is row v % R of query block list[v / R]
+    auto make_table = [&](int t) {
+        if (tid >= ROWS) return;
+        const int v = t * ROWS + tid, at = t % 3 * ROWS + tid;
+        RowInfo r{0xffffff00u, 0xffffff00u, INFINITY, 0.f, -1};  // not there: offsets past every operand, probabilities 0
+        if (v < n_rows) {
+            const int e = v / p.R, row = v - e * p.R, h = g * p.G + row % p.G;
+            const long long i = (long long)list[e] * p.bq + row / p.G;
+            if (i < p.S_q) {
+                r.q = (unsigned)((i * p.q_ts + h * p.q_hs) * 2);
+                r.d = (unsigned)((i * gp.do_ts + h * gp.do_hs) * 2);
+                const float stored = p.lse2[(long long)h * p.S_q + i];
+                r.lse = stored == -INFINITY ? INFINITY : stored;
+                r.delta = gp.delta[(long long)h * p.S_q + i];
+                r.pos = causal ? (int)min(p.q_start + i, (long long)0x7fffffff) : 0x7fffffff;
+            }
+        }
+        t_q[at] = r.q; t_d[at] = r.d; t_lse[at] = r.lse; t_delta[at] = r.delta; t_pos[at] = r.pos;
+    };
+    const u32x4 q_rsrc = raw_rsrc(p.Q, ((p.S_q - 1) * p.q_ts + (p.H - 1) * p.q_hs + D) * 2);
+    const u32x4 d_rsrc = raw_rsrc(gp.dO, ((p.S_q - 1) * gp.do_ts + (p.H - 1) * gp.do_hs + D) * 2);
+    constexpr int RPI = 1024 / Tile::ROWB, UNITS = ROWS / RPI, LOADS = 2 * UNITS / 4;
+    const int in_row = lane / Tile::PIECES, place = lane % Tile::PIECES;
+    auto load_stage = [&](int t, int buf) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int unit = i * 4 + wave, part = unit % UNITS, r = part * RPI + in_row;
+            const bool d = i * 4 >= UNITS;  // the first half: Q, then dO
+            const unsigned row = (d ? t_d : t_q)[t % 3 * ROWS + r];
+            lds_direct_b128(d ? d_rsrc : q_rsrc, lds_offset_of(smem) + buf * Geo::STAGE + (d ? BG_STAGE * Geo::SUB : 0) + part * 1024,
+                            (int)(row + ((unsigned)(place ^ Tile::swz(r & 31)) << 4)));
+        }
+    };
+
+    f32x16 dk[Tile::COLS], dv[Tile::COLS];
+#pragma unroll
+    for (int c = 0; c < Tile::COLS; ++c) dk[c] = dv[c] = f32x16{0};
+    if (n_stage > 0) {
+        make_table(0);
+        if (n_stage > 1) make_table(1);
+        __syncthreads();
+        load_stage(0, 0);
+        settle_stage();
+    }
+    for (int t = 0; t < n_stage; ++t) {
+        __syncthreads();  // stage t and the table of stage t + 1 are there
+        if (t + 1 < n_stage) load_stage(t + 1, (t + 1) & 1);
+        if (t + 2 < n_stage) make_table(t + 2);
+        const char* const sq = smem + (t & 1) * Geo::STAGE;
+        const int table = t % 3 * ROWS;
+#pragma unroll 1
+        for (int j = share; j < BG_STAGE; j += SHARES) {
+            if (t * ROWS + j * 32 >= n_rows) break;
+            const int at = table + j * 32;
+            const int top = __builtin_amdgcn_readfirstlane(t_pos[at + 31]);  // rows ascend: the last one has the highest position, if it is there
+            if (top >= 0 && top < key0) continue;
+            const char* const qs = sq + j * Geo::SUB;
+            const char* const ds_ = qs + BG_STAGE * Geo::SUB;
+            f32x16 acc = {0}, dp = {0};
+#pragma unroll
+            for (int c = 0; c < Tile::CHUNKS; ++c) {
+                mma_chunk<bf16_t>(acc, Tile::row_fragment(qs, c, lane), kf[c]);  // [row][key]
+                mma_chunk<bf16_t>(dp, Tile::row_fragment(ds_, c, lane), vf[c]);
+            }
+            float pr[16], ds[16];
+            const bool masked = __builtin_amdgcn_readfirstlane(t_pos[at]) < key0 + 31;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 lse = *reinterpret_cast<const f32x4*>(t_lse + at + 8 * q + 4 * half);
+                const f32x4 delta = *reinterpret_cast<const f32x4*>(t_delta + at + 8 * q + 4 * half);
+                const int4 rp = *reinterpret_cast<const int4*>(t_pos + at + 8 * q + 4 * half);
+                const int rpos[4] = {rp.x, rp.y, rp.z, rp.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 4 * q + e;
+                    float x = fmaf(acc[r], p.c2, -lse[e]);
+                    if (masked) x = key <= rpos[e] ? x : -INFINITY;
+                    pr[r] = __builtin_amdgcn_exp2f(x);
+                    ds[r] = pr[r] * (dp[r] - delta[e]);
+                }
+            }
+            u32x4 pp[2], pd[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                pp[c] = u32x4{pack_bf16x2_hw(pr[8 * c + 0], pr[8 * c + 1]), pack_bf16x2_hw(pr[8 * c + 2], pr[8 * c + 3]),
+                              pack_bf16x2_hw(pr[8 * c + 4], pr[8 * c + 5]), pack_bf16x2_hw(pr[8 * c + 6], pr[8 * c + 7])};
+                pd[c] = u32x4{pack_bf16x2_hw(ds[8 * c + 0], ds[8 * c + 1]), pack_bf16x2_hw(ds[8 * c + 2], ds[8 * c + 3]),
+                              pack_bf16x2_hw(ds[8 * c + 4], ds[8 * c + 5]), pack_bf16x2_hw(ds[8 * c + 6], ds[8 * c + 7])};
+            }
+#pragma unroll
+            for (int col = 0; col < Tile::COLS; ++col)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    mma_chunk<bf16_t>(dv[col], Tile::column_fragment(ds_, col, c, lane), pp[c]);  // [head column][key]
+                    mma_chunk<bf16_t>(dk[col], Tile::column_fragment(qs, col, c, lane), pd[c]);
+                }
+        }
+        settle_stage();
+    }
+    // dK, then dV: the waves that share keys add in LDS, in wave order
+    constexpr int LPR = D / 8;
+    float* const sums = reinterpret_cast<float*>(smem);
+    const int c0 = lane % LPR * 8;
+    const int slot = gp.slots[item.x];
+    for (int which = 0; which < 2; ++which) {
+        __syncthreads();
+#pragma unroll
+        for (int col = 0; col < Tile::COLS; ++col)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = which ? dv[col][q * 4 + e] : dk[col][q * 4 + e] * gp.scale;
+                *reinterpret_cast<f32x4*>(sums + (wave * 32 + l32) * Geo::PITCH + col * 32 + q * 8 + half * 4) = v;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 32 / SHARES; r += 64 / LPR) {
+            const int in = share * (32 / SHARES) + r + lane / LPR;
+            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < SHARES; ++w) {
+                const float* at = sums + ((w * KW + wave % KW) * 32 + in) * Geo::PITCH + c0;
+                const f32x4 lo = *reinterpret_cast<const f32x4*>(at), hi = *reinterpret_cast<const f32x4*>(at + 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { v[e] += lo[e]; v[e + 4] += hi[e]; }
+            }
+            const int j = key0 + in;
+            if (slot >= 0) {
+                float* part = gp.partial + (((long long)(slot + item.y) * 2 + which) * p.b + (j - n * p.b)) * D + c0;
+                *reinterpret_cast<f32x4*>(part) = f32x4{v[0], v[1], v[2], v[3]};
+                *reinterpret_cast<f32x4*>(part + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            } else if (j < p.S_k) {
+                u32x4 piece;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) piece[e] = pack_bf16x2_hw(v[2 * e], v[2 * e + 1]);
+                *reinterpret_cast<u32x4*>((which ? gp.dV : gp.dK) + ((long long)j * p.H_kv + g) * D + c0) = piece;
+            }
+        }
+    }
+}
+
+// The key blocks that were cut: their parts added in order.
+template <int D> __global__ __launch_bounds__(256) void block_dkv_join_kernel(BlockGradParams gp) {
+    const BlockAttnParams& p = gp.a;
+    const int at = blockIdx.x, g = at / gp.nb, n = at % gp.nb, slot = gp.slots[at];
+    if (slot < 0) return;
+    const int parts = (gp.counts[at] + gp.share - 1) / gp.share;
+    constexpr int LPR = D / 8;
+    for (int u = blockIdx.y * 256 + threadIdx.x; u < 2 * p.b * LPR; u += gridDim.y * 256) {
+        const int which = u / (p.b * LPR), j = u / LPR % p.b, c0 = u % LPR * 8, key = n * p.b + j;
+        if (key >= p.S_k) continue;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < parts; ++w) {
+            const float* part = gp.partial + (((long long)(slot + w) * 2 + which) * p.b + j) * D + c0;
+            const f32x4 lo = *reinterpret_cast<const f32x4*>(part), hi = *reinterpret_cast<const f32x4*>(part + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[e] += lo[e]; v[e + 4] += hi[e]; }
+        }
+        u32x4 piece;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) piece[e] = pack_bf16x2_hw(v[2 * e], v[2 * e + 1]);
+        *reinterpret_cast<u32x4*>((which ? gp.dV : gp.dK) + ((long long)key * p.H_kv + g) * D + c0) = piece;
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------
+
+BlockGradLayout block_grad_layout(long long S_q, long long S_k, int H, int H_kv, int d, int T, int b, int bq) {
+    BlockGradLayout l{};
+    const long long n_qb = (S_q + bq - 1) / bq, nb = (S_k + b - 1) / b, words = (n_qb + 31) / 32, R = (long long)bq * (H / H_kv);
+    const long long entries = n_qb * H_kv * (T < nb ? T : nb);
+    // Items: some two thousand for the whole launch, of 256 rows at least
+    long long share = (entries + 2047) / 2048;
+    const long long least = (256 + R - 1) / R;
+    if (share < least) share = least;
+    l.share = (int)(share < n_qb ? share : n_qb);
+    l.max_items = (int)(entries / l.share + H_kv * nb);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+    l.delta = take((size_t)H * S_q * 4);
+    l.bits = take((size_t)H_kv * words * nb * 4);
+    l.counts = take((size_t)H_kv * nb * 4);
+    l.first = take((size_t)H_kv * nb * 4);
+    l.lists = take((size_t)entries * 4);
+    l.slots = take((size_t)H_kv * nb * 4);
+    l.items = take((size_t)l.max_items * 8);
+    l.totals = take(4);
+    // parts of key blocks with more than one: at most twice as many as their query blocks fill
+    const long long parts = 2 * (entries / l.share) < l.max_items ? 2 * (entries / l.share) : l.max_items;
+    l.partial = take((size_t)parts * 2 * b * d * 4);
+    l.bytes = at;
+    return l;
+}
+
+template <int D, int WAVES, int KS> static int run_dq(const BlockGradParams& gp, hipStream_t st) {
+    hipLaunchKernelGGL((block_dq_kernel<D, WAVES, KS>), dim3((unsigned)((long long)gp.a.n_qb * gp.a.n_rt * gp.a.H_kv)), dim3(WAVES * 64),
+                       (DqGeo<D, WAVES>::lds(gp.a.T * (gp.a.b / 32))), st, gp);
+    return (int)hipGetLastError();
+}
+
+template <int D, int KW> static int run_dkv(const BlockGradParams& gp, hipStream_t st) {
+    hipLaunchKernelGGL((block_dkv_kernel<D, KW>), dim3((unsigned)gp.max_items, (unsigned)(gp.a.b / (32 * KW))), dim3(256), DkvGeo<D>::LDS, st, gp);
+    return (int)hipGetLastError();
+}
+
+template <int D> static int launch_grad(BlockGradParams gp, hipStream_t st) {
+    static const int unready = raise_lds_limits({{reinterpret_cast<const void*>(&block_dq_kernel<D, 8, 1>), DqGeo<D, 8>::lds(MAX_LISTED_SUBTILES)},
+                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 8, 2>), DqGeo<D, 8>::lds(MAX_LISTED_SUBTILES)},
+                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 8, 4>), DqGeo<D, 8>::lds(MAX_LISTED_SUBTILES)},
+                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 4>), DqGeo<D, 4>::lds(MAX_LISTED_SUBTILES)},
+                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 1>), DkvGeo<D>::LDS},
+                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 2>), DkvGeo<D>::LDS},
+                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 4>), DkvGeo<D>::LDS}});
+    if (unready) return unready;
+    BlockAttnParams& p = gp.a;
+    const int tile = block_attention_tile_rows(p.R);
+    p.n_rt = (p.R + tile - 1) / tile;
+    p.n_parts = 1;
+    p.order = head_order(p.H_kv, false, 8);
+    int rc = tile == 256 ? run_dq<D, 8, 1>(gp, st) : tile == 128 ? run_dq<D, 8, 2>(gp, st) : tile == 64 ? run_dq<D, 8, 4>(gp, st) : run_dq<D, 4, 4>(gp, st);
+    if (rc) return rc;
+    hipLaunchKernelGGL(block_bits_kernel, dim3((unsigned)gp.words, (unsigned)p.H_kv), dim3(256), gp.nb * 4, st, gp);
+    hipLaunchKernelGGL(block_count_kernel, dim3((unsigned)((gp.nb + 63) / 64), (unsigned)p.H_kv), dim3(64), 0, st, gp);
+    hipLaunchKernelGGL(block_layout_kernel, dim3(1), dim3(1024), 0, st, gp);
+    hipLaunchKernelGGL(block_lists_kernel, dim3((unsigned)((gp.nb + 63) / 64), (unsigned)p.H_kv), dim3(64), 0, st, gp);
+    rc = (int)hipGetLastError();
+    if (rc) return rc;
+    const int subs = p.b / 32;
+    rc = subs % 4 == 0 ? run_dkv<D, 4>(gp, st) : subs % 2 == 0 ? run_dkv<D, 2>(gp, st) : run_dkv<D, 1>(gp, st);
+    if (rc) return rc;
+    hipLaunchKernelGGL((block_dkv_join_kernel<D>), dim3((unsigned)(p.H_kv * gp.nb), 2), dim3(256), 0, st, gp);
+    return (int)hipGetLastError();
+}
+
+int launch_block_attention_grad(BlockGradParams gp, int d, hipStream_t st) { return d == 64 ? launch_grad<64>(gp, st) : launch_grad<128>(gp, st); }
+
+}  // namespace lemo

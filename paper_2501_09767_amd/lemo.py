@@ -31,7 +31,10 @@ EXPORTS = ("lemo_strerror", "lemo_keep_k", "lemo_kept_count", "lemo_score_worksp
            "lemo_score_blocks_workspace_bytes", "lemo_score_blocks", "lemo_threshold_init", "lemo_select_threshold",
            "lemo_kept_attention_workspace_bytes", "lemo_kept_attention",
            "lemo_gather_gemm_dw_workspace_bytes", "lemo_gather_gemm_dw", "lemo_gather_gemm_dx",
-           "lemo_norm_residual", "lemo_norm_residual_grad_workspace_bytes", "lemo_norm_residual_grad")
+           "lemo_norm_residual", "lemo_norm_residual_grad_workspace_bytes", "lemo_norm_residual_grad",
+           "lemo_block_means", "lemo_select_blocks", "lemo_block_attention_workspace_bytes", "lemo_block_attention",
+           "lemo_block_attention_grad_workspace_bytes", "lemo_block_attention_grad", "lemo_block_means_step", "lemo_select_blocks_step",
+           "lemo_block_attention_step_workspace_bytes", "lemo_block_attention_step")
 
 
 class LemoError(RuntimeError):
@@ -107,6 +110,16 @@ def _load() -> ctypes.CDLL:
     lib.lemo_norm_residual_grad.restype = ctypes.c_int
     lib.lemo_norm_residual_grad.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, i32, f32, f32, vp, vp, i64, vp, i64,
                                             vp, vp, vp, vp, vp, i32, ctypes.c_int, u32, vp, ctypes.c_size_t, vp]
+    size = ctypes.POINTER(ctypes.c_size_t)
+    kinds = {"p": vp, "l": i64, "i": i32, "f": f32, "u": u32, "z": ctypes.c_size_t, "s": size}
+    for name, args in (("block_means", "pliiillipp"), ("select_blocks", "pliiiillplliiiupp"), ("block_attention_workspace_bytes", "liiiiiis"),
+                       ("block_attention", "pppll" "iiii" "llllll" "piiil" "fu" "pllp" "pzp"), ("block_attention_grad_workspace_bytes", "lliiiiiis"),
+                       ("block_attention_grad", "pppppp" "ll" "iiii" "llllllllll" "piiil" "fu" "ppp" "pzp"), ("block_means_step", "piliiilllpipp"),
+                       ("select_blocks_step", "piiiiillplpiipp"), ("block_attention_step_workspace_bytes", "iiiiiis"),
+                       ("block_attention_step", "pppil" "iiii" "llllllll" "ppii" "f" "pll" "pzp")):
+        fn = getattr(lib, "lemo_" + name)
+        fn.restype = ctypes.c_int
+        fn.argtypes = [kinds[k] for k in args]
     return lib
 
 
@@ -729,3 +742,185 @@ def lemo_norm_residual_grad(dN: Optional[torch.Tensor], dR: torch.Tensor, R: tor
                                         _ptr(db_next), _ptr(dgate_sum), C, _dt(R), int(flags), _ptr(workspace),
                                         workspace.numel() * workspace.element_size(), _stream()), "lemo_norm_residual_grad")
     return NormGrads(dY, dgate_sum if shared else dgate, dw_post, db_post, dw_next, db_next)
+
+
+# --------------------------------------------------------------------------------- attention over chosen key blocks
+
+def _heads(t: torch.Tensor, dims: int, name: str):
+    if t.dim() != dims or t.stride(-1) != 1:
+        raise ValueError(f"{name} must have {dims} dimensions, the last (head_dim) contiguous")
+    _dt(t)
+
+
+def _fits(t: torch.Tensor, shape, dtype, name: str):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} {list(shape)}")
+
+
+def _filled(t: Optional[torch.Tensor], shape, dtype, device, name: str) -> torch.Tensor:
+    """A contiguous result of the caller's, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _fits(t, shape, dtype, name)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _blocks_of(n: int, b: int) -> int:
+    if b <= 0:
+        raise ValueError("block sizes must be positive")
+    return -(-n // b)
+
+
+def _bytes(name: str, *args) -> int:
+    n = ctypes.c_size_t(0)
+    _check(getattr(_lib, name)(*args, ctypes.byref(n)), name)
+    return int(n.value)
+
+
+def _scratch(workspace: Optional[torch.Tensor], need: int, device):
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    return workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def lemo_block_means(K: torch.Tensor, b: int, means: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Mean key of every block of b tokens: K [S,H_kv,d] -> [ceil(S/b),H_kv,d] float32."""
+    _here(K, means)
+    _heads(K, 3, "K")
+    S, Hkv, d = K.shape
+    means = _filled(means, (_blocks_of(S, b), Hkv, d), torch.float32, K.device, "means")
+    _check(_lib.lemo_block_means(_ptr(K), S, Hkv, d, _dt(K), K.stride(0), K.stride(1), int(b), _ptr(means), _stream()), "lemo_block_means")
+    return means
+
+
+def lemo_select_blocks(Q: torch.Tensor, means: torch.Tensor, S_k: int, b: int, bq: int, T: int, flags: int = CAUSAL, q_start: int = 0,
+                       blocks: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The T key blocks that each block of bq queries lists, per KV head -> [ceil(S_q/bq),H_kv,T] int32, ascending, -1 behind them."""
+    _here(Q, means, blocks)
+    _heads(Q, 3, "Q")
+    S, H, d = Q.shape
+    Hkv = means.shape[1] if means.dim() == 3 else 0
+    _filled(means, (_blocks_of(S_k, b), Hkv, d), torch.float32, Q.device, "means")
+    blocks = _filled(blocks, (_blocks_of(S, bq), Hkv, T), torch.int32, Q.device, "blocks")
+    _check(_lib.lemo_select_blocks(_ptr(Q), S, H, Hkv, d, _dt(Q), Q.stride(0), Q.stride(1), _ptr(means), int(S_k), int(q_start), int(b), int(bq), int(T),
+                                   int(flags), _ptr(blocks), _stream()), "lemo_select_blocks")
+    return blocks
+
+
+def _attention_sizes(Q, K, V, blocks, b, bq):
+    for name, t in (("Q", Q), ("K", K), ("V", V)):
+        _heads(t, 3, name)
+    S, H, d = Q.shape
+    _fits(K, (K.shape[0], K.shape[1], d), Q.dtype, "K")
+    _fits(V, K.shape, Q.dtype, "V")
+    if blocks.dim() != 3:
+        raise ValueError("blocks must be [query blocks, H_kv, T]")
+    _filled(blocks, (_blocks_of(S, bq), K.shape[1], blocks.shape[2]), torch.int32, Q.device, "blocks")
+    _blocks_of(S, b)
+    return S, K.shape[0], H, K.shape[1], d, blocks.shape[2]
+
+
+def lemo_block_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, blocks: torch.Tensor, b: int, bq: int, flags: int = CAUSAL, scale: float = 0.0,
+                         q_start: int = 0, O: Optional[torch.Tensor] = None, lse2: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None):
+    """Attention of Q [S_q,H,d] over the key blocks that `blocks` lists, K and V [S_k,H_kv,d] -> (O [S_q,H,d], lse2 [H,S_q] float32)."""
+    _here(Q, K, V, blocks, O, lse2, workspace)
+    S, Sk, H, Hkv, d, T = _attention_sizes(Q, K, V, blocks, b, bq)
+    if O is None:
+        O = torch.empty((S, H, d), dtype=Q.dtype, device=Q.device)
+    _heads(O, 3, "O")
+    _fits(O, (S, H, d), Q.dtype, "O")
+    lse2 = _filled(lse2, (H, S), torch.float32, Q.device, "lse2")
+    workspace, size = _scratch(workspace, _bytes("lemo_block_attention_workspace_bytes", S, H, Hkv, d, T, int(b), int(bq)), Q.device)
+    _check(_lib.lemo_block_attention(_ptr(Q), _ptr(K), _ptr(V), S, Sk, H, Hkv, d, _dt(Q), Q.stride(0), Q.stride(1), K.stride(0), K.stride(1), V.stride(0),
+                                     V.stride(1), _ptr(blocks), T, int(b), int(bq), int(q_start), float(scale), int(flags), _ptr(O), O.stride(0),
+                                     O.stride(1), _ptr(lse2), _ptr(workspace), size, _stream()), "lemo_block_attention")
+    return O, lse2
+
+
+def lemo_block_attention_grad(dO: torch.Tensor, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor, lse2: torch.Tensor, blocks: torch.Tensor,
+                              b: int, bq: int, flags: int = CAUSAL, scale: float = 0.0, q_start: int = 0, dQ: Optional[torch.Tensor] = None,
+                              dK: Optional[torch.Tensor] = None, dV: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradients of lemo_block_attention, O and lse2 as it left them -> (dQ [S_q,H,d], dK [S_k,H_kv,d], dV [S_k,H_kv,d])."""
+    _here(dO, Q, K, V, O, lse2, blocks, dQ, dK, dV, workspace)
+    S, Sk, H, Hkv, d, T = _attention_sizes(Q, K, V, blocks, b, bq)
+    for name, t in (("dO", dO), ("O", O)):
+        _heads(t, 3, name)
+        _fits(t, (S, H, d), Q.dtype, name)
+    _filled(lse2, (H, S), torch.float32, Q.device, "lse2")
+    dQ = _filled(dQ, (S, H, d), Q.dtype, Q.device, "dQ")
+    dK = _filled(dK, (Sk, Hkv, d), Q.dtype, Q.device, "dK")
+    dV = _filled(dV, (Sk, Hkv, d), Q.dtype, Q.device, "dV")
+    workspace, size = _scratch(workspace, _bytes("lemo_block_attention_grad_workspace_bytes", S, Sk, H, Hkv, d, T, int(b), int(bq)), Q.device)
+    _check(_lib.lemo_block_attention_grad(_ptr(dO), _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(lse2), S, Sk, H, Hkv, d, _dt(Q), dO.stride(0), dO.stride(1),
+                                          Q.stride(0), Q.stride(1), K.stride(0), K.stride(1), V.stride(0), V.stride(1), O.stride(0), O.stride(1),
+                                          _ptr(blocks), T, int(b), int(bq), int(q_start), float(scale), int(flags), _ptr(dQ), _ptr(dK), _ptr(dV),
+                                          _ptr(workspace), size, _stream()), "lemo_block_attention_grad")
+    return dQ, dK, dV
+
+
+def _lengths(lengths: torch.Tensor, B: int):
+    _filled(lengths, (B,), torch.int32, None, "lengths")
+
+
+def lemo_block_means_step(K: torch.Tensor, lengths: torch.Tensor, b: int, means: torch.Tensor) -> torch.Tensor:
+    """In place: the mean of the block that the newest token of each sequence has filled, if it has.  K [B,S_max,H_kv,d], lengths [B] int32,
+    means [B,ceil(S_max/b),H_kv,d] float32."""
+    _here(K, lengths, means)
+    _heads(K, 4, "K")
+    B, S, Hkv, d = K.shape
+    _lengths(lengths, B)
+    _filled(means, (B, _blocks_of(S, b), Hkv, d), torch.float32, K.device, "means")
+    _check(_lib.lemo_block_means_step(_ptr(K), B, S, Hkv, d, _dt(K), K.stride(0), K.stride(1), K.stride(2), _ptr(lengths), int(b), _ptr(means), _stream()),
+           "lemo_block_means_step")
+    return means
+
+
+def lemo_select_blocks_step(Q: torch.Tensor, means: torch.Tensor, lengths: torch.Tensor, b: int, T: int, blocks: Optional[torch.Tensor] = None,
+                            S_max: Optional[int] = None) -> torch.Tensor:
+    """Key blocks for the newest token of each sequence: Q [B,H,d], means [B,ceil(S_max/b),H_kv,d] float32 -> [B,H_kv,T] int32.
+    S_max: the cache's tokens (all that the means cover if not given)."""
+    _here(Q, means, lengths, blocks)
+    _heads(Q, 3, "Q")
+    B, H, d = Q.shape
+    if means.dim() != 4:
+        raise ValueError("means must be [B, blocks, H_kv, d]")
+    nb, Hkv = means.shape[1], means.shape[2]
+    S_max = nb * b if S_max is None else S_max
+    if _blocks_of(S_max, b) != nb:
+        raise ValueError("means must be [B, ceil(S_max / b), H_kv, d]")
+    _filled(means, (B, nb, Hkv, d), torch.float32, Q.device, "means")
+    _lengths(lengths, B)
+    blocks = _filled(blocks, (B, Hkv, T), torch.int32, Q.device, "blocks")
+    _check(_lib.lemo_select_blocks_step(_ptr(Q), B, H, Hkv, d, _dt(Q), Q.stride(0), Q.stride(1), _ptr(means), int(S_max), _ptr(lengths), int(b), int(T),
+                                        _ptr(blocks), _stream()), "lemo_select_blocks_step")
+    return blocks
+
+
+def lemo_block_attention_step(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lengths: torch.Tensor, blocks: torch.Tensor, b: int, scale: float = 0.0,
+                              O: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the newest token of each sequence over its listed blocks: Q [B,H,d], K and V [B,S_max,H_kv,d] -> O [B,H,d]."""
+    _here(Q, K, V, lengths, blocks, O, workspace)
+    _heads(Q, 3, "Q")
+    _heads(K, 4, "K")
+    _heads(V, 4, "V")
+    B, H, d = Q.shape
+    S, Hkv = K.shape[1], K.shape[2]
+    _fits(K, (B, S, Hkv, d), Q.dtype, "K")
+    _fits(V, (B, S, Hkv, d), Q.dtype, "V")
+    _lengths(lengths, B)
+    if blocks.dim() != 3:
+        raise ValueError("blocks must be [B, H_kv, T]")
+    T = blocks.shape[2]
+    _filled(blocks, (B, Hkv, T), torch.int32, Q.device, "blocks")
+    if O is None:
+        O = torch.empty((B, H, d), dtype=Q.dtype, device=Q.device)
+    _heads(O, 3, "O")
+    _fits(O, (B, H, d), Q.dtype, "O")
+    workspace, size = _scratch(workspace, _bytes("lemo_block_attention_step_workspace_bytes", B, H, Hkv, d, T, int(b)), Q.device)
+    _check(_lib.lemo_block_attention_step(_ptr(Q), _ptr(K), _ptr(V), B, S, H, Hkv, d, _dt(Q), Q.stride(0), Q.stride(1), K.stride(0), K.stride(1), K.stride(2),
+                                          V.stride(0), V.stride(1), V.stride(2), _ptr(lengths), _ptr(blocks), T, int(b), float(scale), _ptr(O), O.stride(0),
+                                          O.stride(1), _ptr(workspace), size, _stream()), "lemo_block_attention_step")
+    return O
