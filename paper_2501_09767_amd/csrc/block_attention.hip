@@ -24,9 +24,6 @@ template <int D, int WAVES> struct BaGeo {
     static constexpr int lds(int subtiles) { return LIST + subtiles * 4; }
 };
 
-// floats of a row's partial result: D values relative to a reference, the reference, the normaliser, room to 16 bytes
-template <int D> constexpr int PART_ROW = D + 4;
-
 template <int D, int WAVES, int KS>
 __global__ __launch_bounds__(WAVES * 64, 1) void block_attention_kernel(BlockAttnParams p) {
     using Geo = BaGeo<D, WAVES>;
@@ -270,13 +267,13 @@ template <int D, int WAVES, int KS> static int run_block_attention(const BlockAt
 }
 
 template <int D> static int launch_block_attention_d(BlockAttnParams p, hipStream_t st) {
-    const int unready = prepare_block_attention<D>();
+    const int unready = D == 128 ? first_error(prepare_block_attention<D>, prepare_block_attention_pipe) : prepare_block_attention<D>();
     if (unready) return unready;
     const int tile = block_attention_tile_rows(p.R);
     p.n_rt = (p.R + tile - 1) / tile;
     p.n_parts = p.parts ? block_attention_parts((long long)p.n_qb * p.n_rt * p.H_kv, (long long)p.T * (p.b / 32)) : 1;
     p.order = head_order(p.H_kv, false, 8);
-    const int rc = tile == 256 ? run_block_attention<D, 8, 1>(p, st) : tile == 128 ? run_block_attention<D, 8, 2>(p, st)
+    const int rc = D == 128 && p.R > 32 ? launch_block_attention_pipe(p, st) : tile == 256 ? run_block_attention<D, 8, 1>(p, st) : tile == 128 ? run_block_attention<D, 8, 2>(p, st)
                  : tile == 64 ? run_block_attention<D, 8, 4>(p, st) : run_block_attention<D, 4, 4>(p, st);
     if (rc || p.n_parts == 1) return rc;
     const long long rows = (long long)p.n_qb * p.H_kv * p.R, per = 256 / (D / 8);

@@ -49,6 +49,8 @@ constexpr int MAX_LISTED_BLOCKS = 16384;   // key blocks that a choice is made f
 int block_attention_parts(long long tiles, long long subtiles);
 int block_attention_tile_rows(int R);
 int launch_block_attention(BlockAttnParams p, int d, hipStream_t st);
+int prepare_block_attention_pipe();
+int launch_block_attention_pipe(const BlockAttnParams& p, hipStream_t st);  // heads of 128; p filled in as for the others
 BlockGradLayout block_grad_layout(long long S_q, long long S_k, int H, int H_kv, int d, int T, int b, int bq);
 int launch_block_attention_grad(BlockGradParams p, int d, hipStream_t st);
 
@@ -65,6 +67,9 @@ int launch_block_means(const void* K, long long S, int H_kv, int d, lemo_dtype_t
 int launch_block_means_step(const void* K, const int* lengths, int B, long long S_max, int H_kv, int d, lemo_dtype_t dt, long long k_ss, long long k_ts,
                             long long k_hs, int b, float* means, int nb, hipStream_t st);
 int launch_select_blocks(const BlockSelectParams& p, lemo_dtype_t dt, hipStream_t st);
+
+// floats of a row's partial result: D values relative to a reference, the reference, the normaliser, room to 16 bytes
+template <int D> constexpr int PART_ROW = D + 4;
 
 #ifdef __HIPCC__
 typedef __attribute__((ext_vector_type(4))) short s16x4;

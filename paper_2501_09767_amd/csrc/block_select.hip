@@ -6,6 +6,8 @@
 // The means read K once and are memory bound.  Scores are formed and compared in 64 bits: which of two nearly equal scores is the larger
 // then does not depend on the order of a sum, and a list is the definition's but for ties closer than 2^-50 of the terms.  2 d flops in
 // 64 bits for every query block and key block are far less than what the attention does with the lists.
+#include <type_traits>
+
 #include "block_attention.hpp"
 
 namespace lemo {
@@ -87,102 +89,196 @@ __device__ __forceinline__ unsigned long long score_key(double s) {
 
 
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void select_blocks_kernel(BlockSelectParams p) {
-    constexpr int E = KeyPiece<T>::E, LANES = D / E;     // lanes of a row when the queries are added up
-    constexpr int TEAMS = 256 / LANES, PER = D / 16;     // (scores: 16 lanes a block, PER values each)
+// the sum over the 16 lanes of a row, in every lane: four rotations within the row
+template <int BY> __device__ __forceinline__ double rotated(double v) {
+    const unsigned long long u = __double_as_longlong(v);
+    const int lo = __builtin_amdgcn_update_dpp(0, (int)u, 0x120 + BY, 0xf, 0xf, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), 0x120 + BY, 0xf, 0xf, false);
+    return __longlong_as_double((unsigned long long)(unsigned)hi << 32 | (unsigned)lo);
+}
+__device__ __forceinline__ double row_total(double v) {
+    v += rotated<8>(v);
+    v += rotated<4>(v);
+    v += rotated<2>(v);
+    return v + rotated<1>(v);
+}
+
+// A workgroup makes the lists of RB query blocks of one group.
+//   1  the queries of a list are added up: teams of lanes that hold a row of 16-byte pieces, several to a list where RB is small
+//   2  scores.  16 lists: 16 lists by 16 key blocks a chain of 64-bit MFMAs (v_mfma_f64_16x16x4: lane l holds row l % 16, one value
+//      of the contraction, the (l / 16)-th; the result's register i is row 4 i + l / 16), at the rate of the vector unit but with
+//      no sums across lanes.  Fewer lists would leave its rows empty: 16 lanes a key block, vector arithmetic.
+//   3  a wave a list: the highest threshold that T scores reach, bit by bit, in the upper halves of the scores first, whose 20
+//      mantissa bits nearly always tell them apart; then the blocks at or above it, in order
+typedef __attribute__((ext_vector_type(4))) double f64x4;
+constexpr int SEL_LEAST = 512, SEL_LDS = 32 << 10;
+
+template <typename T, int D, int RB, int THREADS> struct SelGeo {
+    static constexpr int E = KeyPiece<T>::E, LANES = D / E, TEAMS = THREADS / LANES, TPL = TEAMS > RB ? TEAMS / RB : 1;  // teams a list
+    static constexpr int PITCH = D + 2;                                                                          // of a list's sums
+    static constexpr int SUMS = RB * PITCH * 8, SCRATCH = RB * TPL * D * 8;
+    static constexpr int lds(int nb) { return SUMS + (RB * nb * 8 > SCRATCH ? RB * nb * 8 : SCRATCH); }
+};
+
+template <typename T, int D, int RB, int THREADS>
+__global__ __launch_bounds__(THREADS) void select_blocks_kernel(BlockSelectParams p) {
+    using Geo = SelGeo<T, D, RB, THREADS>;
+    constexpr int WAVES = THREADS / 64;
+    constexpr int E = Geo::E, TPL = Geo::TPL;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    double* const total = reinterpret_cast<double*>(smem);                      // [TEAMS][D], then [D]
-    unsigned long long* const keys = reinterpret_cast<unsigned long long*>(smem + TEAMS * D * 8);
-    const int g = blockIdx.x % p.H_kv, tid = threadIdx.x, lane = tid & 63;
-    const long long qb = blockIdx.x / p.H_kv;
+    __shared__ int counts[RB], owns[RB];
+    double* const sums = reinterpret_cast<double*>(smem);                                  // [RB][PITCH]
+    double* const scratch = reinterpret_cast<double*>(smem + Geo::SUMS);                    // [RB * TPL][D]; then
+    unsigned long long* const keys = reinterpret_cast<unsigned long long*>(smem + Geo::SUMS);  // [RB][nb]
+    const int g = blockIdx.x % p.H_kv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const long long qb0 = (long long)(blockIdx.x / p.H_kv) * RB;
     const bool causal = (p.flags & LEMO_CAUSAL) != 0;
-    const int S = p.lengths ? min(max(p.lengths[qb], 0), p.S_k) : p.S_k;
-    const long long pos0 = p.lengths ? S - 1 : p.q_start + qb * p.bq;
-    const int queries = (int)min((long long)p.bq, p.S_q - qb * p.bq), rows = queries * p.G;
-    const long long last = min(pos0 + queries - 1, (long long)S - 1);
-    const int nb = (S + p.b - 1) / p.b;
-    const int count = S <= 0 ? 0 : causal ? (int)min((long long)nb, last / p.b + 1) : nb;  // candidates: blocks that begin before the last query ends
-    const int own0 = causal ? (int)min(pos0 / p.b, (long long)nb) : nb;                     // causal: blocks from here on hold a query
-    int* const out = p.blocks + (qb * p.H_kv + g) * p.T;
-    if (count <= 0) {  // (uniform) no keys
-        for (int e = tid; e < p.T; e += 256) out[e] = -1;
-        return;
+    const int S = p.lengths ? min(max(p.lengths[qb0], 0), p.S_k) : p.S_k;  // (single tokens: RB = 1)
+    auto queries_of = [&](long long qb) { return (int)max(0ll, min((long long)p.bq, p.S_q - qb * p.bq)); };
+    if (tid < RB) {
+        const long long qb = qb0 + tid, pos0 = p.lengths ? S - 1 : p.q_start + qb * p.bq;
+        const int queries = queries_of(qb), nb = (S + p.b - 1) / p.b;
+        const long long last = min(pos0 + queries - 1, (long long)S - 1);
+        // candidates: blocks that begin before the last query ends; causal: those from `owns` on hold a query
+        counts[tid] = S <= 0 || queries == 0 ? 0 : causal ? (int)min((long long)nb, last / p.b + 1) : nb;
+        owns[tid] = causal ? (int)min(pos0 / p.b, (long long)nb) : nb;
     }
-    {
-        const int team = tid / LANES, c = tid % LANES * E;
+    for (int u = tid / Geo::LANES; u < RB * TPL; u += Geo::TEAMS) {
+        const long long qb = qb0 + u / TPL;
+        const int rows = queries_of(qb) * p.G, c = tid % Geo::LANES * E;
+        const char* const base = reinterpret_cast<const char*>(p.Q) + (qb * p.bq * p.q_ts + (long long)g * p.G * p.q_hs + c) * (16 / E);
         double sum[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] = 0.0;
-        for (int r = team; r < rows; r += TEAMS) {
-            const char* at = reinterpret_cast<const char*>(p.Q) + ((qb * p.bq + r / p.G) * p.q_ts + (long long)(g * p.G + r % p.G) * p.q_hs + c) * (16 / E);
+#pragma unroll 8
+        for (int r = u % TPL; r < rows; r += TPL) {
+            const int i = r / p.G;
             float x[E];
-            KeyPiece<T>::get(*reinterpret_cast<const u32x4*>(at), x);
+            KeyPiece<T>::get(*reinterpret_cast<const u32x4*>(base + (i * p.q_ts + (long long)(r - i * p.G) * p.q_hs) * (16 / E)), x);
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[e] += (double)x[e];
         }
 #pragma unroll
-        for (int e = 0; e < E; ++e) total[team * D + c + e] = sum[e];
-        __syncthreads();
-        double all = 0.0;
-        if (tid < D)
-            for (int t = 0; t < TEAMS; ++t) all += total[t * D + tid];
-        __syncthreads();
-        if (tid < D) total[tid] = all;
-        __syncthreads();
+        for (int e = 0; e < E; ++e) scratch[u * D + c + e] = sum[e];
     }
-    {
-        const int l16 = tid & 15;
-        const float* const means = p.means + (p.lengths ? qb * p.means_ss : 0) + (long long)g * D;
-        double q[PER];
+    __syncthreads();
+    for (int u = tid; u < RB * D; u += THREADS) {
+        const int list = u / D, c = u % D;
+        double all = scratch[list * TPL * D + c];
+        for (int t = 1; t < TPL; ++t) all += scratch[(list * TPL + t) * D + c];
+        sums[list * Geo::PITCH + c] = all;
+    }
+    __syncthreads();
+    int most = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) q[i] = total[(i / 4 * 16 + l16) * 4 + i % 4];
-        for (int n0 = 0; n0 < count; n0 += 16) {
-            const int n = n0 + (tid >> 4);
-            double s = 0.0;
-            if (n < count && n < own0) {
-                const float* at = means + (long long)n * p.H_kv * D;
+    for (int r = 0; r < RB; ++r) most = max(most, counts[r]);
+    const float* const means = p.means + (p.lengths ? qb0 * p.means_ss : 0) + (long long)g * D;
+    if constexpr (RB < 16) {
+        constexpr int PER = D / 16;  // 16 lanes a block, PER columns each
+        const int l16 = lane & 15;
+        double q[RB][PER];
 #pragma unroll
-                for (int i = 0; i < PER; i += 4) {
-                    const f32x4 m = *reinterpret_cast<const f32x4*>(at + (i / 4 * 16 + l16) * 4);
+        for (int r = 0; r < RB; ++r)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s = fma(q[i + e], (double)m[e], s);
+            for (int i = 0; i < PER; ++i) q[r][i] = sums[r * Geo::PITCH + (i / 4 * 16 + l16) * 4 + i % 4];
+        constexpr int AHEAD = RB == 1 ? 4 : 2;  // blocks whose means are under way together
+        for (int n0 = wave * 4; n0 < most; n0 += AHEAD * WAVES * 4) {
+            f32x4 m[AHEAD][PER / 4];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                for (int i = 0; i < PER / 4; ++i)
+                    m[k][i] = *reinterpret_cast<const f32x4*>(means + (long long)min(n0 + k * WAVES * 4 + (lane >> 4), most - 1) * p.H_kv * D + l16 * 4 + i * 64);
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int n = n0 + k * WAVES * 4 + (lane >> 4);
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    double s = 0.0;
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) s = fma(q[r][i], (double)m[k][i / 4][i % 4], s);
+                    s = row_total(s);
+                    if (l16 == 0 && n < counts[r]) keys[r * p.nb + n] = n >= owns[r] ? ~0ull : score_key(s);
                 }
             }
+        }
+    } else {
+        const int l16 = lane & 15, q4 = lane >> 4;
+        double a[D / 4];  // MFMA 4 j + s contracts columns 16 j + 4 (l / 16) + s
 #pragma unroll
-            for (int x = 1; x < 16; x <<= 1) s += __shfl_xor(s, x);
-            if (l16 == 0 && n < count) keys[n] = n >= own0 ? ~0ull : score_key(s);
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) a[4 * j + s] = l16 < RB ? sums[l16 * Geo::PITCH + 16 * j + 4 * q4 + s] : 0.0;
+        for (int n0 = wave * 16; n0 < most; n0 += WAVES * 16) {
+            const int n = min(n0 + l16, most - 1);
+            f32x4 m[D / 16];
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) m[j] = *reinterpret_cast<const f32x4*>(means + (long long)n * p.H_kv * D + 4 * q4 + 16 * j);
+            f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(a[4 * j + s], (double)m[j][s], acc, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int list = 4 * i + q4;
+                if (list < RB && n0 + l16 < counts[list]) keys[list * p.nb + n0 + l16] = n0 + l16 >= owns[list] ? ~0ull : score_key(acc[i]);
+            }
         }
     }
     __syncthreads();
-    if (tid >= 64) return;
-    // the highest threshold that T keys reach, bit by bit; done when exactly T reach it
-    unsigned long long cut = 0;
-    const int wanted = min(p.T, count);
-    bool exact = count <= p.T;
-    if (exact) cut = 1;
-    for (int bit = 63; bit >= 0 && !exact; --bit) {
-        const unsigned long long mark = cut | 1ull << bit;
-        int reach = 0;
-        for (int n = lane; n < count + lane; n += 64) reach += __popcll(__ballot(n < count && keys[n] >= mark));
-        if (reach >= wanted) cut = mark;
-        exact = reach == wanted;
-    }
-    int above = 0;
-    if (!exact)
-        for (int n = lane; n < count + lane; n += 64) above += __popcll(__ballot(n < count && keys[n] > cut));
-    int ties = wanted - above, at = 0;  // of the keys that equal the threshold, the first ones
-    for (int n = lane; n < count + lane; n += 64) {
-        const unsigned long long k = n < count ? keys[n] : 0;
+    for (int list = wave; list < RB; list += WAVES) {
+        if (queries_of(qb0 + list) == 0) break;
+        const int count = counts[list], wanted = min(p.T, count);
+        const unsigned long long* const mine = keys + list * p.nb;
+        int* const out = p.blocks + ((qb0 + list) * p.H_kv + g) * p.T;
+        unsigned long long cut = 1;
+        bool exact = count <= p.T;
+        if (!exact) {
+            unsigned top = 0;
+            auto halves = [&](auto held) {  // upper halves of the first scores stay in registers
+                constexpr int HELD = decltype(held)::value;
+                unsigned high[HELD];
+#pragma unroll
+                for (int i = 0; i < HELD; ++i) high[i] = i * 64 + lane < count ? (unsigned)(mine[i * 64 + lane] >> 32) : 0;
+                for (int bit = 31; bit >= 0 && !exact; --bit) {
+                    const unsigned mark = top | 1u << bit;
+                    int reach = 0;
+#pragma unroll
+                    for (int i = 0; i < HELD; ++i) reach += (int)__popcll(__ballot(high[i] >= mark));
+                    for (int n = HELD * 64 + lane; n < count + lane; n += 64) reach += (int)__popcll(__ballot(n < count && (unsigned)(mine[n] >> 32) >= mark));
+                    if (reach >= wanted) top = mark;
+                    exact = reach == wanted;
+                }
+            };
+            if (count <= 128) halves(std::integral_constant<int, 2>{});
+            else halves(std::integral_constant<int, 8>{});
+            cut = (unsigned long long)top << 32;
+            for (int bit = 31; bit >= 0 && !exact; --bit) {
+                const unsigned long long mark = cut | 1ull << bit;
+                int reach = 0;
+                for (int n = lane; n < count + lane; n += 64) reach += (int)__popcll(__ballot(n < count && mine[n] >= mark));
+                if (reach >= wanted) cut = mark;
+                exact = reach == wanted;
+            }
+        }
+        int ties = 0, at = 0;  // of the keys that equal the threshold, the first ones
+        if (!exact) {
+            ties = wanted;
+            for (int n = lane; n < count + lane; n += 64) ties -= (int)__popcll(__ballot(n < count && mine[n] > cut));
+        }
         const unsigned long long before = (1ull << lane) - 1;
-        const unsigned long long equal = __ballot(!exact && k == cut);
-        const bool taken = exact ? k >= cut : k > cut || (k == cut && (int)__popcll(equal & before) < ties);
-        ties = max(0, ties - (int)__popcll(equal));
-        const unsigned long long all = __ballot(taken);
-        if (taken) out[at + __popcll(all & before)] = n;
-        at += __popcll(all);
+        for (int n = lane; n < count + lane; n += 64) {
+            const unsigned long long k = n < count ? mine[n] : 0;
+            const unsigned long long equal = __ballot(!exact && k == cut);
+            const bool taken = exact ? k >= cut : k > cut || (k == cut && (int)__popcll(equal & before) < ties);
+            ties = max(0, ties - (int)__popcll(equal));
+            const unsigned long long all = __ballot(taken);
+            if (taken) out[at + (int)__popcll(all & before)] = n;
+            at += (int)__popcll(all);
+        }
+        for (int e = at + lane; e < p.T; e += 64) out[e] = -1;
     }
-    for (int e = at + lane; e < p.T; e += 64) out[e] = -1;
 }
 
 int launch_block_means(const void* K, long long S, int H_kv, int d, lemo_dtype_t dt, long long k_ts, long long k_hs, int b, float* means, hipStream_t st) {
@@ -203,12 +299,25 @@ int launch_block_means_step(const void* K, const int* lengths, int B, long long 
     return (int)hipGetLastError();
 }
 
-template <typename T, int D> static int run_select_blocks(const BlockSelectParams& p, hipStream_t st) {
-    constexpr int SUMS = 256 / (D / KeyPiece<T>::E) * D * 8;
-    static const int err = raise_lds_limits({{reinterpret_cast<const void*>(&select_blocks_kernel<T, D>), SUMS + MAX_LISTED_BLOCKS * 8}});
-    if (err) return err;
-    hipLaunchKernelGGL((select_blocks_kernel<T, D>), dim3((unsigned)((long long)p.n_qb * p.H_kv)), dim3(256), SUMS + p.nb * 8, st, p);
+template <typename T, int D, int RB, int THREADS> static int run_select_lists(const BlockSelectParams& p, hipStream_t st) {
+    const long long teams = ((long long)p.n_qb + RB - 1) / RB;
+    hipLaunchKernelGGL((select_blocks_kernel<T, D, RB, THREADS>), dim3((unsigned)(teams * p.H_kv)), dim3(THREADS), (SelGeo<T, D, RB, THREADS>::lds(p.nb)), st, p);
     return (int)hipGetLastError();
+}
+
+template <typename T, int D> static int run_select_blocks(const BlockSelectParams& p, hipStream_t st) {
+    static const int err = raise_lds_limits({{reinterpret_cast<const void*>(&select_blocks_kernel<T, D, 1, 256>), SelGeo<T, D, 1, 256>::lds(MAX_LISTED_BLOCKS)},
+                                             {reinterpret_cast<const void*>(&select_blocks_kernel<T, D, 1, 1024>), SelGeo<T, D, 1, 1024>::lds(MAX_LISTED_BLOCKS)}});
+    if (err) return err;
+    const long long lists = (long long)p.n_qb * p.H_kv;
+    if (p.lengths || lists <= 256) return run_select_lists<T, D, 1, 1024>(p, st);
+    // lists of few rows: the more of them a workgroup makes, the less often it reads the means; their scores take LDS, and there have
+    // to be workgroups
+    if (p.bq * p.G < 64) {
+        if (lists >= 16 * SEL_LEAST && p.nb * 16 * 8 <= SEL_LDS) return run_select_lists<T, D, 16, 256>(p, st);
+        if (lists >= 4 * SEL_LEAST && p.nb * 4 * 8 <= SEL_LDS) return run_select_lists<T, D, 4, 256>(p, st);
+    }
+    return run_select_lists<T, D, 1, 256>(p, st);
 }
 
 int launch_select_blocks(const BlockSelectParams& p, lemo_dtype_t dt, hipStream_t st) {

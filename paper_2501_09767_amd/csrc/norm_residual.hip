@@ -204,14 +204,16 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_residual_kernel(No
 // they stand follows from the order.
 enum { SUM_W_NEXT = 1, SUM_B_NEXT = 2, SUM_W_POST = 4, SUM_B_POST = 8, SUM_GATE = 16 };
 
-template <typename T, int THREADS, int NP>
+// POST: there is a norm of the block's result; SHARED: all rows share the gate.  What a call does not have takes no registers.
+template <typename T, int THREADS, int NP, bool POST, bool SHARED>
 __global__ __launch_bounds__(THREADS) void norm_residual_grad_kernel(NormGradParams p) {
     constexpr int E = Piece<T>::E;
     __shared__ float lds[4 * (THREADS / 64)];
     int turn = 0;
     const int t = threadIdx.x;
     const float inv_C = 1.f / (float)p.C;
-    const bool next = p.next != LEMO_NORM_NONE, post = p.post != LEMO_NORM_NONE;
+    const bool next = p.next != LEMO_NORM_NONE;
+    constexpr bool post = POST;
     float w_next_sum[NP][E], b_next_sum[NP][E], w_post_sum[NP][E], b_post_sum[NP][E], gate_sum[NP][E];
 #pragma unroll
     for (int i = 0; i < NP; ++i)
@@ -309,10 +311,12 @@ __global__ __launch_bounds__(THREADS) void norm_residual_grad_kernel(NormGradPar
                 }
                 const float bdr = p.beta * dr[i][e], dg = bdr * u[e] * slope[e];
                 du[i][e] = p.gate ? bdr * gg[e] : bdr;
-                gate_sum[i][e] += dg;
+                if constexpr (SHARED) gate_sum[i][e] += dg;
                 u[e] = dg;
-                w_post_sum[i][e] = fmaf(du[i][e], yh[i][e], w_post_sum[i][e]);
-                b_post_sum[i][e] += du[i][e];
+                if constexpr (POST) {
+                    w_post_sum[i][e] = fmaf(du[i][e], yh[i][e], w_post_sum[i][e]);
+                    b_post_sum[i][e] += du[i][e];
+                }
                 du[i][e] *= wv;
                 s[0] = fmaf(du[i][e], yh[i][e], s[0]);
                 s[1] += du[i][e];
@@ -353,16 +357,21 @@ __global__ __launch_bounds__(THREADS) void norm_residual_grad_kernel(NormGradPar
     leave(SUM_GATE, gate_sum);
 }
 
-// Adds the workgroups' parts: 64 columns a workgroup, its four waves take every fourth part, in order; no parts give zeros.
-__global__ __launch_bounds__(256) void norm_sums_kernel(const float* __restrict__ parts, int count, int planes, int C, NormSums out) {
-    __shared__ float share[4][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6, plane = blockIdx.y;
+// Adds the workgroups' parts: 64 columns a workgroup, its 16 waves take every sixteenth part, in order; no parts give zeros.
+__global__ __launch_bounds__(1024) void norm_sums_kernel(const float* __restrict__ parts, int count, int planes, int C, NormSums out) {
+    __shared__ float share[16][64];
+    const int lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane, wave = threadIdx.x >> 6, plane = blockIdx.y;
     float s = 0.f;
     if (c < C)
-        for (int n = wave; n < count; n += 4) s += parts[((long long)n * planes + plane) * C + c];
-    share[wave][threadIdx.x & 63] = s;
+#pragma unroll 8
+        for (int n = wave; n < count; n += 16) s += parts[((long long)n * planes + plane) * C + c];
+    share[wave][lane] = s;
     __syncthreads();
-    if (wave == 0 && c < C) out.to[plane][c] = (share[0][threadIdx.x] + share[1][threadIdx.x]) + (share[2][threadIdx.x] + share[3][threadIdx.x]);
+    if (wave != 0 || c >= C) return;
+    s = share[0][lane];
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += share[w][lane];
+    out.to[plane][c] = s;
 }
 
 template <typename T, int TPR, int NP> static int run_norm(const NormParams& p, hipStream_t st) {
@@ -386,10 +395,15 @@ int launch_norm_residual(const NormParams& p, lemo_dtype_t dt, hipStream_t st) {
     return dt == LEMO_BF16 ? go(bf16_t{}) : go(float{});
 }
 
-int norm_grad_parts(int64_t M) { return (int)(M < 512 ? M : 512); }
+// Workgroups: two for every CU, two rows each at least where there are fewer rows
+int norm_grad_parts(int64_t M) { return (int)(M >= 1024 ? 512 : M >= 256 ? M / 2 : M < 128 ? M : 128); }
 
 template <typename T, int THREADS, int NP> static int run_norm_grad(const NormGradParams& p, int parts, hipStream_t st) {
-    hipLaunchKernelGGL((norm_residual_grad_kernel<T, THREADS, NP>), dim3((unsigned)parts), dim3(THREADS), 0, st, p);
+    const bool post = p.post != LEMO_NORM_NONE, shared = (p.sums & SUM_GATE) != 0;
+    if (post && shared) hipLaunchKernelGGL((norm_residual_grad_kernel<T, THREADS, NP, true, true>), dim3((unsigned)parts), dim3(THREADS), 0, st, p);
+    else if (post) hipLaunchKernelGGL((norm_residual_grad_kernel<T, THREADS, NP, true, false>), dim3((unsigned)parts), dim3(THREADS), 0, st, p);
+    else if (shared) hipLaunchKernelGGL((norm_residual_grad_kernel<T, THREADS, NP, false, true>), dim3((unsigned)parts), dim3(THREADS), 0, st, p);
+    else hipLaunchKernelGGL((norm_residual_grad_kernel<T, THREADS, NP, false, false>), dim3((unsigned)parts), dim3(THREADS), 0, st, p);
     return (int)hipGetLastError();
 }
 
@@ -407,7 +421,7 @@ int launch_norm_residual_grad(NormGradParams p, float* dw_next, float* db_next, 
         }
     auto go = [&](auto tag) {
         using T = decltype(tag);
-        constexpr int NP = 16 / Piece<T>::E;  // 16 columns a thread: five sums of each are held in registers
+        constexpr int NP = 16 / Piece<T>::E;  // 16 columns a thread: the sums of each are held in registers
         if (pieces <= 64 * NP) return run_norm_grad<T, 64, NP>(p, parts, st);
         if (pieces <= 128 * NP) return run_norm_grad<T, 128, NP>(p, parts, st);
         if (pieces <= 256 * NP) return run_norm_grad<T, 256, NP>(p, parts, st);
@@ -419,7 +433,7 @@ int launch_norm_residual_grad(NormGradParams p, float* dw_next, float* db_next, 
         if (rc) return rc;
     }
     if (p.planes == 0) return 0;
-    hipLaunchKernelGGL(norm_sums_kernel, dim3((unsigned)((p.C + 63) / 64), (unsigned)p.planes), dim3(256), 0, st, p.parts, parts, p.planes, p.C, out);
+    hipLaunchKernelGGL(norm_sums_kernel, dim3((unsigned)((p.C + 63) / 64), (unsigned)p.planes), dim3(1024), 0, st, p.parts, parts, p.planes, p.C, out);
     return (int)hipGetLastError();
 }
 
