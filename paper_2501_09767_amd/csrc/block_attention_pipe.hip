@@ -65,15 +65,18 @@ __global__ __launch_bounds__(256, 1) void block_attention_pipe_kernel(BlockAttnP
         }
     }
     const bool active = row0 < rows;
-    // a stage is hot if all of its subtiles end at or before the first row's limit (a second subtile of rows that are not there is masked
-    // by nothing: its rows are not stored)
-    const int hot_last = active ? clean[0] : -1;
     __syncthreads();
     const int s_begin = (int)((long long)listed * share / p.n_parts), n_sub = (int)((long long)listed * (share + 1) / p.n_parts) - s_begin;
-    const int nstage = (n_sub + 3) / 4;
     const int* const keys = all_keys + s_begin;
-    int n_hot = 0;
-    for (int s0 = 0; s0 < n_sub; s0 += 64) n_hot += (int)__popcll(__ballot(s0 + lane < n_sub && keys[s0 + lane] + 31 <= hot_last));
+    // subtiles that no row of the workgroup needs a mask for, the first ones of the list.  All but the first stage's are hot: that takes as
+    // few as leave whole stages, and the last stages hold what needs a mask
+    const int wg_clean = rt * ROWS < rows ? limit_of(rt * ROWS) : -1;
+    int n_clean = 0;
+    for (int s0 = 0; s0 < n_sub; s0 += 64) n_clean += (int)__popcll(__ballot(s0 + lane < n_sub && keys[s0 + lane] + 31 <= wg_clean));
+    const int head = n_clean > 0 ? min((n_clean - 1) % 4 + 1, n_sub) : min(4, n_sub);  // subtiles of the first stage
+    const int nstage = (n_sub - head + 3) / 4 + (n_sub > 0);
+    auto stage_begin = [&](int t) { return t == 0 ? 0 : head + 4 * (t - 1); };
+    auto stage_end = [&](int t) { return min(head + 4 * t, n_sub); };
 
     // ---- staging: LDS-direct loads.  Load n (0..15) of a wave: subtile n / 2 (K, then V), rows ((n & 1) * 4 + wave) * 4 + lane / 16
     const char* const kbase = reinterpret_cast<const char*>(p.K + (long long)g * p.k_hs);
@@ -91,8 +94,8 @@ __global__ __launch_bounds__(256, 1) void block_attention_pipe_kernel(BlockAttnP
     auto take_keys = [&](int t) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const int at = t * 4 + s;
-            want[s] = at < n_sub ? __builtin_amdgcn_readfirstlane(keys[min(at, n_sub - 1)]) : S;
+            const int at = stage_begin(t) + s;
+            want[s] = at < stage_end(t) ? __builtin_amdgcn_readfirstlane(keys[min(at, n_sub - 1)]) : S;
         }
     };
     auto stage_load_one = [&](int n, int buf) {
@@ -178,8 +181,8 @@ __global__ __launch_bounds__(256, 1) void block_attention_pipe_kernel(BlockAttnP
         if (active) {
 #pragma unroll 1
             for (int ks = sub0; ks < sub0 + SHARE; ++ks) {
-                if (t * 4 + ks >= n_sub) break;
-                const int key = __builtin_amdgcn_readfirstlane(keys[t * 4 + ks]);
+                if (stage_begin(t) + ks >= stage_end(t)) break;
+                const int key = __builtin_amdgcn_readfirstlane(keys[stage_begin(t) + ks]);
                 if (key > reach[0] && key > reach[1]) break;
                 u32x4 kfr[NCH], vfr[8];
 #pragma unroll
@@ -256,7 +259,7 @@ __global__ __launch_bounds__(256, 1) void block_attention_pipe_kernel(BlockAttnP
         settle_stage();
         take_keys(t + 2);
     };
-    const int t_hot = frozen && active ? max(1, min(n_hot / 4, nstage)) : 1;
+    const int t_hot = frozen && active ? max(1, (n_clean - head) / 4 + 1) : 1;
     if (nstage > 0) slow_stage(0);
     if (t_hot > 1) {
 #pragma unroll
