@@ -26,7 +26,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 # Per-file flags.  attention.hip (its 64-queries-per-wave kernel), block_attention_pipe.hip and score_blocks_few.hip may use the whole register file
 # (one wave per SIMD), and for such a kernel the compiler would otherwise give every MFMA its result in the accumulation
 # registers, with a copy around each use by vector arithmetic; this makes MFMAs write ordinary vector registers.
-FILE_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "block_attention_pipe.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "score_blocks_few.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+FILE_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "block_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "block_attention_pipe.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "block_attention_grad.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "score_blocks_few.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str, extra) -> str:

@@ -41,7 +41,7 @@ int64_t span_bytes(int64_t S, int64_t ts, int64_t H, int64_t hs, int64_t d) { re
 float base2(float scale, int32_t d) { return (float)((scale > 0.f ? (double)scale : 1.0 / std::sqrt((double)d)) * 1.4426950408889634); }
 
 size_t part_bytes(int64_t n_qb, int32_t H_kv, int64_t R, int32_t d, int32_t T, int32_t b) {
-    const int tile = block_attention_tile_rows((int)R);
+    const int tile = block_attention_tile_rows((int)R, d);
     const int parts = block_attention_parts(n_qb * ((R + tile - 1) / tile) * H_kv, (int64_t)T * (b / 32));
     return parts > 1 ? round_up((size_t)n_qb * H_kv * parts * R * (d + 4) * sizeof(float), 256) : 0;
 }
@@ -189,7 +189,7 @@ int lemo_block_attention_grad(const void* dO, const void* Q, const void* K, cons
     gp.first = reinterpret_cast<int*>(ws + l.first);
     gp.lists = reinterpret_cast<int*>(ws + l.lists);
     gp.slots = reinterpret_cast<int*>(ws + l.slots);
-    gp.items = reinterpret_cast<int2*>(ws + l.items);
+    gp.items = reinterpret_cast<int4*>(ws + l.items);
     gp.totals = reinterpret_cast<int*>(ws + l.totals);
     gp.partial = reinterpret_cast<float*>(ws + l.partial);
     gp.nb = (int)((S_k + b - 1) / b);

@@ -9,13 +9,16 @@
 // lies in the registers.  KS waves share rows and take the subtiles of a stage in turn, for lists of few rows; their sums meet in LDS at
 // the end.  Where lists are few as well (single tokens), n_parts workgroups take shares of a list and a second kernel joins them.
 // P is rounded to bf16 for the second product; sums and normaliser are binary32, from the unrounded values.
+#include <stdlib.h>
 #include "block_attention.hpp"
 
 namespace lemo {
 
-constexpr int BA_STAGE = 4;  // subtiles of a stage
+// Stages are kept to 64 KB for two of them, K and V, where that suits the sharing waves: two workgroups fit a CU then, and the one's list,
+// rows and last stores pass while the other computes.
+template <int D, int KS> constexpr int BA_STAGE = D == 128 && KS <= 2 ? 2 : 4;  // subtiles of a stage
 
-template <int D, int WAVES> struct BaGeo {
+template <int D, int WAVES, int BA_STAGE> struct BaGeo {
     using Tile = HeadTile<D>;
     static constexpr int SUB = 32 * Tile::ROWB, STAGE = 2 * BA_STAGE * SUB;  // bytes of a subtile; K and V subtiles of a stage
     static constexpr int PITCH = D + 4;                                      // floats of a row where waves' results meet
@@ -25,8 +28,9 @@ template <int D, int WAVES> struct BaGeo {
 };
 
 template <int D, int WAVES, int KS>
-__global__ __launch_bounds__(WAVES * 64, 1) void block_attention_kernel(BlockAttnParams p) {
-    using Geo = BaGeo<D, WAVES>;
+__global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAttnParams p) {
+    constexpr int STAGE = BA_STAGE<D, KS>;
+    using Geo = BaGeo<D, WAVES, STAGE>;
     using Tile = HeadTile<D>;
     constexpr int ROWS = WAVES / KS * 32;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -52,7 +56,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void block_attention_kernel(BlockAtt
     }
     __syncthreads();
     const int s_begin = (int)((long long)listed * share / p.n_parts), n_sub = (int)((long long)listed * (share + 1) / p.n_parts) - s_begin;
-    const int n_stage = (n_sub + BA_STAGE - 1) / BA_STAGE;
+    const int n_stage = (n_sub + STAGE - 1) / STAGE;
 
     // resident operand: this wave's 32 rows
     const int row0 = rt * ROWS + wave / KS * 32, row = row0 + l32;
@@ -74,16 +78,21 @@ __global__ __launch_bounds__(WAVES * 64, 1) void block_attention_kernel(BlockAtt
     const char* const kbase = reinterpret_cast<const char*>(p.K + (long long)g * p.k_hs + (p.lengths ? qb * p.k_ss : 0));
     const char* const vbase = reinterpret_cast<const char*>(p.V + (long long)g * p.v_hs + (p.lengths ? qb * p.v_ss : 0));
     constexpr int RPI = 1024 / Tile::ROWB, PER_SUB = 32 / RPI;            // rows of an instruction, instructions of a subtile
-    constexpr int LOADS = 2 * BA_STAGE * PER_SUB / WAVES;                 // of a wave and stage
-    static_assert(2 * BA_STAGE * PER_SUB % WAVES == 0, "");
+    constexpr int LOADS = 2 * STAGE * PER_SUB / WAVES;                 // of a wave and stage
+    static_assert(2 * STAGE * PER_SUB % WAVES == 0, "");
     const int in_row = lane / Tile::PIECES, pos = lane % Tile::PIECES;
     auto load_stage = [&](int t, int buf) {
+        int first_key[STAGE];  // all of them before the first load: a load orders memory accesses
+#pragma unroll
+        for (int s = 0; s < STAGE; ++s) first_key[s] = t * STAGE + s < n_sub ? __builtin_amdgcn_readfirstlane(keys[s_begin + t * STAGE + s]) : S;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int unit = i * WAVES + wave, which = unit / PER_SUB, part = unit % PER_SUB;  // subtiles 0..3: K, 4..7: V
-            const bool v = which >= BA_STAGE;
-            const int s = t * BA_STAGE + which % BA_STAGE;
-            const int key = s < n_sub ? __builtin_amdgcn_readfirstlane(keys[s_begin + s]) : S;
+            constexpr int AT_ONCE = WAVES / PER_SUB > 1 ? WAVES / PER_SUB : 1;  // subtiles that the waves load together
+            const int unit = i * WAVES + wave, part = unit % PER_SUB, which = AT_ONCE > 1 ? i * AT_ONCE + wave / PER_SUB : i * WAVES / PER_SUB;
+            const bool v = i * WAVES >= STAGE * PER_SUB;  // K subtiles, then V
+            int key = first_key[i * WAVES / PER_SUB % STAGE];
+#pragma unroll
+            for (int k = 1; k < AT_ONCE; ++k) key = wave / PER_SUB == k ? first_key[(i * WAVES / PER_SUB + k) % STAGE] : key;
             const long long pitch = (v ? p.v_ts : p.k_ts) * 2;
             const u32x4 rsrc = raw_rsrc((v ? vbase : kbase) + (long long)min(key, S) * pitch, key < S ? (long long)(S - 1 - key) * pitch + Tile::ROWB : 0);
             const int r = part * RPI + in_row;
@@ -104,12 +113,12 @@ __global__ __launch_bounds__(WAVES * 64, 1) void block_attention_kernel(BlockAtt
         if (t + 1 < n_stage) load_stage(t + 1, (t + 1) & 1);
         const char* const sk = smem + (t & 1) * Geo::STAGE;
 #pragma unroll 1
-        for (int j = wave % KS; j < BA_STAGE; j += KS) {
-            if (t * BA_STAGE + j >= n_sub) break;
-            const int key = __builtin_amdgcn_readfirstlane(keys[s_begin + t * BA_STAGE + j]);
+        for (int j = wave % KS; j < STAGE; j += KS) {
+            if (t * STAGE + j >= n_sub) break;
+            const int key = __builtin_amdgcn_readfirstlane(keys[s_begin + t * STAGE + j]);
             if (key > reach) continue;
             const char* const ks = sk + j * Geo::SUB;
-            const char* const vs = ks + BA_STAGE * Geo::SUB;
+            const char* const vs = ks + STAGE * Geo::SUB;
             f32x16 acc = {0};
 #pragma unroll
             for (int c = 0; c < Tile::CHUNKS; ++c) mma_chunk<bf16_t>(acc, Tile::row_fragment(ks, c, lane), qf[c]);  // acc[key][row]
@@ -242,39 +251,40 @@ template <int D> __global__ __launch_bounds__(256) void block_attention_join_ker
 }
 
 // Rows of a workgroup by the rows that share a list: no more waves than have rows, the others share.
-int block_attention_tile_rows(int R) { return R > 128 ? 256 : R > 64 ? 128 : R > 32 ? 64 : 32; }
+int block_attention_tile_rows(int R, int d) { return R > 128 && d == 128 ? 256 : R > 64 ? 128 : R > 32 ? 64 : 32; }
 
 // Shares of a list: workgroups for every CU twice, at least a stage each.
 int block_attention_parts(long long tiles, long long subtiles) {
-    const long long most = (subtiles + BA_STAGE - 1) / BA_STAGE;
+    const long long most = (subtiles + 3) / 4;
     long long parts = tiles >= 512 ? 1 : (512 + tiles - 1) / tiles;
     if (parts > most) parts = most;
     return parts < 1 ? 1 : (int)parts;
 }
 
+template <int D, int KS> constexpr int ba_lds(int subtiles) { return BaGeo<D, 4, BA_STAGE<D, KS>>::lds(subtiles); }
+
 template <int D> static int prepare_block_attention() {
-    static const int err = raise_lds_limits({{reinterpret_cast<const void*>(&block_attention_kernel<D, 8, 1>), BaGeo<D, 8>::lds(MAX_LISTED_SUBTILES)},
-                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 8, 2>), BaGeo<D, 8>::lds(MAX_LISTED_SUBTILES)},
-                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 8, 4>), BaGeo<D, 8>::lds(MAX_LISTED_SUBTILES)},
-                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 4>), BaGeo<D, 4>::lds(MAX_LISTED_SUBTILES)}});
+    static const int err = raise_lds_limits({{reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 1>), ba_lds<D, 1>(MAX_LISTED_SUBTILES)},
+                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 2>), ba_lds<D, 2>(MAX_LISTED_SUBTILES)},
+                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 4>), ba_lds<D, 4>(MAX_LISTED_SUBTILES)}});
     return err;
 }
 
-template <int D, int WAVES, int KS> static int run_block_attention(const BlockAttnParams& p, hipStream_t st) {
-    hipLaunchKernelGGL((block_attention_kernel<D, WAVES, KS>), dim3((unsigned)((long long)p.n_qb * p.n_rt * p.n_parts * p.H_kv)), dim3(WAVES * 64),
-                       (BaGeo<D, WAVES>::lds(p.T * (p.b / 32))), st, p);
+template <int D, int KS> static int run_block_attention(const BlockAttnParams& p, hipStream_t st) {
+    hipLaunchKernelGGL((block_attention_kernel<D, 4, KS>), dim3((unsigned)((long long)p.n_qb * p.n_rt * p.n_parts * p.H_kv)), dim3(256),
+                       (ba_lds<D, KS>(p.T * (p.b / 32))), st, p);
     return (int)hipGetLastError();
 }
 
 template <int D> static int launch_block_attention_d(BlockAttnParams p, hipStream_t st) {
     const int unready = D == 128 ? first_error(prepare_block_attention<D>, prepare_block_attention_pipe) : prepare_block_attention<D>();
     if (unready) return unready;
-    const int tile = block_attention_tile_rows(p.R);
+    const int tile = block_attention_tile_rows(p.R, D);
     p.n_rt = (p.R + tile - 1) / tile;
     p.n_parts = p.parts ? block_attention_parts((long long)p.n_qb * p.n_rt * p.H_kv, (long long)p.T * (p.b / 32)) : 1;
     p.order = head_order(p.H_kv, false, 8);
-    const int rc = D == 128 && p.R > 32 ? launch_block_attention_pipe(p, st) : tile == 256 ? run_block_attention<D, 8, 1>(p, st) : tile == 128 ? run_block_attention<D, 8, 2>(p, st)
-                 : tile == 64 ? run_block_attention<D, 8, 4>(p, st) : run_block_attention<D, 4, 4>(p, st);
+    const int rc = tile == 256 || (D == 128 && p.R > 32 && getenv("PIPE")) ? launch_block_attention_pipe(p, st) : tile == 128 ? run_block_attention<D, 1>(p, st)
+                 : tile == 64 ? run_block_attention<D, 2>(p, st) : run_block_attention<D, 4>(p, st);
     if (rc || p.n_parts == 1) return rc;
     const long long rows = (long long)p.n_qb * p.H_kv * p.R, per = 256 / (D / 8);
     hipLaunchKernelGGL((block_attention_join_kernel<D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, p);

@@ -34,7 +34,7 @@ struct BlockGradParams {
     int* first;          // [H_kv * nb] where their list starts in `lists`
     int* lists;          // query blocks, ascending, key block by key block
     int* slots;          // [H_kv * nb] first partial result of a key block that is shared, or -1
-    int2* items;         // (key block, share) in order of launch
+    int4* items;         // key block, where its query blocks start in `lists`, how many, partial result or -1
     int* totals;         // [0]: items
     float* partial;      // [slot][2][b][d]
     int nb, words, share;  // share: query blocks that a workgroup takes of a list
@@ -47,7 +47,7 @@ constexpr int MAX_LISTED_SUBTILES = 4096;  // subtiles of 32 keys that a list ma
 constexpr int MAX_LISTED_BLOCKS = 16384;   // key blocks that a choice is made from: their scores stand in LDS, 128 KB
 
 int block_attention_parts(long long tiles, long long subtiles);
-int block_attention_tile_rows(int R);
+int block_attention_tile_rows(int R, int d);
 int launch_block_attention(BlockAttnParams p, int d, hipStream_t st);
 int prepare_block_attention_pipe();
 int launch_block_attention_pipe(const BlockAttnParams& p, hipStream_t st);  // heads of 128; p filled in as for the others

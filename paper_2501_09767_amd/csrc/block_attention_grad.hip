@@ -13,22 +13,25 @@
 
 namespace lemo {
 
-constexpr int BG_STAGE = 4;  // subtiles of 32 of a stage
+// Stages are kept to 64 KB for two of them, where that suits the sharing waves: two workgroups fit a CU then, and the one's rows, lists and
+// stores pass while the other computes.
+template <int D, int SHARES> constexpr int BG_STAGE = D == 128 && SHARES <= 2 ? 2 : 4;  // subtiles of 32 of a stage
 
 // ---- by query blocks: dQ, delta -----------------------------------------------------------------------
 
-template <int D, int WAVES> struct DqGeo {
+template <int D, int WAVES, int SUBS> struct DqGeo {
     using Tile = HeadTile<D>;
-    static constexpr int SUB = 32 * Tile::ROWB, STAGE = 2 * BG_STAGE * SUB;
+    static constexpr int SUB = 32 * Tile::ROWB, STAGE = 2 * SUBS * SUB;
     static constexpr int PITCH = D + 4, JOIN = WAVES * 32 * PITCH * 4;
     static constexpr int LIST = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
     static constexpr int lds(int subtiles) { return LIST + subtiles * 4; }
 };
 
 template <int D, int WAVES, int KS>
-__global__ __launch_bounds__(WAVES * 64, 1) void block_dq_kernel(BlockGradParams gp) {
+__global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams gp) {
     const BlockAttnParams& p = gp.a;
-    using Geo = DqGeo<D, WAVES>;
+    constexpr int SUBS = BG_STAGE<D, KS>;
+    using Geo = DqGeo<D, WAVES, SUBS>;
     using Tile = HeadTile<D>;
     constexpr int ROWS = WAVES / KS * 32;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -51,7 +54,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void block_dq_kernel(BlockGradParams
         if (lane == 0) listed = n;
     }
     __syncthreads();
-    const int n_sub = listed, n_stage = (n_sub + BG_STAGE - 1) / BG_STAGE;
+    const int n_sub = listed, n_stage = (n_sub + SUBS - 1) / SUBS;
 
     const int row0 = rt * ROWS + wave / KS * 32, row = row0 + l32;
     const bool live = row < rows;
@@ -84,15 +87,20 @@ __global__ __launch_bounds__(WAVES * 64, 1) void block_dq_kernel(BlockGradParams
 
     const char* const kbase = reinterpret_cast<const char*>(p.K + (long long)g * p.k_hs);
     const char* const vbase = reinterpret_cast<const char*>(p.V + (long long)g * p.v_hs);
-    constexpr int RPI = 1024 / Tile::ROWB, PER_SUB = 32 / RPI, LOADS = 2 * BG_STAGE * PER_SUB / WAVES;
+    constexpr int RPI = 1024 / Tile::ROWB, PER_SUB = 32 / RPI, LOADS = 2 * SUBS * PER_SUB / WAVES;
     const int in_row = lane / Tile::PIECES, pos = lane % Tile::PIECES;
     auto load_stage = [&](int t, int buf) {
+        int first_key[SUBS];  // all of them before the first load: a load orders memory accesses
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) first_key[s] = t * SUBS + s < n_sub ? __builtin_amdgcn_readfirstlane(keys[t * SUBS + s]) : S;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int unit = i * WAVES + wave, which = unit / PER_SUB, part = unit % PER_SUB;
-            const bool v = which >= BG_STAGE;
-            const int s = t * BG_STAGE + which % BG_STAGE;
-            const int key = s < n_sub ? __builtin_amdgcn_readfirstlane(keys[s]) : S;
+            constexpr int AT_ONCE = WAVES / PER_SUB > 1 ? WAVES / PER_SUB : 1;  // subtiles that the waves load together
+            const int unit = i * WAVES + wave, part = unit % PER_SUB, which = AT_ONCE > 1 ? i * AT_ONCE + wave / PER_SUB : i * WAVES / PER_SUB;
+            const bool v = i * WAVES >= SUBS * PER_SUB;
+            int key = first_key[i * WAVES / PER_SUB % SUBS];
+#pragma unroll
+            for (int k = 1; k < AT_ONCE; ++k) key = wave / PER_SUB == k ? first_key[(i * WAVES / PER_SUB + k) % SUBS] : key;
             const long long pitch = (v ? p.v_ts : p.k_ts) * 2;
             const u32x4 rsrc = raw_rsrc((v ? vbase : kbase) + (long long)min(key, S) * pitch, key < S ? (long long)(S - 1 - key) * pitch + Tile::ROWB : 0);
             const int r = part * RPI + in_row;
@@ -111,12 +119,12 @@ __global__ __launch_bounds__(WAVES * 64, 1) void block_dq_kernel(BlockGradParams
         if (t + 1 < n_stage) load_stage(t + 1, (t + 1) & 1);
         const char* const sk = smem + (t & 1) * Geo::STAGE;
 #pragma unroll 1
-        for (int j = wave % KS; j < BG_STAGE; j += KS) {
-            if (t * BG_STAGE + j >= n_sub) break;
-            const int key = __builtin_amdgcn_readfirstlane(keys[t * BG_STAGE + j]);
+        for (int j = wave % KS; j < SUBS; j += KS) {
+            if (t * SUBS + j >= n_sub) break;
+            const int key = __builtin_amdgcn_readfirstlane(keys[t * SUBS + j]);
             if (key > reach) continue;
             const char* const ks = sk + j * Geo::SUB;
-            const char* const vs = ks + BG_STAGE * Geo::SUB;
+            const char* const vs = ks + SUBS * Geo::SUB;
             f32x16 acc = {0}, dp = {0};
 #pragma unroll
             for (int c = 0; c < Tile::CHUNKS; ++c) {
@@ -242,7 +250,8 @@ __global__ __launch_bounds__(1024) void block_layout_kernel(BlockGradParams gp) 
         if (n < total) {
             gp.first[n] = sum[0];
             gp.slots[n] = items > 1 ? sum[2] : -1;
-            for (int i = 0; i < items; ++i) gp.items[sum[1] + i] = make_int2(n, i);
+            for (int i = 0; i < items; ++i)
+                gp.items[sum[1] + i] = make_int4(n, sum[0] + i * gp.share, min(gp.share, count - i * gp.share), items > 1 ? sum[2] + i : -1);
         }
     }
     if (threadIdx.x == 0) gp.totals[0] = base[1];
@@ -263,24 +272,27 @@ __global__ __launch_bounds__(64) void block_lists_kernel(BlockGradParams gp) {
 
 // ---- by key blocks: dK, dV ----------------------------------------------------------------------------
 
-// KW waves hold 32 keys each, and 4 / KW waves share keys and take the row subtiles of a stage in turn.
+// KW waves hold 32 keys each, and SHARES as many share them and take the row subtiles of a stage in turn.
 struct RowInfo { unsigned q, d; float lse, delta; int pos; };  // byte offsets of a row in Q and dO, its statistics, its position
 
-template <int D> struct DkvGeo {
+template <int D, int KW, int SHARES> struct DkvGeo {
     using Tile = HeadTile<D>;
-    static constexpr int SUB = 32 * Tile::ROWB, STAGE = 2 * BG_STAGE * SUB, ROWS = BG_STAGE * 32;
-    static constexpr int PITCH = D + 4, JOIN = 4 * 32 * PITCH * 4;
-    static constexpr int TABLE = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;  // three tables of rows stand behind the stages
+    static constexpr int SUBS = SHARES, SUB = 32 * Tile::ROWB, STAGE = 2 * SUBS * SUB, ROWS = SUBS * 32, V = 2 * STAGE;
+    static constexpr int PITCH = D + 4, JOIN = KW * SHARES * 32 * PITCH * 4;
+    static constexpr int TABLE = V + KW * SUB > JOIN ? V + KW * SUB : JOIN;  // three tables of rows stand behind the stages and the keys' V
     static constexpr int LDS = TABLE + 3 * ROWS * 5 * 4;
 };
 
-template <int D, int KW>
-__global__ __launch_bounds__(256, 1) void block_dkv_kernel(BlockGradParams gp) {
+template <int D, int KW, int SHARES>
+__global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGradParams gp) {
     const BlockAttnParams& p = gp.a;
-    using Geo = DkvGeo<D>;
+    using Geo = DkvGeo<D, KW, SHARES>;
     using Tile = HeadTile<D>;
-    constexpr int SHARES = 4 / KW, ROWS = Geo::ROWS;
-    if ((int)blockIdx.x >= gp.totals[0]) return;
+    constexpr int ROWS = Geo::ROWS, SUBS = Geo::SUBS, WAVES = KW * SHARES;
+    // each die takes a contiguous range of the items: those at work on it together share a head's Q and dO in its L2
+    const int total = __builtin_amdgcn_readfirstlane(gp.totals[0]), per_die = (total + NUM_XCD - 1) / NUM_XCD, in_die = blockIdx.x / NUM_XCD;
+    const int at_item = blockIdx.x % NUM_XCD * per_die + in_die;
+    if (in_die >= per_die || at_item >= total) return;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     // tables: [ring of 3][ROWS] of each field
     unsigned* const t_q = reinterpret_cast<unsigned*>(smem + Geo::TABLE);
@@ -289,60 +301,84 @@ __global__ __launch_bounds__(256, 1) void block_dkv_kernel(BlockGradParams gp) {
     float* const t_delta = t_lse + 3 * ROWS;
     int* const t_pos = reinterpret_cast<int*>(t_delta + 3 * ROWS);
 
-    const int2 item = gp.items[blockIdx.x];
+    int4 item = gp.items[at_item];  // (loaded by vector instructions, but uniform)
+    item.x = __builtin_amdgcn_readfirstlane(item.x);
+    item.z = __builtin_amdgcn_readfirstlane(item.z);
     const int g = item.x / gp.nb, n = item.x % gp.nb;
-    const int* const list = gp.lists + gp.first[item.x] + item.y * gp.share;
-    const int in_list = min(gp.share, gp.counts[item.x] - item.y * gp.share);  // query blocks of the item
-    const int n_rows = max(in_list, 0) * p.R, n_stage = (n_rows + ROWS - 1) / ROWS;
+    const int* const list = gp.lists + item.y;
+    const int n_rows = item.z * p.R, n_stage = (n_rows + ROWS - 1) / ROWS;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool causal = (p.flags & LEMO_CAUSAL) != 0;
     const int key0 = n * p.b + (blockIdx.y * KW + wave % KW) * 32, key = key0 + l32;
     const int share = wave / KW;
 
-    u32x4 kf[Tile::CHUNKS], vf[Tile::CHUNKS];
+    // K stays in registers; for V, which comes from LDS, two waves a SIMD leave none
+    u32x4 kf[Tile::CHUNKS];
 #pragma unroll
-    for (int c = 0; c < Tile::CHUNKS; ++c) kf[c] = vf[c] = u32x4{0u, 0u, 0u, 0u};
+    for (int c = 0; c < Tile::CHUNKS; ++c) kf[c] = u32x4{0u, 0u, 0u, 0u};
     if (key < p.S_k) {
         const char* const k = reinterpret_cast<const char*>(p.K + key * p.k_ts + g * p.k_hs);
-        const char* const v = reinterpret_cast<const char*>(p.V + key * p.v_ts + g * p.v_hs);
 #pragma unroll
-        for (int c = 0; c < Tile::CHUNKS; ++c) {
-            kf[c] = *reinterpret_cast<const u32x4*>(k + c * 32 + half * 16);
-            vf[c] = *reinterpret_cast<const u32x4*>(v + c * 32 + half * 16);
-        }
+        for (int c = 0; c < Tile::CHUNKS; ++c) kf[c] = *reinterpret_cast<const u32x4*>(k + c * 32 + half * 16);
     }
+    const char* const sv = smem + Geo::V + wave % KW * Geo::SUB;
 
-    // rows of a stage: row v of the item is row v % R of query block list[v / R]
-    auto make_table = [&](int t) {
-        if (tid >= ROWS) return;
-        const int v = t * ROWS + tid, at = t % 3 * ROWS + tid;
-        RowInfo r{0xffffff00u, 0xffffff00u, INFINITY, 0.f, -1};  // not there: offsets past every operand, probabilities 0
-        if (v < n_rows) {
-            const int e = v / p.R, row = v - e * p.R, h = g * p.G + row % p.G;
-            const long long i = (long long)list[e] * p.bq + row / p.G;
+    // Rows of a stage: row v of the item is row v % R of query block list[v / R].  A thread looks after one row, in three steps a stage
+    // apart, so that nothing waits for what it needs: its query block is loaded, then its statistics, then it goes into the table.
+    int entry = 0;  // query block of the row whose statistics are loaded next
+    auto fetch_entry = [&](int t) {
+        const int v = t * ROWS + tid;
+        if (tid < ROWS && v < n_rows) entry = list[v / p.R];
+    };
+    unsigned r_q, r_d;
+    float r_lse, r_delta;
+    int r_pos;
+    auto fetch_row = [&](int t) {  // of the row that `entry` is for
+        r_q = r_d = 0xffffff00u;   // not there: offsets past every operand, probabilities 0
+        r_lse = INFINITY;
+        r_delta = 0.f;
+        r_pos = -1;
+        const int v = t * ROWS + tid;
+        if (tid < ROWS && v < n_rows) {
+            const int row = v % p.R, h = g * p.G + row % p.G;
+            const long long i = (long long)entry * p.bq + row / p.G;
             if (i < p.S_q) {
-                r.q = (unsigned)((i * p.q_ts + h * p.q_hs) * 2);
-                r.d = (unsigned)((i * gp.do_ts + h * gp.do_hs) * 2);
-                const float stored = p.lse2[(long long)h * p.S_q + i];
-                r.lse = stored == -INFINITY ? INFINITY : stored;
-                r.delta = gp.delta[(long long)h * p.S_q + i];
-                r.pos = causal ? (int)min(p.q_start + i, (long long)0x7fffffff) : 0x7fffffff;
+                r_q = (unsigned)((i * p.q_ts + h * p.q_hs) * 2);
+                r_d = (unsigned)((i * gp.do_ts + h * gp.do_hs) * 2);
+                r_lse = p.lse2[(long long)h * p.S_q + i];
+                r_delta = gp.delta[(long long)h * p.S_q + i];
+                r_pos = causal ? (int)min(p.q_start + i, (long long)0x7fffffff) : 0x7fffffff;
             }
         }
-        t_q[at] = r.q; t_d[at] = r.d; t_lse[at] = r.lse; t_delta[at] = r.delta; t_pos[at] = r.pos;
+    };
+    auto keep_row = [&](int t) {
+        if (tid >= ROWS) return;
+        const int at = t % 3 * ROWS + tid;
+        t_q[at] = r_q; t_d[at] = r_d; t_lse[at] = r_lse == -INFINITY ? INFINITY : r_lse; t_delta[at] = r_delta; t_pos[at] = r_pos;
     };
     const u32x4 q_rsrc = raw_rsrc(p.Q, ((p.S_q - 1) * p.q_ts + (p.H - 1) * p.q_hs + D) * 2);
     const u32x4 d_rsrc = raw_rsrc(gp.dO, ((p.S_q - 1) * gp.do_ts + (p.H - 1) * gp.do_hs + D) * 2);
-    constexpr int RPI = 1024 / Tile::ROWB, UNITS = ROWS / RPI, LOADS = 2 * UNITS / 4;
+    constexpr int RPI = 1024 / Tile::ROWB, UNITS = ROWS / RPI, LOADS = 2 * UNITS / WAVES;
+    static_assert(UNITS % WAVES == 0, "");
     const int in_row = lane / Tile::PIECES, place = lane % Tile::PIECES;
+    {  // V rows past the keys there are arrive as zeros
+        const int begin = n * p.b + blockIdx.y * KW * 32, pitch = (int)p.v_ts * 2;
+        u32x4 rsrc = raw_rsrc(reinterpret_cast<const char*>(p.V + (long long)min(begin, p.S_k - 1) * p.v_ts + (long long)g * p.v_hs),
+                                    begin < p.S_k ? (long long)(p.S_k - 1 - begin) * pitch + Tile::ROWB : 0);
+        for (int i = 0; i < 4; ++i) rsrc[i] = __builtin_amdgcn_readfirstlane(rsrc[i]);  // (64-bit arithmetic left it in vector registers)
+        for (int unit = wave; unit < KW * 32 / RPI; unit += WAVES) {
+            const int r = unit * RPI + in_row;
+            lds_direct_b128(rsrc, lds_offset_of(smem) + Geo::V + unit * 1024, r * pitch + ((place ^ Tile::swz(r & 31)) << 4));
+        }
+    }
     auto load_stage = [&](int t, int buf) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int unit = i * 4 + wave, part = unit % UNITS, r = part * RPI + in_row;
-            const bool d = i * 4 >= UNITS;  // the first half: Q, then dO
+            const int unit = i * WAVES + wave, part = unit % UNITS, r = part * RPI + in_row;
+            const bool d = i * WAVES >= UNITS;  // the first half: Q, then dO
             const unsigned row = (d ? t_d : t_q)[t % 3 * ROWS + r];
-            lds_direct_b128(d ? d_rsrc : q_rsrc, lds_offset_of(smem) + buf * Geo::STAGE + (d ? BG_STAGE * Geo::SUB : 0) + part * 1024,
+            lds_direct_b128(d ? d_rsrc : q_rsrc, lds_offset_of(smem) + buf * Geo::STAGE + (d ? SUBS * Geo::SUB : 0) + part * 1024,
                             (int)(row + ((unsigned)(place ^ Tile::swz(r & 31)) << 4)));
         }
     };
@@ -351,31 +387,37 @@ __global__ __launch_bounds__(256, 1) void block_dkv_kernel(BlockGradParams gp) {
 #pragma unroll
     for (int c = 0; c < Tile::COLS; ++c) dk[c] = dv[c] = f32x16{0};
     if (n_stage > 0) {
-        make_table(0);
-        if (n_stage > 1) make_table(1);
+        fetch_entry(0);
+        fetch_row(0);
+        fetch_entry(1);
+        keep_row(0);
         __syncthreads();
         load_stage(0, 0);
-        settle_stage();
+        fetch_row(1);
+        fetch_entry(2);
+        keep_row(1);
     }
+    settle_stage();
     for (int t = 0; t < n_stage; ++t) {
         __syncthreads();  // stage t and the table of stage t + 1 are there
         if (t + 1 < n_stage) load_stage(t + 1, (t + 1) & 1);
-        if (t + 2 < n_stage) make_table(t + 2);
+        fetch_row(t + 2);
+        fetch_entry(t + 3);
         const char* const sq = smem + (t & 1) * Geo::STAGE;
         const int table = t % 3 * ROWS;
 #pragma unroll 1
-        for (int j = share; j < BG_STAGE; j += SHARES) {
+        for (int j = share; j < SUBS; j += SHARES) {
             if (t * ROWS + j * 32 >= n_rows) break;
             const int at = table + j * 32;
             const int top = __builtin_amdgcn_readfirstlane(t_pos[at + 31]);  // rows ascend: the last one has the highest position, if it is there
             if (top >= 0 && top < key0) continue;
             const char* const qs = sq + j * Geo::SUB;
-            const char* const ds_ = qs + BG_STAGE * Geo::SUB;
+            const char* const ds_ = qs + SUBS * Geo::SUB;
             f32x16 acc = {0}, dp = {0};
 #pragma unroll
             for (int c = 0; c < Tile::CHUNKS; ++c) {
                 mma_chunk<bf16_t>(acc, Tile::row_fragment(qs, c, lane), kf[c]);  // [row][key]
-                mma_chunk<bf16_t>(dp, Tile::row_fragment(ds_, c, lane), vf[c]);
+                mma_chunk<bf16_t>(dp, Tile::row_fragment(ds_, c, lane), Tile::row_fragment(sv, c, lane));
             }
             float pr[16], ds[16];
             const bool masked = __builtin_amdgcn_readfirstlane(t_pos[at]) < key0 + 31;
@@ -410,13 +452,14 @@ __global__ __launch_bounds__(256, 1) void block_dkv_kernel(BlockGradParams gp) {
                     mma_chunk<bf16_t>(dk[col], Tile::column_fragment(qs, col, c, lane), pd[c]);
                 }
         }
+        keep_row(t + 2);
         settle_stage();
     }
     // dK, then dV: the waves that share keys add in LDS, in wave order
     constexpr int LPR = D / 8;
     float* const sums = reinterpret_cast<float*>(smem);
     const int c0 = lane % LPR * 8;
-    const int slot = gp.slots[item.x];
+    const int slot = item.w;
     for (int which = 0; which < 2; ++which) {
         __syncthreads();
 #pragma unroll
@@ -442,7 +485,7 @@ __global__ __launch_bounds__(256, 1) void block_dkv_kernel(BlockGradParams gp) {
             }
             const int j = key0 + in;
             if (slot >= 0) {
-                float* part = gp.partial + (((long long)(slot + item.y) * 2 + which) * p.b + (j - n * p.b)) * D + c0;
+                float* part = gp.partial + (((long long)slot * 2 + which) * p.b + (j - n * p.b)) * D + c0;
                 *reinterpret_cast<f32x4*>(part) = f32x4{v[0], v[1], v[2], v[3]};
                 *reinterpret_cast<f32x4*>(part + 4) = f32x4{v[4], v[5], v[6], v[7]};
             } else if (j < p.S_k) {
@@ -490,7 +533,7 @@ BlockGradLayout block_grad_layout(long long S_q, long long S_k, int H, int H_kv,
     const long long least = (256 + R - 1) / R;
     if (share < least) share = least;
     l.share = (int)(share < n_qb ? share : n_qb);
-    l.max_items = (int)(entries / l.share + H_kv * nb);
+    l.max_items = (int)(entries / l.share + H_kv * nb);  // (each key block one at least)
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
     l.delta = take((size_t)H * S_q * 4);
@@ -499,7 +542,7 @@ BlockGradLayout block_grad_layout(long long S_q, long long S_k, int H, int H_kv,
     l.first = take((size_t)H_kv * nb * 4);
     l.lists = take((size_t)entries * 4);
     l.slots = take((size_t)H_kv * nb * 4);
-    l.items = take((size_t)l.max_items * 8);
+    l.items = take((size_t)l.max_items * 16);
     l.totals = take(4);
     // parts of key blocks with more than one: at most twice as many as their query blocks fill
     const long long parts = 2 * (entries / l.share) < l.max_items ? 2 * (entries / l.share) : l.max_items;
@@ -508,32 +551,33 @@ BlockGradLayout block_grad_layout(long long S_q, long long S_k, int H, int H_kv,
     return l;
 }
 
-template <int D, int WAVES, int KS> static int run_dq(const BlockGradParams& gp, hipStream_t st) {
-    hipLaunchKernelGGL((block_dq_kernel<D, WAVES, KS>), dim3((unsigned)((long long)gp.a.n_qb * gp.a.n_rt * gp.a.H_kv)), dim3(WAVES * 64),
-                       (DqGeo<D, WAVES>::lds(gp.a.T * (gp.a.b / 32))), st, gp);
+template <int D, int KS> constexpr int dq_lds(int subtiles) { return DqGeo<D, 4, BG_STAGE<D, KS>>::lds(subtiles); }
+
+template <int D, int KS> static int run_dq(const BlockGradParams& gp, hipStream_t st) {
+    hipLaunchKernelGGL((block_dq_kernel<D, 4, KS>), dim3((unsigned)((long long)gp.a.n_qb * gp.a.n_rt * gp.a.H_kv)), dim3(256), (dq_lds<D, KS>(gp.a.T * (gp.a.b / 32))), st, gp);
     return (int)hipGetLastError();
 }
 
-template <int D, int KW> static int run_dkv(const BlockGradParams& gp, hipStream_t st) {
-    hipLaunchKernelGGL((block_dkv_kernel<D, KW>), dim3((unsigned)gp.max_items, (unsigned)(gp.a.b / (32 * KW))), dim3(256), DkvGeo<D>::LDS, st, gp);
+template <int D, int KW, int SHARES> static int run_dkv(const BlockGradParams& gp, hipStream_t st) {
+    hipLaunchKernelGGL((block_dkv_kernel<D, KW, SHARES>), dim3((unsigned)((gp.max_items + NUM_XCD - 1) / NUM_XCD * NUM_XCD), (unsigned)(gp.a.b / (32 * KW))), dim3(KW * SHARES * 64),
+                       (DkvGeo<D, KW, SHARES>::LDS), st, gp);
     return (int)hipGetLastError();
 }
 
 template <int D> static int launch_grad(BlockGradParams gp, hipStream_t st) {
-    static const int unready = raise_lds_limits({{reinterpret_cast<const void*>(&block_dq_kernel<D, 8, 1>), DqGeo<D, 8>::lds(MAX_LISTED_SUBTILES)},
-                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 8, 2>), DqGeo<D, 8>::lds(MAX_LISTED_SUBTILES)},
-                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 8, 4>), DqGeo<D, 8>::lds(MAX_LISTED_SUBTILES)},
-                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 4>), DqGeo<D, 4>::lds(MAX_LISTED_SUBTILES)},
-                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 1>), DkvGeo<D>::LDS},
-                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 2>), DkvGeo<D>::LDS},
-                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 4>), DkvGeo<D>::LDS}});
+    static const int unready = raise_lds_limits({{reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 1>), dq_lds<D, 1>(MAX_LISTED_SUBTILES)},
+                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 2>), dq_lds<D, 2>(MAX_LISTED_SUBTILES)},
+                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 4>), dq_lds<D, 4>(MAX_LISTED_SUBTILES)},
+                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 1, 4>), DkvGeo<D, 1, 4>::LDS},
+                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 2, 4>), DkvGeo<D, 2, 4>::LDS},
+                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 4, 2>), DkvGeo<D, 4, 2>::LDS}});
     if (unready) return unready;
     BlockAttnParams& p = gp.a;
-    const int tile = block_attention_tile_rows(p.R);
+    const int tile = block_attention_tile_rows(p.R, 64);
     p.n_rt = (p.R + tile - 1) / tile;
     p.n_parts = 1;
     p.order = head_order(p.H_kv, false, 8);
-    int rc = tile == 256 ? run_dq<D, 8, 1>(gp, st) : tile == 128 ? run_dq<D, 8, 2>(gp, st) : tile == 64 ? run_dq<D, 8, 4>(gp, st) : run_dq<D, 4, 4>(gp, st);
+    int rc = tile == 128 ? run_dq<D, 1>(gp, st) : tile == 64 ? run_dq<D, 2>(gp, st) : run_dq<D, 4>(gp, st);
     if (rc) return rc;
     hipLaunchKernelGGL(block_bits_kernel, dim3((unsigned)gp.words, (unsigned)p.H_kv), dim3(256), gp.nb * 4, st, gp);
     hipLaunchKernelGGL(block_count_kernel, dim3((unsigned)((gp.nb + 63) / 64), (unsigned)p.H_kv), dim3(64), 0, st, gp);
@@ -542,7 +586,7 @@ template <int D> static int launch_grad(BlockGradParams gp, hipStream_t st) {
     rc = (int)hipGetLastError();
     if (rc) return rc;
     const int subs = p.b / 32;
-    rc = subs % 4 == 0 ? run_dkv<D, 4>(gp, st) : subs % 2 == 0 ? run_dkv<D, 2>(gp, st) : run_dkv<D, 1>(gp, st);
+    rc = subs % 4 == 0 ? run_dkv<D, 4, 2>(gp, st) : subs % 2 == 0 ? run_dkv<D, 2, 4>(gp, st) : run_dkv<D, 1, 4>(gp, st);
     if (rc) return rc;
     hipLaunchKernelGGL((block_dkv_join_kernel<D>), dim3((unsigned)(p.H_kv * gp.nb), 2), dim3(256), 0, st, gp);
     return (int)hipGetLastError();
