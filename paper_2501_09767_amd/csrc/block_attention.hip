@@ -24,7 +24,7 @@ template <int D, int WAVES, int BA_STAGE> struct BaGeo {
     static constexpr int PITCH = D + 4;                                      // floats of a row where waves' results meet
     static constexpr int JOIN = WAVES * 32 * (PITCH * 4 + 8);
     static constexpr int LIST = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;         // the list's subtiles stand behind both
-    static constexpr int lds(int subtiles) { return LIST + subtiles * 4; }
+    static constexpr int lds(int subtiles) { return LIST + 16 + subtiles * 4; }  // (the number of them first)
 };
 
 template <int D, int WAVES, int KS>
@@ -34,8 +34,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAtt
     using Tile = HeadTile<D>;
     constexpr int ROWS = WAVES / KS * 32;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ int listed;
-    int* const keys = reinterpret_cast<int*>(smem + Geo::LIST);
+    int* const keys = reinterpret_cast<int*>(smem + Geo::LIST) + 4;
+    int& listed = keys[-4];
 
     int g, rank;
     decode_block(p.order, p.H_kv, p.n_qb * p.n_rt * p.n_parts, g, rank);

@@ -99,6 +99,34 @@ template <int D> struct HeadTile {
     }
 };
 
+// The same reads from addresses that differ by constants alone: a lane's place in a subtile once, then an exclusive or and an offset
+// in the instruction for each fragment, so that no kernel has to keep (or spill) an address for every one.  Subtiles must begin at
+// multiples of 256 bytes of LDS: workgroup memory that is dynamic only begins at 0.
+template <typename T> __device__ __forceinline__ T __attribute__((address_space(3)))* lds_pointer(unsigned at) {
+    return (T __attribute__((address_space(3)))*)(uintptr_t)at;
+}
+template <int D> struct TilePlace {
+    using Tile = HeadTile<D>;
+    unsigned row, col;
+    __device__ explicit TilePlace(int lane) {
+        const int half = lane >> 5, l32 = lane & 31, r = 4 * half + ((l32 & 15) >> 2);
+        row = l32 * Tile::ROWB + ((half ^ Tile::swz(l32)) << 4);
+        col = r * Tile::ROWB + ((((l32 >> 4) * 2 + ((l32 & 3) >> 1)) ^ Tile::swz(r)) << 4) + (l32 & 1) * 8;
+    }
+    // chunk c of row l32 of the subtile at `sub` (bytes of LDS)
+    __device__ u32x4 row_fragment(unsigned sub, int c) const {
+        return *lds_pointer<const u32x4>((sub + row) ^ (unsigned)(c << 5));
+    }
+    // columns 32 t + l32, rows 16 c + 4 half + {0..3} and 16 c + 8 + 4 half + {0..3}: 8 rows on, the exchange of pieces differs by 2
+    __device__ u32x4 column_fragment(unsigned sub, int t, int c) const {
+        const unsigned at = (sub + col) ^ (unsigned)(t << 6);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_pointer<s16x4>(at + 16 * c * Tile::ROWB));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_pointer<s16x4>((at ^ 32u) + (16 * c + 8) * Tile::ROWB));
+        const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+        return u32x4{l2.x, l2.y, h2.x, h2.y};
+    }
+};
+
 // The list of a query block as the rule for it says: an entry counts if it names a block, [0, nb), and lies above every such entry
 // before it.  One wave; `take(entry, counts)` is called for 64 entries at a time, by all lanes.
 template <typename F> __device__ __forceinline__ void walk_list(const int* list, int T, int nb, int lane, F&& take) {

@@ -24,7 +24,7 @@ template <int D, int WAVES, int SUBS> struct DqGeo {
     static constexpr int SUB = 32 * Tile::ROWB, STAGE = 2 * SUBS * SUB;
     static constexpr int PITCH = D + 4, JOIN = WAVES * 32 * PITCH * 4;
     static constexpr int LIST = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
-    static constexpr int lds(int subtiles) { return LIST + subtiles * 4; }
+    static constexpr int lds(int subtiles) { return LIST + 16 + subtiles * 4; }  // (the number of them first)
 };
 
 template <int D, int WAVES, int KS>
@@ -35,8 +35,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams
     using Tile = HeadTile<D>;
     constexpr int ROWS = WAVES / KS * 32;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ int listed;
-    int* const keys = reinterpret_cast<int*>(smem + Geo::LIST);
+    int* const keys = reinterpret_cast<int*>(smem + Geo::LIST) + 4;
+    int& listed = keys[-4];
 
     int g, rank;
     decode_block(p.order, p.H_kv, p.n_qb * p.n_rt, g, rank);
@@ -273,8 +273,6 @@ __global__ __launch_bounds__(64) void block_lists_kernel(BlockGradParams gp) {
 // ---- by key blocks: dK, dV ----------------------------------------------------------------------------
 
 // KW waves hold 32 keys each, and SHARES as many share them and take the row subtiles of a stage in turn.
-struct RowInfo { unsigned q, d; float lse, delta; int pos; };  // byte offsets of a row in Q and dO, its statistics, its position
-
 template <int D, int KW, int SHARES> struct DkvGeo {
     using Tile = HeadTile<D>;
     static constexpr int SUBS = SHARES, SUB = 32 * Tile::ROWB, STAGE = 2 * SUBS * SUB, ROWS = SUBS * 32, V = 2 * STAGE;
@@ -310,52 +308,45 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool causal = (p.flags & LEMO_CAUSAL) != 0;
-    const int key0 = n * p.b + (blockIdx.y * KW + wave % KW) * 32, key = key0 + l32;
+    const int key0 = n * p.b + (blockIdx.y * KW + wave % KW) * 32;
     const int share = wave / KW;
 
     // K stays in registers; for V, which comes from LDS, two waves a SIMD leave none
     u32x4 kf[Tile::CHUNKS];
 #pragma unroll
     for (int c = 0; c < Tile::CHUNKS; ++c) kf[c] = u32x4{0u, 0u, 0u, 0u};
-    if (key < p.S_k) {
-        const char* const k = reinterpret_cast<const char*>(p.K + key * p.k_ts + g * p.k_hs);
+    if (key0 + l32 < p.S_k) {
+        const char* const k = reinterpret_cast<const char*>(p.K + (key0 + l32) * p.k_ts + g * p.k_hs);
 #pragma unroll
         for (int c = 0; c < Tile::CHUNKS; ++c) kf[c] = *reinterpret_cast<const u32x4*>(k + c * 32 + half * 16);
     }
-    const char* const sv = smem + Geo::V + wave % KW * Geo::SUB;
+    const unsigned sv = lds_offset_of(smem) + Geo::V + wave % KW * Geo::SUB;
 
     // Rows of a stage: row v of the item is row v % R of query block list[v / R].  A thread looks after one row, in three steps a stage
     // apart, so that nothing waits for what it needs: its query block is loaded, then its statistics, then it goes into the table.
-    int entry = 0;  // query block of the row whose statistics are loaded next
+    int next_entry = 0, entry = 0;  // query blocks of the row whose statistics are loaded next, and of the one they were loaded for
+    float r_lse = 0.f, r_delta = 0.f;
     auto fetch_entry = [&](int t) {
         const int v = t * ROWS + tid;
-        if (tid < ROWS && v < n_rows) entry = list[v / p.R];
+        if (tid < ROWS && v < n_rows) next_entry = list[v / p.R];
     };
-    unsigned r_q, r_d;
-    float r_lse, r_delta;
-    int r_pos;
-    auto fetch_row = [&](int t) {  // of the row that `entry` is for
-        r_q = r_d = 0xffffff00u;   // not there: offsets past every operand, probabilities 0
-        r_lse = INFINITY;
-        r_delta = 0.f;
-        r_pos = -1;
+    auto fetch_row = [&](int t) {
+        entry = next_entry;
         const int v = t * ROWS + tid;
-        if (tid < ROWS && v < n_rows) {
-            const int row = v % p.R, h = g * p.G + row % p.G;
-            const long long i = (long long)entry * p.bq + row / p.G;
-            if (i < p.S_q) {
-                r_q = (unsigned)((i * p.q_ts + h * p.q_hs) * 2);
-                r_d = (unsigned)((i * gp.do_ts + h * gp.do_hs) * 2);
-                r_lse = p.lse2[(long long)h * p.S_q + i];
-                r_delta = gp.delta[(long long)h * p.S_q + i];
-                r_pos = causal ? (int)min(p.q_start + i, (long long)0x7fffffff) : 0x7fffffff;
-            }
-        }
+        if (tid >= ROWS || v >= n_rows) return;
+        const int row = v % p.R, h = g * p.G + row % p.G, i = min(entry * p.bq + row / p.G, p.S_q - 1);
+        r_lse = p.lse2[(long long)h * p.S_q + i];
+        r_delta = gp.delta[(long long)h * p.S_q + i];
     };
     auto keep_row = [&](int t) {
         if (tid >= ROWS) return;
-        const int at = t % 3 * ROWS + tid;
-        t_q[at] = r_q; t_d[at] = r_d; t_lse[at] = r_lse == -INFINITY ? INFINITY : r_lse; t_delta[at] = r_delta; t_pos[at] = r_pos;
+        const int at = t % 3 * ROWS + tid, v = t * ROWS + tid, row = v % p.R, h = g * p.G + row % p.G, i = entry * p.bq + row / p.G;
+        const bool there = v < n_rows && i < p.S_q;  // otherwise: offsets past every operand, probabilities 0
+        t_q[at] = there ? (unsigned)((i * p.q_ts + h * p.q_hs) * 2) : 0xffffff00u;
+        t_d[at] = there ? (unsigned)((i * gp.do_ts + h * gp.do_hs) * 2) : 0xffffff00u;
+        t_lse[at] = there && r_lse != -INFINITY ? r_lse : INFINITY;
+        t_delta[at] = there ? r_delta : 0.f;
+        t_pos[at] = !there ? -1 : causal ? (int)min(p.q_start + i, (long long)0x7fffffff) : 0x7fffffff;
     };
     const u32x4 q_rsrc = raw_rsrc(p.Q, ((p.S_q - 1) * p.q_ts + (p.H - 1) * p.q_hs + D) * 2);
     const u32x4 d_rsrc = raw_rsrc(gp.dO, ((p.S_q - 1) * gp.do_ts + (p.H - 1) * gp.do_hs + D) * 2);
@@ -373,6 +364,9 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
         }
     }
     auto load_stage = [&](int t, int buf) {
+        int lane_here = lane;
+        asm volatile("" : "+v"(lane_here));
+        const int in_row = lane_here / Tile::PIECES, place = lane_here % Tile::PIECES;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int unit = i * WAVES + wave, part = unit % UNITS, r = part * RPI + in_row;
@@ -411,13 +405,35 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
             const int at = table + j * 32;
             const int top = __builtin_amdgcn_readfirstlane(t_pos[at + 31]);  // rows ascend: the last one has the highest position, if it is there
             if (top >= 0 && top < key0) continue;
-            const char* const qs = sq + j * Geo::SUB;
-            const char* const ds_ = qs + SUBS * Geo::SUB;
+            const unsigned qs = lds_offset_of(sq) + j * Geo::SUB, ds_ = qs + SUBS * Geo::SUB;
+            int lane_here = lane;  // what follows from it is formed here, not kept through the loop: registers are short
+            asm volatile("" : "+v"(lane_here));
+            const TilePlace<D> place_in(lane_here);
+            const int half = lane_here >> 5, key = key0 + (lane_here & 31);
             f32x16 acc = {0}, dp = {0};
+            // Fragments come AHEAD steps before their products, and no earlier: all of them at once would not fit the registers, and what
+            // then went to scratch would come back only after the stage's loads, which a wait for memory cannot tell from it.
+            constexpr int AHEAD = 2;
+            {
+                u32x4 fq[AHEAD], fd[AHEAD], fv[AHEAD];
 #pragma unroll
-            for (int c = 0; c < Tile::CHUNKS; ++c) {
-                mma_chunk<bf16_t>(acc, Tile::row_fragment(qs, c, lane), kf[c]);  // [row][key]
-                mma_chunk<bf16_t>(dp, Tile::row_fragment(ds_, c, lane), Tile::row_fragment(sv, c, lane));
+                for (int c = 0; c < AHEAD; ++c) {
+                    fq[c] = place_in.row_fragment(qs, c);
+                    fd[c] = place_in.row_fragment(ds_, c);
+                    fv[c] = place_in.row_fragment(sv, c);
+                }
+#pragma unroll
+                for (int c = 0; c < Tile::CHUNKS; ++c) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    mma_chunk<bf16_t>(acc, fq[c % AHEAD], kf[c]);  // [row][key]
+                    mma_chunk<bf16_t>(dp, fd[c % AHEAD], fv[c % AHEAD]);
+                    if (c + AHEAD < Tile::CHUNKS) {
+                        fq[c % AHEAD] = place_in.row_fragment(qs, c + AHEAD);
+                        fd[c % AHEAD] = place_in.row_fragment(ds_, c + AHEAD);
+                        fv[c % AHEAD] = place_in.row_fragment(sv, c + AHEAD);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
             float pr[16], ds[16];
             const bool masked = __builtin_amdgcn_readfirstlane(t_pos[at]) < key0 + 31;
@@ -444,13 +460,26 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
                 pd[c] = u32x4{pack_bf16x2_hw(ds[8 * c + 0], ds[8 * c + 1]), pack_bf16x2_hw(ds[8 * c + 2], ds[8 * c + 3]),
                               pack_bf16x2_hw(ds[8 * c + 4], ds[8 * c + 5]), pack_bf16x2_hw(ds[8 * c + 6], ds[8 * c + 7])};
             }
+            {
+                constexpr int STEPS = 2 * Tile::COLS;  // step i: column tile i / 2, chunk i % 2
+                u32x4 fd[AHEAD], fq[AHEAD];
 #pragma unroll
-            for (int col = 0; col < Tile::COLS; ++col)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    mma_chunk<bf16_t>(dv[col], Tile::column_fragment(ds_, col, c, lane), pp[c]);  // [head column][key]
-                    mma_chunk<bf16_t>(dk[col], Tile::column_fragment(qs, col, c, lane), pd[c]);
+                for (int i = 0; i < AHEAD; ++i) {
+                    fd[i] = place_in.column_fragment(ds_, i / 2, i % 2);
+                    fq[i] = place_in.column_fragment(qs, i / 2, i % 2);
                 }
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    mma_chunk<bf16_t>(dv[i / 2], fd[i % AHEAD], pp[i % 2]);  // [head column][key]
+                    mma_chunk<bf16_t>(dk[i / 2], fq[i % AHEAD], pd[i % 2]);
+                    if (i + AHEAD < STEPS) {
+                        fd[i % AHEAD] = place_in.column_fragment(ds_, (i + AHEAD) / 2, (i + AHEAD) % 2);
+                        fq[i % AHEAD] = place_in.column_fragment(qs, (i + AHEAD) / 2, (i + AHEAD) % 2);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         keep_row(t + 2);
         settle_stage();
