@@ -40,10 +40,16 @@ int64_t span_bytes(int64_t S, int64_t ts, int64_t H, int64_t hs, int64_t d) { re
 
 float base2(float scale, int32_t d) { return (float)((scale > 0.f ? (double)scale : 1.0 / std::sqrt((double)d)) * 1.4426950408889634); }
 
-size_t part_bytes(int64_t n_qb, int32_t H_kv, int64_t R, int32_t d, int32_t T, int32_t b) {
-    const int tile = block_attention_tile_rows((int)R, d);
-    const int parts = block_attention_parts(n_qb * ((R + tile - 1) / tile) * H_kv, (int64_t)T * (b / 32));
-    return parts > 1 ? round_up((size_t)n_qb * H_kv * parts * R * (d + 4) * sizeof(float), 256) : 0;
+// room for the shares of the lists; S_k bounds what lists of few rows name together (single tokens do not come together)
+size_t part_bytes(int64_t n_qb, int64_t bq, int64_t S_k, int32_t H, int32_t H_kv, int32_t d, int32_t T, int32_t b, bool step) {
+    BlockAttnParams p{};
+    static const int one = 0;
+    p.lengths = step ? &one : nullptr;  // (not read)
+    p.n_qb = (int)n_qb; p.bq = (int)bq; p.S_k = (int)S_k; p.H_kv = H_kv; p.T = T; p.b = b;
+    p.R = (int)(bq * (H / H_kv));
+    const int subtiles = block_attention_packed(p), tile = block_attention_tile_rows(p.R, d);
+    const int parts = block_attention_parts((int64_t)p.n_qb * ((p.R + tile - 1) / tile) * H_kv, subtiles);
+    return parts > 1 ? round_up((size_t)p.n_qb * H_kv * parts * p.R * (d + 4) * sizeof(float), 256) : 0;
 }
 
 // what forward and gradient take alike; fills the parameter block
@@ -116,13 +122,13 @@ int lemo_select_blocks(const void* Q, int64_t S_q, int32_t H, int32_t H_kv, int3
     return hip_rc(launch_select_blocks(p, dt, static_cast<hipStream_t>(stream)));
 }
 
-int lemo_block_attention_workspace_bytes(int64_t S_q, int32_t H, int32_t H_kv, int32_t d, int32_t T, int32_t b, int32_t bq, size_t* bytes) {
+int lemo_block_attention_workspace_bytes(int64_t S_q, int64_t S_k, int32_t H, int32_t H_kv, int32_t d, int32_t T, int32_t b, int32_t bq, size_t* bytes) {
     if (!bytes) return LEMO_ERR_NULL;
     int rc = check_sizes(H, H_kv, d, LEMO_BF16, b);
-    if (rc == LEMO_OK) rc = check_lists(S_q, 1, 0, H, H_kv, T, b, bq);
+    if (rc == LEMO_OK) rc = check_lists(S_q, S_k, 0, H, H_kv, T, b, bq);
     if (rc != LEMO_OK) return rc;
     const int64_t q = bq < S_q ? bq : S_q;
-    *bytes = part_bytes((S_q + q - 1) / q, H_kv, q * (H / H_kv), d, T, b);
+    *bytes = part_bytes((S_q + q - 1) / q, q, S_k, H, H_kv, d, T, b, false);
     return LEMO_OK;
 }
 
@@ -137,7 +143,7 @@ int lemo_block_attention(const void* Q, const void* K, const void* V, int64_t S_
     rc = check_strides(O, o_tok_stride, o_head_stride, dt);
     if (rc != LEMO_OK) return rc;
     if (reinterpret_cast<uintptr_t>(lse2) & 3u) return LEMO_ERR_ALIGN;
-    const size_t need = part_bytes(p.n_qb, H_kv, p.R, d, T, b);
+    const size_t need = part_bytes(p.n_qb, p.bq, S_k, H, H_kv, d, T, b, false);
     if (need && !workspace) return LEMO_ERR_NULL;
     if (need && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return LEMO_ERR_ALIGN;
     if (workspace_bytes < need) return LEMO_ERR_WORKSPACE;
@@ -238,7 +244,11 @@ int lemo_select_blocks_step(const void* Q, int32_t B, int32_t H, int32_t H_kv, i
 int lemo_block_attention_step_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t d, int32_t T, int32_t b, size_t* bytes) {
     if (!bytes) return LEMO_ERR_NULL;
     if (B < 0) return LEMO_ERR_SHAPE;
-    return lemo_block_attention_workspace_bytes(B > 0 ? B : 1, H, H_kv, d, T, b, 1, bytes);
+    int rc = check_sizes(H, H_kv, d, LEMO_BF16, b);
+    if (rc == LEMO_OK) rc = check_lists(B > 0 ? B : 1, 1, 0, H, H_kv, T, b, 1);
+    if (rc != LEMO_OK) return rc;
+    *bytes = part_bytes(B > 0 ? B : 1, 1, 1, H, H_kv, d, T, b, true);
+    return LEMO_OK;
 }
 
 int lemo_block_attention_step(const void* Q, const void* K, const void* V, int32_t B, int64_t S_max, int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt,
@@ -259,7 +269,7 @@ int lemo_block_attention_step(const void* Q, const void* K, const void* V, int32
     rc = check_strides(O, o_tok_stride, o_head_stride, dt);
     if (rc != LEMO_OK) return rc;
     if (k_seq_stride % 8 || v_seq_stride % 8 || (reinterpret_cast<uintptr_t>(lengths) & 3u)) return LEMO_ERR_ALIGN;
-    const size_t need = part_bytes(B, H_kv, p.R, d, T, b);
+    const size_t need = part_bytes(B, 1, S_max, H, H_kv, d, T, b, true);
     if (need && !workspace) return LEMO_ERR_NULL;
     if (need && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return LEMO_ERR_ALIGN;
     if (workspace_bytes < need) return LEMO_ERR_WORKSPACE;

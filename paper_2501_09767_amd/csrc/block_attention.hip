@@ -9,7 +9,6 @@
 // lies in the registers.  KS waves share rows and take the subtiles of a stage in turn, for lists of few rows; their sums meet in LDS at
 // the end.  Where lists are few as well (single tokens), n_parts workgroups take shares of a list and a second kernel joins them.
 // P is rounded to bf16 for the second product; sums and normaliser are binary32, from the unrounded values.
-#include <stdlib.h>
 #include "block_attention.hpp"
 
 namespace lemo {
@@ -27,7 +26,8 @@ template <int D, int WAVES, int BA_STAGE> struct BaGeo {
     static constexpr int lds(int subtiles) { return LIST + 16 + subtiles * 4; }  // (the number of them first)
 };
 
-template <int D, int WAVES, int KS>
+// PACK: the rows belong to several lists, whose union is worked on; a row sees the subtiles that its own list names.
+template <int D, int WAVES, int KS, bool PACK>
 __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAttnParams p) {
     constexpr int STAGE = BA_STAGE<D, KS>;
     using Geo = BaGeo<D, WAVES, STAGE>;
@@ -50,11 +50,20 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAtt
     // last key that a row may see
     auto limit_of = [&](int row) { return causal ? (int)min(pos0 + row / p.G, (long long)S - 1) : S - 1; };
 
-    if (wave == 0) {
-        const int n = rt * ROWS < rows ? list_subtiles(p.blocks + ((long long)qb * p.H_kv + g) * p.T, p.T, p.b, (p.S_k + p.b - 1) / p.b, limit_of(row_end - 1), keys, lane) : 0;
-        if (lane == 0) listed = n;
+    int room = 0;  // (PACK) of the union's subtiles
+    if constexpr (PACK) {
+        const long long first = (long long)qb * p.pack;
+        const int nb = (p.S_k + p.b - 1) / p.b, lists = (int)min((long long)p.pack, p.n_lists - first);
+        room = min(p.pack * p.T, nb) * (p.b / 32);
+        union_subtiles<WAVES>(p.blocks + (first * p.H_kv + g) * p.T, (long long)p.H_kv * p.T, lists, p.T, p.b, nb, limit_of(rows - 1), reinterpret_cast<unsigned*>(smem), keys,
+                              room, &listed, wave, lane);
+    } else {
+        if (wave == 0) {
+            const int n = rt * ROWS < rows ? list_subtiles(p.blocks + ((long long)qb * p.H_kv + g) * p.T, p.T, p.b, (p.S_k + p.b - 1) / p.b, limit_of(row_end - 1), keys, lane) : 0;
+            if (lane == 0) listed = n;
+        }
+        __syncthreads();
     }
-    __syncthreads();
     const int s_begin = (int)((long long)listed * share / p.n_parts), n_sub = (int)((long long)listed * (share + 1) / p.n_parts) - s_begin;
     const int n_stage = (n_sub + STAGE - 1) / STAGE;
 
@@ -62,6 +71,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAtt
     const int row0 = rt * ROWS + wave / KS * 32, row = row0 + l32;
     const bool live = row < rows;
     const int lim = live ? limit_of(row) : -1;
+    const int member = PACK ? l32 / (p.R / p.pack) : 0;  // the row's list (there is one tile of rows)
     const int clean = row0 < rows ? limit_of(row0) : -1;              // a subtile that ends at or before it needs no mask
     const int reach = row0 < rows ? limit_of(min(row0 + 31, rows - 1)) : -1;  // one that begins behind it is nothing to the wave
     u32x4 qf[Tile::CHUNKS];
@@ -122,9 +132,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAtt
             f32x16 acc = {0};
 #pragma unroll
             for (int c = 0; c < Tile::CHUNKS; ++c) mma_chunk<bf16_t>(acc, Tile::row_fragment(ks, c, lane), qf[c]);  // acc[key][row]
-            if (key + 31 > clean) {
+            int mine = lim;
+            bool whole = key + 31 <= clean;
+            if constexpr (PACK) {
+                const unsigned bits = keys[room + s_begin + t * STAGE + j];
+                whole = whole && __popc(bits) == p.pack;
+                mine = bits >> member & 1 ? lim : -1;
+            }
+            if (!whole) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[r] = key + acc_row(r, lane) <= lim ? acc[r] : -INFINITY;
+                for (int r = 0; r < 16; ++r) acc[r] = key + acc_row(r, lane) <= mine ? acc[r] : -INFINITY;
             }
             float top = acc[0];
 #pragma unroll
@@ -253,10 +270,31 @@ template <int D> __global__ __launch_bounds__(256) void block_attention_join_ker
 // Rows of a workgroup by the rows that share a list: no more waves than have rows, the others share.
 int block_attention_tile_rows(int R, int d) { return R > 128 && d == 128 ? 256 : R > 64 ? 128 : R > 32 ? 64 : 32; }
 
-// Shares of a list: workgroups for every CU twice, at least a stage each.
+// Lists of few rows together, as many as fill 32 rows; the union of what they name has to fit the workgroup's memory.  1000 queries with a
+// list each, 16 / 4 heads of 64: see launch_block_attention_d.
+static int block_attention_pack(int R, int T, int b, long long nb, long long lists) {
+    int pack = R >= 32 ? 1 : 32 / R;
+    if (nb > 16384) return 1;
+    while (pack > 1 && (pack > lists || (pack * (long long)T < nb ? pack * (long long)T : nb) * (b / 32) > MAX_PACKED_SUBTILES)) --pack;
+    return pack;
+}
+
+// Makes the lists that are worked on together one query block; returns the subtiles that its list may have.
+int block_attention_packed(BlockAttnParams& p) {
+    const int nb = (p.S_k + p.b - 1) / p.b;
+    p.n_lists = p.n_qb;
+    p.pack = p.lengths ? 1 : block_attention_pack(p.R, p.T, p.b, nb, p.n_qb);
+    if (p.pack == 1) return p.T * (p.b / 32);
+    p.bq *= p.pack;
+    p.R *= p.pack;
+    p.n_qb = (p.n_qb + p.pack - 1) / p.pack;
+    return (p.pack * p.T < nb ? p.pack * p.T : nb) * (p.b / 32);
+}
+
+// Shares of a list: a workgroup for every CU, at least a stage each.
 int block_attention_parts(long long tiles, long long subtiles) {
     const long long most = (subtiles + 3) / 4;
-    long long parts = tiles >= 512 ? 1 : (512 + tiles - 1) / tiles;
+    long long parts = tiles >= 256 ? 1 : (256 + tiles - 1) / tiles;
     if (parts > most) parts = most;
     return parts < 1 ? 1 : (int)parts;
 }
@@ -264,27 +302,30 @@ int block_attention_parts(long long tiles, long long subtiles) {
 template <int D, int KS> constexpr int ba_lds(int subtiles) { return BaGeo<D, 4, BA_STAGE<D, KS>>::lds(subtiles); }
 
 template <int D> static int prepare_block_attention() {
-    static const int err = raise_lds_limits({{reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 1>), ba_lds<D, 1>(MAX_LISTED_SUBTILES)},
-                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 2>), ba_lds<D, 2>(MAX_LISTED_SUBTILES)},
-                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 4>), ba_lds<D, 4>(MAX_LISTED_SUBTILES)}});
+    static const int err = raise_lds_limits({{reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 1, false>), ba_lds<D, 1>(MAX_LISTED_SUBTILES)},
+                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 2, false>), ba_lds<D, 2>(MAX_LISTED_SUBTILES)},
+                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 4, false>), ba_lds<D, 4>(MAX_LISTED_SUBTILES)},
+                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 4, true>), ba_lds<D, 4>(2 * MAX_PACKED_SUBTILES)}});
     return err;
 }
 
-template <int D, int KS> static int run_block_attention(const BlockAttnParams& p, hipStream_t st) {
-    hipLaunchKernelGGL((block_attention_kernel<D, 4, KS>), dim3((unsigned)((long long)p.n_qb * p.n_rt * p.n_parts * p.H_kv)), dim3(256),
-                       (ba_lds<D, KS>(p.T * (p.b / 32))), st, p);
+template <int D, int KS, bool PACK> static int run_block_attention(const BlockAttnParams& p, int subtiles, hipStream_t st) {
+    hipLaunchKernelGGL((block_attention_kernel<D, 4, KS, PACK>), dim3((unsigned)((long long)p.n_qb * p.n_rt * p.n_parts * p.H_kv)), dim3(256),
+                       (ba_lds<D, KS>(PACK ? 2 * subtiles : subtiles)), st, p);
     return (int)hipGetLastError();
 }
 
 template <int D> static int launch_block_attention_d(BlockAttnParams p, hipStream_t st) {
     const int unready = D == 128 ? first_error(prepare_block_attention<D>, prepare_block_attention_pipe) : prepare_block_attention<D>();
     if (unready) return unready;
+    const int subtiles = block_attention_packed(p);
     const int tile = block_attention_tile_rows(p.R, D);
     p.n_rt = (p.R + tile - 1) / tile;
-    p.n_parts = p.parts ? block_attention_parts((long long)p.n_qb * p.n_rt * p.H_kv, (long long)p.T * (p.b / 32)) : 1;
+    p.n_parts = p.parts ? block_attention_parts((long long)p.n_qb * p.n_rt * p.H_kv, subtiles) : 1;
     p.order = head_order(p.H_kv, false, 8);
-    const int rc = tile == 256 || (D == 128 && p.R > 32 && getenv("PIPE")) ? launch_block_attention_pipe(p, st) : tile == 128 ? run_block_attention<D, 1>(p, st)
-                 : tile == 64 ? run_block_attention<D, 2>(p, st) : run_block_attention<D, 4>(p, st);
+    const int rc = tile == 256 ? launch_block_attention_pipe(p, st) : tile == 128 ? run_block_attention<D, 1, false>(p, subtiles, st)
+                 : tile == 64 ? run_block_attention<D, 2, false>(p, subtiles, st) : p.pack == 1 ? run_block_attention<D, 4, false>(p, subtiles, st)
+                 : run_block_attention<D, 4, true>(p, subtiles, st);
     if (rc || p.n_parts == 1) return rc;
     const long long rows = (long long)p.n_qb * p.H_kv * p.R, per = 256 / (D / 8);
     hipLaunchKernelGGL((block_attention_join_kernel<D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, p);

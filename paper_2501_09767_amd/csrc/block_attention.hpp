@@ -15,6 +15,7 @@ struct BlockAttnParams {
     float* parts;        // where a list is shared by several workgroups: their results, see PART_ROW
     int S_q, S_k, H, H_kv, G, T, b, bq, n_qb;
     int R, n_rt, n_parts;  // rows of a query block, tiles of them, shares of a list
+    int pack, n_lists;     // lists that are worked on together (bq, n_qb, R then count `pack` blocks as one), and all there are
     long long q_start;
     long long q_ts, q_hs, k_ts, k_hs, k_ss, v_ts, v_hs, v_ss, o_ts, o_hs;  // element strides: token, head, sequence
     float c2;
@@ -44,10 +45,12 @@ struct BlockGradParams {
 struct BlockGradLayout { size_t delta, bits, counts, first, lists, slots, items, totals, partial, bytes; int share, max_items; };
 
 constexpr int MAX_LISTED_SUBTILES = 4096;  // subtiles of 32 keys that a list may name: they stand in LDS, 16 KB
+constexpr int MAX_PACKED_SUBTILES = 2048;  // of the union of lists, with a word of bits each
 constexpr int MAX_LISTED_BLOCKS = 16384;   // key blocks that a choice is made from: their scores stand in LDS, 128 KB
 
 int block_attention_parts(long long tiles, long long subtiles);
 int block_attention_tile_rows(int R, int d);
+int block_attention_packed(BlockAttnParams& p);
 int launch_block_attention(BlockAttnParams p, int d, hipStream_t st);
 int prepare_block_attention_pipe();
 int launch_block_attention_pipe(const BlockAttnParams& p, hipStream_t st);  // heads of 128; p filled in as for the others
@@ -163,6 +166,60 @@ __device__ __forceinline__ int list_subtiles(const int* list, int T, int b, int 
         count += __shfl(sum, 63);
     });
     return count;
+}
+
+// Several lists of few rows as one: the subtiles of all blocks that any of `lists` consecutive lists names, with a bit for each list that
+// does.  Work on 32 rows costs the matrix cores the same whether one list fills 4 of them or eight lists fill all, so the union is
+// never more than the lists one by one, and less by what they share.  All of the workgroup's waves; `marks` has room for nb words, `at`
+// for the result: first keys, and `room` behind them the bits.  The count is written to *count.
+template <int WAVES>
+__device__ __forceinline__ void union_subtiles(const int* list, long long pitch, int lists, int T, int b, int nb, int limit, unsigned* marks, int* at, int room,
+                                               int* count, int wave, int lane) {
+    const int reach = min(nb, limit / b + 1);  // blocks that begin at or before the limit
+    for (int n = threadIdx.x; n < reach; n += WAVES * 64) marks[n] = 0;
+    __syncthreads();
+    if (T <= 16) {  // four lists at a time, each in 16 lanes
+        const int e = lane & 15;
+        for (int m0 = wave * 4; m0 < lists; m0 += WAVES * 4) {
+            const int m = m0 + (lane >> 4), raw = m < lists && e < T ? list[m * pitch + e] : -1, n = raw >= 0 && raw < nb ? raw : -1;
+            int high = n;
+#pragma unroll
+            for (int s = 1; s < 16; s <<= 1) {
+                const int other = __shfl_up(high, s, 16);
+                if (e >= s) high = max(high, other);
+            }
+            const int before = __shfl_up(high, 1, 16);
+            if (n > (e > 0 ? before : -1) && n < reach) atomicOr(marks + n, 1u << m);
+        }
+    } else {
+        for (int m = wave; m < lists; m += WAVES)
+            walk_list(list + m * pitch, T, nb, lane, [&](int n, bool counts) {
+                if (counts && n < reach) atomicOr(marks + n, 1u << m);
+            });
+    }
+    __syncthreads();
+    if (wave == 0) {
+        int total = 0;
+        const int most = b / 32;
+        for (int n0 = 0; n0 < reach; n0 += 64) {
+            const int n = n0 + lane;
+            const unsigned bits = n < reach ? marks[n] : 0;
+            const int mine = bits ? min(most, (limit - n * b) / 32 + 1) : 0;
+            int sum = mine;
+#pragma unroll
+            for (int s = 1; s < 64; s <<= 1) {
+                const int other = __shfl_up(sum, s);
+                if (lane >= s) sum += other;
+            }
+            for (int i = 0; i < mine; ++i) {
+                at[total + sum - mine + i] = n * b + 32 * i;
+                at[room + total + sum - mine + i] = (int)bits;
+            }
+            total += __shfl(sum, 63);
+        }
+        if (lane == 0) *count = total;
+    }
+    __syncthreads();
 }
 
 // before a barrier that hands a stage over: this wave's LDS-direct loads have landed, its LDS reads have returned

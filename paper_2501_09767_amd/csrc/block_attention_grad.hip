@@ -27,7 +27,7 @@ template <int D, int WAVES, int SUBS> struct DqGeo {
     static constexpr int lds(int subtiles) { return LIST + 16 + subtiles * 4; }  // (the number of them first)
 };
 
-template <int D, int WAVES, int KS>
+template <int D, int WAVES, int KS, bool PACK>
 __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams gp) {
     const BlockAttnParams& p = gp.a;
     constexpr int SUBS = BG_STAGE<D, KS>;
@@ -49,16 +49,26 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams
     const int rows = min(p.bq, p.S_q - qb * p.bq) * p.G, row_end = min(rows, (rt + 1) * ROWS);
     auto limit_of = [&](int row) { return causal ? (int)min(pos0 + row / p.G, (long long)S - 1) : S - 1; };
 
-    if (wave == 0) {
-        const int n = rt * ROWS < rows ? list_subtiles(p.blocks + ((long long)qb * p.H_kv + g) * p.T, p.T, p.b, gp.nb, limit_of(row_end - 1), keys, lane) : 0;
-        if (lane == 0) listed = n;
+    int room = 0;  // (PACK) of the union's subtiles
+    if constexpr (PACK) {
+        const long long first = (long long)qb * p.pack;
+        const int lists = (int)min((long long)p.pack, p.n_lists - first);
+        room = min(p.pack * p.T, gp.nb) * (p.b / 32);
+        union_subtiles<WAVES>(p.blocks + (first * p.H_kv + g) * p.T, (long long)p.H_kv * p.T, lists, p.T, p.b, gp.nb, limit_of(rows - 1), reinterpret_cast<unsigned*>(smem), keys,
+                              room, &listed, wave, lane);
+    } else {
+        if (wave == 0) {
+            const int n = rt * ROWS < rows ? list_subtiles(p.blocks + ((long long)qb * p.H_kv + g) * p.T, p.T, p.b, gp.nb, limit_of(row_end - 1), keys, lane) : 0;
+            if (lane == 0) listed = n;
+        }
+        __syncthreads();
     }
-    __syncthreads();
     const int n_sub = listed, n_stage = (n_sub + SUBS - 1) / SUBS;
 
     const int row0 = rt * ROWS + wave / KS * 32, row = row0 + l32;
     const bool live = row < rows;
     const int lim = live ? limit_of(row) : -1;
+    const int member = PACK ? l32 / (p.R / p.pack) : 0;  // the row's list
     const int clean = row0 < rows ? limit_of(row0) : -1, reach = row0 < rows ? limit_of(min(row0 + 31, rows - 1)) : -1;
     const long long i_row = (long long)qb * p.bq + row / p.G;
     const int h_row = g * p.G + row % p.G;
@@ -132,11 +142,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams
                 mma_chunk<bf16_t>(dp, Tile::row_fragment(vs, c, lane), dof[c]);
             }
             float ds[16];
-            const bool masked = key + 31 > clean;
+            int mine = lim;
+            bool masked = key + 31 > clean;
+            if constexpr (PACK) {
+                const unsigned bits = keys[room + t * SUBS + j];
+                masked = masked || __popc(bits) != p.pack;
+                mine = bits >> member & 1 ? lim : -1;
+            }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 float x = fmaf(acc[r], p.c2, -lse);
-                if (masked) x = key + acc_row(r, lane) <= lim ? x : -INFINITY;
+                if (masked) x = key + acc_row(r, lane) <= mine ? x : -INFINITY;
                 ds[r] = __builtin_amdgcn_exp2f(x) * (dp[r] - delta);
             }
             u32x4 pb[2];
@@ -557,8 +573,9 @@ BlockGradLayout block_grad_layout(long long S_q, long long S_k, int H, int H_kv,
     BlockGradLayout l{};
     const long long n_qb = (S_q + bq - 1) / bq, nb = (S_k + b - 1) / b, words = (n_qb + 31) / 32, R = (long long)bq * (H / H_kv);
     const long long entries = n_qb * H_kv * (T < nb ? T : nb);
-    // Items: some two thousand for the whole launch, of 256 rows at least
-    long long share = (entries + 2047) / 2048;
+    // Items: some thousand for the whole launch and one a key block, of 256 rows at least.  dK and dV with the join, us, for about 512 / 1024 /
+    // 2048 / 4096: 8192 tokens, 32 heads, 16 blocks of 64 541 / 515 / 613 / 653; 2999 tokens, 32 / 8 heads, 12 blocks 165 / 164 / 199 / 277
+    long long share = (entries + 1023) / 1024;
     const long long least = (256 + R - 1) / R;
     if (share < least) share = least;
     l.share = (int)(share < n_qb ? share : n_qb);
@@ -582,8 +599,9 @@ BlockGradLayout block_grad_layout(long long S_q, long long S_k, int H, int H_kv,
 
 template <int D, int KS> constexpr int dq_lds(int subtiles) { return DqGeo<D, 4, BG_STAGE<D, KS>>::lds(subtiles); }
 
-template <int D, int KS> static int run_dq(const BlockGradParams& gp, hipStream_t st) {
-    hipLaunchKernelGGL((block_dq_kernel<D, 4, KS>), dim3((unsigned)((long long)gp.a.n_qb * gp.a.n_rt * gp.a.H_kv)), dim3(256), (dq_lds<D, KS>(gp.a.T * (gp.a.b / 32))), st, gp);
+template <int D, int KS, bool PACK> static int run_dq(const BlockGradParams& gp, int subtiles, hipStream_t st) {
+    hipLaunchKernelGGL((block_dq_kernel<D, 4, KS, PACK>), dim3((unsigned)((long long)gp.a.n_qb * gp.a.n_rt * gp.a.H_kv)), dim3(256),
+                       (dq_lds<D, KS>(PACK ? 2 * subtiles : subtiles)), st, gp);
     return (int)hipGetLastError();
 }
 
@@ -594,25 +612,32 @@ template <int D, int KW, int SHARES> static int run_dkv(const BlockGradParams& g
 }
 
 template <int D> static int launch_grad(BlockGradParams gp, hipStream_t st) {
-    static const int unready = raise_lds_limits({{reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 1>), dq_lds<D, 1>(MAX_LISTED_SUBTILES)},
-                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 2>), dq_lds<D, 2>(MAX_LISTED_SUBTILES)},
-                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 4>), dq_lds<D, 4>(MAX_LISTED_SUBTILES)},
+    static const int unready = raise_lds_limits({{reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 1, false>), dq_lds<D, 1>(MAX_LISTED_SUBTILES)},
+                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 2, false>), dq_lds<D, 2>(MAX_LISTED_SUBTILES)},
+                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 4, false>), dq_lds<D, 4>(MAX_LISTED_SUBTILES)},
+                                                 {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 4, true>), dq_lds<D, 4>(2 * MAX_PACKED_SUBTILES)},
                                                  {reinterpret_cast<const void*>(&block_dkv_kernel<D, 1, 4>), DkvGeo<D, 1, 4>::LDS},
                                                  {reinterpret_cast<const void*>(&block_dkv_kernel<D, 2, 4>), DkvGeo<D, 2, 4>::LDS},
                                                  {reinterpret_cast<const void*>(&block_dkv_kernel<D, 4, 2>), DkvGeo<D, 4, 2>::LDS}});
     if (unready) return unready;
     BlockAttnParams& p = gp.a;
-    const int tile = block_attention_tile_rows(p.R, 64);
-    p.n_rt = (p.R + tile - 1) / tile;
-    p.n_parts = 1;
-    p.order = head_order(p.H_kv, false, 8);
-    int rc = tile == 128 ? run_dq<D, 1>(gp, st) : tile == 64 ? run_dq<D, 2>(gp, st) : run_dq<D, 4>(gp, st);
-    if (rc) return rc;
+    BlockGradParams by_rows = gp;  // (the pass by query blocks may take several lists together)
+    {
+        BlockAttnParams& q = by_rows.a;
+        q.lengths = nullptr;
+        const int subtiles = block_attention_packed(q), tile = block_attention_tile_rows(q.R, 64);
+        q.n_rt = (q.R + tile - 1) / tile;
+        q.n_parts = 1;
+        q.order = head_order(q.H_kv, false, 8);
+        const int rc = tile == 128 ? run_dq<D, 1, false>(by_rows, subtiles, st) : tile == 64 ? run_dq<D, 2, false>(by_rows, subtiles, st)
+                     : q.pack == 1 ? run_dq<D, 4, false>(by_rows, subtiles, st) : run_dq<D, 4, true>(by_rows, subtiles, st);
+        if (rc) return rc;
+    }
     hipLaunchKernelGGL(block_bits_kernel, dim3((unsigned)gp.words, (unsigned)p.H_kv), dim3(256), gp.nb * 4, st, gp);
     hipLaunchKernelGGL(block_count_kernel, dim3((unsigned)((gp.nb + 63) / 64), (unsigned)p.H_kv), dim3(64), 0, st, gp);
     hipLaunchKernelGGL(block_layout_kernel, dim3(1), dim3(1024), 0, st, gp);
     hipLaunchKernelGGL(block_lists_kernel, dim3((unsigned)((gp.nb + 63) / 64), (unsigned)p.H_kv), dim3(64), 0, st, gp);
-    rc = (int)hipGetLastError();
+    int rc = (int)hipGetLastError();
     if (rc) return rc;
     const int subs = p.b / 32;
     rc = subs % 4 == 0 ? run_dkv<D, 4, 2>(gp, st) : subs % 2 == 0 ? run_dkv<D, 2, 4>(gp, st) : run_dkv<D, 1, 4>(gp, st);

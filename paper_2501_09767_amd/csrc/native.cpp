@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "lemo.h"
@@ -244,6 +245,286 @@ PyObject* scatter_grad(PyObject* const* a) {  // G kept_idx dX mode
     return call([=] { return lemo_scatter_grad(g, g0, ki, M, x, x0, xs, c, gt, xt, mode, st); });
 }
 
+// ---- the calls around chosen key blocks and the norms: results that are not given are allocated here, and come back in a tuple
+// behind the return code.  Their tensors have to live on the current device, as lemo.py asks.
+
+struct Place {
+    int64_t device;
+    void* stream;
+    at::TensorOptions options;
+    Place() {
+        PyObject* dev = PyObject_CallNoArgs(current_device);
+        if (!dev) { PyErr_Clear(); throw NotPlain{}; }
+        device = PyLong_AsLongLong(dev);
+        PyObject* s = PyObject_CallOneArg(raw_stream, dev);
+        Py_DECREF(dev);
+        if (!s) { PyErr_Clear(); throw NotPlain{}; }
+        stream = PyLong_AsVoidPtr(s);
+        Py_DECREF(s);
+        if (PyErr_Occurred()) { PyErr_Clear(); throw NotPlain{}; }
+        options = at::TensorOptions().device(at::kCUDA, (c10::DeviceIndex)device);
+    }
+    const at::Tensor& at(const at::Tensor& t) const {
+        need(t.device().index() == device);
+        return t;
+    }
+    // a contiguous result of the caller's, or a new one
+    at::Tensor result(PyObject* o, at::IntArrayRef shape, at::ScalarType type) const {
+        if (o == Py_None) return at::empty(shape, options.dtype(type));
+        const at::Tensor& t = at(tensor(o, (int64_t)shape.size()));
+        need(t.scalar_type() == type && t.sizes() == shape && t.is_contiguous());
+        return t;
+    }
+    at::Tensor fresh(bool wanted, at::IntArrayRef shape, at::ScalarType type) const { return wanted ? at::empty(shape, options.dtype(type)) : at::Tensor(); }
+    Bytes scratch(PyObject* o, size_t bytes, at::Tensor& keep) const {
+        if (o != Py_None) {
+            const Bytes b = workspace(o);
+            need(THPVariable_Unpack(o).device().index() == device);
+            return b;
+        }
+        if (bytes == 0) return {nullptr, 0};
+        keep = at::empty({(int64_t)bytes}, options.dtype(at::kByte));
+        return {keep.data_ptr(), bytes};
+    }
+};
+void* address(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// (return code, results...), or None where the C ABI refused
+template <typename F> PyObject* call_for(F f, std::initializer_list<at::Tensor> results) {
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = f();
+    Py_END_ALLOW_THREADS;
+    if (rc != LEMO_OK && rc != LEMO_ERR_HIP) Py_RETURN_NONE;
+    PyObject* out = PyTuple_New(1 + (Py_ssize_t)results.size());
+    if (!out) throw NotPlain{};
+    PyTuple_SET_ITEM(out, 0, PyLong_FromLong(rc));
+    Py_ssize_t i = 1;
+    for (const at::Tensor& t : results) PyTuple_SET_ITEM(out, i++, t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None));
+    return out;
+}
+
+const at::Tensor* maybe_matrix(PyObject* o, const Place& here, int64_t M, int64_t C, at::ScalarType type) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = here.at(matrix(o));
+    need(t.size(0) == M && t.size(1) == C && t.scalar_type() == type);
+    return &t;
+}
+const void* channels(PyObject* o, const Place& here, int64_t C, at::ScalarType type) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = here.at(tensor(o, 1));
+    need(t.size(0) == C && t.scalar_type() == type && t.is_contiguous());
+    return t.data_ptr();
+}
+struct NormSizes { int64_t M, S, C; const at::Tensor *Y, *gate, *kept; bool shared; const void* gate_at; int64_t ldg; };
+NormSizes norm_sizes(PyObject* y, const at::Tensor& R, PyObject* k, PyObject* g, const Place& here) {
+    NormSizes n{};
+    n.S = R.size(0);
+    n.C = R.size(1);
+    n.kept = index(k);
+    if (n.kept) here.at(*n.kept);
+    n.M = y != Py_None ? matrix(y).size(0) : n.kept ? n.kept->numel() : n.S;
+    need(!n.kept || n.kept->numel() == n.M);
+    n.Y = maybe_matrix(y, here, n.M, n.C, R.scalar_type());
+    if (g != Py_None) {
+        need(THPVariable_CheckExact(g));
+        n.shared = THPVariable_Unpack(g).dim() == 1;
+        if (n.shared) n.gate_at = channels(g, here, n.C, R.scalar_type());
+        else {
+            n.gate = maybe_matrix(g, here, n.M, n.C, R.scalar_type());
+            n.gate_at = n.gate->data_ptr();
+            n.ldg = n.gate->stride(0);
+        }
+    }
+    return n;
+}
+
+PyObject* norm_residual(PyObject* const* a) {  // Y R kept gate post next w_post b_post w_next b_next eps residual_scale block_scale flags N stats
+    const Place here;
+    const at::Tensor& R = here.at(matrix(a[1]));
+    const lemo_dtype_t dt = dtype(R);
+    const at::ScalarType type = R.scalar_type();
+    const NormSizes n = norm_sizes(a[0], R, a[2], a[3], here);
+    const int32_t post = whole32(a[4]), next = whole32(a[5]), flags = whole32(a[13]), C = size32(n.C);
+    const void *wp = channels(a[6], here, n.C, type), *bp = channels(a[7], here, n.C, type), *wn = channels(a[8], here, n.C, type), *bn = channels(a[9], here, n.C, type);
+    const float eps = real(a[10]), rs = real(a[11]), bs = real(a[12]);
+    at::Tensor N;
+    if (a[14] != Py_None) N = *maybe_matrix(a[14], here, n.M, n.C, type);
+    else if (next != LEMO_NORM_NONE) N = at::empty({n.M, n.C}, here.options.dtype(type));
+    const at::Tensor stats = here.result(a[15], {n.M, 4}, at::kFloat);
+    const void* y = n.Y ? n.Y->data_ptr() : nullptr;
+    void *r = R.data_ptr(), *out = address(N), *st = stats.data_ptr();
+    const int64_t ldy = n.Y ? n.Y->stride(0) : n.C, ldn = N.defined() ? N.stride(0) : n.C, ldr = R.stride(0);
+    const int32_t* ki = rows(n.kept);
+    return call_for([=] {
+        return lemo_norm_residual(y, ldy, n.gate_at, n.ldg, r, ldr, n.S, ki, n.M, wp, bp, post, wn, bn, next, eps, rs, bs, out, ldn, (float*)st, C, dt, (uint32_t)flags, here.stream);
+    }, {N, stats});
+}
+
+PyObject* norm_residual_grad(PyObject* const* a) {  // dN dR R Y kept stats gate post next w_post b_post w_next residual_scale block_scale flags workspace
+    const Place here;
+    const at::Tensor &dR = here.at(matrix(a[1])), &R = here.at(matrix(a[2])), &stats = here.at(tensor(a[5], 2));
+    const lemo_dtype_t dt = dtype(R);
+    const at::ScalarType type = R.scalar_type();
+    const NormSizes n = norm_sizes(a[3], R, a[4], a[6], here);
+    need(dR.sizes() == R.sizes() && dR.scalar_type() == type && stats.scalar_type() == at::kFloat && stats.is_contiguous() && stats.size(0) == n.M && stats.size(1) == 4);
+    const at::Tensor* dN = maybe_matrix(a[0], here, n.M, n.C, type);
+    const int32_t post = whole32(a[7]), next = whole32(a[8]), flags = whole32(a[14]), C = size32(n.C);
+    const void *wp = channels(a[9], here, n.C, type), *bp = channels(a[10], here, n.C, type), *wn = channels(a[11], here, n.C, type);
+    const float rs = real(a[12]), bs = real(a[13]);
+    size_t bytes = 0;
+    need(lemo_norm_residual_grad_workspace_bytes(n.M, C, &bytes) == LEMO_OK);
+    at::Tensor keep;
+    const Bytes ws = here.scratch(a[15], bytes, keep);
+    const bool p = post != LEMO_NORM_NONE, q = next != LEMO_NORM_NONE;
+    const at::Tensor dY = here.fresh(n.Y, {n.M, n.C}, type), dgate = here.fresh(n.gate, {n.M, n.C}, type), dgs = here.fresh(n.shared, {n.C}, at::kFloat);
+    const at::Tensor dwp = here.fresh(p, {n.C}, at::kFloat), dbp = here.fresh(p && (bp || post == LEMO_NORM_LAYER), {n.C}, at::kFloat);
+    const at::Tensor dwn = here.fresh(q, {n.C}, at::kFloat), dbn = here.fresh(q, {n.C}, at::kFloat);
+    const void *y = n.Y ? n.Y->data_ptr() : nullptr, *dn = dN ? dN->data_ptr() : nullptr, *r = R.data_ptr(), *stp = stats.data_ptr();
+    void *dr = dR.data_ptr(), *dy = address(dY), *dg = address(dgate), *s0 = address(dwp), *s1 = address(dbp), *s2 = address(dwn), *s3 = address(dbn), *s4 = address(dgs);
+    const int64_t ldy = n.Y ? n.Y->stride(0) : n.C, lddn = dN ? dN->stride(0) : n.C, ldr = R.stride(0), lddr = dR.stride(0);
+    const int32_t* ki = rows(n.kept);
+    return call_for([=] {
+        return lemo_norm_residual_grad(dn, lddn, dr, lddr, n.S, r, ldr, y, ldy, n.gate_at, n.ldg, ki, n.M, wp, bp, post, wn, next, rs, bs, (const float*)stp, dy, n.C, dg, n.C,
+                                       (float*)s0, (float*)s1, (float*)s2, (float*)s3, (float*)s4, C, dt, (uint32_t)flags, ws.p, ws.n, here.stream);
+    }, {dY, n.shared ? dgs : dgate, dwp, dbp, dwn, dbn});
+}
+
+int64_t blocks_of(int64_t n, int64_t b) {
+    need(b > 0);
+    return (n + b - 1) / b;
+}
+
+PyObject* block_means(PyObject* const* a) {  // K b means
+    const Place here;
+    const at::Tensor& K = here.at(heads(a[0]));
+    const lemo_dtype_t dt = dtype(K);
+    const int32_t b = whole32(a[1]), hkv = size32(K.size(1)), d = size32(K.size(2));
+    const at::Tensor means = here.result(a[2], {blocks_of(K.size(0), b), K.size(1), K.size(2)}, at::kFloat);
+    void *k = K.data_ptr(), *m = means.data_ptr();
+    const int64_t S = K.size(0), k0 = K.stride(0), k1 = K.stride(1);
+    return call_for([=] { return lemo_block_means(k, S, hkv, d, dt, k0, k1, b, (float*)m, here.stream); }, {means});
+}
+
+PyObject* select_blocks(PyObject* const* a) {  // Q means S_k b bq T flags q_start blocks
+    const Place here;
+    const at::Tensor &Q = here.at(heads(a[0])), &means = here.at(tensor(a[1], 3));
+    const lemo_dtype_t dt = dtype(Q);
+    const int64_t Sk = whole(a[2]), start = whole(a[7]), S = Q.size(0);
+    const int32_t b = whole32(a[3]), bq = whole32(a[4]), T = whole32(a[5]), flags = whole32(a[6]), h = size32(Q.size(1)), hkv = size32(means.size(1)), d = size32(Q.size(2));
+    need(Sk > 0 && T > 0 && means.scalar_type() == at::kFloat && means.is_contiguous() && means.size(0) == blocks_of(Sk, b) && means.size(2) == d);
+    const at::Tensor blocks = here.result(a[8], {blocks_of(S, bq), means.size(1), T}, at::kInt);
+    void *q = Q.data_ptr(), *m = means.data_ptr(), *o = blocks.data_ptr();
+    const int64_t q0 = Q.stride(0), q1 = Q.stride(1);
+    return call_for([=] { return lemo_select_blocks(q, S, h, hkv, d, dt, q0, q1, (const float*)m, Sk, start, b, bq, T, (uint32_t)flags, (int32_t*)o, here.stream); }, {blocks});
+}
+
+struct AttentionSizes { int64_t S, Sk; int32_t h, hkv, d, T; };
+AttentionSizes attention_sizes(const at::Tensor& Q, const at::Tensor& K, const at::Tensor& V, const at::Tensor& blocks, int64_t bq) {
+    need(K.size(2) == Q.size(2) && V.sizes() == K.sizes() && K.scalar_type() == Q.scalar_type() && V.scalar_type() == Q.scalar_type());
+    need(blocks.scalar_type() == at::kInt && blocks.is_contiguous() && blocks.size(0) == blocks_of(Q.size(0), bq) && blocks.size(1) == K.size(1));
+    return {Q.size(0), K.size(0), size32(Q.size(1)), size32(K.size(1)), size32(Q.size(2)), size32(blocks.size(2))};
+}
+
+PyObject* block_attention(PyObject* const* a) {  // Q K V blocks b bq flags scale q_start O lse2 workspace
+    const Place here;
+    const at::Tensor &Q = here.at(heads(a[0])), &K = here.at(heads(a[1])), &V = here.at(heads(a[2])), &blocks = here.at(tensor(a[3], 3));
+    const lemo_dtype_t dt = dtype(Q);
+    const int32_t b = whole32(a[4]), bq = whole32(a[5]), flags = whole32(a[6]);
+    const float scale = real(a[7]);
+    const int64_t start = whole(a[8]);
+    const AttentionSizes n = attention_sizes(Q, K, V, blocks, bq);
+    const at::Tensor O = a[9] == Py_None ? at::empty({n.S, n.h, n.d}, here.options.dtype(Q.scalar_type())) : here.at(heads(a[9]));
+    need(O.scalar_type() == Q.scalar_type() && O.sizes() == Q.sizes());
+    const at::Tensor lse2 = here.result(a[10], {n.h, n.S}, at::kFloat);
+    size_t bytes = 0;
+    need(lemo_block_attention_workspace_bytes(n.S, n.Sk, n.h, n.hkv, n.d, n.T, b, bq, &bytes) == LEMO_OK);
+    at::Tensor keep;
+    const Bytes ws = here.scratch(a[11], bytes, keep);
+    void *q = Q.data_ptr(), *k = K.data_ptr(), *v = V.data_ptr(), *bl = blocks.data_ptr(), *o = O.data_ptr(), *l = lse2.data_ptr();
+    const int64_t q0 = Q.stride(0), q1 = Q.stride(1), k0 = K.stride(0), k1 = K.stride(1), v0 = V.stride(0), v1 = V.stride(1), o0 = O.stride(0), o1 = O.stride(1);
+    return call_for([=] {
+        return lemo_block_attention(q, k, v, n.S, n.Sk, n.h, n.hkv, n.d, dt, q0, q1, k0, k1, v0, v1, (const int32_t*)bl, n.T, b, bq, start, scale, (uint32_t)flags, o, o0, o1,
+                                    (float*)l, ws.p, ws.n, here.stream);
+    }, {O, lse2});
+}
+
+PyObject* block_attention_grad(PyObject* const* a) {  // dO Q K V O lse2 blocks b bq flags scale q_start dQ dK dV workspace
+    const Place here;
+    const at::Tensor &dO = here.at(heads(a[0])), &Q = here.at(heads(a[1])), &K = here.at(heads(a[2])), &V = here.at(heads(a[3])), &O = here.at(heads(a[4]));
+    const at::Tensor &lse2 = here.at(tensor(a[5], 2)), &blocks = here.at(tensor(a[6], 3));
+    const lemo_dtype_t dt = dtype(Q);
+    const at::ScalarType type = Q.scalar_type();
+    const int32_t b = whole32(a[7]), bq = whole32(a[8]), flags = whole32(a[9]);
+    const float scale = real(a[10]);
+    const int64_t start = whole(a[11]);
+    const AttentionSizes n = attention_sizes(Q, K, V, blocks, bq);
+    need(dO.sizes() == Q.sizes() && O.sizes() == Q.sizes() && dO.scalar_type() == type && O.scalar_type() == type);
+    need(lse2.scalar_type() == at::kFloat && lse2.is_contiguous() && lse2.size(0) == n.h && lse2.size(1) == n.S);
+    const at::Tensor dQ = here.result(a[12], {n.S, n.h, n.d}, type), dK = here.result(a[13], {n.Sk, n.hkv, n.d}, type), dV = here.result(a[14], {n.Sk, n.hkv, n.d}, type);
+    size_t bytes = 0;
+    need(lemo_block_attention_grad_workspace_bytes(n.S, n.Sk, n.h, n.hkv, n.d, n.T, b, bq, &bytes) == LEMO_OK);
+    at::Tensor keep;
+    const Bytes ws = here.scratch(a[15], bytes, keep);
+    void *g = dO.data_ptr(), *q = Q.data_ptr(), *k = K.data_ptr(), *v = V.data_ptr(), *o = O.data_ptr(), *l = lse2.data_ptr(), *bl = blocks.data_ptr();
+    void *gq = dQ.data_ptr(), *gk = dK.data_ptr(), *gv = dV.data_ptr();
+    const int64_t g0 = dO.stride(0), g1 = dO.stride(1), q0 = Q.stride(0), q1 = Q.stride(1), k0 = K.stride(0), k1 = K.stride(1), v0 = V.stride(0), v1 = V.stride(1),
+                  o0 = O.stride(0), o1 = O.stride(1);
+    return call_for([=] {
+        return lemo_block_attention_grad(g, q, k, v, o, (const float*)l, n.S, n.Sk, n.h, n.hkv, n.d, dt, g0, g1, q0, q1, k0, k1, v0, v1, o0, o1, (const int32_t*)bl, n.T, b, bq,
+                                         start, scale, (uint32_t)flags, gq, gk, gv, ws.p, ws.n, here.stream);
+    }, {dQ, dK, dV});
+}
+
+const at::Tensor& cache(PyObject* o, const Place& here) {  // [B,S,H_kv,d], d contiguous
+    const at::Tensor& t = here.at(tensor(o, 4));
+    need(t.stride(3) == 1);
+    return t;
+}
+const int32_t* sequence_lengths(PyObject* o, const Place& here, int64_t B) {
+    const at::Tensor* t = index(o);
+    need(t && t->numel() == B);
+    here.at(*t);
+    return rows(t);
+}
+
+PyObject* select_blocks_step(PyObject* const* a) {  // Q means lengths b T blocks S_max
+    const Place here;
+    const at::Tensor &Q = here.at(heads(a[0])), &means = here.at(tensor(a[1], 4));
+    const lemo_dtype_t dt = dtype(Q);
+    const int32_t b = whole32(a[3]), T = whole32(a[4]), B = size32(Q.size(0)), h = size32(Q.size(1)), hkv = size32(means.size(2)), d = size32(Q.size(2));
+    const int64_t S = a[6] == Py_None ? means.size(1) * b : whole(a[6]);
+    need(S > 0 && T > 0 && means.scalar_type() == at::kFloat && means.is_contiguous() && means.size(0) == B && means.size(1) == blocks_of(S, b) && means.size(3) == d);
+    const int32_t* len = sequence_lengths(a[2], here, B);
+    const at::Tensor blocks = here.result(a[5], {B, means.size(2), T}, at::kInt);
+    void *q = Q.data_ptr(), *m = means.data_ptr(), *o = blocks.data_ptr();
+    const int64_t q0 = Q.stride(0), q1 = Q.stride(1);
+    return call_for([=] { return lemo_select_blocks_step(q, B, h, hkv, d, dt, q0, q1, (const float*)m, S, len, b, T, (int32_t*)o, here.stream); }, {blocks});
+}
+
+PyObject* block_attention_step(PyObject* const* a) {  // Q K V lengths blocks b scale O workspace
+    const Place here;
+    const at::Tensor &Q = here.at(heads(a[0])), &K = cache(a[1], here), &V = cache(a[2], here), &blocks = here.at(tensor(a[4], 3));
+    const lemo_dtype_t dt = dtype(Q);
+    const int32_t b = whole32(a[5]), B = size32(Q.size(0)), h = size32(Q.size(1)), hkv = size32(K.size(2)), d = size32(Q.size(2)), T = size32(blocks.size(2));
+    const float scale = real(a[6]);
+    need(K.size(0) == B && K.size(3) == d && V.sizes() == K.sizes() && K.scalar_type() == Q.scalar_type() && V.scalar_type() == Q.scalar_type());
+    need(blocks.scalar_type() == at::kInt && blocks.is_contiguous() && blocks.size(0) == B && blocks.size(1) == hkv);
+    const int32_t* len = sequence_lengths(a[3], here, B);
+    const at::Tensor O = a[7] == Py_None ? at::empty({B, h, d}, here.options.dtype(Q.scalar_type())) : here.at(heads(a[7]));
+    need(O.scalar_type() == Q.scalar_type() && O.sizes() == Q.sizes());
+    size_t bytes = 0;
+    need(lemo_block_attention_step_workspace_bytes(B, h, hkv, d, T, b, &bytes) == LEMO_OK);
+    at::Tensor keep;
+    const Bytes ws = here.scratch(a[8], bytes, keep);
+    void *q = Q.data_ptr(), *k = K.data_ptr(), *v = V.data_ptr(), *bl = blocks.data_ptr(), *o = O.data_ptr();
+    const int64_t S = K.size(1), q0 = Q.stride(0), q1 = Q.stride(1), k0 = K.stride(0), k1 = K.stride(1), k2 = K.stride(2), v0 = V.stride(0), v1 = V.stride(1), v2 = V.stride(2),
+                  o0 = O.stride(0), o1 = O.stride(1);
+    return call_for([=] {
+        return lemo_block_attention_step(q, k, v, B, S, h, hkv, d, dt, q0, q1, k0, k1, k2, v0, v1, v2, len, (const int32_t*)bl, T, b, scale, o, o0, o1, ws.p, ws.n, here.stream);
+    }, {O});
+}
+
 PyObject* set_stream_source(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 2) {
         PyErr_SetString(PyExc_TypeError, "set_stream_source(current_device, raw_stream)");
@@ -257,6 +538,8 @@ PyObject* set_stream_source(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define LEMO_FAST(name, n) {#name, (PyCFunction)(void*)(guarded<n, name>), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LEMO_FAST(score_segments, 9), LEMO_FAST(select_topk, 4), LEMO_FAST(kept_attention, 9), LEMO_FAST(gather_gemm, 6),
                          LEMO_FAST(gather_gemm_add, 7), LEMO_FAST(gather_gemm_dx, 4), LEMO_FAST(gather_gemm_dw, 5), LEMO_FAST(scatter_grad, 4),
+                         LEMO_FAST(norm_residual, 16), LEMO_FAST(norm_residual_grad, 16), LEMO_FAST(block_means, 3), LEMO_FAST(select_blocks, 9),
+                         LEMO_FAST(block_attention, 12), LEMO_FAST(block_attention_grad, 16), LEMO_FAST(select_blocks_step, 7), LEMO_FAST(block_attention_step, 9),
                          {"set_stream_source", (PyCFunction)(void*)set_stream_source, METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "lemo_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -112,7 +112,7 @@ def _load() -> ctypes.CDLL:
                                             vp, vp, vp, vp, vp, i32, ctypes.c_int, u32, vp, ctypes.c_size_t, vp]
     size = ctypes.POINTER(ctypes.c_size_t)
     kinds = {"p": vp, "l": i64, "i": i32, "f": f32, "u": u32, "z": ctypes.c_size_t, "s": size}
-    for name, args in (("block_means", "pliiillipp"), ("select_blocks", "pliiiillplliiiupp"), ("block_attention_workspace_bytes", "liiiiiis"),
+    for name, args in (("block_means", "pliiillipp"), ("select_blocks", "pliiiillplliiiupp"), ("block_attention_workspace_bytes", "lliiiiiis"),
                        ("block_attention", "pppll" "iiii" "llllll" "piiil" "fu" "pllp" "pzp"), ("block_attention_grad_workspace_bytes", "lliiiiiis"),
                        ("block_attention_grad", "pppppp" "ll" "iiii" "llllllllll" "piiil" "fu" "ppp" "pzp"), ("block_means_step", "piliiilllpipp"),
                        ("select_blocks_step", "piiiiillplpiipp"), ("block_attention_step_workspace_bytes", "iiiiiis"),
@@ -687,6 +687,10 @@ def lemo_norm_residual(Y: Optional[torch.Tensor], R: torch.Tensor, kept_idx: Opt
                        block_scale: float = 1.0, flags: int = 0, N: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None):
     """In place: R[kept_idx] = residual_scale * R[kept_idx] + block_scale * gate * post(Y) -> (N = next(R[kept_idx]) [M,C] or None,
     stats [M,4] float32).  Y [M,C] or None, R [S,C], gate [M,C] or one row [C]."""
+    done = _native.norm_residual(Y, R, kept_idx, gate, post, next, w_post, b_post, w_next, b_next, eps, residual_scale, block_scale, flags, N, stats)
+    if done is not None:
+        _check(done[0], "lemo_norm_residual")
+        return done[1], done[2]
     _here(Y, R, kept_idx, gate, w_post, b_post, w_next, b_next, N, stats)
     M, S, C, ldy, ldg, ldr = _norm_args(Y, R, kept_idx, gate, w_post, b_post, w_next, b_next)
     if N is None and next != NORM_NONE:
@@ -714,6 +718,10 @@ def lemo_norm_residual_grad(dN: Optional[torch.Tensor], dR: torch.Tensor, R: tor
                             residual_scale: float = 1.0, block_scale: float = 1.0, flags: int = 0, workspace: Optional[torch.Tensor] = None) -> NormGrads:
     """Gradients of lemo_norm_residual: dR [S,C] (of the new residual rows) becomes that of the old ones in place; returns the others.
     R, Y, gate, stats as the forward call left or took them."""
+    done = _native.norm_residual_grad(dN, dR, R, Y, kept_idx, stats, gate, post, next, w_post, b_post, w_next, residual_scale, block_scale, flags, workspace)
+    if done is not None:
+        _check(done[0], "lemo_norm_residual_grad")
+        return NormGrads(*done[1:])
     _here(dN, dR, R, Y, kept_idx, stats, gate, w_post, b_post, w_next, workspace)
     M, S, C, ldy, ldg, ldr = _norm_args(Y, R, kept_idx, gate, w_post, b_post, w_next, None)
     if tuple(dR.shape) != (S, C) or dR.dtype != R.dtype or (dR.stride(1) != 1 and C > 1):
@@ -787,6 +795,10 @@ def _scratch(workspace: Optional[torch.Tensor], need: int, device):
 
 def lemo_block_means(K: torch.Tensor, b: int, means: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Mean key of every block of b tokens: K [S,H_kv,d] -> [ceil(S/b),H_kv,d] float32."""
+    done = _native.block_means(K, b, means)
+    if done is not None:
+        _check(done[0], "lemo_block_means")
+        return done[1]
     _here(K, means)
     _heads(K, 3, "K")
     S, Hkv, d = K.shape
@@ -798,6 +810,10 @@ def lemo_block_means(K: torch.Tensor, b: int, means: Optional[torch.Tensor] = No
 def lemo_select_blocks(Q: torch.Tensor, means: torch.Tensor, S_k: int, b: int, bq: int, T: int, flags: int = CAUSAL, q_start: int = 0,
                        blocks: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The T key blocks that each block of bq queries lists, per KV head -> [ceil(S_q/bq),H_kv,T] int32, ascending, -1 behind them."""
+    done = _native.select_blocks(Q, means, S_k, b, bq, T, flags, q_start, blocks)
+    if done is not None:
+        _check(done[0], "lemo_select_blocks")
+        return done[1]
     _here(Q, means, blocks)
     _heads(Q, 3, "Q")
     S, H, d = Q.shape
@@ -826,6 +842,10 @@ def lemo_block_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, bloc
                          q_start: int = 0, O: Optional[torch.Tensor] = None, lse2: Optional[torch.Tensor] = None,
                          workspace: Optional[torch.Tensor] = None):
     """Attention of Q [S_q,H,d] over the key blocks that `blocks` lists, K and V [S_k,H_kv,d] -> (O [S_q,H,d], lse2 [H,S_q] float32)."""
+    done = _native.block_attention(Q, K, V, blocks, b, bq, flags, scale, q_start, O, lse2, workspace)
+    if done is not None:
+        _check(done[0], "lemo_block_attention")
+        return done[1], done[2]
     _here(Q, K, V, blocks, O, lse2, workspace)
     S, Sk, H, Hkv, d, T = _attention_sizes(Q, K, V, blocks, b, bq)
     if O is None:
@@ -833,7 +853,7 @@ def lemo_block_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, bloc
     _heads(O, 3, "O")
     _fits(O, (S, H, d), Q.dtype, "O")
     lse2 = _filled(lse2, (H, S), torch.float32, Q.device, "lse2")
-    workspace, size = _scratch(workspace, _bytes("lemo_block_attention_workspace_bytes", S, H, Hkv, d, T, int(b), int(bq)), Q.device)
+    workspace, size = _scratch(workspace, _bytes("lemo_block_attention_workspace_bytes", S, Sk, H, Hkv, d, T, int(b), int(bq)), Q.device)
     _check(_lib.lemo_block_attention(_ptr(Q), _ptr(K), _ptr(V), S, Sk, H, Hkv, d, _dt(Q), Q.stride(0), Q.stride(1), K.stride(0), K.stride(1), V.stride(0),
                                      V.stride(1), _ptr(blocks), T, int(b), int(bq), int(q_start), float(scale), int(flags), _ptr(O), O.stride(0),
                                      O.stride(1), _ptr(lse2), _ptr(workspace), size, _stream()), "lemo_block_attention")
@@ -844,6 +864,10 @@ def lemo_block_attention_grad(dO: torch.Tensor, Q: torch.Tensor, K: torch.Tensor
                               b: int, bq: int, flags: int = CAUSAL, scale: float = 0.0, q_start: int = 0, dQ: Optional[torch.Tensor] = None,
                               dK: Optional[torch.Tensor] = None, dV: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """Gradients of lemo_block_attention, O and lse2 as it left them -> (dQ [S_q,H,d], dK [S_k,H_kv,d], dV [S_k,H_kv,d])."""
+    done = _native.block_attention_grad(dO, Q, K, V, O, lse2, blocks, b, bq, flags, scale, q_start, dQ, dK, dV, workspace)
+    if done is not None:
+        _check(done[0], "lemo_block_attention_grad")
+        return done[1], done[2], done[3]
     _here(dO, Q, K, V, O, lse2, blocks, dQ, dK, dV, workspace)
     S, Sk, H, Hkv, d, T = _attention_sizes(Q, K, V, blocks, b, bq)
     for name, t in (("dO", dO), ("O", O)):
@@ -882,6 +906,10 @@ def lemo_select_blocks_step(Q: torch.Tensor, means: torch.Tensor, lengths: torch
                             S_max: Optional[int] = None) -> torch.Tensor:
     """Key blocks for the newest token of each sequence: Q [B,H,d], means [B,ceil(S_max/b),H_kv,d] float32 -> [B,H_kv,T] int32.
     S_max: the cache's tokens (all that the means cover if not given)."""
+    done = _native.select_blocks_step(Q, means, lengths, b, T, blocks, S_max)
+    if done is not None:
+        _check(done[0], "lemo_select_blocks_step")
+        return done[1]
     _here(Q, means, lengths, blocks)
     _heads(Q, 3, "Q")
     B, H, d = Q.shape
@@ -902,6 +930,10 @@ def lemo_select_blocks_step(Q: torch.Tensor, means: torch.Tensor, lengths: torch
 def lemo_block_attention_step(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lengths: torch.Tensor, blocks: torch.Tensor, b: int, scale: float = 0.0,
                               O: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the newest token of each sequence over its listed blocks: Q [B,H,d], K and V [B,S_max,H_kv,d] -> O [B,H,d]."""
+    done = _native.block_attention_step(Q, K, V, lengths, blocks, b, scale, O, workspace)
+    if done is not None:
+        _check(done[0], "lemo_block_attention_step")
+        return done[1]
     _here(Q, K, V, lengths, blocks, O, workspace)
     _heads(Q, 3, "Q")
     _heads(K, 4, "K")

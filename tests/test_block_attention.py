@@ -432,9 +432,9 @@ def test_argument_errors():
     assert f(flags=2) == -2 and f(H=3) == -2 and f(T=1) == -2 and f(bq=64, T=2) == -2 and f(dt=-1) == -3 and f(ts=100) == -5 and f(out=P[2] + 1) == -5
     assert f(d=32) == -6 and f(b=40) == -6 and f(Sk=32 * 16384 + 1) == -6 and f(T=5000) == -6 and f(bq=1 << 24, S=1 << 25) == -6
     n = ctypes.c_size_t()
-    assert lib.lemo_block_attention_workspace_bytes(100, 4, 2, 64, 4, 32, 16, None) == -1 and lib.lemo_block_attention_workspace_bytes(100, 4, 3, 64, 4, 32, 16, ctypes.byref(n)) == -2
-    assert lib.lemo_block_attention_workspace_bytes(65536, 32, 8, 128, 16, 64, 64, ctypes.byref(n)) == 0 and n.value == 0
-    assert lib.lemo_block_attention_workspace_bytes(1, 32, 8, 128, 16, 64, 1, ctypes.byref(n)) == 0 and n.value > 0
+    assert lib.lemo_block_attention_workspace_bytes(100, 1000, 4, 2, 64, 4, 32, 16, None) == -1 and lib.lemo_block_attention_workspace_bytes(100, 1000, 4, 3, 64, 4, 32, 16, ctypes.byref(n)) == -2
+    assert lib.lemo_block_attention_workspace_bytes(65536, 65536, 32, 8, 128, 16, 64, 64, ctypes.byref(n)) == 0 and n.value == 0
+    assert lib.lemo_block_attention_workspace_bytes(1, 32768, 32, 8, 128, 16, 64, 1, ctypes.byref(n)) == 0 and n.value > 0
     names = "Q K V S Sk H Hkv d dt qt qh kt kh vt vh blocks T b bq start scale flags O ot oh lse ws wsb st"
     ok = dict(Q=P[0], K=P[1], V=P[2], S=100, Sk=1000, H=4, Hkv=2, d=64, dt=1, qt=256, qh=64, kt=128, kh=64, vt=128, vh=64, blocks=P[3], T=16, b=32, bq=16, start=0,
               scale=0.0, flags=1, O=P[4], ot=256, oh=64, lse=P[5], ws=P[6], wsb=1 << 30, st=None)
