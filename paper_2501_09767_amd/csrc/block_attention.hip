@@ -103,10 +103,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAtt
             int key = first_key[i * WAVES / PER_SUB % STAGE];
 #pragma unroll
             for (int k = 1; k < AT_ONCE; ++k) key = wave / PER_SUB == k ? first_key[(i * WAVES / PER_SUB + k) % STAGE] : key;
-            const long long pitch = (v ? p.v_ts : p.k_ts) * 2;
-            const u32x4 rsrc = raw_rsrc((v ? vbase : kbase) + (long long)min(key, S) * pitch, key < S ? (long long)(S - 1 - key) * pitch + Tile::ROWB : 0);
+            const int pitch = (int)(v ? p.v_ts : p.k_ts) * 2;
+            const u32x4 rsrc = subtile_rsrc<D>(v ? vbase : kbase, min(key, S), S, pitch);
             const int r = part * RPI + in_row;
-            lds_direct_b128(rsrc, lds_offset_of(smem) + buf * Geo::STAGE + which * Geo::SUB + part * 1024, r * (int)pitch + ((pos ^ Tile::swz(r)) << 4));
+            lds_direct_b128(rsrc, lds_offset_of(smem) + buf * Geo::STAGE + which * Geo::SUB + part * 1024, r * pitch + ((pos ^ Tile::swz(r)) << 4));
         }
     };
 
@@ -299,19 +299,23 @@ int block_attention_parts(long long tiles, long long subtiles) {
     return parts < 1 ? 1 : (int)parts;
 }
 
-template <int D, int KS> constexpr int ba_lds(int subtiles) { return BaGeo<D, 4, BA_STAGE<D, KS>>::lds(subtiles); }
+template <int D> constexpr int FEW = D == 128 ? 2 : 4;  // waves that share lists of few rows, where there are many of these
+
+template <int D, int WAVES, int KS> constexpr int ba_lds(int subtiles) { return BaGeo<D, WAVES, BA_STAGE<D, KS>>::lds(subtiles); }
 
 template <int D> static int prepare_block_attention() {
-    static const int err = raise_lds_limits({{reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 1, false>), ba_lds<D, 1>(MAX_LISTED_SUBTILES)},
-                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 2, false>), ba_lds<D, 2>(MAX_LISTED_SUBTILES)},
-                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 4, false>), ba_lds<D, 4>(MAX_LISTED_SUBTILES)},
-                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 4, true>), ba_lds<D, 4>(2 * MAX_PACKED_SUBTILES)}});
+    static const int err = raise_lds_limits({{reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 1, false>), ba_lds<D, 4, 1>(MAX_LISTED_SUBTILES)},
+                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 2, false>), ba_lds<D, 4, 2>(MAX_LISTED_SUBTILES)},
+                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, FEW<D>, FEW<D>, false>), ba_lds<D, FEW<D>, FEW<D>>(MAX_LISTED_SUBTILES)},
+                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, FEW<D>, FEW<D>, true>), ba_lds<D, FEW<D>, FEW<D>>(2 * MAX_PACKED_SUBTILES)},
+                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 4, false>), ba_lds<D, 4, 4>(MAX_LISTED_SUBTILES)},
+                                             {reinterpret_cast<const void*>(&block_attention_kernel<D, 4, 4, true>), ba_lds<D, 4, 4>(2 * MAX_PACKED_SUBTILES)}});
     return err;
 }
 
-template <int D, int KS, bool PACK> static int run_block_attention(const BlockAttnParams& p, int subtiles, hipStream_t st) {
-    hipLaunchKernelGGL((block_attention_kernel<D, 4, KS, PACK>), dim3((unsigned)((long long)p.n_qb * p.n_rt * p.n_parts * p.H_kv)), dim3(256),
-                       (ba_lds<D, KS>(PACK ? 2 * subtiles : subtiles)), st, p);
+template <int D, int WAVES, int KS, bool PACK> static int run_block_attention(const BlockAttnParams& p, int subtiles, hipStream_t st) {
+    hipLaunchKernelGGL((block_attention_kernel<D, WAVES, KS, PACK>), dim3((unsigned)((long long)p.n_qb * p.n_rt * p.n_parts * p.H_kv)), dim3(WAVES * 64),
+                       (ba_lds<D, WAVES, KS>(PACK ? 2 * subtiles : subtiles)), st, p);
     return (int)hipGetLastError();
 }
 
@@ -323,9 +327,14 @@ template <int D> static int launch_block_attention_d(BlockAttnParams p, hipStrea
     p.n_rt = (p.R + tile - 1) / tile;
     p.n_parts = p.parts ? block_attention_parts((long long)p.n_qb * p.n_rt * p.H_kv, subtiles) : 1;
     p.order = head_order(p.H_kv, false, 8);
-    const int rc = tile == 256 ? launch_block_attention_pipe(p, st) : tile == 128 ? run_block_attention<D, 1, false>(p, subtiles, st)
-                 : tile == 64 ? run_block_attention<D, 2, false>(p, subtiles, st) : p.pack == 1 ? run_block_attention<D, 4, false>(p, subtiles, st)
-                 : run_block_attention<D, 4, true>(p, subtiles, st);
+    // lists of few rows: four waves share them; many of them, heads of 128: two waves with stages of 64 keys, so that two workgroups fit a CU
+    // (us, 4 / 2 waves: one token of 1, 8, 64, 256 sequences, 32 / 8 heads, 16 blocks of 64: 14.8 / 16.1, 15.8 / 18.9, 53.5 / 50.8, 217 / 207;
+    // 8192 tokens, 32 heads, a list for 16: 1134 / 1070, 16 heads, 12 blocks of 32: 315 / 278)
+    const bool many = D == 128 && (long long)p.n_qb * p.n_parts * p.H_kv >= 512;
+    const int rc = tile == 256 ? launch_block_attention_pipe(p, st) : tile == 128 ? run_block_attention<D, 4, 1, false>(p, subtiles, st)
+                 : tile == 64 ? run_block_attention<D, 4, 2, false>(p, subtiles, st)
+                 : p.pack == 1 ? (many ? run_block_attention<D, FEW<D>, FEW<D>, false>(p, subtiles, st) : run_block_attention<D, 4, 4, false>(p, subtiles, st))
+                 : many ? run_block_attention<D, FEW<D>, FEW<D>, true>(p, subtiles, st) : run_block_attention<D, 4, 4, true>(p, subtiles, st);
     if (rc || p.n_parts == 1) return rc;
     const long long rows = (long long)p.n_qb * p.H_kv * p.R, per = 256 / (D / 8);
     hipLaunchKernelGGL((block_attention_join_kernel<D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, p);

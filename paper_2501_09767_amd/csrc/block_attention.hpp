@@ -44,7 +44,7 @@ struct BlockGradParams {
 
 struct BlockGradLayout { size_t delta, bits, counts, first, lists, slots, items, totals, partial, bytes; int share, max_items; };
 
-constexpr int MAX_LISTED_SUBTILES = 4096;  // subtiles of 32 keys that a list may name: they stand in LDS, 16 KB
+constexpr int MAX_LISTED_SUBTILES = 3840;  // subtiles of 32 keys that a list may name: they stand in LDS, 15 KB (two lists of them beside two stages)
 constexpr int MAX_PACKED_SUBTILES = 2048;  // of the union of lists, with a word of bits each
 constexpr int MAX_LISTED_BLOCKS = 16384;   // key blocks that a choice is made from: their scores stand in LDS, 128 KB
 
@@ -130,12 +130,26 @@ template <int D> struct TilePlace {
     }
 };
 
+// Descriptor of the rows of a subtile from key `key` on, as many of the 32 as there are (none: S == key): what lies behind them arrives as
+// zeros.  32-bit scalar arithmetic and no branch: 64-bit selections would put one beside every load.
+template <int D> __device__ __forceinline__ u32x4 subtile_rsrc(const char* base, int key, int S, int pitch) {
+    const unsigned long long a = reinterpret_cast<unsigned long long>(base) + (unsigned long long)(unsigned)key * (unsigned)pitch;
+    u32x4 r;
+    r[0] = (unsigned)a;
+    r[1] = (unsigned)(a >> 32) & 0xffffu;
+    r[2] = (unsigned)max((min(S - key, 32) - 1) * pitch + HeadTile<D>::ROWB, 0);  // (a pitch below a row's bytes: the row before ends where this does)
+    r[3] = 0x00020000u;
+    return r;
+}
+
 // The list of a query block as the rule for it says: an entry counts if it names a block, [0, nb), and lies above every such entry
-// before it.  One wave; `take(entry, counts)` is called for 64 entries at a time, by all lanes.
-template <typename F> __device__ __forceinline__ void walk_list(const int* list, int T, int nb, int lane, F&& take) {
+// before it.  One wave; `take(entry, counts)` is called for 64 entries at a time, by all lanes.  `head`: this lane's entry of the
+// first 64 (what lies past the list is -1).
+__device__ __forceinline__ int list_head(const int* list, int T, int lane) { return lane < T ? list[lane] : -1; }
+template <typename F> __device__ __forceinline__ void walk_list(const int* list, int T, int nb, int lane, int head, F&& take) {
     int top = -1;  // highest block so far
     for (int e0 = 0; e0 < T; e0 += 64) {
-        const int raw = e0 + lane < T ? list[e0 + lane] : -1, n = raw >= 0 && raw < nb ? raw : -1;
+        const int raw = e0 == 0 ? head : e0 + lane < T ? list[e0 + lane] : -1, n = raw >= 0 && raw < nb ? raw : -1;
         int high = n;
 #pragma unroll
         for (int s = 1; s < 64; s <<= 1) {
@@ -147,12 +161,15 @@ template <typename F> __device__ __forceinline__ void walk_list(const int* list,
         top = max(top, __shfl(high, 63));
     }
 }
+template <typename F> __device__ __forceinline__ void walk_list(const int* list, int T, int nb, int lane, F&& take) {
+    walk_list(list, T, nb, lane, list_head(list, T, lane), take);
+}
 
 // The subtiles of a list up to key `limit`, as first keys in `keys` (LDS); returns how many.  One wave.
-__device__ __forceinline__ int list_subtiles(const int* list, int T, int b, int nb, int limit, int* keys, int lane) {
+__device__ __forceinline__ int list_subtiles(const int* list, int T, int b, int nb, int limit, int* keys, int lane, int head) {
     int count = 0;
     const int most = b / 32;
-    walk_list(list, T, nb, lane, [&](int n, bool counts) {
+    walk_list(list, T, nb, lane, head, [&](int n, bool counts) {
         const int first = n * b;
         const int mine = counts && first <= limit ? min(most, (limit - first) / 32 + 1) : 0;
         int sum = mine;
@@ -166,6 +183,10 @@ __device__ __forceinline__ int list_subtiles(const int* list, int T, int b, int 
         count += __shfl(sum, 63);
     });
     return count;
+}
+
+__device__ __forceinline__ int list_subtiles(const int* list, int T, int b, int nb, int limit, int* keys, int lane) {
+    return list_subtiles(list, T, b, nb, limit, keys, lane, list_head(list, T, lane));
 }
 
 // Several lists of few rows as one: the subtiles of all blocks that any of `lists` consecutive lists names, with a bit for each list that

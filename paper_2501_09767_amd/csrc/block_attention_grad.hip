@@ -111,10 +111,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams
             int key = first_key[i * WAVES / PER_SUB % SUBS];
 #pragma unroll
             for (int k = 1; k < AT_ONCE; ++k) key = wave / PER_SUB == k ? first_key[(i * WAVES / PER_SUB + k) % SUBS] : key;
-            const long long pitch = (v ? p.v_ts : p.k_ts) * 2;
-            const u32x4 rsrc = raw_rsrc((v ? vbase : kbase) + (long long)min(key, S) * pitch, key < S ? (long long)(S - 1 - key) * pitch + Tile::ROWB : 0);
+            const int pitch = (int)(v ? p.v_ts : p.k_ts) * 2;
+            const u32x4 rsrc = subtile_rsrc<D>(v ? vbase : kbase, min(key, S), S, pitch);
             const int r = part * RPI + in_row;
-            lds_direct_b128(rsrc, lds_offset_of(smem) + buf * Geo::STAGE + which * Geo::SUB + part * 1024, r * (int)pitch + ((pos ^ Tile::swz(r)) << 4));
+            lds_direct_b128(rsrc, lds_offset_of(smem) + buf * Geo::STAGE + which * Geo::SUB + part * 1024, r * pitch + ((pos ^ Tile::swz(r)) << 4));
         }
     };
     f32x16 dq[Tile::COLS];

@@ -310,7 +310,9 @@ template <typename T, int D> static int run_select_blocks(const BlockSelectParam
                                              {reinterpret_cast<const void*>(&select_blocks_kernel<T, D, 1, 1024>), SelGeo<T, D, 1, 1024>::lds(MAX_LISTED_BLOCKS)}});
     if (err) return err;
     const long long lists = (long long)p.n_qb * p.H_kv;
-    if (p.lengths || lists <= 256) return run_select_lists<T, D, 1, 1024>(p, st);
+    // few lists: 16 waves each (us, 1024 / 256 threads, one token of 1, 8, 64, 256 sequences, 32 / 8 heads, 512 to 64 blocks: 11.9 / 13.5,
+    // 10.2 / 10.2, 27 / 22, 42 / 10)
+    if (lists <= 64) return run_select_lists<T, D, 1, 1024>(p, st);
     // lists of few rows: the more of them a workgroup makes, the less often it reads the means; their scores take LDS, and there have
     // to be workgroups
     if (p.bq * p.G < 64) {

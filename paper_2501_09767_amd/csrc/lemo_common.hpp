@@ -150,9 +150,9 @@ inline HeadOrder head_order(int H, bool causal, int limit) {
     const int heads = per_xcd ? per_xcd : H, together = (causal ? limit : 1) * (per_xcd ? 1 : NUM_XCD);
     return {per_xcd, heads < (1 << 15) ? (heads + together - 1) / together : 1};  // (the products of decode_block fit 32 bits)
 }
-__device__ __forceinline__ void decode_block(HeadOrder o, int H, int nblk, int& h, int& rank) {
+__device__ __forceinline__ void decode_block(HeadOrder o, int H, int nblk, int& h, int& rank, int block = blockIdx.x) {
     const bool dealt = o.per_xcd == 0;
-    const int x = dealt ? 0 : blockIdx.x % NUM_XCD, w = dealt ? blockIdx.x : blockIdx.x / NUM_XCD, heads = dealt ? H : o.per_xcd;
+    const int x = dealt ? 0 : block % NUM_XCD, w = dealt ? block : block / NUM_XCD, heads = dealt ? H : o.per_xcd;
     int first = 0, width = heads;
     if (o.groups > 1) {  // group g holds heads [g * heads / groups, (g + 1) * heads / groups)
         const int g = ((w / nblk + 1) * o.groups - 1) / heads;

@@ -139,6 +139,11 @@ CASES = [
     _c(600, 600, 2, 2, 128, 64, 1, 3, kind="first"),
     _c(40, 64, 4, 2, 128, 32, 8, 2, q_start=24, kind="none"),
     _c(64, 40, 4, 2, 64, 32, 16, 2, q_start=500),
+    # more tiles of 256 rows than there are CUs: a workgroup walks over several lists
+    _c(700, 700, 80, 20, 128, 32, 48, 9),
+    _c(330, 500, 72, 24, 128, 64, 50, 6, q_start=100, kind="any"),
+    _c(250, 300, 96, 48, 128, 32, 100, 12, causal=False, kind="any"),
+    _c(400, 400, 66, 33, 128, 32, 70, 5, kind="none"),
 ]
 
 
@@ -160,6 +165,26 @@ def test_attention_and_gradients_against_64_bits(lemo, n):
     check_grads(grads, ref)
     again = lemo.lemo_block_attention_grad(d[4], d[0], d[1], d[2], O, lse2, d[3], case["b"], case["bq"], flags, q_start=case["q_start"])
     assert all(torch.equal(x, y) for x, y in zip(grads, again))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,H_kv,d,S,bq", [(4, 1, 128, 640, 64), (80, 20, 128, 640, 64), (2, 2, 128, 640, 64), (4, 1, 64, 640, 64), (8, 2, 128, 320, 1)])
+def test_keys_that_outgrow_the_first_ones(lemo, H, H_kv, d, S, bq):
+    """Logits whose later values lie hundreds above the first: references that a first stage left have to give way."""
+    case = _c(S, S, H, H_kv, d, 32, bq, 16)
+    Q, K, V = draw(3, (S, H, d), (S, H_kv, d), (S, H_kv, d))
+    blocks = torch.full((-(-S // bq), H_kv, 16), -1, dtype=torch.int32)
+    for m in range(len(blocks)):
+        last = (min((m + 1) * bq, S) - 1) // 32
+        pick = list(range(last + 1))[-16:]
+        blocks[m, :, :len(pick)] = torch.tensor(pick, dtype=torch.int32)
+    # every third query looks along one direction, and one key in 150 lies far out along it
+    Q[::3] = 4.0
+    K[149::150] = 30.0 * torch.linspace(0.2, 1.0, len(K[149::150]))[:, None, None].to(torch.bfloat16)
+    O, lse2 = lemo.lemo_block_attention(Q.cuda(), K.cuda(), V.cuda(), blocks.cuda(), 32, bq)
+    ref = reference(case, Q, K, V, blocks)
+    assert ref["lse2"].max() - ref["lse2"].min() > 150
+    check_forward(O, lse2, ref)
 
 
 @pytest.mark.gpu
