@@ -227,37 +227,32 @@ __global__ __launch_bounds__(THREADS) void select_blocks_kernel(BlockSelectParam
         }
     }
     __syncthreads();
-    for (int list = wave; list < RB; list += WAVES) {
-        if (queries_of(qb0 + list) == 0) break;
+    // The whole 64 bits of a list's scores, one wave: where the upper halves do not tell (or are too many for the registers)
+    auto choose = [&](int list) {
         const int count = counts[list], wanted = min(p.T, count);
         const unsigned long long* const mine = keys + list * p.nb;
         int* const out = p.blocks + ((qb0 + list) * p.H_kv + g) * p.T;
         unsigned long long cut = 1;
         bool exact = count <= p.T;
         if (!exact) {
-            unsigned top = 0;
-            auto halves = [&](auto held) {  // upper halves of the first scores stay in registers
-                constexpr int HELD = decltype(held)::value;
-                unsigned high[HELD];
+            constexpr int HELD = 8;  // upper halves of the first 512 scores stay in registers
+            unsigned high[HELD], top = 0;
 #pragma unroll
-                for (int i = 0; i < HELD; ++i) high[i] = i * 64 + lane < count ? (unsigned)(mine[i * 64 + lane] >> 32) : 0;
-                for (int bit = 31; bit >= 0 && !exact; --bit) {
-                    const unsigned mark = top | 1u << bit;
-                    int reach = 0;
+            for (int i = 0; i < HELD; ++i) high[i] = i * 64 + lane < count ? (unsigned)(mine[i * 64 + lane] >> 32) : 0;
+            for (int bit = 31; bit >= 0 && !exact; --bit) {
+                const unsigned mark = top | 1u << bit;
+                int reach = 0;
 #pragma unroll
-                    for (int i = 0; i < HELD; ++i) reach += (int)__popcll(__ballot(high[i] >= mark));
-                    for (int n = HELD * 64 + lane; n < count + lane; n += 64) reach += (int)__popcll(__ballot(n < count && (unsigned)(mine[n] >> 32) >= mark));
-                    if (reach >= wanted) top = mark;
-                    exact = reach == wanted;
-                }
-            };
-            if (count <= 128) halves(std::integral_constant<int, 2>{});
-            else halves(std::integral_constant<int, 8>{});
+                for (int i = 0; i < HELD; ++i) reach += (int)__popcll(__ballot(high[i] >= mark));
+                for (int n0 = HELD * 64; n0 < count; n0 += 64) reach += (int)__popcll(__ballot(n0 + lane < count && (unsigned)(mine[n0 + lane] >> 32) >= mark));
+                if (reach >= wanted) top = mark;
+                exact = reach == wanted;
+            }
             cut = (unsigned long long)top << 32;
             for (int bit = 31; bit >= 0 && !exact; --bit) {
                 const unsigned long long mark = cut | 1ull << bit;
                 int reach = 0;
-                for (int n = lane; n < count + lane; n += 64) reach += (int)__popcll(__ballot(n < count && mine[n] >= mark));
+                for (int n0 = 0; n0 < count; n0 += 64) reach += (int)__popcll(__ballot(n0 + lane < count && mine[n0 + lane] >= mark));
                 if (reach >= wanted) cut = mark;
                 exact = reach == wanted;
             }
@@ -265,19 +260,65 @@ __global__ __launch_bounds__(THREADS) void select_blocks_kernel(BlockSelectParam
         int ties = 0, at = 0;  // of the keys that equal the threshold, the first ones
         if (!exact) {
             ties = wanted;
-            for (int n = lane; n < count + lane; n += 64) ties -= (int)__popcll(__ballot(n < count && mine[n] > cut));
+            for (int n0 = 0; n0 < count; n0 += 64) ties -= (int)__popcll(__ballot(n0 + lane < count && mine[n0 + lane] > cut));
         }
         const unsigned long long before = (1ull << lane) - 1;
-        for (int n = lane; n < count + lane; n += 64) {
-            const unsigned long long k = n < count ? mine[n] : 0;
+        for (int n0 = 0; n0 < count; n0 += 64) {
+            const unsigned long long k = n0 + lane < count ? mine[n0 + lane] : 0;
             const unsigned long long equal = __ballot(!exact && k == cut);
             const bool taken = exact ? k >= cut : k > cut || (k == cut && (int)__popcll(equal & before) < ties);
             ties = max(0, ties - (int)__popcll(equal));
             const unsigned long long all = __ballot(taken);
-            if (taken) out[at + (int)__popcll(all & before)] = n;
+            if (taken) out[at + (int)__popcll(all & before)] = n0 + lane;
             at += (int)__popcll(all);
         }
         for (int e = at + lane; e < p.T; e += 64) out[e] = -1;
+    };
+    if constexpr (RB < 16) {
+        for (int list = wave; list < RB; list += WAVES)
+            if (queries_of(qb0 + list) > 0) choose(list);
+    } else {
+        // four lists a wave at a time, each in 16 lanes, by the upper halves of the scores
+        const int list = wave * 4 + (lane >> 4), l16 = lane & 15, shift = lane & 48;
+        const bool there = queries_of(qb0 + list) > 0;
+        const int count = there ? counts[list] : 0, wanted = min(p.T, count);
+        const unsigned long long* const mine = keys + list * p.nb;
+        bool exact = count <= p.T;
+        unsigned top = 0;
+        auto by_halves = [&](auto held) {
+            constexpr int HELD = decltype(held)::value;
+            unsigned high[HELD];
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) high[i] = i * 16 + l16 < count ? (unsigned)(mine[i * 16 + l16] >> 32) : 0;
+            for (int bit = 31; bit >= 0 && !__all(exact); --bit) {
+                const unsigned mark = top | 1u << bit;
+                int reach = 0;
+#pragma unroll
+                for (int i = 0; i < HELD; ++i) reach += high[i] >= mark;
+                reach += __builtin_amdgcn_update_dpp(0, reach, 0x128, 0xf, 0xf, false);  // (the sum of the 16 lanes, by rotations)
+                reach += __builtin_amdgcn_update_dpp(0, reach, 0x124, 0xf, 0xf, false);
+                reach += __builtin_amdgcn_update_dpp(0, reach, 0x122, 0xf, 0xf, false);
+                reach += __builtin_amdgcn_update_dpp(0, reach, 0x121, 0xf, 0xf, false);
+                if (!exact) {
+                    if (reach >= wanted) top = mark;
+                    exact = reach == wanted;
+                }
+            }
+            int at = 0;
+            int* const out = p.blocks + ((qb0 + list) * p.H_kv + g) * p.T;
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                const bool taken = exact && i * 16 + l16 < count && high[i] >= top;
+                const unsigned all = (unsigned)(__ballot(taken) >> shift) & 0xffffu;
+                if (taken) out[at + __popc(all & ((1u << l16) - 1))] = i * 16 + l16;
+                at += __popc(all);
+            }
+            if (there && exact)
+                for (int e = at + l16; e < p.T; e += 16) out[e] = -1;
+        };
+        if (most <= 128) by_halves(std::integral_constant<int, 8>{});
+        else by_halves(std::integral_constant<int, SEL_LDS / (16 * 8) / 16>{});
+        for (unsigned long long rest = __ballot(!exact && l16 == 0); rest; rest &= rest - 1) choose(wave * 4 + (__ffsll(rest) - 1) / 16);
     }
 }
 

@@ -263,6 +263,9 @@ def chosen64(Q, means, S_k, b, bq, T, causal, q_start):
     (100, 1000, 4, 2, 128, 96, 7, 3, False, 0, torch.float32),
     (64, 30, 2, 1, 64, 32, 16, 4, True, 200, torch.bfloat16),
     (40, 9000, 2, 2, 64, 32, 8, 100, False, 17, torch.bfloat16),
+    (600, 600, 16, 16, 64, 32, 1, 5, True, 0, torch.bfloat16),       # thousands of lists of few rows: several to a workgroup
+    (530, 6000, 32, 16, 128, 32, 1, 12, True, 5400, torch.bfloat16),
+    (300, 5000, 8, 8, 64, 32, 1, 9, False, 0, torch.float32),
 ])
 def test_means_and_choice_against_64_bits(lemo, S_q, S_k, H, H_kv, d, b, bq, T, causal, q_start, dtype):
     g = torch.Generator().manual_seed(S_q + S_k)
@@ -284,6 +287,13 @@ def test_choice_of_ties_and_of_what_is_not_a_number(lemo):
     means[[7, 150]] = 1.0
     got = lemo.lemo_select_blocks(Q, means, 200 * 32, 32, 10, 5, 0)
     assert got.tolist() == [[[0, 1, 2, 7, 150]]]
+    # many lists, all scores equal, and equal but in the last bits of their upper halves
+    Q = torch.ones(600, 16, 64, dtype=torch.bfloat16, device="cuda")
+    same = torch.ones(40, 16, 64, device="cuda")
+    assert (lemo.lemo_select_blocks(Q, same, 40 * 32, 32, 1, 6, 0) == torch.arange(6, device="cuda")).all()
+    same += torch.arange(40, device="cuda")[:, None, None] * 2.0 ** -23
+    assert (lemo.lemo_select_blocks(Q, same, 40 * 32, 32, 1, 6, 0) == torch.arange(34, 40, device="cuda")).all()
+    Q = torch.ones(10, 2, 64, dtype=torch.bfloat16, device="cuda")
     for bad in (math.nan, math.inf, -math.inf):
         means[3:100] = bad
         means[50, 0, 5] = -bad
