@@ -47,7 +47,7 @@ size_t part_bytes(int64_t n_qb, int64_t bq, int64_t S_k, int32_t H, int32_t H_kv
     p.lengths = step ? &one : nullptr;  // (not read)
     p.n_qb = (int)n_qb; p.bq = (int)bq; p.S_k = (int)S_k; p.H_kv = H_kv; p.T = T; p.b = b;
     p.R = (int)(bq * (H / H_kv));
-    const int subtiles = block_attention_packed(p), tile = block_attention_tile_rows(p.R, d);
+    const int subtiles = block_attention_packed(p), tile = block_attention_tile_rows(p.R, d == 128 && !step);
     const int parts = block_attention_parts((int64_t)p.n_qb * ((p.R + tile - 1) / tile) * H_kv, subtiles);
     return parts > 1 ? round_up((size_t)p.n_qb * H_kv * parts * p.R * (d + 4) * sizeof(float), 256) : 0;
 }

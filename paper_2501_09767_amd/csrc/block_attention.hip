@@ -267,8 +267,9 @@ template <int D> __global__ __launch_bounds__(256) void block_attention_join_ker
     if (p.lse2 && c0 == 0) p.lse2[(long long)h * p.S_q + i] = total == 0.f ? -INFINITY : top + log2f(total);
 }
 
-// Rows of a workgroup by the rows that share a list: no more waves than have rows, the others share.
-int block_attention_tile_rows(int R, int d) { return R > 128 && d == 128 ? 256 : R > 64 ? 128 : R > 32 ? 64 : 32; }
+// Rows of a workgroup by the rows that share a list: no more waves than have rows, the others share.  `walk`: there may be workgroups that
+// walk over the lists (not for single tokens, whose sequences have keys and lengths of their own).
+int block_attention_tile_rows(int R, bool walk) { return R > 128 && walk ? 256 : R > 64 ? 128 : R > 32 ? 64 : 32; }
 
 // Lists of few rows together, as many as fill 32 rows; the union of what they name has to fit the workgroup's memory.  1000 queries with a
 // list each, 16 / 4 heads of 64: see launch_block_attention_d.
@@ -323,7 +324,7 @@ template <int D> static int launch_block_attention_d(BlockAttnParams p, hipStrea
     const int unready = D == 128 ? first_error(prepare_block_attention<D>, prepare_block_attention_pipe) : prepare_block_attention<D>();
     if (unready) return unready;
     const int subtiles = block_attention_packed(p);
-    const int tile = block_attention_tile_rows(p.R, D);
+    const int tile = block_attention_tile_rows(p.R, D == 128 && !p.lengths);
     p.n_rt = (p.R + tile - 1) / tile;
     p.n_parts = p.parts ? block_attention_parts((long long)p.n_qb * p.n_rt * p.H_kv, subtiles) : 1;
     p.order = head_order(p.H_kv, false, 8);

@@ -49,7 +49,7 @@ constexpr int MAX_PACKED_SUBTILES = 2048;  // of the union of lists, with a word
 constexpr int MAX_LISTED_BLOCKS = 16384;   // key blocks that a choice is made from: their scores stand in LDS, 128 KB
 
 int block_attention_parts(long long tiles, long long subtiles);
-int block_attention_tile_rows(int R, int d);
+int block_attention_tile_rows(int R, bool walk);
 int block_attention_packed(BlockAttnParams& p);
 int launch_block_attention(BlockAttnParams p, int d, hipStream_t st);
 int prepare_block_attention_pipe();

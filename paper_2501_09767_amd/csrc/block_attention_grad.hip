@@ -625,7 +625,7 @@ template <int D> static int launch_grad(BlockGradParams gp, hipStream_t st) {
     {
         BlockAttnParams& q = by_rows.a;
         q.lengths = nullptr;
-        const int subtiles = block_attention_packed(q), tile = block_attention_tile_rows(q.R, 64);
+        const int subtiles = block_attention_packed(q), tile = block_attention_tile_rows(q.R, false);
         q.n_rt = (q.R + tile - 1) / tile;
         q.n_parts = 1;
         q.order = head_order(q.H_kv, false, 8);

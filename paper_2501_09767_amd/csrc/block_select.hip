@@ -87,8 +87,6 @@ __device__ __forceinline__ unsigned long long score_key(double s) {
     return k == 0 ? 1 : k == ~0ull ? ~0ull - 1 : k;
 }
 
-
-
 // the sum over the 16 lanes of a row, in every lane: four rotations within the row
 template <int BY> __device__ __forceinline__ double rotated(double v) {
     const unsigned long long u = __double_as_longlong(v);
@@ -355,8 +353,8 @@ template <typename T, int D> static int run_select_blocks(const BlockSelectParam
     // 10.2 / 10.2, 27 / 22, 42 / 10)
     if (lists <= 64) return run_select_lists<T, D, 1, 1024>(p, st);
     // lists of few rows: the more of them a workgroup makes, the less often it reads the means; their scores take LDS, and there have
-    // to be workgroups
-    if (p.bq * p.G < 64) {
+    // to be workgroups (single tokens have means of their own each)
+    if (p.bq * p.G < 64 && !p.lengths) {
         if (lists >= 16 * SEL_LEAST && p.nb * 16 * 8 <= SEL_LDS) return run_select_lists<T, D, 16, 256>(p, st);
         if (lists >= 4 * SEL_LEAST && p.nb * 4 * 8 <= SEL_LDS) return run_select_lists<T, D, 4, 256>(p, st);
     }

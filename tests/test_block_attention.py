@@ -307,6 +307,7 @@ def test_choice_of_ties_and_of_what_is_not_a_number(lemo):
     (4, 4, 64, 32, 3, 200, [97, 96]),
     (32, 8, 128, 64, 16, 3000, [3000]),
     (16, 1, 64, 96, 5, 1000, [1000, 31, 480] * 20),
+    (160, 1, 128, 32, 4, 300, [300, 77, 64, 0]),
 ])
 def test_single_tokens(lemo, H, H_kv, d, b, T, S, lengths):
     B, nb = len(lengths), -(-S // b)
@@ -340,6 +341,19 @@ def test_single_tokens(lemo, H, H_kv, d, b, T, S, lengths):
         assert torch.equal(blocks[s].cpu(), chosen64(Q[s:s + 1], mine, n, b, 1, T, True, n - 1)[0])
         ref = reference(case, Q[s:s + 1], K[s, :n], V[s, :n], blocks[s:s + 1].cpu())
         close("O", O[s:s + 1], ref["O"], HALF * ref["O"].abs() + (1 + HALF) * (HALF + 4 * ref["E"] + 2.0 ** -14)[..., None] * ref["O_mag"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B", [300, 1100])
+def test_choice_for_many_sequences(lemo, B):
+    """As for eight of them at a time."""
+    H, d, b, T, S = 8, 64, 32, 3, 200
+    Q = draw(B, (B, H, d))[0].cuda()
+    means = draw(B + 1, (B, 7, H, d))[0].float().cuda()
+    lengths = (torch.arange(B, dtype=torch.int32, device="cuda") * 37) % (S + 1)
+    got = lemo.lemo_select_blocks_step(Q, means, lengths, b, T, S_max=S)
+    for s in range(0, B, 8):
+        assert torch.equal(got[s:s + 8], lemo.lemo_select_blocks_step(Q[s:s + 8], means[s:s + 8], lengths[s:s + 8], b, T, S_max=S)), s
 
 
 @pytest.mark.gpu
