@@ -353,7 +353,8 @@ template <typename T, int D> static int run_select_blocks(const BlockSelectParam
     // 10.2 / 10.2, 27 / 22, 42 / 10)
     if (lists <= 64) return run_select_lists<T, D, 1, 1024>(p, st);
     // lists of few rows: the more of them a workgroup makes, the less often it reads the means; their scores take LDS, and there have
-    // to be workgroups (single tokens have means of their own each)
+    // to be workgroups (single tokens have means of their own each).  us for 16 / 4 / 1 lists a workgroup: 3001 queries, 16 heads of 64, a list
+    // each from 94 blocks 30 / 78 / 137; 8192, 16 of 128, a list for 8 from 128 blocks 22 / 47 / 79; 800, 8 of 64, from 25 - / 12 / 19
     if (p.bq * p.G < 64 && !p.lengths) {
         if (lists >= 16 * SEL_LEAST && p.nb * 16 * 8 <= SEL_LDS) return run_select_lists<T, D, 16, 256>(p, st);
         if (lists >= 4 * SEL_LEAST && p.nb * 4 * 8 <= SEL_LDS) return run_select_lists<T, D, 4, 256>(p, st);

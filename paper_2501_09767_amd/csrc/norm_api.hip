@@ -54,7 +54,7 @@ int lemo_norm_residual(const void* Y, int64_t ldy, const void* gate, int64_t ld_
 int lemo_norm_residual_grad_workspace_bytes(int64_t M, int32_t C, size_t* bytes) {
     if (!bytes) return LEMO_ERR_NULL;
     if (M < 0 || M >= (int64_t)1 << 31 || C <= 0) return LEMO_ERR_SHAPE;
-    *bytes = round_up((size_t)norm_grad_parts(M) * 5 * (size_t)C * sizeof(float), 256);
+    *bytes = round_up((size_t)norm_grad_parts(M, C) * 5 * (size_t)C * sizeof(float), 256);
     return LEMO_OK;
 }
 

@@ -14,6 +14,8 @@
 // nothing cancels.  Gradients: a workgroup owns a row at a time and walks the rows in steps of the grid, because the sums over
 // the rows stay in the registers of the thread that owns a column; what the workgroups hold at the end goes through the
 // workspace and is added in their order by a second kernel (no atomics: the same bits on every run).
+#include <algorithm>
+
 #include "lemo_common.hpp"
 #include "norm_residual.hpp"
 
@@ -380,13 +382,16 @@ template <typename T, int TPR, int NP> static int run_norm(const NormParams& p, 
     return (int)hipGetLastError();
 }
 
+// Short rows: a wave each, which needs no LDS and no barrier; from 256 pieces on (bf16: 2048 columns) a workgroup, whose threads have more
+// loads under way and less to add up.  bf16 with gate and both norms, us, wave / workgroup: 8192 rows of 1024 18.2 / 21.9, of 2048
+// 32.0 / 28.4, of 4096 73.3 / 53.7 (5.0 TB/s, as fast as a copy); 8 rows of 1024 5.8 / 5.8, of 2048 6.8 / 5.8, of 4096 10.6 / 5.6.
 int launch_norm_residual(const NormParams& p, lemo_dtype_t dt, hipStream_t st) {
     const int pieces = p.C / (dt == LEMO_BF16 ? 8 : 4);
     auto go = [&](auto tag) {
         using T = decltype(tag);
         if (pieces <= 64) return run_norm<T, 64, 1>(p, st);
         if (pieces <= 128) return run_norm<T, 64, 2>(p, st);
-        if (pieces <= 256) return run_norm<T, 64, 4>(p, st);
+        if (pieces <= 256) return run_norm<T, 256, 1>(p, st);
         if (pieces <= 512) return run_norm<T, 256, 2>(p, st);
         if (pieces <= 1024) return run_norm<T, 256, 4>(p, st);
         if (pieces <= 2048) return run_norm<T, 512, 4>(p, st);
@@ -395,8 +400,16 @@ int launch_norm_residual(const NormParams& p, lemo_dtype_t dt, hipStream_t st) {
     return dt == LEMO_BF16 ? go(bf16_t{}) : go(float{});
 }
 
-// Workgroups: two for every CU, two rows each at least where there are fewer rows
-int norm_grad_parts(int64_t M) { return (int)(M >= 1024 ? 512 : M >= 256 ? M / 2 : M < 128 ? M : 128); }
+// Threads that own a row, 16 columns each, and workgroups: two waves a SIMD, but two rows a workgroup at least, whose sums are one more
+// row to write and to read.  bf16 with gate and both norms, us for 256 / 512 / 1024 / 2048 workgroups: 8192 rows of 1024 (a wave each) 117 /
+// 70 / 54 / 47; of 2048 134 / 82 / 64 / -; of 4096 (256 threads) 175 / 130 / 136 / -.  One workgroup for 4, 2 or 1 rows: 512 rows of 4096
+// 25 / 20 / 23.  8192 rows of 4096 without a norm of the block's result (537 MB): 125 us, 4.3 TB/s; what is missing to a copy's rate is
+// the barrier between a row's loads and its stores, with two waves a SIMD to cover it: registers hold the columns' sums.
+static int norm_grad_threads(int C) { return C <= 1024 ? 64 : C <= 2048 ? 128 : C <= 4096 ? 256 : C <= 8192 ? 512 : 1024; }
+int norm_grad_parts(int64_t M, int C) {
+    const int most = std::max(512, 512 * 256 / norm_grad_threads(C));
+    return (int)(M >= 2 * most ? most : M >= 256 ? M / 2 : M < 128 ? M : 128);
+}
 
 template <typename T, int THREADS, int NP> static int run_norm_grad(const NormGradParams& p, int parts, hipStream_t st) {
     const bool post = p.post != LEMO_NORM_NONE, shared = (p.sums & SUM_GATE) != 0;
@@ -409,7 +422,7 @@ template <typename T, int THREADS, int NP> static int run_norm_grad(const NormGr
 
 int launch_norm_residual_grad(NormGradParams p, float* dw_next, float* db_next, float* dw_post, float* db_post, float* dgate_sum, void* workspace,
                               lemo_dtype_t dt, hipStream_t st) {
-    const int pieces = p.C / (dt == LEMO_BF16 ? 8 : 4), parts = norm_grad_parts(p.M);
+    const int threads = norm_grad_threads(p.C), parts = norm_grad_parts(p.M, p.C);
     NormSums out{};
     p.sums = p.planes = 0;
     p.parts = static_cast<float*>(workspace);
@@ -422,10 +435,10 @@ int launch_norm_residual_grad(NormGradParams p, float* dw_next, float* db_next, 
     auto go = [&](auto tag) {
         using T = decltype(tag);
         constexpr int NP = 16 / Piece<T>::E;  // 16 columns a thread: the sums of each are held in registers
-        if (pieces <= 64 * NP) return run_norm_grad<T, 64, NP>(p, parts, st);
-        if (pieces <= 128 * NP) return run_norm_grad<T, 128, NP>(p, parts, st);
-        if (pieces <= 256 * NP) return run_norm_grad<T, 256, NP>(p, parts, st);
-        if (pieces <= 512 * NP) return run_norm_grad<T, 512, NP>(p, parts, st);
+        if (threads == 64) return run_norm_grad<T, 64, NP>(p, parts, st);
+        if (threads == 128) return run_norm_grad<T, 128, NP>(p, parts, st);
+        if (threads == 256) return run_norm_grad<T, 256, NP>(p, parts, st);
+        if (threads == 512) return run_norm_grad<T, 512, NP>(p, parts, st);
         return run_norm_grad<T, 1024, NP>(p, parts, st);
     };
     if (p.M > 0) {

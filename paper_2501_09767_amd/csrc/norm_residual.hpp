@@ -38,7 +38,7 @@ struct NormSums { float* to[5]; };
 constexpr int NORM_MAX_C = 16384;  // what the threads of a workgroup hold of a row in registers
 
 int launch_norm_residual(const NormParams& p, lemo_dtype_t dt, hipStream_t st);
-int norm_grad_parts(int64_t M);  // workgroups of the gradient, each with a part of the column sums
+int norm_grad_parts(int64_t M, int C);  // workgroups of the gradient, each with a part of the column sums
 int launch_norm_residual_grad(NormGradParams p, float* dw_next, float* db_next, float* dw_post, float* db_post, float* dgate_sum, void* workspace,
                               lemo_dtype_t dt, hipStream_t st);
 
