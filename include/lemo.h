@@ -12,7 +12,10 @@
  * Beside them: the paper's block-wise criterion and threshold rule (lemo_score_blocks, lemo_threshold_init,
  * lemo_select_threshold; Sec. 4.2 Eq. 2, Alg. 1 step 1), the attention block over the kept tokens with its
  * projection added back in place (lemo_kept_attention, lemo_gather_gemm_add; Sec. 4.4), and the gradients
- * of the selective-load GEMM (lemo_gather_gemm_dx, lemo_gather_gemm_dw).
+ * of the selective-load GEMM (lemo_gather_gemm_dx, lemo_gather_gemm_dw).  Then what a layer has around and instead of
+ * these: the norms, gate and residual scale between two blocks, on the kept rows in place (lemo_norm_residual), and attention over
+ * key blocks that a cheap score selects for each query (lemo_block_means, lemo_select_blocks, lemo_block_attention), both with
+ * their gradients, the latter also for single tokens over caches (lemo_*_step).
  *
  * Conventions shared by every call
  *   - Pointers are DEVICE pointers unless the comment says "host".  The caller owns every buffer;
