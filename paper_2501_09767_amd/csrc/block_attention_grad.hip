@@ -11,11 +11,11 @@
 // reading dS (2 bytes a pair) would.
 // delta comes from O as it is stored and dS goes to the products as bf16: each moves dQ and dK by up to 2^-9 of what they sum up;
 // P, dS and delta are formed in binary32, and so are all sums.
-// 8192 tokens, 32 heads of 128, 16 blocks of 64 for 64 queries: 725 us (dQ 37 %, the lists 4 %, dK and dV 59 %), 430 TFLOP/s of the
-// definition's 5 products, 600 of the 7.  A stage of 128 rows of the second pass takes 5250 cycles: its CU's LDS is read for 2600 and
-// written for 500 of them, a matrix core works for 2050; loads and barriers are waited for in 50 and 300.  28 % of that pass is the
-// begin and the end of items.  The same work in other orders takes the same time to 1 %: fragments 3 or 4 steps ahead, a part of V in
-// registers and two workgroups a CU, rows' places without divisions, precedence for waves in their products.
+// 8192 tokens, 32 heads of 128, 16 blocks of 64 for 64 queries: 670 us (dQ 42 %, the lists 4 %, dK and dV 54 %), 470 TFLOP/s of the
+// definition's 5 products, 650 of the 7.  With eight waves on the same 64 keys and one workgroup a CU it was 725: a stage of 128 rows of the
+// second pass took 5250 cycles, of which LDS was read for 2200 and written for 500, a matrix core worked for 2050 and loads and
+// barriers were waited for in 50 and 300, and the begin and the end of items took 28 % of the pass.  What the waves of a stage do they do
+// at the same time; fragments 3 or 4 steps ahead or precedence for waves in their products change nothing by more than 1 %.
 #include "block_attention.hpp"
 
 namespace lemo {
@@ -295,12 +295,14 @@ __global__ __launch_bounds__(64) void block_lists_kernel(BlockGradParams gp) {
 
 // ---- by key blocks: dK, dV ----------------------------------------------------------------------------
 
-// KW waves hold 32 keys each, and SHARES as many share them and take the row subtiles of a stage in turn.
+// KW waves hold 32 keys each, and SHARES as many share them and take the row subtiles of a stage in turn.  K stays in registers, and of V
+// what fits beside it: with heads of 128 the columns from 16 V_HELD on come from LDS, 16 bytes of 32 keys side by side.
 template <int D, int KW, int SHARES> struct DkvGeo {
     using Tile = HeadTile<D>;
-    static constexpr int SUBS = SHARES, SUB = 32 * Tile::ROWB, STAGE = 2 * SUBS * SUB, ROWS = SUBS * 32, V = 2 * STAGE;
+    static constexpr int SUBS = SHARES, SUB = 32 * Tile::ROWB, STAGE = 2 * SUBS * SUB, ROWS = SUBS * 32;
+    static constexpr int V = 2 * STAGE, V_HELD = D == 128 ? 2 : D / 16, V_SUB = (D / 16 - V_HELD) * 1024;  // where the keys' V stands; bytes of it for 32 keys
     static constexpr int PITCH = D + 4, JOIN = KW * SHARES * 32 * PITCH * 4;
-    static constexpr int TABLE = V + KW * SUB > JOIN ? V + KW * SUB : JOIN;  // three tables of rows stand behind the stages and the keys' V
+    static constexpr int TABLE = V + KW * V_SUB > JOIN ? V + KW * V_SUB : JOIN;  // three tables of rows stand behind
     static constexpr int LDS = TABLE + 3 * ROWS * 5 * 4;
 };
 
@@ -334,56 +336,72 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
     const int key0 = n * p.b + (blockIdx.y * KW + wave % KW) * 32;
     const int share = wave / KW;
 
-    // K stays in registers; for V, which comes from LDS, two waves a SIMD leave none
-    u32x4 kf[Tile::CHUNKS];
+    constexpr int V_HELD = Geo::V_HELD;
+    u32x4 kf[Tile::CHUNKS], vf[V_HELD];
 #pragma unroll
     for (int c = 0; c < Tile::CHUNKS; ++c) kf[c] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int c = 0; c < V_HELD; ++c) vf[c] = u32x4{0u, 0u, 0u, 0u};
     if (key0 + l32 < p.S_k) {
         const char* const k = reinterpret_cast<const char*>(p.K + (key0 + l32) * p.k_ts + g * p.k_hs);
+        const char* const v = reinterpret_cast<const char*>(p.V + (key0 + l32) * p.v_ts + g * p.v_hs);
 #pragma unroll
         for (int c = 0; c < Tile::CHUNKS; ++c) kf[c] = *reinterpret_cast<const u32x4*>(k + c * 32 + half * 16);
+#pragma unroll
+        for (int c = 0; c < V_HELD; ++c) vf[c] = *reinterpret_cast<const u32x4*>(v + c * 32 + half * 16);
     }
-    const unsigned sv = lds_offset_of(smem) + Geo::V + wave % KW * Geo::SUB;
+    const unsigned sv = lds_offset_of(smem) + Geo::V + wave % KW * Geo::V_SUB;
 
     // Rows of a stage: row v of the item is row v % R of query block list[v / R].  A thread looks after one row, in three steps a stage
-    // apart, so that nothing waits for what it needs: its query block is loaded, then its statistics, then it goes into the table.
-    int next_entry = 0, entry = 0;  // query blocks of the row whose statistics are loaded next, and of the one they were loaded for
-    float r_lse = 0.f, r_delta = 0.f;
-    auto fetch_entry = [&](int t) {
-        const int v = t * ROWS + tid;
-        if (tid < ROWS && v < n_rows) next_entry = list[v / p.R];
+    // apart, so that nothing waits for what it needs: its query block is loaded; its place goes into the table and its statistics are
+    // loaded; they go into the table.  v / R and v % R are carried on from stage to stage, not divided anew.
+    unsigned run_entry = (unsigned)tid / (unsigned)p.R, run_row = (unsigned)tid % (unsigned)p.R;
+    const unsigned step_entry = (unsigned)ROWS / (unsigned)p.R, step_row = (unsigned)ROWS % (unsigned)p.R;
+    int entry = -1;  // query block of the row that is placed next, and which of its rows that is
+    unsigned row = 0;
+    float r_lse = -INFINITY, r_delta = 0.f;
+    auto fetch_entry = [&] {
+        row = run_row;
+        entry = -1;
+        if (tid < ROWS && run_entry < (unsigned)item.z) entry = list[run_entry];
+        run_entry += step_entry;
+        run_row += step_row;
+        if (run_row >= (unsigned)p.R) {
+            run_row -= p.R;
+            ++run_entry;
+        }
     };
-    auto fetch_row = [&](int t) {
-        entry = next_entry;
-        const int v = t * ROWS + tid;
-        if (tid >= ROWS || v >= n_rows) return;
-        const int row = v % p.R, h = g * p.G + row % p.G, i = min(entry * p.bq + row / p.G, p.S_q - 1);
-        r_lse = p.lse2[(long long)h * p.S_q + i];
-        r_delta = gp.delta[(long long)h * p.S_q + i];
+    auto place_row = [&](int t) {
+        if (tid >= ROWS) return;
+        const int at = t % 3 * ROWS + tid, in = (int)(row / (unsigned)p.G), h = g * p.G + (int)row - in * p.G, i = entry * p.bq + in;
+        const bool there = entry >= 0 && i < p.S_q;  // otherwise: offsets past every operand, probabilities 0
+        t_q[at] = there ? (unsigned)((i * p.q_ts + h * p.q_hs) * 2) : 0xffffff00u;
+        t_d[at] = there ? (unsigned)((i * gp.do_ts + h * gp.do_hs) * 2) : 0xffffff00u;
+        t_pos[at] = !there ? -1 : causal ? (int)min(p.q_start + i, (long long)0x7fffffff) : 0x7fffffff;
+        r_lse = -INFINITY;
+        r_delta = 0.f;
+        if (there) {
+            r_lse = p.lse2[(long long)h * p.S_q + i];
+            r_delta = gp.delta[(long long)h * p.S_q + i];
+        }
     };
     auto keep_row = [&](int t) {
         if (tid >= ROWS) return;
-        const int at = t % 3 * ROWS + tid, v = t * ROWS + tid, row = v % p.R, h = g * p.G + row % p.G, i = entry * p.bq + row / p.G;
-        const bool there = v < n_rows && i < p.S_q;  // otherwise: offsets past every operand, probabilities 0
-        t_q[at] = there ? (unsigned)((i * p.q_ts + h * p.q_hs) * 2) : 0xffffff00u;
-        t_d[at] = there ? (unsigned)((i * gp.do_ts + h * gp.do_hs) * 2) : 0xffffff00u;
-        t_lse[at] = there && r_lse != -INFINITY ? r_lse : INFINITY;
-        t_delta[at] = there ? r_delta : 0.f;
-        t_pos[at] = !there ? -1 : causal ? (int)min(p.q_start + i, (long long)0x7fffffff) : 0x7fffffff;
+        const int at = t % 3 * ROWS + tid;
+        t_lse[at] = r_lse == -INFINITY ? INFINITY : r_lse;
+        t_delta[at] = r_delta;
     };
     const u32x4 q_rsrc = raw_rsrc(p.Q, ((p.S_q - 1) * p.q_ts + (p.H - 1) * p.q_hs + D) * 2);
     const u32x4 d_rsrc = raw_rsrc(gp.dO, ((p.S_q - 1) * gp.do_ts + (p.H - 1) * gp.do_hs + D) * 2);
     constexpr int RPI = 1024 / Tile::ROWB, UNITS = ROWS / RPI, LOADS = 2 * UNITS / WAVES;
     static_assert(UNITS % WAVES == 0, "");
-    const int in_row = lane / Tile::PIECES, place = lane % Tile::PIECES;
-    {  // V rows past the keys there are arrive as zeros
-        const int begin = n * p.b + blockIdx.y * KW * 32, pitch = (int)p.v_ts * 2;
-        u32x4 rsrc = raw_rsrc(reinterpret_cast<const char*>(p.V + (long long)min(begin, p.S_k - 1) * p.v_ts + (long long)g * p.v_hs),
-                                    begin < p.S_k ? (long long)(p.S_k - 1 - begin) * pitch + Tile::ROWB : 0);
-        for (int i = 0; i < 4; ++i) rsrc[i] = __builtin_amdgcn_readfirstlane(rsrc[i]);  // (64-bit arithmetic left it in vector registers)
-        for (int unit = wave; unit < KW * 32 / RPI; unit += WAVES) {
-            const int r = unit * RPI + in_row;
-            lds_direct_b128(rsrc, lds_offset_of(smem) + Geo::V + unit * 1024, r * pitch + ((place ^ Tile::swz(r & 31)) << 4));
+    if constexpr (Geo::V_SUB > 0) {  // keys that are not there arrive as zeros
+        for (int sub = wave; sub < KW; sub += WAVES) {
+            const int begin = n * p.b + (blockIdx.y * KW + sub) * 32, pitch = (int)p.v_ts * 2;
+            const u32x4 rsrc = subtile_rsrc<D>(reinterpret_cast<const char*>(p.V + (long long)g * p.v_hs), min(begin, p.S_k), p.S_k, pitch);
+#pragma unroll
+            for (int i = 0; i < Geo::V_SUB / 1024; ++i)
+                lds_direct_b128(rsrc, lds_offset_of(smem) + Geo::V + sub * Geo::V_SUB + i * 1024, l32 * pitch + (V_HELD + i) * 32 + half * 16);
         }
     }
     auto load_stage = [&](int t, int buf) {
@@ -404,22 +422,22 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
 #pragma unroll
     for (int c = 0; c < Tile::COLS; ++c) dk[c] = dv[c] = f32x16{0};
     if (n_stage > 0) {
-        fetch_entry(0);
-        fetch_row(0);
-        fetch_entry(1);
-        keep_row(0);
+        fetch_entry();
+        place_row(0);
+        fetch_entry();
         __syncthreads();
         load_stage(0, 0);
-        fetch_row(1);
-        fetch_entry(2);
+        keep_row(0);
+        place_row(1);
+        fetch_entry();
         keep_row(1);
     }
     settle_stage();
     for (int t = 0; t < n_stage; ++t) {
         __syncthreads();  // stage t and the table of stage t + 1 are there
+        place_row(t + 2);
+        fetch_entry();
         if (t + 1 < n_stage) load_stage(t + 1, (t + 1) & 1);
-        fetch_row(t + 2);
-        fetch_entry(t + 3);
         const char* const sq = smem + (t & 1) * Geo::STAGE;
         const int table = t % 3 * ROWS;
 #pragma unroll 1
@@ -437,13 +455,14 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
             // Fragments come AHEAD steps before their products, and no earlier: all of them at once would not fit the registers, and what
             // then went to scratch would come back only after the stage's loads, which a wait for memory cannot tell from it.
             constexpr int AHEAD = 2;
+            auto v_fragment = [&](int c) { return c < V_HELD ? vf[min(c, V_HELD - 1)] : *lds_pointer<const u32x4>(sv + lane_here * 16 + (c - V_HELD) * 1024); };
             {
                 u32x4 fq[AHEAD], fd[AHEAD], fv[AHEAD];
 #pragma unroll
                 for (int c = 0; c < AHEAD; ++c) {
                     fq[c] = place_in.row_fragment(qs, c);
                     fd[c] = place_in.row_fragment(ds_, c);
-                    fv[c] = place_in.row_fragment(sv, c);
+                    fv[c] = v_fragment(c);
                 }
 #pragma unroll
                 for (int c = 0; c < Tile::CHUNKS; ++c) {
@@ -453,7 +472,7 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
                     if (c + AHEAD < Tile::CHUNKS) {
                         fq[c % AHEAD] = place_in.row_fragment(qs, c + AHEAD);
                         fd[c % AHEAD] = place_in.row_fragment(ds_, c + AHEAD);
-                        fv[c % AHEAD] = place_in.row_fragment(sv, c + AHEAD);
+                        fv[c % AHEAD] = v_fragment(c + AHEAD);
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -580,8 +599,9 @@ BlockGradLayout block_grad_layout(long long S_q, long long S_k, int H, int H_kv,
     BlockGradLayout l{};
     const long long n_qb = (S_q + bq - 1) / bq, nb = (S_k + b - 1) / b, words = (n_qb + 31) / 32, R = (long long)bq * (H / H_kv);
     const long long entries = n_qb * H_kv * (T < nb ? T : nb);
-    // Items: some thousand for the whole launch and one a key block, of 256 rows at least.  dK and dV with the join, us, for about 512 / 1024 /
-    // 2048 / 4096: 8192 tokens, 32 heads, 16 blocks of 64 541 / 515 / 613 / 653; 2999 tokens, 32 / 8 heads, 12 blocks 165 / 164 / 199 / 277
+    // Items: some thousand for the whole launch and one a key block, of 256 rows at least.  The whole call, us, for about 512 / 1024 / 1536 / 2048:
+    // 8192 tokens, 32 heads, 16 blocks of 64 666 / 667 / 733 / 750, with 8 key heads 789 / 683 / 660 / 659; 32768, 32 / 8 heads 2400 / 2786 / 2407 /
+    // 2534; 2999, 32 / 8 heads, lists of 12 for 16 queries 262 / 243 / 233 / 247
     long long share = (entries + 1023) / 1024;
     const long long least = (256 + R - 1) / R;
     if (share < least) share = least;
@@ -612,7 +632,14 @@ template <int D, int KS, bool PACK> static int run_dq(const BlockGradParams& gp,
     return (int)hipGetLastError();
 }
 
-template <int D, int KW, int SHARES> static int run_dkv(const BlockGradParams& gp, hipStream_t st) {
+// Waves that share keys in the pass by key blocks.  Heads of 128: so many that two workgroups fit a CU, and the one's begin and end pass
+// while the other computes; heads of 64, whose tiles are half as large: more.  us of the whole call, 8192 tokens: 32 heads of 128, 8
+// blocks of 128 keys 735 with 1 / 746 with 2; 16 of 64 678 with 2 / 725 with 4; 32 of 32 997 with 2 / 1083 with 4; 32 / 8 heads of 64,
+// lists for 16 queries, 8 of 128 489 with 1 / 480 with 2; 16 of 64 513 with 2 / 526 with 4; 32 of 32 643 with 2 / 578 with 4.
+template <int D, int KW> constexpr int DKV_SHARES = KW == 4 ? (D == 128 ? 1 : 2) : KW == 2 || D == 128 ? 2 : 4;
+
+template <int D, int KW> static int run_dkv(const BlockGradParams& gp, hipStream_t st) {
+    constexpr int SHARES = DKV_SHARES<D, KW>;
     hipLaunchKernelGGL((block_dkv_kernel<D, KW, SHARES>), dim3((unsigned)((gp.max_items + NUM_XCD - 1) / NUM_XCD * NUM_XCD), (unsigned)(gp.a.b / (32 * KW))), dim3(KW * SHARES * 64),
                        (DkvGeo<D, KW, SHARES>::LDS), st, gp);
     return (int)hipGetLastError();
@@ -623,9 +650,9 @@ template <int D> static int launch_grad(BlockGradParams gp, hipStream_t st) {
                                                  {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 2, false>), dq_lds<D, 2>(MAX_LISTED_SUBTILES)},
                                                  {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 4, false>), dq_lds<D, 4>(MAX_LISTED_SUBTILES)},
                                                  {reinterpret_cast<const void*>(&block_dq_kernel<D, 4, 4, true>), dq_lds<D, 4>(2 * MAX_PACKED_SUBTILES)},
-                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 1, 4>), DkvGeo<D, 1, 4>::LDS},
-                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 2, 4>), DkvGeo<D, 2, 4>::LDS},
-                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 4, 2>), DkvGeo<D, 4, 2>::LDS}});
+                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 1, DKV_SHARES<D, 1>>), DkvGeo<D, 1, DKV_SHARES<D, 1>>::LDS},
+                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 2, DKV_SHARES<D, 2>>), DkvGeo<D, 2, DKV_SHARES<D, 2>>::LDS},
+                                                 {reinterpret_cast<const void*>(&block_dkv_kernel<D, 4, DKV_SHARES<D, 4>>), DkvGeo<D, 4, DKV_SHARES<D, 4>>::LDS}});
     if (unready) return unready;
     BlockAttnParams& p = gp.a;
     BlockGradParams by_rows = gp;  // (the pass by query blocks may take several lists together)
@@ -646,10 +673,10 @@ template <int D> static int launch_grad(BlockGradParams gp, hipStream_t st) {
     hipLaunchKernelGGL(block_lists_kernel, dim3((unsigned)((gp.nb + 63) / 64), (unsigned)p.H_kv), dim3(64), 0, st, gp);
     int rc = (int)hipGetLastError();
     if (rc) return rc;
-    // as many keys a workgroup as a key block has, so that rows are gathered for all of them at once.  us of the whole call with 32 / 64 / 128 keys,
-    // 8192 tokens: 32 heads of 128, 8 blocks of 128 1229 / 827 / 746, 16 of 64 1077 / 722 / -; 32 / 8 heads of 64, lists for 16 530 / 511 / 493, 550 / 521 / -
+    // as many keys a workgroup as a key block has, so that rows are gathered for all of them at once (us of the whole call with eight, eight and
+    // four waves on 128, 64 and 32 keys, 8192 tokens: 32 heads of 128, 8 blocks of 128 746 / 827 / 1229)
     const int subs = p.b / 32;
-    rc = subs % 4 == 0 ? run_dkv<D, 4, 2>(gp, st) : subs % 2 == 0 ? run_dkv<D, 2, 4>(gp, st) : run_dkv<D, 1, 4>(gp, st);
+    rc = subs % 4 == 0 ? run_dkv<D, 4>(gp, st) : subs % 2 == 0 ? run_dkv<D, 2>(gp, st) : run_dkv<D, 1>(gp, st);
     if (rc) return rc;
     hipLaunchKernelGGL((block_dkv_join_kernel<D>), dim3((unsigned)(p.H_kv * gp.nb), 2), dim3(256), 0, st, gp);
     return (int)hipGetLastError();
