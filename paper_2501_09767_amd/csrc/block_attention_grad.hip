@@ -11,7 +11,7 @@
 // reading dS (2 bytes a pair) would.
 // delta comes from O as it is stored and dS goes to the products as bf16: each moves dQ and dK by up to 2^-9 of what they sum up;
 // P, dS and delta are formed in binary32, and so are all sums.
-// 8192 tokens, 32 heads of 128, 16 blocks of 64 for 64 queries: 670 us (dQ 42 %, the lists 4 %, dK and dV 54 %), 470 TFLOP/s of the
+// 8192 tokens, 32 heads of 128, 16 blocks of 64 for 64 queries: 670 us (dQ 39 %, the lists 4 %, dK and dV 57 %), 470 TFLOP/s of the
 // definition's 5 products, 650 of the 7.  With eight waves on the same 64 keys and one workgroup a CU it was 725: a stage of 128 rows of the
 // second pass took 5250 cycles, of which LDS was read for 2200 and written for 500, a matrix core worked for 2050 and loads and
 // barriers were waited for in 50 and 300, and the begin and the end of items took 28 % of the pass.  What the waves of a stage do they do
