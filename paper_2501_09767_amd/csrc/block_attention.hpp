@@ -30,7 +30,7 @@ struct BlockGradParams {
     uint16_t *dQ, *dK, *dV;  // contiguous
     float scale;
     float* delta;        // [H, S_q]: sum over a row of dO O
-    unsigned* bits;      // [H_kv][words][nb]: bit i of word w: query block 32 w + i lists key block n
+    unsigned* bits;      // [H_kv][nb][words]: bit i of word w: query block 32 w + i lists key block n
     int* counts;         // [H_kv * nb] query blocks that list a key block
     int* first;          // [H_kv * nb] where their list starts in `lists`
     int* lists;          // query blocks, ascending, key block by key block

@@ -52,6 +52,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool causal = (p.flags & LEMO_CAUSAL) != 0;
     const int S = p.S_k;
+    for (long long n = (long long)blockIdx.x * (WAVES * 64) + tid; n < p.H_kv * gp.nb; n += (long long)gridDim.x * (WAVES * 64)) gp.counts[n] = 0;  // for the lists turned round
     const long long pos0 = p.q_start + (long long)qb * p.bq;
     const int rows = min(p.bq, p.S_q - qb * p.bq) * p.G, row_end = min(rows, (rt + 1) * ROWS);
     auto limit_of = [&](int row) { return causal ? (int)min(pos0 + row / p.G, (long long)S - 1) : S - 1; };
@@ -208,7 +209,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams
 
 // ---- the lists turned round ---------------------------------------------------------------------------
 
-// A workgroup: 32 query blocks of one group; its four waves walk eight lists each and leave the blocks' bits in LDS.
+// A workgroup: 32 query blocks of one group; its four waves walk eight lists each and leave the blocks' bits in LDS.  The counts are zeros
+// when it starts: the pass by query blocks cleared them.
 __global__ __launch_bounds__(256) void block_bits_kernel(BlockGradParams gp) {
     const BlockAttnParams& p = gp.a;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -225,16 +227,10 @@ __global__ __launch_bounds__(256) void block_bits_kernel(BlockGradParams gp) {
         });
     }
     __syncthreads();
-    for (int n = threadIdx.x; n < gp.nb; n += 256) gp.bits[((long long)g * gp.words + w) * gp.nb + n] = bits[n];
-}
-
-__global__ __launch_bounds__(64) void block_count_kernel(BlockGradParams gp) {
-    const int n = blockIdx.x * 64 + threadIdx.x, g = blockIdx.y;
-    if (n >= gp.nb) return;
-    int count = 0;
-#pragma unroll 8
-    for (int w = 0; w < gp.words; ++w) count += __popc(gp.bits[((long long)g * gp.words + w) * gp.nb + n]);
-    gp.counts[g * gp.nb + n] = count;
+    for (int n = threadIdx.x; n < gp.nb; n += 256) {
+        gp.bits[((long long)g * gp.nb + n) * gp.words + w] = bits[n];
+        if (bits[n]) atomicAdd(gp.counts + g * gp.nb + n, __popc(bits[n]));  // (whole numbers: the order is nothing to the sum)
+    }
 }
 
 // One workgroup: where every key block's list, items and partial results start.
@@ -280,16 +276,23 @@ __global__ __launch_bounds__(1024) void block_layout_kernel(BlockGradParams gp) 
     if (threadIdx.x == 0) gp.totals[0] = base[1];
 }
 
-__global__ __launch_bounds__(64) void block_lists_kernel(BlockGradParams gp) {
-    const int n = blockIdx.x * 64 + threadIdx.x, g = blockIdx.y;
+// A wave: the list of a key block, a word of bits a lane.
+__global__ __launch_bounds__(256) void block_lists_kernel(BlockGradParams gp) {
+    const int n = blockIdx.x * 4 + (threadIdx.x >> 6), g = blockIdx.y, lane = threadIdx.x & 63;
     if (n >= gp.nb) return;
     int* out = gp.lists + gp.first[g * gp.nb + n];
-    for (int w = 0; w < gp.words; ++w) {
-        unsigned set = gp.bits[((long long)g * gp.words + w) * gp.nb + n];
-        while (set) {
-            *out++ = w * 32 + __ffs(set) - 1;
-            set &= set - 1;
+    for (int w0 = 0; w0 < gp.words; w0 += 64) {
+        const int w = w0 + lane;
+        unsigned set = w < gp.words ? gp.bits[((long long)g * gp.nb + n) * gp.words + w] : 0;
+        const int mine = __popc(set);
+        int sum = mine;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const int other = __shfl_up(sum, s);
+            if (lane >= s) sum += other;
         }
+        for (int* at = out + sum - mine; set; set &= set - 1) *at++ = w * 32 + __ffs(set) - 1;
+        out += __shfl(sum, 63);
     }
 }
 
@@ -668,9 +671,8 @@ template <int D> static int launch_grad(BlockGradParams gp, hipStream_t st) {
         if (rc) return rc;
     }
     hipLaunchKernelGGL(block_bits_kernel, dim3((unsigned)gp.words, (unsigned)p.H_kv), dim3(256), gp.nb * 4, st, gp);
-    hipLaunchKernelGGL(block_count_kernel, dim3((unsigned)((gp.nb + 63) / 64), (unsigned)p.H_kv), dim3(64), 0, st, gp);
     hipLaunchKernelGGL(block_layout_kernel, dim3(1), dim3(1024), 0, st, gp);
-    hipLaunchKernelGGL(block_lists_kernel, dim3((unsigned)((gp.nb + 63) / 64), (unsigned)p.H_kv), dim3(64), 0, st, gp);
+    hipLaunchKernelGGL(block_lists_kernel, dim3((unsigned)((gp.nb + 3) / 4), (unsigned)p.H_kv), dim3(256), 0, st, gp);
     int rc = (int)hipGetLastError();
     if (rc) return rc;
     // as many keys a workgroup as a key block has, so that rows are gathered for all of them at once (us of the whole call with eight, eight and
