@@ -144,6 +144,11 @@ CASES = [
     _c(330, 500, 72, 24, 128, 64, 50, 6, q_start=100, kind="any"),
     _c(250, 300, 96, 48, 128, 32, 100, 12, causal=False, kind="any"),
     _c(400, 400, 66, 33, 128, 32, 70, 5, kind="none"),
+    # rows of a key block's list that do not divide what a workgroup takes at a time; more query blocks than a wave takes words of
+    _c(333, 333, 6, 2, 128, 128, 5, 3),
+    _c(333, 400, 5, 1, 64, 128, 7, 2, q_start=67),
+    _c(150, 290, 14, 2, 128, 96, 11, 2, causal=False, kind="any"),
+    _c(2150, 2150, 2, 1, 64, 32, 1, 3),
 ]
 
 

@@ -85,6 +85,9 @@ SHAPES = [  # dtype, M, S, C, post, next, gate, rows
     (torch.float32, 6, 6, 16384, 1, 2, "sigmoid", "kept"),
     (torch.float32, 9, 9, 8, 2, 2, "none", None),
     (torch.bfloat16, 9, 20, 72, 2, 2, "sigmoid", "kept"),
+    (torch.bfloat16, 4500, 5000, 512, 1, 2, "rows", "kept"),
+    (torch.bfloat16, 2100, 2100, 2048, 2, 1, "sigmoid", None),
+    (torch.float32, 4100, 4200, 132, 2, 2, "row", "dropped"),
 ]
 
 
