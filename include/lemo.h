@@ -468,7 +468,7 @@ int lemo_norm_residual_grad(const void* dN, int64_t lddn, void* dR, int64_t lddr
  * dK and dV sum over the heads of a group before they are rounded.  No atomics on results: the same bits on every run.  Values that are
  * not finite in K or V at a key behind a query spoil the query's result only if the key lies in the same 32 keys (counted from its
  * block's start) as one that the query, or one of the 31 rows beside it, sees; in the gradient those in Q, O or dO of a query spoil
- * dK and dV at keys behind it likewise, within the blocks that its list names.
+ * dK and dV at keys behind it likewise, within the blocks that its list names.  Blocks that a query's list does not name do nothing to it.
  * Supported: d in {64, 128}; b % 32 == 0, b <= 65536; H % H_kv == 0; T * b <= 122880; S_q, S_k below 2^31 - 4096; the choice and the gradient:
  * nb <= 16384; means and choice LEMO_F32 and LEMO_BF16, attention LEMO_BF16; the gradient: Q and dO each spanning less than 4 GiB - 4096.
  * Results overlap neither operands nor each other.

@@ -23,7 +23,7 @@ template <int D, int WAVES, int BA_STAGE> struct BaGeo {
     static constexpr int PITCH = D + 4;                                      // floats of a row where waves' results meet
     static constexpr int JOIN = WAVES * 32 * (PITCH * 4 + 8);
     static constexpr int LIST = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;         // the list's subtiles stand behind both
-    static constexpr int lds(int subtiles) { return LIST + 16 + subtiles * 4; }  // (the number of them first)
+    static constexpr int lds(int subtiles) { return LIST + 16 + subtiles * 4; }  // (the number of them first, and whether sums are not finite)
 };
 
 // PACK: the rows belong to several lists, whose union is worked on; a row sees the subtiles that its own list names.
@@ -35,7 +35,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAtt
     constexpr int ROWS = WAVES / KS * 32;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     int* const keys = reinterpret_cast<int*>(smem + Geo::LIST) + 4;
-    int& listed = keys[-4];
+    int &listed = keys[-4], &not_finite = keys[-3];
 
     int g, rank;
     decode_block(p.order, p.H_kv, p.n_qb * p.n_rt * p.n_parts, g, rank);
@@ -52,6 +52,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAtt
 
     int room = 0;  // (PACK) of the union's subtiles
     if constexpr (PACK) {
+        if (tid == 0) not_finite = 0;
         const long long first = (long long)qb * p.pack;
         const int nb = (p.S_k + p.b - 1) / p.b, lists = (int)min((long long)p.pack, p.n_lists - first);
         room = min(p.pack * p.T, nb) * (p.b / 32);
@@ -111,9 +112,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAtt
     };
 
     f32x16 o[Tile::COLS];
+    float ref, l = 0.f;  // reference of the exponentials (same in both half-waves); this half-wave's share of the normaliser
+    // PACK: what is not finite in V of a block that only some rows list comes to the others as 0 times it, which is not 0.  Then the
+    // workgroup goes through its list once more and adds to the sums of the rows that see a subtile alone: code of its own, since a branch
+    // beside the products would cost the first turn 7 % (a list for each of 8192 queries, 32 / 8 heads, 1170 us / 1240).
+#pragma unroll
+    for (int turn = 0; turn < (PACK ? 2 : 1); ++turn) {
 #pragma unroll
     for (int dv = 0; dv < Tile::COLS; ++dv) o[dv] = f32x16{0};
-    float ref = -INFINITY, l = 0.f;  // reference of the exponentials (same in both half-waves); this half-wave's share of the normaliser
+    ref = -INFINITY;
+    l = 0.f;
     if (n_stage > 0) {
         load_stage(0, 0);
         settle_stage();
@@ -170,12 +178,33 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAtt
             for (int c = 0; c < 2; ++c)
                 pb[c] = u32x4{pack_bf16x2_hw(pr[8 * c + 0], pr[8 * c + 1]), pack_bf16x2_hw(pr[8 * c + 2], pr[8 * c + 3]),
                               pack_bf16x2_hw(pr[8 * c + 4], pr[8 * c + 5]), pack_bf16x2_hw(pr[8 * c + 6], pr[8 * c + 7])};
+            if (turn == 0) {
 #pragma unroll
-            for (int dv = 0; dv < Tile::COLS; ++dv)
+                for (int dv = 0; dv < Tile::COLS; ++dv)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) mma_chunk<bf16_t>(o[dv], Tile::column_fragment(vs, dv, c, lane), pb[c]);  // o[value column][row]
+                    for (int c = 0; c < 2; ++c) mma_chunk<bf16_t>(o[dv], Tile::column_fragment(vs, dv, c, lane), pb[c]);  // o[value column][row]
+            } else {
+#pragma unroll
+                for (int dv = 0; dv < Tile::COLS; ++dv) {
+                    f32x16 sum = o[dv];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) mma_chunk<bf16_t>(sum, Tile::column_fragment(vs, dv, c, lane), pb[c]);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[dv][r] = key <= mine ? sum[r] : o[dv][r];
+                }
+            }
         }
         settle_stage();
+    }
+    if (!PACK || turn == 1) break;
+    float zero = 0.f;
+#pragma unroll
+    for (int dv = 0; dv < Tile::COLS; ++dv)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) zero = fmaf(o[dv][r], 0.f, zero);
+    if (zero != 0.f) not_finite = 1;
+    __syncthreads();
+    if (!__builtin_amdgcn_readfirstlane(not_finite)) break;
     }
 
     // the waves that share rows bring their sums to the largest reference of them, in LDS (the stages are done with), and each finishes

@@ -31,7 +31,7 @@ template <int D, int WAVES, int SUBS> struct DqGeo {
     static constexpr int SUB = 32 * Tile::ROWB, STAGE = 2 * SUBS * SUB;
     static constexpr int PITCH = D + 4, JOIN = WAVES * 32 * PITCH * 4;
     static constexpr int LIST = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
-    static constexpr int lds(int subtiles) { return LIST + 16 + subtiles * 4; }  // (the number of them first)
+    static constexpr int lds(int subtiles) { return LIST + 16 + subtiles * 4; }  // (the number of them first, and whether sums are not finite)
 };
 
 template <int D, int WAVES, int KS, bool PACK>
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams
     constexpr int ROWS = WAVES / KS * 32;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     int* const keys = reinterpret_cast<int*>(smem + Geo::LIST) + 4;
-    int& listed = keys[-4];
+    int &listed = keys[-4], &not_finite = keys[-3];
 
     int g, rank;
     decode_block(p.order, p.H_kv, p.n_qb * p.n_rt, g, rank);
@@ -59,6 +59,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams
 
     int room = 0;  // (PACK) of the union's subtiles
     if constexpr (PACK) {
+        if (tid == 0) not_finite = 0;
         const long long first = (long long)qb * p.pack;
         const int lists = (int)min((long long)p.pack, p.n_lists - first);
         room = min(p.pack * p.T, gp.nb) * (p.b / 32);
@@ -126,6 +127,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams
         }
     };
     f32x16 dq[Tile::COLS];
+    // PACK: what is not finite in K or V of blocks that other rows list, as in the forward pass
+#pragma unroll
+    for (int turn = 0; turn < (PACK ? 2 : 1); ++turn) {
 #pragma unroll
     for (int c = 0; c < Tile::COLS; ++c) dq[c] = f32x16{0};
     if (n_stage > 0) {
@@ -168,12 +172,33 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams
             for (int c = 0; c < 2; ++c)
                 pb[c] = u32x4{pack_bf16x2_hw(ds[8 * c + 0], ds[8 * c + 1]), pack_bf16x2_hw(ds[8 * c + 2], ds[8 * c + 3]),
                               pack_bf16x2_hw(ds[8 * c + 4], ds[8 * c + 5]), pack_bf16x2_hw(ds[8 * c + 6], ds[8 * c + 7])};
+            if (turn == 0) {
 #pragma unroll
-            for (int col = 0; col < Tile::COLS; ++col)
+                for (int col = 0; col < Tile::COLS; ++col)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) mma_chunk<bf16_t>(dq[col], Tile::column_fragment(ks, col, c, lane), pb[c]);  // [head column][row]
+                    for (int c = 0; c < 2; ++c) mma_chunk<bf16_t>(dq[col], Tile::column_fragment(ks, col, c, lane), pb[c]);  // [head column][row]
+            } else {
+#pragma unroll
+                for (int col = 0; col < Tile::COLS; ++col) {
+                    f32x16 sum = dq[col];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) mma_chunk<bf16_t>(sum, Tile::column_fragment(ks, col, c, lane), pb[c]);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) dq[col][r] = key <= mine ? sum[r] : dq[col][r];
+                }
+            }
         }
         settle_stage();
+    }
+    if (!PACK || turn == 1) break;
+    float zero = 0.f;
+#pragma unroll
+    for (int col = 0; col < Tile::COLS; ++col)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) zero = fmaf(dq[col][r], 0.f, zero);
+    if (zero != 0.f) not_finite = 1;
+    __syncthreads();
+    if (!__builtin_amdgcn_readfirstlane(not_finite)) break;
     }
     // the waves that share rows add in LDS, in wave order
     __syncthreads();

@@ -1,0 +1,67 @@
+"""Attention over listed key blocks: values at the ends of what a type holds.  Bounds as in test_block_attention.py."""
+import math
+
+import pytest
+import torch
+
+import test_block_attention as base
+from test_block_attention import HALF, draw
+
+BAD = [math.nan, math.inf, -math.inf]
+
+
+@pytest.fixture(scope="module")
+def lemo():
+    from paper_2501_09767_amd import lemo
+    return lemo
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("where", ["K", "V"])
+@pytest.mark.parametrize("S,H,H_kv,d,b,bq,causal", [(200, 4, 4, 64, 32, 1, True), (200, 8, 2, 128, 32, 1, True), (150, 2, 2, 128, 64, 3, False), (333, 16, 4, 64, 32, 2, False),
+                                                    (600, 16, 16, 128, 32, 1, True)])
+def test_blocks_that_only_other_queries_list(lemo, S, H, H_kv, d, b, bq, causal, where):
+    """Lists of few rows are worked on together.  One key block holds what is not finite; every third list names it, the other queries'
+    results are those of a run in which it holds zeros."""
+    case = base._c(S, S, H, H_kv, d, b, bq, 3, causal=causal)
+    Q, K, V, dO = draw(S + d, (S, H, d), (S, H_kv, d), (S, H_kv, d), (S, H, d))
+    n_qb, bad = -(-S // bq), 1
+    blocks = torch.full((n_qb, H_kv, 3), -1, dtype=torch.int32)
+    for m in range(n_qb):
+        last = min((min((m + 1) * bq, S) - 1) // b, (S - 1) // b) if causal else (S - 1) // b
+        others = [n for n in range(last + 1) if n != bad]
+        for g in range(H_kv):
+            pick = sorted({others[(m + g) % len(others)], others[-1]} | ({bad} if (m + g) % 3 == 0 and last >= bad else set()))
+            blocks[m, g, :len(pick)] = torch.tensor(pick, dtype=torch.int32)
+    spoiled = (blocks == bad).any(2).repeat_interleave(bq, 0)[:S].repeat_interleave(H // H_kv, 1)  # [S,H]
+    assert spoiled.any() and not spoiled.all()
+    for x in (K, V):
+        x[bad * b:(bad + 1) * b] = 0
+    K2, V2 = K.clone(), V.clone()
+    target = K2 if where == "K" else V2
+    for i, value in enumerate(BAD):
+        target[bad * b + 5 * i:bad * b + 5 * i + 3, :, i::7] = value
+    flags = lemo.CAUSAL if causal else 0
+    q, do, bl = Q.cuda(), dO.cuda(), blocks.cuda()
+    O, lse2 = lemo.lemo_block_attention(q, K.cuda(), V.cuda(), bl, b, bq, flags)
+    O2, lse2_2 = lemo.lemo_block_attention(q, K2.cuda(), V2.cuda(), bl, b, bq, flags)
+    ref = base.reference(case, Q, K, V, blocks, dO, O.cpu())
+    clear = ~spoiled
+    off = (O2.double().cpu() - ref["O"]).abs() - (HALF * ref["O"].abs() + (1 + HALF) * (HALF + 4 * ref["E"] + 2.0 ** -14)[..., None] * ref["O_mag"])
+    assert off[clear].max() <= 1e-30  # (a NaN is no smaller)
+    assert torch.equal(O2.cpu()[clear], O.cpu()[clear]) and torch.equal(lse2_2.cpu().t()[clear], lse2.cpu().t()[clear])
+    if where == "V":
+        assert not torch.isfinite(O2.cpu()[spoiled & (torch.arange(S) >= (bad + 1) * b)[:, None]]).all()
+    grads = lemo.lemo_block_attention_grad(do, q, K2.cuda(), V2.cuda(), O2, lse2_2, bl, b, bq, flags)
+    off = (grads[0].double().cpu() - ref["dQ"]).abs() - (HALF * ref["dQ"].abs() + (1 + HALF) * ref["dQ_mag"] * (1 + 2.0 ** -10))
+    assert off[clear].max() <= 1e-30
+    # key blocks that no spoiled query lists
+    for g in range(H_kv):
+        for n in range(-(-S // b)):
+            naming = (blocks[:, g] == n).any(1)
+            if n == bad or ((blocks[:, g] == bad).any(1) & naming).any():
+                continue
+            at = slice(n * b, (n + 1) * b)
+            for name, got in (("dK", grads[1]), ("dV", grads[2])):
+                off = (got.double().cpu()[at, g] - ref[name][at, g]).abs() - (HALF * ref[name][at, g].abs() + (1 + HALF) * ref[name + "_mag"][at, g] * (1 + 2.0 ** -10))
+                assert off.max() <= 1e-30, (name, g, n)
