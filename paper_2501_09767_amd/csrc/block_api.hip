@@ -36,6 +36,13 @@ int check_lists(int64_t S_q, int64_t S_k, int64_t q_start, int32_t H, int32_t H_
     return q * (H / H_kv) >= (1 << 24) || (S_q + q - 1) / q * H_kv >= (int64_t)1 << 28 ? LEMO_ERR_UNSUPPORTED : LEMO_OK;
 }
 
+// sizes of the gradient: places in the lists turned round, and in the rows that a key block gathers, are ints
+int check_turned_lists(int64_t S_q, int64_t S_k, int32_t H, int32_t H_kv, int32_t T, int32_t b, int32_t bq) {
+    const int64_t q = bq < S_q ? bq : S_q, n_qb = (S_q + q - 1) / q, nb = (S_k - 1) / b + 1, limit = (int64_t)1 << 31;
+    if (nb > MAX_LISTED_BLOCKS) return LEMO_ERR_UNSUPPORTED;
+    return n_qb * H_kv * (T < nb ? T : nb) >= limit || n_qb * q * (H / H_kv) >= limit - 4096 ? LEMO_ERR_UNSUPPORTED : LEMO_OK;
+}
+
 int64_t span_bytes(int64_t S, int64_t ts, int64_t H, int64_t hs, int64_t d) { return ((S - 1) * ts + (H - 1) * hs + d) * 2; }
 
 float base2(float scale, int32_t d) { return (float)((scale > 0.f ? (double)scale : 1.0 / std::sqrt((double)d)) * 1.4426950408889634); }
@@ -156,8 +163,8 @@ int lemo_block_attention_grad_workspace_bytes(int64_t S_q, int64_t S_k, int32_t 
     if (!bytes) return LEMO_ERR_NULL;
     int rc = check_sizes(H, H_kv, d, LEMO_BF16, b);
     if (rc == LEMO_OK) rc = check_lists(S_q, S_k, 0, H, H_kv, T, b, bq);
+    if (rc == LEMO_OK) rc = check_turned_lists(S_q, S_k, H, H_kv, T, b, bq);
     if (rc != LEMO_OK) return rc;
-    if ((S_k + b - 1) / b > MAX_LISTED_BLOCKS) return LEMO_ERR_UNSUPPORTED;
     *bytes = block_grad_layout(S_q, S_k, H, H_kv, d, T, b, (int)(bq < S_q ? bq : S_q)).bytes;
     return LEMO_OK;
 }
@@ -177,7 +184,8 @@ int lemo_block_attention_grad(const void* dO, const void* Q, const void* K, cons
     if (rc != LEMO_OK) return rc;
     if (!aligned16(dQ) || !aligned16(dK) || !aligned16(dV) || (reinterpret_cast<uintptr_t>(lse2) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
         return LEMO_ERR_ALIGN;
-    if ((S_k + b - 1) / b > MAX_LISTED_BLOCKS) return LEMO_ERR_UNSUPPORTED;
+    rc = check_turned_lists(S_q, S_k, H, H_kv, T, b, bq);
+    if (rc != LEMO_OK) return rc;
     // the rows that a key block gathers are addressed with 32-bit offsets
     const int64_t most = ((int64_t)1 << 32) - 4096;
     if (span_bytes(S_q, q_tok_stride, H, q_head_stride, d) > most || span_bytes(S_q, do_tok_stride, H, do_head_stride, d) > most) return LEMO_ERR_UNSUPPORTED;
