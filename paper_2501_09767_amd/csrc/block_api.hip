@@ -8,7 +8,7 @@ using namespace lemo;
 
 namespace {
 
-constexpr int64_t MOST_TOKENS = ((int64_t)1 << 31) - 4096;  // positions, and the ends of the blocks they lie in, are ints
+constexpr int64_t MOST_TOKENS = ((int64_t)1 << 31) - 4096;  // positions, and those of the next few subtiles of keys, are ints (a block may end past them)
 
 bool pitch_fits(int64_t ts) { return ts < (1 << 22); }
 
