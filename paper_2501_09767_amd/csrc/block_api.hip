@@ -1,5 +1,7 @@
 // Host side of the attention over chosen key blocks (lemo.h): argument validation and kernel launches only.
+#include <algorithm>
 #include <cmath>
+#include <numeric>
 
 #include "api_checks.hpp"
 #include "block_attention.hpp"
@@ -41,6 +43,18 @@ int check_turned_lists(int64_t S_q, int64_t S_k, int32_t H, int32_t H_kv, int32_
     const int64_t q = bq < S_q ? bq : S_q, n_qb = (S_q + q - 1) / q, nb = (S_k - 1) / b + 1, limit = (int64_t)1 << 31;
     if (nb > MAX_LISTED_BLOCKS) return LEMO_ERR_UNSUPPORTED;
     return n_qb * H_kv * (T < nb ? T : nb) >= limit || n_qb * q * (H / H_kv) >= limit - 4096 ? LEMO_ERR_UNSUPPORTED : LEMO_OK;
+}
+
+// whether T blocks hold the positions of any query block, b keys each.  How a query block of q lies to the blocks repeats after b / gcd(q, b)
+// of them at most; blocks at the far ends of queries and keys only have fewer positions.
+bool room_for_own_blocks(int64_t S_q, int64_t S_k, int64_t q_start, int64_t b, int64_t q, int64_t T) {
+    if (T >= (q + b - 2) / b + 1) return true;
+    const int64_t n_qb = (S_q + q - 1) / q, period = b / std::gcd(q, b);
+    for (int64_t m = 0; m < n_qb && m < period; ++m) {
+        const int64_t first = q_start + m * q, last = std::min(q_start + std::min((m + 1) * q, S_q), S_k) - 1;
+        if (last / b - first / b + 1 > T) return false;
+    }
+    return true;
 }
 
 int64_t span_bytes(int64_t S, int64_t ts, int64_t H, int64_t hs, int64_t d) { return ((S - 1) * ts + (H - 1) * hs + d) * 2; }
@@ -117,8 +131,7 @@ int lemo_select_blocks(const void* Q, int64_t S_q, int32_t H, int32_t H_kv, int3
     if ((S_k + b - 1) / b > MAX_LISTED_BLOCKS) return LEMO_ERR_UNSUPPORTED;
     const int32_t q = bq < S_q ? bq : (int32_t)S_q;
     if (flags & LEMO_CAUSAL) {  // the blocks that hold the queries themselves are always listed: there has to be room for them
-        const int64_t own = b % q == 0 && q_start % q == 0 ? 1 : q % b == 0 && q_start % b == 0 ? q / b : ((int64_t)q + b - 2) / b + 1;
-        if (T < own) return LEMO_ERR_SHAPE;
+        if (!room_for_own_blocks(S_q, S_k, q_start, b, q, T)) return LEMO_ERR_SHAPE;
     }
     BlockSelectParams p{};
     p.Q = Q; p.means = means; p.blocks = blocks;

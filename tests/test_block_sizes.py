@@ -5,6 +5,8 @@ import math
 import pytest
 import torch
 
+from test_block_attention import chosen64
+
 
 @pytest.fixture(scope="module")
 def lemo():
@@ -55,3 +57,40 @@ def test_blocks_of_keys_next_to_2_31(lemo, H, H_kv, d, bq):
         assert ((O.double().cpu() - want).abs() <= (2.0 ** -8 * (2 + 2.0 ** -8) + count * 2.0 ** -27) * want.abs()).all()
         x = (Q.double() * k.double()[0].repeat_interleave(H // H_kv, 0)).sum(2) / math.sqrt(d) * math.log2(math.e) + math.log2(count)
         assert ((lse2.double().cpu().t() - x).abs() <= 2.0 ** -10).all()
+
+
+def own_blocks(S_q, S_k, q_start, b, bq):
+    """The most blocks that hold positions of one query block's queries, from the definition."""
+    return max(len({i // b for i in range(q_start + m, min(q_start + min(m + bq, S_q), S_k))}) for m in range(0, S_q, bq))
+
+
+# S_q, S_k, q_start, b, bq: query blocks of one, of all queries, shorter and longer than key blocks, across their ends or not, past the keys
+OWN = [(100, 100, 0, 128, 100), (40, 40, 0, 64, 64), (300, 300, 0, 128, 300), (100, 200, 100, 128, 1000), (33, 33, 0, 32, 33), (64, 64, 0, 96, 32), (96, 200, 50, 32, 48),
+       (90, 90, 0, 32, 40), (50, 20, 0, 32, 50), (64, 40, 500, 32, 16), (20, 70, 60, 32, 7), (1, 1, 0, 32, 1), (500, 500, 0, 96, 36), (65, 200, 32, 32, 64)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", range(len(OWN)))
+def test_lists_with_room_for_the_queries_own_blocks_and_no_more(lemo, n):
+    S_q, S_k, q_start, b, bq = OWN[n]
+    T = max(1, own_blocks(*OWN[n]))
+    g = torch.Generator().manual_seed(n)
+    Q, means = torch.randn(S_q, 4, 64, generator=g).to(torch.bfloat16), torch.randn(-(-S_k // b), 2, 64, generator=g)
+    for room in (T, T + 1):
+        got = lemo.lemo_select_blocks(Q.cuda(), means.cuda(), S_k, b, bq, room, q_start=q_start)
+        assert torch.equal(got.cpu(), chosen64(Q, means, S_k, b, bq, room, True, q_start))
+    if T > 1:
+        with pytest.raises(lemo.LemoError):
+            lemo.lemo_select_blocks(Q.cuda(), means.cuda(), S_k, b, bq, T - 1, q_start=q_start)
+
+
+def test_refused_where_the_own_blocks_do_not_fit():
+    """On the host alone: addresses are never touched."""
+    from paper_2501_09767_amd import lemo
+    for S_q, S_k, q_start, b, bq in OWN:
+        for T in range(1, own_blocks(S_q, S_k, q_start, b, bq)):
+            rc = lemo._lib.lemo_select_blocks(0x100000, S_q, 4, 2, 64, 1, 256, 64, 0x200000, S_k, q_start, b, bq, T, 1, 0x300000, None)
+            assert rc == -2, (S_q, S_k, q_start, b, bq, T)
+    # (blocks of 65536 keys, 12345 queries each: only the sixth block of them goes across an end)
+    f = lambda S, T: lemo._lib.lemo_select_blocks(0x100000, S, 4, 2, 64, 1, 256, 64, 0x200000, S, 0, 65536, 12345, T, 1, 0x300000, None)  # noqa: E731
+    assert f(12345 * 6, 1) == -2
