@@ -465,6 +465,7 @@ int lemo_norm_residual_grad(const void* dN, int64_t lddn, void* dR, int64_t lddr
  *   lemo_block_attention_step   O [B,H,d]
  *
  * Probabilities (and in the gradient dS) are rounded to bf16 for the products that follow; sums in binary32; one rounding at the store.
+ * The sums over V are divided at the end: values of V up to 2^100 do not pass their range.
  * dK and dV sum over the heads of a group before they are rounded.  No atomics on results: the same bits on every run.  Values that are
  * not finite in K or V at a key behind a query spoil the query's result only if the key lies in the same 32 keys (counted from its
  * block's start) as one that the query, or one of the 31 rows beside it, sees; in the gradient those in Q, O or dO of a query spoil

@@ -342,6 +342,16 @@ __global__ __launch_bounds__(256, 1) void block_attention_pipe_kernel(BlockAttnP
         o_ref[qs] = mrun[qs];
         bad |= lim[qs] >= 0 && !(ltot[qs] < BP_FROZEN_LIMIT);
     }
+    if (t_hot > 1) {  // probabilities up to the limit, times large values, may have passed binary32 where the ordinary softmax does not
+        float zero = 0.f;
+#pragma unroll
+        for (int qs = 0; qs < 2; ++qs)
+#pragma unroll
+            for (int dv = 0; dv < 4; ++dv)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) zero = fmaf(o[qs][dv][r], 0.f, zero);
+        bad |= zero != 0.f;
+    }
     if (!__syncthreads_or(frozen && bad)) break;  // (the barrier also ends the last stage: its buffer is free)
     // once more with the ordinary softmax: the first stage comes again, into the buffer that the next tile's has just filled
     frozen = false;

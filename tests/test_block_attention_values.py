@@ -65,3 +65,24 @@ def test_blocks_that_only_other_queries_list(lemo, S, H, H_kv, d, b, bq, causal,
             for name, got in (("dK", grads[1]), ("dV", grads[2])):
                 off = (got.double().cpu()[at, g] - ref[name][at, g]).abs() - (HALF * ref[name][at, g].abs() + (1 + HALF) * ref[name + "_mag"][at, g] * (1 + 2.0 ** -10))
                 assert off.max() <= 1e-30, (name, g, n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,H_kv,d,S,bq", [(4, 1, 128, 640, 64), (80, 20, 128, 640, 64), (2, 2, 128, 640, 64), (4, 1, 64, 640, 64), (8, 2, 128, 320, 1)])
+def test_later_logits_within_the_range_of_the_reference_and_large_values(lemo, H, H_kv, d, S, bq):
+    """Later logits up to 2^97 above the first ones, values of 2^40: their products pass the range of binary32, their quotient does not."""
+    case = base._c(S, S, H, H_kv, d, 32, bq, 16)
+    Q, K, V = draw(5, (S, H, d), (S, H_kv, d), (S, H_kv, d))
+    V = V * 2.0 ** 40
+    blocks = torch.full((-(-S // bq), H_kv, 16), -1, dtype=torch.int32)
+    for m in range(len(blocks)):
+        last = (min((m + 1) * bq, S) - 1) // 32
+        pick = list(range(last + 1))[-16:]
+        blocks[m, :, :len(pick)] = torch.tensor(pick, dtype=torch.int32)
+    Q[::3] = 4.0
+    K *= 0.125
+    K[149::150] = 94.0 / (4.0 * d / math.sqrt(d) * math.log2(math.e))  # one key in 150: 94 (and its rounding to bf16) for these queries
+    O, lse2 = lemo.lemo_block_attention(Q.cuda(), K.cuda(), V.cuda(), blocks.cuda(), 32, bq)
+    ref = base.reference(case, Q, K, V, blocks)
+    assert 90 < ref["lse2"].max() < 100
+    base.check_forward(O, lse2, ref)
