@@ -18,7 +18,7 @@ bool pitch_fits(int64_t ts) { return ts < (1 << 22); }
 int check_sizes(int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt, int32_t b) {
     if (!valid_dtype(dt)) return LEMO_ERR_DTYPE;
     if (H <= 0 || H_kv <= 0 || H % H_kv || b <= 0) return LEMO_ERR_SHAPE;
-    return (d != 64 && d != 128) || b % 32 || b > 65536 ? LEMO_ERR_UNSUPPORTED : LEMO_OK;
+    return (d != 64 && d != 128) || b % 32 || b > 65536 || H_kv > 65535 ? LEMO_ERR_UNSUPPORTED : LEMO_OK;
 }
 
 // element strides of a [tokens, heads, d] tensor

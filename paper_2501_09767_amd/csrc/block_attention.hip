@@ -38,7 +38,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAtt
     int &listed = keys[-4], &not_finite = keys[-3];
 
     int g, rank;
-    decode_block(p.order, p.H_kv, p.n_qb * p.n_rt * p.n_parts, g, rank);
+    decode_block(p.order, p.H_kv, p.n_qb * p.n_rt * p.n_parts, g, rank, p.first + blockIdx.x);
     const int share = rank % p.n_parts, rt = rank / p.n_parts % p.n_rt, qb = rank / p.n_parts / p.n_rt;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -344,10 +344,11 @@ template <int D> static int prepare_block_attention() {
     return err;
 }
 
-template <int D, int WAVES, int KS, bool PACK> static int run_block_attention(const BlockAttnParams& p, int subtiles, hipStream_t st) {
-    hipLaunchKernelGGL((block_attention_kernel<D, WAVES, KS, PACK>), dim3((unsigned)((long long)p.n_qb * p.n_rt * p.n_parts * p.H_kv)), dim3(WAVES * 64),
-                       (ba_lds<D, WAVES, KS>(PACK ? 2 * subtiles : subtiles)), st, p);
-    return (int)hipGetLastError();
+template <int D, int WAVES, int KS, bool PACK> static int run_block_attention(BlockAttnParams p, int subtiles, hipStream_t st) {
+    return launch_in_turns((long long)p.n_qb * p.n_rt * p.n_parts * p.H_kv, WAVES * 64, [&](long long first, unsigned count) {
+        p.first = (int)first;
+        hipLaunchKernelGGL((block_attention_kernel<D, WAVES, KS, PACK>), dim3(count), dim3(WAVES * 64), (ba_lds<D, WAVES, KS>(PACK ? 2 * subtiles : subtiles)), st, p);
+    });
 }
 
 template <int D> static int launch_block_attention_d(BlockAttnParams p, hipStream_t st) {

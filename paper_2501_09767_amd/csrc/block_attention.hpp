@@ -15,6 +15,7 @@ struct BlockAttnParams {
     float* parts;        // where a list is shared by several workgroups: their results, see PART_ROW
     int S_q, S_k, H, H_kv, G, T, b, bq, n_qb;
     int R, n_rt, n_parts;  // rows of a query block, tiles of them, shares of a list
+    int first;             // workgroup of the launch's first one
     int pack, n_lists;     // lists that are worked on together (bq, n_qb, R then count `pack` blocks as one), and all there are
     long long q_start;
     long long q_ts, q_hs, k_ts, k_hs, k_ss, v_ts, v_hs, v_ss, o_ts, o_hs;  // element strides: token, head, sequence
@@ -63,6 +64,7 @@ struct BlockSelectParams {
     const int* lengths;   // single tokens, or null
     int* blocks;          // [n_qb, H_kv, T]
     int S_q, S_k, H, H_kv, G, d, T, b, bq, n_qb, nb;
+    int first;            // workgroup of the launch's first one
     long long q_start, q_ts, q_hs, means_ss;
     unsigned flags;
 };

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_dq_kernel(BlockGradParams
     int &listed = keys[-4], &not_finite = keys[-3];
 
     int g, rank;
-    decode_block(p.order, p.H_kv, p.n_qb * p.n_rt, g, rank);
+    decode_block(p.order, p.H_kv, p.n_qb * p.n_rt, g, rank, p.first + blockIdx.x);
     const int rt = rank % p.n_rt, qb = rank / p.n_rt;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -341,8 +341,9 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
     using Tile = HeadTile<D>;
     constexpr int ROWS = Geo::ROWS, SUBS = Geo::SUBS, WAVES = KW * SHARES;
     // each die takes a contiguous range of the items: those at work on it together share a head's Q and dO in its L2
-    const int total = __builtin_amdgcn_readfirstlane(gp.totals[0]), per_die = (total + NUM_XCD - 1) / NUM_XCD, in_die = blockIdx.x / NUM_XCD;
-    const int at_item = blockIdx.x % NUM_XCD * per_die + in_die;
+    const int total = __builtin_amdgcn_readfirstlane(gp.totals[0]), per_die = (total + NUM_XCD - 1) / NUM_XCD;
+    const unsigned block = p.first + blockIdx.x;
+    const int in_die = block / NUM_XCD, at_item = block % NUM_XCD * per_die + in_die;
     if (in_die >= per_die || at_item >= total) return;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     // tables: [ring of 3][ROWS] of each field
@@ -600,7 +601,7 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
 // The key blocks that were cut: their parts added in order.
 template <int D> __global__ __launch_bounds__(256) void block_dkv_join_kernel(BlockGradParams gp) {
     const BlockAttnParams& p = gp.a;
-    const int at = blockIdx.x, g = at / gp.nb, n = at % gp.nb, slot = gp.slots[at];
+    const int at = p.first + blockIdx.x, g = at / gp.nb, n = at % gp.nb, slot = gp.slots[at];
     if (slot < 0) return;
     const int parts = (gp.counts[at] + gp.share - 1) / gp.share;
     constexpr int LPR = D / 8;
@@ -654,10 +655,11 @@ BlockGradLayout block_grad_layout(long long S_q, long long S_k, int H, int H_kv,
 
 template <int D, int KS> constexpr int dq_lds(int subtiles) { return DqGeo<D, 4, BG_STAGE<D, KS>>::lds(subtiles); }
 
-template <int D, int KS, bool PACK> static int run_dq(const BlockGradParams& gp, int subtiles, hipStream_t st) {
-    hipLaunchKernelGGL((block_dq_kernel<D, 4, KS, PACK>), dim3((unsigned)((long long)gp.a.n_qb * gp.a.n_rt * gp.a.H_kv)), dim3(256),
-                       (dq_lds<D, KS>(PACK ? 2 * subtiles : subtiles)), st, gp);
-    return (int)hipGetLastError();
+template <int D, int KS, bool PACK> static int run_dq(BlockGradParams gp, int subtiles, hipStream_t st) {
+    return launch_in_turns((long long)gp.a.n_qb * gp.a.n_rt * gp.a.H_kv, 256, [&](long long first, unsigned count) {
+        gp.a.first = (int)first;
+        hipLaunchKernelGGL((block_dq_kernel<D, 4, KS, PACK>), dim3(count), dim3(256), (dq_lds<D, KS>(PACK ? 2 * subtiles : subtiles)), st, gp);
+    });
 }
 
 // Waves that share keys in the pass by key blocks.  Heads of 128: so many that two workgroups fit a CU, and the one's begin and end pass
@@ -666,11 +668,12 @@ template <int D, int KS, bool PACK> static int run_dq(const BlockGradParams& gp,
 // lists for 16 queries, 8 of 128 489 with 1 / 480 with 2; 16 of 64 513 with 2 / 526 with 4; 32 of 32 643 with 2 / 578 with 4.
 template <int D, int KW> constexpr int DKV_SHARES = KW == 4 ? (D == 128 ? 1 : 2) : KW == 2 || D == 128 ? 2 : 4;
 
-template <int D, int KW> static int run_dkv(const BlockGradParams& gp, hipStream_t st) {
+template <int D, int KW> static int run_dkv(BlockGradParams gp, hipStream_t st) {
     constexpr int SHARES = DKV_SHARES<D, KW>;
-    hipLaunchKernelGGL((block_dkv_kernel<D, KW, SHARES>), dim3((unsigned)((gp.max_items + NUM_XCD - 1) / NUM_XCD * NUM_XCD), (unsigned)(gp.a.b / (32 * KW))), dim3(KW * SHARES * 64),
-                       (DkvGeo<D, KW, SHARES>::LDS), st, gp);
-    return (int)hipGetLastError();
+    return launch_in_turns(((long long)gp.max_items + NUM_XCD - 1) / NUM_XCD * NUM_XCD, KW * SHARES * 64, [&](long long first, unsigned count) {
+        gp.a.first = (int)first;
+        hipLaunchKernelGGL((block_dkv_kernel<D, KW, SHARES>), dim3(count, (unsigned)(gp.a.b / (32 * KW))), dim3(KW * SHARES * 64), (DkvGeo<D, KW, SHARES>::LDS), st, gp);
+    });
 }
 
 template <int D> static int launch_grad(BlockGradParams gp, hipStream_t st) {
@@ -705,8 +708,10 @@ template <int D> static int launch_grad(BlockGradParams gp, hipStream_t st) {
     const int subs = p.b / 32;
     rc = subs % 4 == 0 ? run_dkv<D, 4>(gp, st) : subs % 2 == 0 ? run_dkv<D, 2>(gp, st) : run_dkv<D, 1>(gp, st);
     if (rc) return rc;
-    hipLaunchKernelGGL((block_dkv_join_kernel<D>), dim3((unsigned)(p.H_kv * gp.nb), 2), dim3(256), 0, st, gp);
-    return (int)hipGetLastError();
+    return launch_in_turns((long long)p.H_kv * gp.nb, 256, [&](long long first, unsigned count) {
+        p.first = (int)first;
+        hipLaunchKernelGGL((block_dkv_join_kernel<D>), dim3(count, 2), dim3(256), 0, st, gp);
+    });
 }
 
 int launch_block_attention_grad(BlockGradParams gp, int d, hipStream_t st) { return d == 64 ? launch_grad<64>(gp, st) : launch_grad<128>(gp, st); }

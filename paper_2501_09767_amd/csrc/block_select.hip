@@ -63,16 +63,17 @@ __device__ __forceinline__ void block_mean(const char* K, long long first, int k
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void block_means_kernel(const void* K, long long S, int H_kv, int d, long long k_ts, long long k_hs, int b, float* means) {
-    const long long first = (long long)blockIdx.x * b;
-    block_mean<T>(static_cast<const char*>(K), first, (int)min((long long)b, S - first), H_kv, d, k_ts, k_hs, means + (long long)blockIdx.x * H_kv * d);
+__global__ __launch_bounds__(256) void block_means_kernel(const void* K, long long S, int H_kv, int d, long long k_ts, long long k_hs, int b, float* means,
+                                                          long long first_block) {
+    const long long n = first_block + blockIdx.x, first = n * b;
+    block_mean<T>(static_cast<const char*>(K), first, (int)min((long long)b, S - first), H_kv, d, k_ts, k_hs, means + n * H_kv * d);
 }
 
 // Single tokens: the block that the newest token of a sequence has filled, if it has.
 template <typename T>
 __global__ __launch_bounds__(256) void block_means_step_kernel(const void* K, const int* lengths, long long S_max, int H_kv, int d, long long k_ss,
-                                                               long long k_ts, long long k_hs, int b, float* means, int nb) {
-    const int s = blockIdx.x, S = (int)min((long long)lengths[s], S_max);
+                                                               long long k_ts, long long k_hs, int b, float* means, int nb, int first) {
+    const int s = first + blockIdx.x, S = (int)min((long long)lengths[s], S_max);
     if (S <= 0 || S % b != 0) return;  // the whole workgroup
     const long long n = S / b - 1;
     block_mean<T>(static_cast<const char*>(K) + s * k_ss * (long long)(16 / KeyPiece<T>::E), n * b, b, H_kv, d, k_ts, k_hs,
@@ -128,8 +129,9 @@ __global__ __launch_bounds__(THREADS) void select_blocks_kernel(BlockSelectParam
     double* const sums = reinterpret_cast<double*>(smem);                                  // [RB][PITCH]
     double* const scratch = reinterpret_cast<double*>(smem + Geo::SUMS);                    // [RB * TPL][D]; then
     unsigned long long* const keys = reinterpret_cast<unsigned long long*>(smem + Geo::SUMS);  // [RB][nb]
-    const int g = blockIdx.x % p.H_kv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const long long qb0 = (long long)(blockIdx.x / p.H_kv) * RB;
+    const unsigned block = p.first + blockIdx.x;
+    const int g = block % p.H_kv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const long long qb0 = (long long)(block / p.H_kv) * RB;
     const bool causal = (p.flags & LEMO_CAUSAL) != 0;
     const int S = p.lengths ? min(max(p.lengths[qb0], 0), p.S_k) : p.S_k;  // (single tokens: RB = 1)
     auto queries_of = [&](long long qb) { return (int)max(0ll, min((long long)p.bq, p.S_q - qb * p.bq)); };
@@ -322,26 +324,29 @@ __global__ __launch_bounds__(THREADS) void select_blocks_kernel(BlockSelectParam
 
 int launch_block_means(const void* K, long long S, int H_kv, int d, lemo_dtype_t dt, long long k_ts, long long k_hs, int b, float* means, hipStream_t st) {
     const int pieces = H_kv * (d / (dt == LEMO_BF16 ? 8 : 4));
-    const dim3 grid((unsigned)((S + b - 1) / b), (unsigned)((pieces + 63) / 64));
-    if (dt == LEMO_BF16) hipLaunchKernelGGL((block_means_kernel<bf16_t>), grid, dim3(256), 0, st, K, S, H_kv, d, k_ts, k_hs, b, means);
-    else hipLaunchKernelGGL((block_means_kernel<float>), grid, dim3(256), 0, st, K, S, H_kv, d, k_ts, k_hs, b, means);
-    return (int)hipGetLastError();
+    return launch_in_turns((S + b - 1) / b, 256, [&](long long first, unsigned count) {
+        const dim3 grid(count, (unsigned)((pieces + 63) / 64));
+        if (dt == LEMO_BF16) hipLaunchKernelGGL((block_means_kernel<bf16_t>), grid, dim3(256), 0, st, K, S, H_kv, d, k_ts, k_hs, b, means, first);
+        else hipLaunchKernelGGL((block_means_kernel<float>), grid, dim3(256), 0, st, K, S, H_kv, d, k_ts, k_hs, b, means, first);
+    });
 }
 
 int launch_block_means_step(const void* K, const int* lengths, int B, long long S_max, int H_kv, int d, lemo_dtype_t dt, long long k_ss, long long k_ts,
                             long long k_hs, int b, float* means, int nb, hipStream_t st) {
     const int pieces = H_kv * (d / (dt == LEMO_BF16 ? 8 : 4));
-    const dim3 grid((unsigned)B, (unsigned)((pieces + 63) / 64));
-    if (dt == LEMO_BF16)
-        hipLaunchKernelGGL((block_means_step_kernel<bf16_t>), grid, dim3(256), 0, st, K, lengths, S_max, H_kv, d, k_ss, k_ts, k_hs, b, means, nb);
-    else hipLaunchKernelGGL((block_means_step_kernel<float>), grid, dim3(256), 0, st, K, lengths, S_max, H_kv, d, k_ss, k_ts, k_hs, b, means, nb);
-    return (int)hipGetLastError();
+    return launch_in_turns(B, 256, [&](long long first, unsigned count) {
+        const dim3 grid(count, (unsigned)((pieces + 63) / 64));
+        if (dt == LEMO_BF16)
+            hipLaunchKernelGGL((block_means_step_kernel<bf16_t>), grid, dim3(256), 0, st, K, lengths, S_max, H_kv, d, k_ss, k_ts, k_hs, b, means, nb, (int)first);
+        else hipLaunchKernelGGL((block_means_step_kernel<float>), grid, dim3(256), 0, st, K, lengths, S_max, H_kv, d, k_ss, k_ts, k_hs, b, means, nb, (int)first);
+    });
 }
 
-template <typename T, int D, int RB, int THREADS> static int run_select_lists(const BlockSelectParams& p, hipStream_t st) {
-    const long long teams = ((long long)p.n_qb + RB - 1) / RB;
-    hipLaunchKernelGGL((select_blocks_kernel<T, D, RB, THREADS>), dim3((unsigned)(teams * p.H_kv)), dim3(THREADS), (SelGeo<T, D, RB, THREADS>::lds(p.nb)), st, p);
-    return (int)hipGetLastError();
+template <typename T, int D, int RB, int THREADS> static int run_select_lists(BlockSelectParams p, hipStream_t st) {
+    return launch_in_turns(((long long)p.n_qb + RB - 1) / RB * p.H_kv, THREADS, [&](long long first, unsigned count) {
+        p.first = (int)first;
+        hipLaunchKernelGGL((select_blocks_kernel<T, D, RB, THREADS>), dim3(count), dim3(THREADS), (SelGeo<T, D, RB, THREADS>::lds(p.nb)), st, p);
+    });
 }
 
 template <typename T, int D> static int run_select_blocks(const BlockSelectParams& p, hipStream_t st) {

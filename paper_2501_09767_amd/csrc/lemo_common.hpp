@@ -170,6 +170,19 @@ inline bool spans_meet(const void* a, long long a_bytes, const void* b, long lon
     return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
 }
 
+// ---- host: a launch holds fewer than 2^32 threads ---------------------------------------------------
+// `launch(first, count)` for workgroups [first, first + count) of as many as there are: half of what a launch holds at a time, so a
+// multiple of the dies.
+template <typename F> int launch_in_turns(long long workgroups, int threads, F&& launch) {
+    const long long most = (1ll << 31) / threads;
+    for (long long first = 0; first < workgroups; first += most) {
+        launch(first, (unsigned)(workgroups - first < most ? workgroups - first : most));
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return (int)err;
+    }
+    return 0;
+}
+
 // ---- host: dynamic-LDS limits -------------------------------------------------------------------------
 // The limit of a kernel is raised once, which a stream capture cannot hold, and which kernel a call takes depends on its sizes: so
 // an entry point raises the limits of all the kernels that calls of one type and head size may take in the first of them

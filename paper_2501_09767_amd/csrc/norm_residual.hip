@@ -87,7 +87,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_residual_kernel(No
     constexpr int E = Piece<T>::E, TEAMS = TPR < 256 ? 256 / TPR : 1;
     __shared__ float lds[4 * (TPR / 64)];
     int turn = 0;
-    const long long m = (long long)blockIdx.x * TEAMS + threadIdx.x / TPR;
+    const long long m = (p.first + blockIdx.x) * TEAMS + threadIdx.x / TPR;
     if (m >= p.M) return;  // (a team is a wave, or the whole workgroup)
     const int t = threadIdx.x % TPR;
     const long long row = p.idx ? (long long)p.idx[m] : m;
@@ -376,10 +376,12 @@ __global__ __launch_bounds__(1024) void norm_sums_kernel(const float* __restrict
     out.to[plane][c] = s;
 }
 
-template <typename T, int TPR, int NP> static int run_norm(const NormParams& p, hipStream_t st) {
-    constexpr int TEAMS = TPR < 256 ? 256 / TPR : 1;
-    hipLaunchKernelGGL((norm_residual_kernel<T, TPR, NP>), dim3((unsigned)((p.M + TEAMS - 1) / TEAMS)), dim3(TPR < 256 ? 256 : TPR), 0, st, p);
-    return (int)hipGetLastError();
+template <typename T, int TPR, int NP> static int run_norm(NormParams p, hipStream_t st) {
+    constexpr int TEAMS = TPR < 256 ? 256 / TPR : 1, THREADS = TPR < 256 ? 256 : TPR;
+    return launch_in_turns((p.M + TEAMS - 1) / TEAMS, THREADS, [&](long long first, unsigned count) {
+        p.first = first;
+        hipLaunchKernelGGL((norm_residual_kernel<T, TPR, NP>), dim3(count), dim3(THREADS), 0, st, p);
+    });
 }
 
 // Short rows: a wave each, which needs no LDS and no barrier; from 256 pieces on (bf16: 2048 columns) a workgroup, whose threads have more

@@ -13,6 +13,7 @@ struct NormParams {
     void* N;           // [M, C]
     float* stats;      // [M, 4]: mean and 1 / deviation of post, of next; or null
     long long ldy, ldg, ldr, ldn, S, M;
+    long long first;   // workgroup of the launch's first one
     int C, post, next;
     unsigned flags;
     float eps, a, beta;
