@@ -1,11 +1,11 @@
-"""Attention over listed key blocks: values at the ends of what a type holds.  Bounds as in test_block_attention.py."""
+"""Attention over listed key blocks: values at the ends of what a type holds, scales of the caller's.  Bounds as in test_block_attention.py."""
 import math
 
 import pytest
 import torch
 
 import test_block_attention as base
-from test_block_attention import HALF, draw
+from test_block_attention import HALF, close, draw, lists
 
 BAD = [math.nan, math.inf, -math.inf]
 
@@ -86,3 +86,49 @@ def test_later_logits_within_the_range_of_the_reference_and_large_values(lemo, H
     ref = base.reference(case, Q, K, V, blocks)
     assert 90 < ref["lse2"].max() < 100
     base.check_forward(O, lse2, ref)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", range(7))
+def test_scales_of_the_caller(lemo, n):
+    case, scale = [
+        (base._c(257, 257, 8, 2, 128, 64, 64, 4), 0.2),                              # 256 rows a list
+        (base._c(300, 300, 4, 2, 128, 32, 48, 4), 0.03),                             # 96
+        (base._c(161, 161, 4, 2, 64, 32, 16, 4, causal=False), 0.25),                # 32
+        (base._c(130, 300, 8, 1, 128, 32, 1, 5, q_start=170), 0.11),                 # lists together
+        (base._c(200, 200, 4, 4, 64, 64, 1, 3), 0.3),
+        (base._c(1, 3000, 8, 2, 128, 64, 1, 16, q_start=2999), 0.17),                # one list, several workgroups
+        (base._c(64, 4000, 4, 2, 128, 64, 64, 30, q_start=3936), 0.05),
+    ][n]
+    print(case, scale, flush=True)
+    S_q, S_k, H, H_kv, d, b, bq = (case[k] for k in ("S_q", "S_k", "H", "H_kv", "d", "b", "bq"))
+    Q, K, V, dO = draw(n + 40, (S_q, H, d), (S_k, H_kv, d), (S_k, H_kv, d), (S_q, H, d))
+    blocks = lists(case, "own", n)
+    flags = lemo.CAUSAL if case["causal"] else 0
+    x = [t.cuda() for t in (Q, K, V, blocks, dO)]
+    O, lse2 = lemo.lemo_block_attention(*x[:4], b, bq, flags, scale, case["q_start"])
+    # the definition takes 1 / sqrt(d): the same logits from queries that are larger by scale sqrt(d), in 64 bits
+    factor = scale * math.sqrt(d)
+    ref = base.reference(case, Q.double() * factor, K, V, blocks, dO, O.cpu())
+    ref["dQ"], ref["dQ_mag"] = ref["dQ"] * factor, ref["dQ_mag"] * factor
+    base.check_forward(O, lse2, ref)
+    base.check_grads(lemo.lemo_block_attention_grad(x[4], *x[:3], O, lse2, x[3], b, bq, flags, scale, case["q_start"]), ref)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,H_kv,d,b,T,S,lengths,scale", [(8, 2, 128, 64, 4, 500, [500, 1, 64, 449, 0], 0.2), (4, 4, 64, 32, 3, 200, [97, 200], 0.02)])
+def test_scales_of_the_caller_single_tokens(lemo, H, H_kv, d, b, T, S, lengths, scale):
+    B = len(lengths)
+    Q, K, V = draw(H + T, (B, H, d), (B, S, H_kv, d), (B, S, H_kv, d))
+    blocks = torch.full((B, H_kv, T), -1, dtype=torch.int32)
+    for s, n in enumerate(lengths):
+        pick = list(range(-(-n // b)))[-T:]
+        blocks[s, :, :len(pick)] = torch.tensor(pick, dtype=torch.int32)
+    O = lemo.lemo_block_attention_step(Q.cuda(), K.cuda(), V.cuda(), torch.tensor(lengths, dtype=torch.int32, device="cuda"), blocks.cuda(), b, scale)
+    for s, n in enumerate(lengths):
+        if n == 0:
+            assert not O[s].any()
+            continue
+        case = base._c(1, n, H, H_kv, d, b, 1, T, q_start=n - 1)
+        ref = base.reference(case, Q[s:s + 1].double() * (scale * math.sqrt(d)), K[s, :n], V[s, :n], blocks[s:s + 1])
+        close("O", O[s:s + 1], ref["O"], HALF * ref["O"].abs() + (1 + HALF) * (HALF + 4 * ref["E"] + 2.0 ** -14)[..., None] * ref["O_mag"])
