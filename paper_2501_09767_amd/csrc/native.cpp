@@ -361,7 +361,7 @@ PyObject* norm_residual(PyObject* const* a) {  // Y R kept gate post next w_post
     }, {N, stats});
 }
 
-PyObject* norm_residual_grad(PyObject* const* a) {  // dN dR R Y kept stats gate post next w_post b_post w_next residual_scale block_scale flags workspace
+PyObject* norm_residual_grad(PyObject* const* a) {  // dN dR R Y kept stats gate post next w_post b_post w_next residual_scale block_scale flags workspace dY dgate weights
     const Place here;
     const at::Tensor &dR = here.at(matrix(a[1])), &R = here.at(matrix(a[2])), &stats = here.at(tensor(a[5], 2));
     const lemo_dtype_t dt = dtype(R);
@@ -372,20 +372,24 @@ PyObject* norm_residual_grad(PyObject* const* a) {  // dN dR R Y kept stats gate
     const int32_t post = whole32(a[7]), next = whole32(a[8]), flags = whole32(a[14]), C = size32(n.C);
     const void *wp = channels(a[9], here, n.C, type), *bp = channels(a[10], here, n.C, type), *wn = channels(a[11], here, n.C, type);
     const float rs = real(a[12]), bs = real(a[13]);
+    need(PyBool_Check(a[18]) && (n.Y || a[16] == Py_None) && (n.gate || n.shared || a[17] == Py_None));
+    const bool p = a[18] == Py_True && post != LEMO_NORM_NONE, q = a[18] == Py_True && next != LEMO_NORM_NONE;
     size_t bytes = 0;
-    need(lemo_norm_residual_grad_workspace_bytes(n.M, C, &bytes) == LEMO_OK);
+    need(!(p || q || n.shared) || lemo_norm_residual_grad_workspace_bytes(n.M, C, &bytes) == LEMO_OK);
     at::Tensor keep;
     const Bytes ws = here.scratch(a[15], bytes, keep);
-    const bool p = post != LEMO_NORM_NONE, q = next != LEMO_NORM_NONE;
-    const at::Tensor dY = here.fresh(n.Y, {n.M, n.C}, type), dgate = here.fresh(n.gate, {n.M, n.C}, type), dgs = here.fresh(n.shared, {n.C}, at::kFloat);
+    const at::Tensor *dy_given = maybe_matrix(a[16], here, n.M, n.C, type), *dg_given = n.shared ? nullptr : maybe_matrix(a[17], here, n.M, n.C, type);
+    const at::Tensor dY = dy_given ? *dy_given : here.fresh(n.Y, {n.M, n.C}, type), dgate = dg_given ? *dg_given : here.fresh(n.gate, {n.M, n.C}, type);
+    const at::Tensor dgs = n.shared ? here.result(a[17], {n.C}, at::kFloat) : at::Tensor();
     const at::Tensor dwp = here.fresh(p, {n.C}, at::kFloat), dbp = here.fresh(p && (bp || post == LEMO_NORM_LAYER), {n.C}, at::kFloat);
     const at::Tensor dwn = here.fresh(q, {n.C}, at::kFloat), dbn = here.fresh(q, {n.C}, at::kFloat);
     const void *y = n.Y ? n.Y->data_ptr() : nullptr, *dn = dN ? dN->data_ptr() : nullptr, *r = R.data_ptr(), *stp = stats.data_ptr();
     void *dr = dR.data_ptr(), *dy = address(dY), *dg = address(dgate), *s0 = address(dwp), *s1 = address(dbp), *s2 = address(dwn), *s3 = address(dbn), *s4 = address(dgs);
     const int64_t ldy = n.Y ? n.Y->stride(0) : n.C, lddn = dN ? dN->stride(0) : n.C, ldr = R.stride(0), lddr = dR.stride(0);
+    const int64_t lddy = dY.defined() ? dY.stride(0) : n.C, lddg = dgate.defined() ? dgate.stride(0) : n.C;
     const int32_t* ki = rows(n.kept);
     return call_for([=] {
-        return lemo_norm_residual_grad(dn, lddn, dr, lddr, n.S, r, ldr, y, ldy, n.gate_at, n.ldg, ki, n.M, wp, bp, post, wn, next, rs, bs, (const float*)stp, dy, n.C, dg, n.C,
+        return lemo_norm_residual_grad(dn, lddn, dr, lddr, n.S, r, ldr, y, ldy, n.gate_at, n.ldg, ki, n.M, wp, bp, post, wn, next, rs, bs, (const float*)stp, dy, lddy, dg, lddg,
                                        (float*)s0, (float*)s1, (float*)s2, (float*)s3, (float*)s4, C, dt, (uint32_t)flags, ws.p, ws.n, here.stream);
     }, {dY, n.shared ? dgs : dgate, dwp, dbp, dwn, dbn});
 }
@@ -538,7 +542,7 @@ PyObject* set_stream_source(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define LEMO_FAST(name, n) {#name, (PyCFunction)(void*)(guarded<n, name>), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LEMO_FAST(score_segments, 9), LEMO_FAST(select_topk, 4), LEMO_FAST(kept_attention, 9), LEMO_FAST(gather_gemm, 6),
                          LEMO_FAST(gather_gemm_add, 7), LEMO_FAST(gather_gemm_dx, 4), LEMO_FAST(gather_gemm_dw, 5), LEMO_FAST(scatter_grad, 4),
-                         LEMO_FAST(norm_residual, 16), LEMO_FAST(norm_residual_grad, 16), LEMO_FAST(block_means, 3), LEMO_FAST(select_blocks, 9),
+                         LEMO_FAST(norm_residual, 16), LEMO_FAST(norm_residual_grad, 19), LEMO_FAST(block_means, 3), LEMO_FAST(select_blocks, 9),
                          LEMO_FAST(block_attention, 12), LEMO_FAST(block_attention_grad, 16), LEMO_FAST(select_blocks_step, 7), LEMO_FAST(block_attention_step, 9),
                          {"set_stream_source", (PyCFunction)(void*)set_stream_source, METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "lemo_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

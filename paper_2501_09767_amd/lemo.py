@@ -715,14 +715,17 @@ def lemo_norm_residual_grad_workspace_bytes(M: int, C: int) -> int:
 def lemo_norm_residual_grad(dN: Optional[torch.Tensor], dR: torch.Tensor, R: torch.Tensor, Y: Optional[torch.Tensor], kept_idx: Optional[torch.Tensor],
                             stats: torch.Tensor, *, gate: Optional[torch.Tensor] = None, post: int = NORM_NONE, next: int = NORM_RMS,
                             w_post: Optional[torch.Tensor] = None, b_post: Optional[torch.Tensor] = None, w_next: Optional[torch.Tensor] = None,
-                            residual_scale: float = 1.0, block_scale: float = 1.0, flags: int = 0, workspace: Optional[torch.Tensor] = None) -> NormGrads:
+                            residual_scale: float = 1.0, block_scale: float = 1.0, flags: int = 0, workspace: Optional[torch.Tensor] = None,
+                            dY: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None, weights: bool = True) -> NormGrads:
     """Gradients of lemo_norm_residual: dR [S,C] (of the new residual rows) becomes that of the old ones in place; returns the others.
-    R, Y, gate, stats as the forward call left or took them."""
-    done = _native.norm_residual_grad(dN, dR, R, Y, kept_idx, stats, gate, post, next, w_post, b_post, w_next, residual_scale, block_scale, flags, workspace)
+    R, Y, gate, stats as the forward call left or took them.  dY may be dN, dgate (of a gate with rows of its own) may be gate; weights=False
+    leaves out the sums for the norms' weights and biases."""
+    done = _native.norm_residual_grad(dN, dR, R, Y, kept_idx, stats, gate, post, next, w_post, b_post, w_next, residual_scale, block_scale, flags, workspace,
+                                      dY, dgate, weights)
     if done is not None:
         _check(done[0], "lemo_norm_residual_grad")
         return NormGrads(*done[1:])
-    _here(dN, dR, R, Y, kept_idx, stats, gate, w_post, b_post, w_next, workspace)
+    _here(dN, dR, R, Y, kept_idx, stats, gate, w_post, b_post, w_next, workspace, dY, dgate)
     M, S, C, ldy, ldg, ldr = _norm_args(Y, R, kept_idx, gate, w_post, b_post, w_next, None)
     if tuple(dR.shape) != (S, C) or dR.dtype != R.dtype or (dR.stride(1) != 1 and C > 1):
         raise ValueError("dR must be [S,C] of the residual's dtype, rows contiguous")
@@ -737,18 +740,21 @@ def lemo_norm_residual_grad(dN: Optional[torch.Tensor], dR: torch.Tensor, R: tor
         return torch.empty(C, dtype=torch.float32, device=R.device) if wanted else None
 
     shared = gate is not None and gate.dim() == 1
-    dY = rows() if Y is not None else None
-    dgate = rows() if gate is not None and not shared else None
-    dgate_sum = sums(shared)
-    dw_post, db_post = sums(post != NORM_NONE), sums(post != NORM_NONE and (b_post is not None or post == NORM_LAYER))
-    dw_next, db_next = sums(next != NORM_NONE), sums(next != NORM_NONE)
-    if workspace is None:
-        workspace = torch.empty(lemo_norm_residual_grad_workspace_bytes(M, C), dtype=torch.uint8, device=R.device)
+    if (dY is not None and Y is None) or (dgate is not None and gate is None):
+        raise ValueError("dY needs Y, dgate needs a gate")
+    if dY is None and Y is not None:
+        dY = rows()
+    dgate_sum = _filled(dgate, (C,), torch.float32, R.device, "dgate") if shared else None
+    dgate = None if shared else rows() if dgate is None and gate is not None else dgate
+    lddy, lddg = _rows_of(dY, M, C, R.dtype, "dY"), _rows_of(dgate, M, C, R.dtype, "dgate")
+    dw_post, db_post = sums(weights and post != NORM_NONE), sums(weights and post != NORM_NONE and (b_post is not None or post == NORM_LAYER))
+    dw_next, db_next = sums(weights and next != NORM_NONE), sums(weights and next != NORM_NONE)
+    needs = dgate_sum is not None or dw_post is not None or dw_next is not None
+    workspace, size = _scratch(workspace, lemo_norm_residual_grad_workspace_bytes(M, C) if needs else 0, R.device)
     _check(_lib.lemo_norm_residual_grad(_ptr(dN), lddn, _ptr(dR), dR.stride(0) if S > 1 else C, S, _ptr(R), ldr, _ptr(Y), ldy, _ptr(gate), ldg,
                                         _ptr(kept_idx), M, _ptr(w_post), _ptr(b_post), int(post), _ptr(w_next), int(next), float(residual_scale),
-                                        float(block_scale), _ptr(stats), _ptr(dY), C, _ptr(dgate), C, _ptr(dw_post), _ptr(db_post), _ptr(dw_next),
-                                        _ptr(db_next), _ptr(dgate_sum), C, _dt(R), int(flags), _ptr(workspace),
-                                        workspace.numel() * workspace.element_size(), _stream()), "lemo_norm_residual_grad")
+                                        float(block_scale), _ptr(stats), _ptr(dY), lddy, _ptr(dgate), lddg, _ptr(dw_post), _ptr(db_post), _ptr(dw_next),
+                                        _ptr(db_next), _ptr(dgate_sum), C, _dt(R), int(flags), _ptr(workspace), size, _stream()), "lemo_norm_residual_grad")
     return NormGrads(dY, dgate_sum if shared else dgate, dw_post, db_post, dw_next, db_next)
 
 
