@@ -12,7 +12,7 @@
 // Memory bound: a row is read once into registers, and all that is known about it follows from there.  Forward: a wave, or a
 // workgroup for long rows and few of them, owns a row; the mean and the squares about it are two sums over registers, so that
 // nothing cancels.  Gradients: a workgroup owns a row at a time and walks the rows in steps of the grid, because the sums over
-// the rows stay in the registers of the thread that owns a column; what the workgroups hold at the end goes through the
+// the rows stay with the thread that owns a column, in registers up to 8192 columns; what the workgroups hold at the end goes through the
 // workspace and is added in their order by a second kernel (no atomics: the same bits on every run).
 #include <algorithm>
 
@@ -396,8 +396,10 @@ int launch_norm_residual(const NormParams& p, lemo_dtype_t dt, hipStream_t st) {
         if (pieces <= 256) return run_norm<T, 256, 1>(p, st);
         if (pieces <= 512) return run_norm<T, 256, 2>(p, st);
         if (pieces <= 1024) return run_norm<T, 256, 4>(p, st);
-        if (pieces <= 2048) return run_norm<T, 512, 4>(p, st);
-        return run_norm<T, 1024, 4>(p, st);
+        if constexpr (Piece<T>::E == 4) {  // (bf16 has no more pieces)
+            if (pieces > 2048) return run_norm<T, 1024, 4>(p, st);
+        }
+        return run_norm<T, 512, 4>(p, st);
     };
     return dt == LEMO_BF16 ? go(bf16_t{}) : go(float{});
 }
@@ -406,7 +408,9 @@ int launch_norm_residual(const NormParams& p, lemo_dtype_t dt, hipStream_t st) {
 // row to write and to read.  bf16 with gate and both norms, us for 256 / 512 / 1024 / 2048 workgroups: 8192 rows of 1024 (a wave each) 117 /
 // 70 / 54 / 47; of 2048 134 / 82 / 64 / -; of 4096 (256 threads) 175 / 130 / 136 / -.  One workgroup for 4, 2 or 1 rows: 512 rows of 4096
 // 25 / 20 / 23.  8192 rows of 4096 without a norm of the block's result (537 MB): 125 us, 4.3 TB/s; what is missing to a copy's rate is
-// the barrier between a row's loads and its stores, with two waves a SIMD to cover it: registers hold the columns' sums.
+// the barrier between a row's loads and its stores, with two waves a SIMD to cover it: registers hold the columns' sums.  Beyond 8192
+// columns they do not: 1024 threads have 128 registers each, and 68 to 280 of what a thread holds goes through scratch in the loop over the
+// rows.  bf16 with gate and both norms, as many bytes each: 8192 rows of 4096 134 us, 4096 of 8192 153, 2048 of 16384 442.
 static int norm_grad_threads(int C) { return C <= 1024 ? 64 : C <= 2048 ? 128 : C <= 4096 ? 256 : C <= 8192 ? 512 : 1024; }
 int norm_grad_parts(int64_t M, int C) {
     const int most = std::max(512, 512 * 256 / norm_grad_threads(C));
@@ -436,7 +440,7 @@ int launch_norm_residual_grad(NormGradParams p, float* dw_next, float* db_next, 
         }
     auto go = [&](auto tag) {
         using T = decltype(tag);
-        constexpr int NP = 16 / Piece<T>::E;  // 16 columns a thread: the sums of each are held in registers
+        constexpr int NP = 16 / Piece<T>::E;  // 16 columns a thread, whose sums it holds
         if (threads == 64) return run_norm_grad<T, 64, NP>(p, parts, st);
         if (threads == 128) return run_norm_grad<T, 128, NP>(p, parts, st);
         if (threads == 256) return run_norm_grad<T, 256, NP>(p, parts, st);
