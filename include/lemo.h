@@ -470,6 +470,7 @@ int lemo_norm_residual_grad(const void* dN, int64_t lddn, void* dR, int64_t lddr
  * not finite in K or V at a key behind a query spoil the query's result only if the key lies in the same 32 keys (counted from its
  * block's start) as one that the query, or one of the 31 rows beside it, sees; in the gradient those in Q, O or dO of a query spoil
  * dK and dV at keys behind it likewise, within the blocks that its list names.  Blocks that a query's list does not name do nothing to it.
+ * Under LEMO_CAUSAL keys behind the last query are not read.
  * Supported: d in {64, 128}; b % 32 == 0, b <= 65536; H % H_kv == 0, H_kv <= 65535; T * b <= 122880; S_q, S_k below 2^31 - 4096; with bq taken
  * as S_q where it is larger, bq * (H / H_kv) < 2^24 and n_qb * H_kv < 2^28 (single tokens: B * H_kv < 2^28); the choice and the gradient:
  * nb <= 16384; means and choice LEMO_F32 and LEMO_BF16, attention LEMO_BF16; the gradient: Q and dO each spanning less than 4 GiB - 4096,

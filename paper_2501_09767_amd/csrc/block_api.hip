@@ -66,7 +66,7 @@ size_t part_bytes(int64_t n_qb, int64_t bq, int64_t S_k, int32_t H, int32_t H_kv
     BlockAttnParams p{};
     static const int one = 0;
     p.lengths = step ? &one : nullptr;  // (not read)
-    p.n_qb = (int)n_qb; p.bq = (int)bq; p.S_k = (int)S_k; p.H_kv = H_kv; p.T = T; p.b = b;
+    p.n_qb = (int)n_qb; p.bq = (int)bq; p.nb = (int)((S_k - 1) / b + 1); p.H_kv = H_kv; p.T = T; p.b = b;
     p.R = (int)(bq * (H / H_kv));
     const int subtiles = block_attention_packed(p), tile = block_attention_tile_rows(p.R, d == 128 && !step);
     const int parts = block_attention_parts((int64_t)p.n_qb * ((p.R + tile - 1) / tile) * H_kv, subtiles);
@@ -92,6 +92,7 @@ int check_attention(const void* Q, const void* K, const void* V, int64_t S_q, in
     p.Q = static_cast<const uint16_t*>(Q); p.K = static_cast<const uint16_t*>(K); p.V = static_cast<const uint16_t*>(V);
     p.blocks = blocks;
     p.S_q = (int)S_q; p.S_k = (int)S_k; p.H = H; p.H_kv = H_kv; p.G = H / H_kv; p.T = T; p.b = b;
+    p.nb = (int)((S_k - 1) / b + 1);
     p.bq = (int)(bq < S_q ? bq : S_q);
     p.n_qb = (int)((S_q + p.bq - 1) / p.bq);
     p.R = p.bq * p.G;
@@ -101,6 +102,9 @@ int check_attention(const void* Q, const void* K, const void* V, int64_t S_q, in
     p.flags = flags;
     return LEMO_OK;
 }
+
+// Keys up to the last query's under the mask: what stands behind them (a cache's room, for instance) is never loaded
+int keys_seen(const BlockAttnParams& p) { return p.flags & LEMO_CAUSAL ? (int)std::min<int64_t>(p.S_k, p.q_start + p.S_q) : p.S_k; }
 
 }  // namespace
 
@@ -167,6 +171,7 @@ int lemo_block_attention(const void* Q, const void* K, const void* V, int64_t S_
     if (need && !workspace) return LEMO_ERR_NULL;
     if (need && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return LEMO_ERR_ALIGN;
     if (workspace_bytes < need) return LEMO_ERR_WORKSPACE;
+    p.S_k = keys_seen(p);
     p.O = static_cast<uint16_t*>(O); p.o_ts = o_tok_stride; p.o_hs = o_head_stride; p.lse2 = lse2;
     p.parts = need ? static_cast<float*>(workspace) : nullptr;
     return hip_rc(launch_block_attention(p, d, static_cast<hipStream_t>(stream)));
@@ -219,7 +224,9 @@ int lemo_block_attention_grad(const void* dO, const void* Q, const void* K, cons
     gp.items = reinterpret_cast<int4*>(ws + l.items);
     gp.totals = reinterpret_cast<int*>(ws + l.totals);
     gp.partial = reinterpret_cast<float*>(ws + l.partial);
-    gp.nb = (int)((S_k + b - 1) / b);
+    gp.nb = p.nb;
+    gp.S_all = p.S_k;
+    p.S_k = keys_seen(p);
     gp.words = (p.n_qb + 31) / 32;
     gp.share = l.share;
     gp.max_items = l.max_items;

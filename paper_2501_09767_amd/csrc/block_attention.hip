@@ -54,13 +54,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void block_attention_kernel(BlockAtt
     if constexpr (PACK) {
         if (tid == 0) not_finite = 0;
         const long long first = (long long)qb * p.pack;
-        const int nb = (p.S_k - 1) / p.b + 1, lists = (int)min((long long)p.pack, p.n_lists - first);
-        room = min(p.pack * p.T, nb) * (p.b / 32);
-        union_subtiles<WAVES>(p.blocks + (first * p.H_kv + g) * p.T, (long long)p.H_kv * p.T, lists, p.T, p.b, nb, limit_of(rows - 1), reinterpret_cast<unsigned*>(smem), keys,
+        const int lists = (int)min((long long)p.pack, p.n_lists - first);
+        room = min(p.pack * p.T, p.nb) * (p.b / 32);
+        union_subtiles<WAVES>(p.blocks + (first * p.H_kv + g) * p.T, (long long)p.H_kv * p.T, lists, p.T, p.b, p.nb, limit_of(rows - 1), reinterpret_cast<unsigned*>(smem), keys,
                               room, &listed, wave, lane);
     } else {
         if (wave == 0) {
-            const int n = rt * ROWS < rows ? list_subtiles(p.blocks + ((long long)qb * p.H_kv + g) * p.T, p.T, p.b, (p.S_k - 1) / p.b + 1, limit_of(row_end - 1), keys, lane) : 0;
+            const int n = rt * ROWS < rows ? list_subtiles(p.blocks + ((long long)qb * p.H_kv + g) * p.T, p.T, p.b, p.nb, limit_of(row_end - 1), keys, lane) : 0;
             if (lane == 0) listed = n;
         }
         __syncthreads();
@@ -312,7 +312,7 @@ static int block_attention_pack(int R, int T, int b, long long nb, long long lis
 
 // Makes the lists that are worked on together one query block; returns the subtiles that its list may have.
 int block_attention_packed(BlockAttnParams& p) {
-    const int nb = (p.S_k - 1) / p.b + 1;
+    const int nb = p.nb;
     p.n_lists = p.n_qb;
     p.pack = p.lengths ? 1 : block_attention_pack(p.R, p.T, p.b, nb, p.n_qb);
     if (p.pack == 1) return p.T * (p.b / 32);

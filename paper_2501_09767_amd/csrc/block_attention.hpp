@@ -13,7 +13,8 @@ struct BlockAttnParams {
     const int* blocks;   // [n_qb, H_kv, T]
     const int* lengths;  // single tokens: [n_qb] keys of every sequence, or null
     float* parts;        // where a list is shared by several workgroups: their results, see PART_ROW
-    int S_q, S_k, H, H_kv, G, T, b, bq, n_qb;
+    int S_q, S_k, H, H_kv, G, T, b, bq, n_qb;  // S_k: keys that any query may see; under the mask none behind the last query is touched
+    int nb;                // key blocks, of all keys
     int R, n_rt, n_parts;  // rows of a query block, tiles of them, shares of a list
     int first;             // workgroup of the launch's first one
     int pack, n_lists;     // lists that are worked on together (bq, n_qb, R then count `pack` blocks as one), and all there are
@@ -40,6 +41,7 @@ struct BlockGradParams {
     int* totals;         // [0]: items
     float* partial;      // [slot][2][b][d]
     int nb, words, share;  // share: query blocks that a workgroup takes of a list
+    int S_all;             // keys that have a gradient
     int max_items;
 };
 

@@ -371,7 +371,7 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
     for (int c = 0; c < Tile::CHUNKS; ++c) kf[c] = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
     for (int c = 0; c < V_HELD; ++c) vf[c] = u32x4{0u, 0u, 0u, 0u};
-    if (key0 + l32 < p.S_k) {
+    if (key0 + l32 < p.S_k) {  // (what no query sees are zeros, whatever it holds)
         const char* const k = reinterpret_cast<const char*>(p.K + (key0 + l32) * p.k_ts + g * p.k_hs);
         const char* const v = reinterpret_cast<const char*>(p.V + (key0 + l32) * p.v_ts + g * p.v_hs);
 #pragma unroll
@@ -588,7 +588,7 @@ __global__ __launch_bounds__(KW * SHARES * 64, 2) void block_dkv_kernel(BlockGra
                 float* part = gp.partial + (((long long)slot * 2 + which) * p.b + (j - n * p.b)) * D + c0;
                 *reinterpret_cast<f32x4*>(part) = f32x4{v[0], v[1], v[2], v[3]};
                 *reinterpret_cast<f32x4*>(part + 4) = f32x4{v[4], v[5], v[6], v[7]};
-            } else if (j < p.S_k) {
+            } else if (j < gp.S_all) {
                 u32x4 piece;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) piece[e] = pack_bf16x2_hw(v[2 * e], v[2 * e + 1]);
@@ -607,7 +607,7 @@ template <int D> __global__ __launch_bounds__(256) void block_dkv_join_kernel(Bl
     constexpr int LPR = D / 8;
     for (int u = blockIdx.y * 256 + threadIdx.x; u < 2 * p.b * LPR; u += gridDim.y * 256) {
         const int which = u / (p.b * LPR), j = u / LPR % p.b, c0 = u % LPR * 8, key = n * p.b + j;
-        if (key >= p.S_k) continue;
+        if (key >= gp.S_all) continue;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         for (int w = 0; w < parts; ++w) {
             const float* part = gp.partial + (((long long)(slot + w) * 2 + which) * p.b + j) * D + c0;

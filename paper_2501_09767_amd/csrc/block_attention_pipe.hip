@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256, 1) void block_attention_pipe_kernel(BlockAttnP
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool causal = (p.flags & LEMO_CAUSAL) != 0;
-    const int S = p.S_k, nb = (p.S_k - 1) / p.b + 1;
+    const int S = p.S_k, nb = p.nb;
     auto list_at = [&](int buf) { return reinterpret_cast<int*>(smem + 2 * BP_STAGE) + buf * (4 + room) + 4; };  // [-4]: how many
 
     // ---- a tile of rows and its list

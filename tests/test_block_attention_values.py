@@ -132,3 +132,35 @@ def test_scales_of_the_caller_single_tokens(lemo, H, H_kv, d, b, T, S, lengths, 
         case = base._c(1, n, H, H_kv, d, b, 1, T, q_start=n - 1)
         ref = base.reference(case, Q[s:s + 1].double() * (scale * math.sqrt(d)), K[s, :n], V[s, :n], blocks[s:s + 1])
         close("O", O[s:s + 1], ref["O"], HALF * ref["O"].abs() + (1 + HALF) * (HALF + 4 * ref["E"] + 2.0 ** -14)[..., None] * ref["O_mag"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", range(8))
+def test_what_lies_behind_the_last_query(lemo, n):
+    """A part of a prompt over a cache that has room for more: what stands there is nobody's key yet, NaN among it."""
+    case = [
+        base._c(70, 300, 8, 2, 128, 64, 64, 4, q_start=100),      # 256 rows a list
+        base._c(300, 500, 80, 20, 128, 32, 48, 6, q_start=23),    # and more tiles than there are workgroups
+        base._c(90, 200, 4, 2, 128, 32, 48, 4, q_start=37),       # 96 rows
+        base._c(45, 128, 4, 2, 64, 32, 16, 3, q_start=40),        # 32
+        base._c(77, 140, 8, 1, 128, 32, 1, 4, q_start=20),        # lists together
+        base._c(50, 90, 4, 4, 64, 64, 1, 2, q_start=0),
+        base._c(1, 3000, 8, 2, 128, 64, 1, 16, q_start=1999),     # one list, several workgroups
+        base._c(130, 333, 6, 2, 128, 128, 5, 2, q_start=66),
+    ][n]
+    print(case, flush=True)
+    S_q, S_k, H, H_kv, d, b, bq = (case[k] for k in ("S_q", "S_k", "H", "H_kv", "d", "b", "bq"))
+    Q, K, V, dO = draw(n + 60, (S_q, H, d), (S_k, H_kv, d), (S_k, H_kv, d), (S_q, H, d))
+    blocks = lists(case, "own", n)
+    blocks[0, :, -1] = (S_k - 1) // b  # (a list that names blocks behind its queries as well)
+    end = case["q_start"] + S_q
+    K2, V2 = K.clone(), V.clone()
+    for x in (K2, V2):
+        x[end:] = torch.tensor(BAD)[torch.arange(S_k - end) % 3][:, None, None].to(torch.bfloat16)
+    x = [t.cuda() for t in (Q, K2, V2, blocks, dO)]
+    O, lse2 = lemo.lemo_block_attention(*x[:4], b, bq, q_start=case["q_start"])
+    ref = base.reference(case, Q, K, V, blocks, dO, O.cpu())
+    base.check_forward(O, lse2, ref)
+    grads = lemo.lemo_block_attention_grad(x[4], *x[:3], O, lse2, x[3], b, bq, q_start=case["q_start"])
+    base.check_grads(grads, ref)
+    assert not grads[1][end:].any() and not grads[2][end:].any()
