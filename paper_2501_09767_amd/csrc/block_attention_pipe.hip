@@ -26,7 +26,7 @@ __device__ __forceinline__ void bp_pin(float& x) { asm volatile("" : "+v"(x)); }
 
 __global__ __launch_bounds__(256, 1) void block_attention_pipe_kernel(BlockAttnParams p, int tiles, int room) {
     using Tile = HeadTile<128>;
-    constexpr int NCH = 8, SHARE = 4, sub0 = 0;
+    constexpr int NCH = 8, SUBS = 4;  // chunks of a head row, subtiles of a stage
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256, 1) void block_attention_pipe_kernel(BlockAttnP
         stage_load((par + t + 1) & 1);  // (descriptors of size zero where no stage follows)
         if (active) {
 #pragma unroll 1
-            for (int ks = sub0; ks < sub0 + SHARE; ++ks) {
+            for (int ks = 0; ks < SUBS; ++ks) {
                 if (stage_begin(s_now, t) + ks >= stage_end(s_now, t)) break;
                 const int key = __builtin_amdgcn_readfirstlane(s_now.keys[stage_begin(s_now, t) + ks]);
                 if (key > reach[0] && key > reach[1]) break;
@@ -295,14 +295,14 @@ __global__ __launch_bounds__(256, 1) void block_attention_pipe_kernel(BlockAttnP
         const char* const st = smem + ((par + t) & 1) * BP_STAGE;
         const int nbuf = (par + t + 1) & 1;
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) kf[c] = k_frag(st, sub0, c);
+        for (int c = 0; c < NCH; ++c) kf[c] = k_frag(st, 0, c);
         auto ride = [&](int n) { stage_load_one(n, nbuf); };  // (no next stage: descriptors of size zero)
         auto no_ride = [&](int) {};
-        group(OddT{}, st, sub0, false, ride);
+        group(OddT{}, st, 0, false, ride);
 #pragma unroll
-        for (int ks = 0; ks < SHARE; ++ks) {
-            group(EvenT{}, st, sub0 + ks, ks < SHARE - 1, no_ride);
-            if (ks < SHARE - 1) group(OddT{}, st, sub0 + ks, false, no_ride);
+        for (int ks = 0; ks < SUBS; ++ks) {
+            group(EvenT{}, st, ks, ks < SUBS - 1, no_ride);
+            if (ks < SUBS - 1) group(OddT{}, st, ks, false, no_ride);
         }
         settle_stage();
         take_next(t + 2);
