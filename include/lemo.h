@@ -398,7 +398,7 @@ int lemo_scatter_grad(const void* G, int64_t ldg, const int32_t* kept_idx, int64
  *   gate [M, C] row stride ld_gate, or with ld_gate 0 one row [C] for all, or NULL for ones.  g is the gate's value, with
  *     LEMO_GATE_SIGMOID its logistic function.
  *   R [S, C] row stride ldr, read and written at the rows kept_idx names (NULL: rows 0..M-1).  Each row at most once (not
- *     checked); other rows are not touched.  A value outside [0, S) drops the row: its N and stats are zeros.
+ *     checked), M <= S; other rows are not touched.  A value outside [0, S) drops the row: its N and stats are zeros.
  *   N [M, C] row stride ldn.  The second norm is that of the row as it is stored, so that this call and a call with Y = NULL
  *     behind it give the same bits.
  *   stats [M, 4] float, 16-byte aligned, or NULL: mean and 1 / deviation of post, then of next (0 where a norm is NONE; the mean
@@ -440,8 +440,8 @@ int lemo_norm_residual_grad(const void* dN, int64_t lddn, void* dR, int64_t lddr
  *   lemo_select_blocks   s[m, g, n] = sum over the queries i of block m and the heads h of g of <Q[i, h], means[n, g]>;
  *                        blocks[m, g, :] = the T blocks of highest s, ties to the LOWER index (-0.0 ties +0.0), in ascending
  *                        order, -1 behind them.  LEMO_CAUSAL: blocks that begin behind the last query of m are left out, and those that
- *                        hold a position of a query of m are always listed (LEMO_ERR_SHAPE if T has no room for them; their means
- *                        are not read).  Sums and comparisons in 64 bits.  Scores that are not numbers give lists that are
+ *                        hold a position of a query of m are always listed (LEMO_ERR_SHAPE if T has no room for them), whatever
+ *                        their means hold.  Sums and comparisons in 64 bits.  Scores that are not numbers give lists that are
  *                        unspecified but in range.
  *   lemo_block_attention O[i, h, :] = sum_j softmax_j( scale * <Q[i, h], K[j, g]> ) V[j, g, :] over the keys j of the blocks that
  *                        i's list names (LEMO_CAUSAL: j <= q_start + i).  An entry of a list counts if it lies in [0, nb) and
@@ -454,7 +454,8 @@ int lemo_norm_residual_grad(const void* dN, int64_t lddn, void* dR, int64_t lddr
  *   of a query's exponentials, or NULL (forward).  dQ [S_q,H,d], dK and dV [S_k,H_kv,d] contiguous, written in full: keys that no
  *   list names get zeros.
  *   workspace: lemo_block_attention_workspace_bytes() (may be 0: then NULL will do), lemo_block_attention_grad_workspace_bytes()
- *   bytes, 256-byte aligned.
+ *   bytes, 256-byte aligned.  The gradient's holds, among others, a bit for every query block, key block and key head: 2.1 GB where each
+ *   of 131072 queries has a list of its own for 32 key heads, blocks of 32.
  *
  * Single tokens of a batch of B sequences, each with its keys and values in a cache of S_max tokens (sequence stride, 64-bit) and its
  * length on the device: the newest token, position lengths[s] - 1, attends its list.  Lengths outside [0, S_max] are taken as the
@@ -469,7 +470,7 @@ int lemo_norm_residual_grad(const void* dN, int64_t lddn, void* dR, int64_t lddr
  * dK and dV sum over the heads of a group before they are rounded.  No atomics on results: the same bits on every run.  Values that are
  * not finite in K or V at a key behind a query spoil the query's result only if the key lies in the same 32 keys (counted from its
  * block's start) as one that the query, or one of the 31 rows beside it, sees; in the gradient those in Q, O or dO of a query spoil
- * dK and dV at keys behind it likewise, within the blocks that its list names.  Blocks that a query's list does not name do nothing to it.
+ * dK and dV at keys behind it likewise, within the blocks that its list names, and those in V at a key spoil the key's dK.  Blocks that a query's list does not name do nothing to it.
  * Under LEMO_CAUSAL keys behind the last query are not read.
  * Supported: d in {64, 128}; b % 32 == 0, b <= 65536; H % H_kv == 0, H_kv <= 65535; T * b <= 122880; S_q, S_k below 2^31 - 4096; with bq taken
  * as S_q where it is larger, bq * (H / H_kv) < 2^24 and n_qb * H_kv < 2^28 (single tokens: B * H_kv < 2^28); the choice and the gradient:

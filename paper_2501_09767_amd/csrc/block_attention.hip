@@ -302,7 +302,7 @@ int block_attention_tile_rows(int R, bool walk) { return R > 128 && walk ? 256 :
 
 // Lists of few rows together, as many as fill 32 rows; the union of what they name has to fit the workgroup's memory.  us one by one /
 // together, a list for every query: 1000 queries, 16 / 4 heads of 64, 8 blocks of 32 52.5 / 17.2 (gradients 87 / 53); 3001, 16 of 64, 12
-// blocks 697 / 83 (794 / 163); 8192, 32 / 8 of 128, 16 blocks of 64 2672 / 1174 (4484 / 1974).
+// blocks 697 / 85 (794 / 165); 8192, 32 / 8 of 128, 16 blocks of 64 2672 / 1167 (4484 / 2024).
 static int block_attention_pack(int R, int T, int b, long long nb, long long lists) {
     int pack = R >= 32 ? 1 : 32 / R;
     if (nb > 16384) return 1;

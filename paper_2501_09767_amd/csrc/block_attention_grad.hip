@@ -9,13 +9,13 @@
 // of at most `share` query blocks, since a popular block may be on every list.  The parts of a block that was cut are added in
 // order.  Each pass forms its logits and probabilities again: 7 products for the 5 of the definition, which costs less than writing and
 // reading dS (2 bytes a pair) would.
-// delta comes from O as it is stored and dS goes to the products as bf16: each moves dQ and dK by up to 2^-9 of what they sum up;
-// P, dS and delta are formed in binary32, and so are all sums.
-// 8192 tokens, 32 heads of 128, 16 blocks of 64 for 64 queries: 670 us (dQ 39 %, the lists 4 %, dK and dV 57 %), 470 TFLOP/s of the
-// definition's 5 products, 650 of the 7.  With eight waves on the same 64 keys and one workgroup a CU it was 725: a stage of 128 rows of the
-// second pass took 5250 cycles, of which LDS was read for 2200 and written for 500, a matrix core worked for 2050 and loads and
-// barriers were waited for in 50 and 300, and the begin and the end of items took 28 % of the pass.  What the waves of a stage do they do
-// at the same time; fragments 3 or 4 steps ahead or precedence for waves in their products change nothing by more than 1 %.
+// delta comes from O as the forward call left it, rounded to bf16 (the gradient of the results that there are: O and lse2), and dS goes to
+// the products as bf16: a value of either is off by at most 2^-8 of it.  P, dS and delta are formed in binary32, and so are all sums.
+// 8192 tokens, 32 heads of 128, 16 blocks of 64 for 64 queries: 680 us (dQ 40 %, the lists 3 %, dK and dV 57 %), 460 TFLOP/s of the
+// definition's 5 products, 640 of the 7; matrix cores are busy for 28 % of the first pass' cycles and 27 % of the second's, vector
+// arithmetic for 36 and 37 %, LDS is read in 17 and 27 %.  None of them bounds the passes: between two barriers a wave has one subtile of 32 rows
+// or keys, whose logits, exponentials and products wait for each other, and two waves a SIMD cover it in part.  Eight waves on the same 64
+// keys and one workgroup a CU: 725 us; fragments 3 or 4 steps ahead or precedence for waves in their products: within 1 %.
 #include "block_attention.hpp"
 
 namespace lemo {
