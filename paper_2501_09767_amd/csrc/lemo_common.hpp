@@ -171,6 +171,7 @@ inline bool spans_meet(const void* a, long long a_bytes, const void* b, long lon
 }
 
 // ---- host: a launch holds fewer than 2^32 threads ---------------------------------------------------
+// (beyond, the number of workgroups is taken modulo 2^32 threads, and no error is returned).
 // `launch(first, count)` for workgroups [first, first + count) of as many as there are: half of what a launch holds at a time, so a
 // multiple of the dies.
 template <typename F> int launch_in_turns(long long workgroups, int threads, F&& launch) {

@@ -38,8 +38,9 @@ template <> struct Vec8<float> {
 template <typename TG, typename TX, bool ZERO_PAD>
 __global__ __launch_bounds__(SCAT_THREADS) void scatter_rows_kernel(const TG* __restrict__ G, long long ldg,
                                                                     const int* __restrict__ idx, long long M,
-                                                                    TX* __restrict__ dX, long long lddx, long long S, int C) {
-    const long long m = blockIdx.x;  // ACCUMULATE: grid = M;  ZERO_PAD: grid = M + 1 (the extra one clears the tail)
+                                                                    TX* __restrict__ dX, long long lddx, long long S, int C,
+                                                                    long long first) {
+    const long long m = first + blockIdx.x;  // ACCUMULATE: grid = M;  ZERO_PAD: grid = M + 1 (the extra one clears the tail)
     const int nvec = C >> 3;
     if (ZERO_PAD) {
         const long long lo = m == 0 ? 0 : (long long)idx[m - 1] + 1;
@@ -70,13 +71,15 @@ __global__ __launch_bounds__(SCAT_THREADS) void scatter_rows_kernel(const TG* __
 template <typename TG, typename TX>
 static int launch_scatter_t(const void* G, long long ldg, const int* idx, long long M, void* dX, long long lddx, long long S,
                             int C, int mode, hipStream_t st) {
-    if (mode == LEMO_SCATTER_ZERO_PAD)
-        hipLaunchKernelGGL((scatter_rows_kernel<TG, TX, true>), dim3((unsigned)(M + 1)), dim3(SCAT_THREADS), 0, st,
-                           static_cast<const TG*>(G), ldg, idx, M, static_cast<TX*>(dX), lddx, S, C);
-    else if (M > 0)
-        hipLaunchKernelGGL((scatter_rows_kernel<TG, TX, false>), dim3((unsigned)M), dim3(SCAT_THREADS), 0, st,
-                           static_cast<const TG*>(G), ldg, idx, M, static_cast<TX*>(dX), lddx, S, C);
-    return (int)hipGetLastError();
+    const bool pad = mode == LEMO_SCATTER_ZERO_PAD;
+    return launch_in_turns(pad ? M + 1 : M, SCAT_THREADS, [&](long long first, unsigned count) {
+        if (pad)
+            hipLaunchKernelGGL((scatter_rows_kernel<TG, TX, true>), dim3(count), dim3(SCAT_THREADS), 0, st,
+                               static_cast<const TG*>(G), ldg, idx, M, static_cast<TX*>(dX), lddx, S, C, first);
+        else
+            hipLaunchKernelGGL((scatter_rows_kernel<TG, TX, false>), dim3(count), dim3(SCAT_THREADS), 0, st,
+                               static_cast<const TG*>(G), ldg, idx, M, static_cast<TX*>(dX), lddx, S, C, first);
+    });
 }
 
 int launch_scatter(const void* G, long long ldg, const int* idx, long long M, void* dX, long long lddx, long long S, int C,

@@ -164,9 +164,9 @@ __device__ __forceinline__ int segment_keep(int len, int L, int k) {
 // 3.6, 4.6 / 4.6; 256 4.0 / 4.0, 4.9 / 4.9)
 template <int T>
 __global__ __launch_bounds__(T) void select_topk_kernel(const float* __restrict__ scores, int S, int L, int k,
-                                                                  int* __restrict__ kept) {
+                                                                  int* __restrict__ kept, int first) {
     extern __shared__ uint32_t keys[];  // [len]
-    const int seg = blockIdx.x, tid = threadIdx.x;
+    const int seg = first + blockIdx.x, tid = threadIdx.x;
     const int start = seg * L;  // host guarantees start < S and no overflow
     const int len = min(L, S - start);
     __shared__ __attribute__((aligned(16))) SelectLds<T> lds;
@@ -189,9 +189,9 @@ __global__ __launch_bounds__(T) void select_topk_kernel(const float* __restrict_
 constexpr int FUSED_THREADS = 1024;
 __global__ __launch_bounds__(FUSED_THREADS) void head_mean_select_kernel(const float* __restrict__ colsum, const float* __restrict__ diag,
                                                                          int S, int H, int exclude_self, int L, int k,
-                                                                         float* __restrict__ scores, int* __restrict__ kept) {
+                                                                         float* __restrict__ scores, int* __restrict__ kept, int first) {
     extern __shared__ uint32_t keys[];  // [len]
-    const int seg = blockIdx.x, tid = threadIdx.x;
+    const int seg = first + blockIdx.x, tid = threadIdx.x;
     const int start = seg * L;
     const int len = min(L, S - start);
     __shared__ __attribute__((aligned(16))) SelectLds<FUSED_THREADS> lds;
@@ -322,9 +322,10 @@ int launch_head_mean_select(const float* colsum, const float* diag, int S, int H
         attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&head_mean_select_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 32768 * 4);
     });
     if (attr_err != hipSuccess) return (int)attr_err;
-    hipLaunchKernelGGL(head_mean_select_kernel, dim3(nseg), dim3(FUSED_THREADS), (size_t)Leff * sizeof(uint32_t), st, colsum, diag, S, H,
-                       exclude_self, L, k, scores, kept);
-    return (int)hipGetLastError();
+    return launch_in_turns(nseg, FUSED_THREADS, [&](long long first, unsigned count) {
+        hipLaunchKernelGGL(head_mean_select_kernel, dim3(count), dim3(FUSED_THREADS), (size_t)Leff * sizeof(uint32_t), st, colsum, diag, S, H,
+                           exclude_self, L, k, scores, kept, (int)first);
+    });
 }
 
 int launch_select(const float* scores, int S, int L, int k, int* kept, hipStream_t st) {
@@ -337,10 +338,11 @@ int launch_select(const float* scores, int S, int L, int k, int* kept, hipStream
     });
     if (attr_err != 0) return attr_err;
     const size_t lds = (size_t)Leff * sizeof(uint32_t);
-    if (Leff <= 128) hipLaunchKernelGGL(select_topk_kernel<256>, dim3(nseg), dim3(256), lds, st, scores, S, L, k, kept);
-    else if (Leff <= 2048) hipLaunchKernelGGL(select_topk_kernel<512>, dim3(nseg), dim3(512), lds, st, scores, S, L, k, kept);
-    else hipLaunchKernelGGL(select_topk_kernel<1024>, dim3(nseg), dim3(1024), lds, st, scores, S, L, k, kept);
-    return (int)hipGetLastError();
+    return launch_in_turns(nseg, Leff <= 128 ? 256 : Leff <= 2048 ? 512 : 1024, [&](long long first, unsigned count) {
+        if (Leff <= 128) hipLaunchKernelGGL(select_topk_kernel<256>, dim3(count), dim3(256), lds, st, scores, S, L, k, kept, (int)first);
+        else if (Leff <= 2048) hipLaunchKernelGGL(select_topk_kernel<512>, dim3(count), dim3(512), lds, st, scores, S, L, k, kept, (int)first);
+        else hipLaunchKernelGGL(select_topk_kernel<1024>, dim3(count), dim3(1024), lds, st, scores, S, L, k, kept, (int)first);
+    });
 }
 
 }  // namespace lemo

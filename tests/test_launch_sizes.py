@@ -1,4 +1,4 @@
-"""Calls that need more threads than a launch holds, 2^32: rows and lists are taken in turns.  What comes out is compared with calls on a few
+"""Calls that need more threads than a launch holds, 2^32 (what is beyond is left out without an error): rows and lists are taken in turns.  What comes out is compared with calls on a few
 rows or sequences at both ends and around the places where a turn may end."""
 import pytest
 import torch
@@ -67,6 +67,41 @@ def test_means_of_more_than_2_24_blocks(lemo):
     assert means.shape[0] == 2 ** 24 + 3
     for a, z in ranges(2 ** 24 + 3, (2 ** 22, 2 ** 23, 2 ** 24)):
         assert torch.equal(means[a:z], lemo.lemo_block_means(K[a * b:min(z * b, S)], b)), a
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mode", [0, 1])
+def test_scatter_of_more_than_2_24_rows(lemo, mode):
+    M, C = 2 ** 24 + 41, 8
+    S = M + 1000
+    g = torch.Generator(device="cuda").manual_seed(4)
+    G, dX = (torch.randn(n, C, generator=g, device="cuda", dtype=torch.bfloat16) for n in (M, S))
+    idx = torch.randperm(S, generator=g, device="cuda")[:M].sort().values.int()
+    want = dX.float() if mode == 0 else torch.zeros(S, C, device="cuda")
+    want[idx.long()] += G.float()
+    lemo.lemo_scatter_grad(G, idx, dX, mode)
+    assert torch.equal(dX, want.bfloat16())
+
+
+@pytest.mark.gpu
+def test_choice_from_more_segments_than_a_launch_holds_workgroups(lemo):
+    """Segments of two tokens, one of them kept: 256 threads a segment, 1024 where the mean over the heads is taken as well."""
+    for n in (2 ** 24 + 5, 2 ** 22 + 5):
+        S = 2 * n
+        scores = torch.randn(S, generator=torch.Generator(device="cuda").manual_seed(n), device="cuda")
+        pairs = scores.view(n, 2)
+        want = (pairs[:, 1] > pairs[:, 0]).int() + torch.arange(n, device="cuda", dtype=torch.int32) * 2
+        assert torch.equal(lemo.lemo_select_topk(scores, 2, 1), want)
+    got, kept = lemo.lemo_head_mean_select_topk(scores.view(1, S), torch.zeros(1, S, device="cuda"), 2, 1)
+    assert torch.equal(got, scores) and torch.equal(kept, want)
+
+
+@pytest.mark.gpu
+def test_weight_gradient_of_no_rows_and_2_24_outputs(lemo):
+    N, C = 2 ** 24 + 4, 4
+    dW = torch.ones(N, C, device="cuda")
+    empty = torch.empty(0, N, device="cuda"), torch.empty(5, C, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    lemo.lemo_gather_gemm_dw(*empty, dW=dW)
+    assert not dW.any()
 
 
 def test_more_key_heads_than_a_launch_has_rows_of_workgroups():
