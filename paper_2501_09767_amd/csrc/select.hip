@@ -315,7 +315,7 @@ int launch_empty(hipStream_t st) {
 int launch_head_mean_select(const float* colsum, const float* diag, int S, int H, int exclude_self, int L, int k, float* scores, int* kept,
                             hipStream_t st) {
     const int Leff = L < S ? L : S;
-    const int nseg = (S + L - 1) / L;
+    const int nseg = (S - 1) / L + 1;
     static std::once_flag once;
     static hipError_t attr_err = hipSuccess;
     std::call_once(once, [] {  // a 32768-token segment needs 128 KB of dynamic LDS
@@ -330,7 +330,7 @@ int launch_head_mean_select(const float* colsum, const float* diag, int S, int H
 
 int launch_select(const float* scores, int S, int L, int k, int* kept, hipStream_t st) {
     const int Leff = L < S ? L : S;
-    const int nseg = (S + L - 1) / L;  // L <= 32768 here (keys of one segment live in LDS), no overflow
+    const int nseg = (S - 1) / L + 1;
     static std::once_flag once;
     static int attr_err = 0;
     std::call_once(once, [] {  // a 32768-token segment needs 128 KB of dynamic LDS

@@ -96,6 +96,20 @@ def test_choice_from_more_segments_than_a_launch_holds_workgroups(lemo):
 
 
 @pytest.mark.gpu
+def test_choice_from_nearly_2_31_scores(lemo):
+    """The last segment ends where 32-bit sums of a length and a segment do not."""
+    S, L, k = 2 ** 31 - 1, 32768, 16
+    scores = torch.zeros(S, device="cuda")
+    n = 2 ** 16
+    mark = torch.arange(n, device="cuda") * L + torch.arange(n, device="cuda") % 16384
+    scores[mark] = 1.0
+    kept = lemo.lemo_select_topk(scores, L, k)
+    want = torch.arange(n, device="cuda")[:, None] * L + torch.arange(k, device="cuda")  # the first of equal scores, but for the marked one
+    want[:, -1] = torch.where(mark % L >= k, mark, want[:, -1])
+    assert kept.numel() == n * k and torch.equal(kept.view(n, k).long(), want)
+
+
+@pytest.mark.gpu
 def test_weight_gradient_of_no_rows_and_2_24_outputs(lemo):
     N, C = 2 ** 24 + 4, 4
     dW = torch.ones(N, C, device="cuda")
