@@ -34,9 +34,9 @@ PEAK_HBM_GBS = 8000.0       # MI355X HBM3E, published
 # The figures belong to the kernel sources they were measured on: "sources" is sources_digest() at that time, and the
 # bench reports traffic as null when the sources have changed since.
 MEASURED_TRAFFIC_BYTES = {
-    "sources": "c23ef904361759c6",
-    "C5:rowstats": 2533914837, "C5:colsum": 2675785771, "C5:head_mean_select": 8635051,
-    "C5:gather_gemm": 1687251883, "C5:scatter": 242886059,
+    "sources": "27cec1cbc9c1582b",
+    "C5:rowstats": 2549091643, "C5:colsum": 2679616646, "C5:head_mean_select": 8650907,
+    "C5:gather_gemm": 1687178573, "C5:scatter": 242879169,
 }
 
 

@@ -12,8 +12,8 @@
 // delta comes from O as the forward call left it, rounded to bf16 (the gradient of the results that there are: O and lse2), and dS goes to
 // the products as bf16: a value of either is off by at most 2^-8 of it.  P, dS and delta are formed in binary32, and so are all sums.
 // 8192 tokens, 32 heads of 128, 16 blocks of 64 for 64 queries: 680 us (dQ 40 %, the lists 3 %, dK and dV 57 %), 460 TFLOP/s of the
-// definition's 5 products, 640 of the 7; matrix cores are busy for 28 % of the first pass' cycles and 27 % of the second's, vector
-// arithmetic for 36 and 37 %, LDS is read in 17 and 27 %.  None of them bounds the passes: between two barriers a wave has one subtile of 32 rows
+// definition's 5 products, 640 of the 7; matrix cores are busy for 28 % of the first pass' cycles and 27 % of the second's, instructions
+// go to them or the vector unit in 36 and 37 %, LDS is read in 17 and 27 %.  None of them bounds the passes: between two barriers a wave has one subtile of 32 rows
 // or keys, whose logits, exponentials and products wait for each other, and two waves a SIMD cover it in part.  Eight waves on the same 64
 // keys and one workgroup a CU: 725 us; fragments 3 or 4 steps ahead or precedence for waves in their products: within 1 %.
 #include "block_attention.hpp"
