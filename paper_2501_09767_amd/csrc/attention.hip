@@ -722,6 +722,16 @@ __global__ __launch_bounds__(AP_THREADS, 1) void kept_attention_pipe_kernel(Attn
         o_ref[qs] = mrun[qs];
         bad |= !(ltot[qs] < AP_FROZEN_LIMIT);
     }
+    if (t_hot > 1) {  // probabilities up to the limit, times large values, may have passed binary32 where the ordinary softmax does not
+        float zero = 0.f;
+#pragma unroll
+        for (int qs = 0; qs < 2; ++qs)
+#pragma unroll
+            for (int dv = 0; dv < 4; ++dv)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) zero = fmaf(o[qs][dv][r], 0.f, zero);
+        bad |= zero != 0.f;
+    }
     if (!frozen || !__syncthreads_or(bad)) break;
     frozen = false;
     }
