@@ -504,6 +504,81 @@ int lemo_block_attention_step(const void* Q, const void* K, const void* V, int32
                               int32_t b, float scale, void* O, int64_t o_tok_stride, int64_t o_head_stride, void* workspace, size_t workspace_bytes,
                               void* stream);
 
+/*
+ * What a layer has before the scoring: the norm of every head of the queries and keys, and their rotation by the tokens' positions
+ * (the Q and K that Sec. 4.2 scores), in one pass:
+ *
+ *     u = norm(x)   (over the d channels of a head; LEMO_NORM_NONE, _RMS, _LAYER as in lemo_norm_residual, with a weight and no bias)
+ *     of u's first rot channels every pair (a, b), n < rot / 2:   (a cos t - b sin t, b cos t + a sin t) * amplitude,  t = position * inv_freq[n]
+ *
+ *   Pairs are channels (n, n + rot / 2), or with LEMO_ROTATE_PAIRS (2 n, 2 n + 1).  Channels from rot on are not turned.
+ *   Q [M,H,d], K [M,H_kv,d]: element strides (token, head), d contiguous, 16-byte rule: also slices of a fused projection.  H or H_kv may be 0:
+ *     then its pointers are not looked at.  Q_out, K_out: the results, likewise; either may be its operand (same base and strides).
+ *   positions [M] int32 or NULL for 0 ... M-1; pos_start is added.  Rows of kept tokens: positions = kept_idx.
+ *   inv_freq [rot / 2] float, at any multiple of 4 bytes, device memory; the angle is formed in 64 bits, so that far positions are as exact as
+ *     near ones.  amplitude multiplies cos and sin (1: none; what some extensions of the context use).
+ *   w_q [d], w_k [d] of dtype dt, shared by the heads, or with LEMO_WEIGHTS_PER_HEAD [H,d], [H_kv,d]; NULL for ones.  Not read with NONE.
+ *
+ * lemo_qk_rotate_grad: dQ, dK of the operands from those of the results.  Q, K: the operands as the forward call took them (not looked at with
+ *   NONE, when the rotation alone is turned back).  dQ may be dQ_out (same base and strides), dK dK_out.  dw_q, dw_k: float, of the weights' shapes, or
+ *   NULL; sums over the tokens (and, of shared weights, heads); with NONE they must be NULL.  M == 0 writes zeros to them.
+ *   workspace: lemo_qk_rotate_grad_workspace_bytes() bytes, 256-byte aligned; not needed if neither sum is asked for.
+ *
+ * lemo_qk_rotate_step: one new token for each of B sequences, the newest of lengths[s] tokens (device), at position lengths[s] - 1: rotated Q [B,H,d]
+ *   to Q_out, rotated K [B,H_kv,d] and V (as it is; or NULL, V_cache too) to row lengths[s] - 1 of sequence s of the caches [B,S_max,H_kv,d]
+ *   (sequence stride, 64-bit).  Lengths outside [0, S_max] are taken as the nearer end; a sequence of length 0 gets zeros in Q_out and nothing in
+ *   its caches.  Other rows of the caches are not touched.
+ *
+ * binary32 arithmetic, one rounding at the store; no atomics: the same bits on every run.  What is not finite in a head spoils that head's
+ * row only (and the sums over the tokens).  M == 0 is a no-op.  Results overlap neither operands, but as said, nor each other.
+ * Supported: d in {64, 128}, bf16 and fp32; rot <= d, a multiple of 16 (bf16) / 8 (fp32); H + H_kv <= 65535, M < 2^31; positions and
+ * pos_start of magnitude below 2^31.
+ */
+enum { LEMO_ROTATE_PAIRS = 1u, LEMO_WEIGHTS_PER_HEAD = 2u };
+int lemo_qk_rotate(const void* Q, int64_t q_tok_stride, int64_t q_head_stride, const void* K, int64_t k_tok_stride, int64_t k_head_stride, int64_t M,
+                   int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt, const int32_t* positions, int64_t pos_start, const float* inv_freq, int32_t rot,
+                   float amplitude, int32_t norm, const void* w_q, const void* w_k, float eps, uint32_t flags, void* Q_out, int64_t qo_tok_stride,
+                   int64_t qo_head_stride, void* K_out, int64_t ko_tok_stride, int64_t ko_head_stride, void* stream);
+int lemo_qk_rotate_grad_workspace_bytes(int64_t M, int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt, uint32_t flags, size_t* bytes);
+int lemo_qk_rotate_grad(const void* dQ_out, int64_t dqo_tok_stride, int64_t dqo_head_stride, const void* dK_out, int64_t dko_tok_stride, int64_t dko_head_stride,
+                        const void* Q, int64_t q_tok_stride, int64_t q_head_stride, const void* K, int64_t k_tok_stride, int64_t k_head_stride, int64_t M,
+                        int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt, const int32_t* positions, int64_t pos_start, const float* inv_freq, int32_t rot,
+                        float amplitude, int32_t norm, const void* w_q, const void* w_k, float eps, uint32_t flags, void* dQ, int64_t dq_tok_stride,
+                        int64_t dq_head_stride, void* dK, int64_t dk_tok_stride, int64_t dk_head_stride, float* dw_q, float* dw_k, void* workspace,
+                        size_t workspace_bytes, void* stream);
+int lemo_qk_rotate_step(const void* Q, int64_t q_tok_stride, int64_t q_head_stride, const void* K, int64_t k_tok_stride, int64_t k_head_stride, const void* V,
+                        int64_t v_tok_stride, int64_t v_head_stride, int32_t B, int64_t S_max, int32_t H, int32_t H_kv, int32_t d, lemo_dtype_t dt,
+                        const int32_t* lengths, const float* inv_freq, int32_t rot, float amplitude, int32_t norm, const void* w_q, const void* w_k, float eps,
+                        uint32_t flags, void* Q_out, int64_t qo_tok_stride, int64_t qo_head_stride, void* K_cache, int64_t kc_seq_stride,
+                        int64_t kc_tok_stride, int64_t kc_head_stride, void* V_cache, int64_t vc_seq_stride, int64_t vc_tok_stride, int64_t vc_head_stride,
+                        void* stream);
+
+/*
+ * Dropout of a block's result and its add into the residual rows (the in-place add of Sec. 4.4 with dropout before it); the mask is
+ * formed where it is used and never stored:
+ *
+ *     R[k_m, c] += keep(k_m, c) ? Y[m, c] * 65536 / q : 0        k_m = kept_idx[m],  q = max(1, floor((1 - p) * 65536 + 1/2))
+ *     keep(k, c): of the Philox 4x32-10 block (Salmon et al., 2011) with key (rng[0]) and counter (c / 8, k, rng[1] + site), least significant
+ *     32 bits of a 64-bit word first, the 16 bits at 16 * (c mod 8) are below q
+ *
+ *   Y [M, C] row stride ldy;  R [S, C] row stride ldr, in place at the rows kept_idx names (NULL: rows 0..M-1; each at most once, not checked).
+ *     A value outside [0, S) drops the row.  Other rows are not touched.
+ *   p in [0, 1): the probability of a zero, to the nearest 2^-16.
+ *   rng: two 64-bit words in device memory, seed and stream: what changes from step to step, read when the kernel runs, so that a captured call
+ *     takes what stands there at each replay.  site: which dropout of the step this is.  The mask goes by the token, not by its place among
+ *     the kept rows.
+ *
+ * lemo_dropout_add_grad: dY[m, c] = keep(k_m, c) ? dR[k_m, c] * 65536 / q : 0, with the same p, rng and site; dR [S, C] is that of R before
+ *   and after the call.  Zeros for dropped rows.  Without kept_idx it is plain dropout of rows 0..M-1 and dY may be dR (same base and row stride).
+ *
+ * What a dropped element holds does not matter, infinities and NaN included.  One rounding at the store.  M == 0 is a no-op.
+ * Supported: C % 8 == 0 (bf16) / % 4 (fp32), M <= S < 2^31; 16-byte rule; rng at a multiple of 8 bytes.  R and Y do not overlap.
+ */
+int lemo_dropout_add(const void* Y, int64_t ldy, void* R, int64_t ldr, int64_t S, const int32_t* kept_idx, int64_t M, double p, const uint64_t* rng,
+                     uint64_t site, int32_t C, lemo_dtype_t dt, void* stream);
+int lemo_dropout_add_grad(const void* dR, int64_t lddr, int64_t S, const int32_t* kept_idx, int64_t M, double p, const uint64_t* rng, uint64_t site,
+                          void* dY, int64_t lddy, int32_t C, lemo_dtype_t dt, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

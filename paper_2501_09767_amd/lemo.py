@@ -34,7 +34,9 @@ EXPORTS = ("lemo_strerror", "lemo_keep_k", "lemo_kept_count", "lemo_score_worksp
            "lemo_norm_residual", "lemo_norm_residual_grad_workspace_bytes", "lemo_norm_residual_grad",
            "lemo_block_means", "lemo_select_blocks", "lemo_block_attention_workspace_bytes", "lemo_block_attention",
            "lemo_block_attention_grad_workspace_bytes", "lemo_block_attention_grad", "lemo_block_means_step", "lemo_select_blocks_step",
-           "lemo_block_attention_step_workspace_bytes", "lemo_block_attention_step")
+           "lemo_block_attention_step_workspace_bytes", "lemo_block_attention_step",
+           "lemo_qk_rotate", "lemo_qk_rotate_grad_workspace_bytes", "lemo_qk_rotate_grad", "lemo_qk_rotate_step",
+           "lemo_dropout_add", "lemo_dropout_add_grad")
 
 
 class LemoError(RuntimeError):
@@ -111,12 +113,16 @@ def _load() -> ctypes.CDLL:
     lib.lemo_norm_residual_grad.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, i32, f32, f32, vp, vp, i64, vp, i64,
                                             vp, vp, vp, vp, vp, i32, ctypes.c_int, u32, vp, ctypes.c_size_t, vp]
     size = ctypes.POINTER(ctypes.c_size_t)
-    kinds = {"p": vp, "l": i64, "i": i32, "f": f32, "u": u32, "z": ctypes.c_size_t, "s": size}
+    kinds = {"p": vp, "l": i64, "i": i32, "f": f32, "u": u32, "z": ctypes.c_size_t, "s": size, "d": ctypes.c_double, "q": ctypes.c_uint64}
     for name, args in (("block_means", "pliiillipp"), ("select_blocks", "pliiiillplliiiupp"), ("block_attention_workspace_bytes", "lliiiiiis"),
                        ("block_attention", "pppll" "iiii" "llllll" "piiil" "fu" "pllp" "pzp"), ("block_attention_grad_workspace_bytes", "lliiiiiis"),
                        ("block_attention_grad", "pppppp" "ll" "iiii" "llllllllll" "piiil" "fu" "ppp" "pzp"), ("block_means_step", "piliiilllpipp"),
                        ("select_blocks_step", "piiiiillplpiipp"), ("block_attention_step_workspace_bytes", "iiiiiis"),
-                       ("block_attention_step", "pppil" "iiii" "llllllll" "ppii" "f" "pll" "pzp")):
+                       ("block_attention_step", "pppil" "iiii" "llllllll" "ppii" "f" "pll" "pzp"),
+                       ("qk_rotate", "pll" "pll" "l" "iiii" "plpi" "fi" "pp" "fu" "pll" "pll" "p"), ("qk_rotate_grad_workspace_bytes", "liiiius"),
+                       ("qk_rotate_grad", "pll" "pll" "pll" "pll" "l" "iiii" "plpi" "fi" "pp" "fu" "pll" "pll" "pp" "pzp"),
+                       ("qk_rotate_step", "pll" "pll" "pll" "il" "iiii" "ppi" "fi" "pp" "fu" "pll" "plll" "plll" "p"),
+                       ("dropout_add", "plpll" "pl" "dpq" "ii" "p"), ("dropout_add_grad", "pll" "pl" "dpq" "pl" "ii" "p")):
         fn = getattr(lib, "lemo_" + name)
         fn.restype = ctypes.c_int
         fn.argtypes = [kinds[k] for k in args]
@@ -962,3 +968,167 @@ def lemo_block_attention_step(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
                                           V.stride(0), V.stride(1), V.stride(2), _ptr(lengths), _ptr(blocks), T, int(b), float(scale), _ptr(O), O.stride(0),
                                           O.stride(1), _ptr(workspace), size, _stream()), "lemo_block_attention_step")
     return O
+
+
+# --------------------------------------------------------------------------------- norms and rotation of queries and keys
+
+ROTATE_PAIRS, WEIGHTS_PER_HEAD = 1, 2
+
+
+class RotateGrads(NamedTuple):
+    """What lemo_qk_rotate_grad returns: None where there is no such operand, or nothing to take a gradient of."""
+    dQ: Optional[torch.Tensor]
+    dK: Optional[torch.Tensor]
+    dw_q: Optional[torch.Tensor]  # float32, of the weights' shapes
+    dw_k: Optional[torch.Tensor]
+
+
+def _steps(t: Optional[torch.Tensor]):
+    """Strides of every dimension but the last; 0 where there is nothing to step over."""
+    return tuple(st if n > 1 else 0 for n, st in zip(t.shape[:-1], t.stride()[:-1]))
+
+
+def _side(t: Optional[torch.Tensor], M: int, d: int, dtype, name: str):
+    """An [M,heads,d] operand or None -> (pointer, token stride, head stride), heads."""
+    if t is None:
+        return (None, 0, 0), 0
+    _heads(t, 3, name)
+    _fits(t, (M, t.shape[1], d), dtype, name)
+    return (_ptr(t), *_steps(t)), t.shape[1]
+
+
+def _rotate_sizes(Q, K, inv_freq, norm, w_q, w_k, flags):
+    """M, d, heads, dtype, rot, flags of the calls on heads."""
+    one = Q if Q is not None else K
+    if one is None:
+        raise ValueError("Q or K is needed")
+    _heads(one, 3, "Q" if Q is not None else "K")
+    M, d = one.shape[0], one.shape[2]
+    H, Hkv = (0 if t is None or t.dim() != 3 else t.shape[1] for t in (Q, K))
+    per_head = None
+    for name, w, heads, t in (("w_q", w_q, H, Q), ("w_k", w_k, Hkv, K)):
+        if w is None:
+            continue
+        if norm == NORM_NONE or t is None:
+            raise ValueError(f"{name} has nothing to weigh")
+        if per_head not in (None, w.dim() == 2) or w.dim() not in (1, 2):
+            raise ValueError("w_q and w_k must both be [d] or both [heads,d]")
+        per_head = w.dim() == 2
+        _filled(w, (heads, d) if per_head else (d,), one.dtype, None, name)
+    if inv_freq is not None and (inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous()):
+        raise ValueError("inv_freq must be contiguous float32 [rot / 2]")
+    return M, d, H, Hkv, one.dtype, 0 if inv_freq is None else 2 * inv_freq.numel(), int(flags) | (WEIGHTS_PER_HEAD if per_head else 0)
+
+
+def _heads_like(out: Optional[torch.Tensor], t: Optional[torch.Tensor], name: str):
+    if t is None:
+        if out is not None:
+            raise ValueError(f"{name} has no operand")
+        return None
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device) if out is None else out
+
+
+def lemo_qk_rotate(Q: Optional[torch.Tensor], K: Optional[torch.Tensor], inv_freq: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None, *,
+                   pos_start: int = 0, norm: int = NORM_RMS, w_q: Optional[torch.Tensor] = None, w_k: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                   amplitude: float = 1.0, flags: int = 0, Q_out: Optional[torch.Tensor] = None, K_out: Optional[torch.Tensor] = None):
+    """Norm of every head of Q [M,H,d] and K [M,H_kv,d], and rotation by positions [M] int32 (0 ... M-1 if not given) + pos_start, inv_freq
+    [rot/2] float32 -> (Q_out, K_out).  Weights [d], or [heads,d].  Q or K may be None; a result may be its operand."""
+    _here(Q, K, inv_freq, positions, w_q, w_k, Q_out, K_out)
+    M, d, H, Hkv, dtype, rot, flags = _rotate_sizes(Q, K, inv_freq, norm, w_q, w_k, flags)
+    _index(positions, M, "positions")
+    Q_out, K_out = _heads_like(Q_out, Q, "Q_out"), _heads_like(K_out, K, "K_out")
+    sides = [_side(t, M, d, dtype, name) for name, t in (("Q", Q), ("K", K), ("Q_out", Q_out), ("K_out", K_out))]
+    if sides[2][1] != H or sides[3][1] != Hkv:
+        raise ValueError("Q_out and K_out must have the heads of Q and K")
+    _check(_lib.lemo_qk_rotate(*sides[0][0], *sides[1][0], M, H, Hkv, d, F32 if dtype == torch.float32 else BF16, _ptr(positions), int(pos_start),
+                               _ptr(inv_freq), rot, float(amplitude), int(norm), _ptr(w_q), _ptr(w_k), float(eps), flags, *sides[2][0], *sides[3][0],
+                               _stream()), "lemo_qk_rotate")
+    return Q_out, K_out
+
+
+def lemo_qk_rotate_grad(dQ_out: Optional[torch.Tensor], dK_out: Optional[torch.Tensor], Q: Optional[torch.Tensor], K: Optional[torch.Tensor],
+                        inv_freq: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None, *, pos_start: int = 0, norm: int = NORM_RMS,
+                        w_q: Optional[torch.Tensor] = None, w_k: Optional[torch.Tensor] = None, eps: float = 1e-6, amplitude: float = 1.0, flags: int = 0,
+                        dQ: Optional[torch.Tensor] = None, dK: Optional[torch.Tensor] = None, weights: bool = True,
+                        workspace: Optional[torch.Tensor] = None) -> RotateGrads:
+    """Gradients of lemo_qk_rotate, Q and K as it took them (with NORM_NONE they may be None).  dQ may be dQ_out, dK dK_out; weights=False leaves out
+    those of w_q and w_k."""
+    _here(dQ_out, dK_out, Q, K, inv_freq, positions, w_q, w_k, dQ, dK, workspace)
+    M, d, H, Hkv, dtype, rot, flags = _rotate_sizes(dQ_out, dK_out, inv_freq, norm, w_q, w_k, flags)
+    _index(positions, M, "positions")
+    dQ, dK = _heads_like(dQ, dQ_out, "dQ"), _heads_like(dK, dK_out, "dK")
+    used = (Q, K) if norm != NORM_NONE else (None, None)
+    sides = [_side(t, M, d, dtype, name) for name, t in (("dQ_out", dQ_out), ("dK_out", dK_out), ("Q", used[0]), ("K", used[1]), ("dQ", dQ), ("dK", dK))]
+    if sides[4][1] != H or sides[5][1] != Hkv or (norm != NORM_NONE and (sides[2][1] != H or sides[3][1] != Hkv)):
+        raise ValueError("the gradients must have the heads of Q and K")
+    dw_q, dw_k = (torch.empty(w.shape, dtype=torch.float32, device=w.device) if weights and w is not None else None for w in (w_q, w_k))
+    need = 0
+    if dw_q is not None or dw_k is not None:
+        need = _bytes("lemo_qk_rotate_grad_workspace_bytes", M, H, Hkv, d, F32 if dtype == torch.float32 else BF16, flags)
+    workspace, size = _scratch(workspace, need, (dQ_out if dQ_out is not None else dK_out).device)
+    _check(_lib.lemo_qk_rotate_grad(*sides[0][0], *sides[1][0], *sides[2][0], *sides[3][0], M, H, Hkv, d, F32 if dtype == torch.float32 else BF16,
+                                    _ptr(positions), int(pos_start), _ptr(inv_freq), rot, float(amplitude), int(norm), _ptr(w_q), _ptr(w_k), float(eps),
+                                    flags, *sides[4][0], *sides[5][0], _ptr(dw_q), _ptr(dw_k), _ptr(workspace), size, _stream()), "lemo_qk_rotate_grad")
+    return RotateGrads(dQ, dK, dw_q, dw_k)
+
+
+def lemo_qk_rotate_step(Q: torch.Tensor, K: torch.Tensor, V: Optional[torch.Tensor], K_cache: torch.Tensor, V_cache: Optional[torch.Tensor],
+                        lengths: torch.Tensor, inv_freq: Optional[torch.Tensor], *, norm: int = NORM_RMS, w_q: Optional[torch.Tensor] = None,
+                        w_k: Optional[torch.Tensor] = None, eps: float = 1e-6, amplitude: float = 1.0, flags: int = 0,
+                        Q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The newest token of each sequence, at position lengths - 1: Q [B,H,d] -> Q_out; K, V [B,H_kv,d] go to their rows of the caches
+    [B,S_max,H_kv,d] in place."""
+    _here(Q, K, V, K_cache, V_cache, lengths, inv_freq, w_q, w_k, Q_out)
+    B, d, H, Hkv, dtype, rot, flags = _rotate_sizes(Q, K, inv_freq, norm, w_q, w_k, flags)
+    _lengths(lengths, B)
+    if (V is None) != (V_cache is None):
+        raise ValueError("V and V_cache come together")
+    _heads(K_cache, 4, "K_cache")
+    S = K_cache.shape[1]
+    for name, t in (("K_cache", K_cache), ("V_cache", V_cache)):
+        if t is not None:
+            _heads(t, 4, name)
+            _fits(t, (B, S, Hkv, d), dtype, name)
+    Q_out = _heads_like(Q_out, Q, "Q_out")
+    sides = [_side(t, B, d, dtype, name) for name, t in (("Q", Q), ("K", K), ("V", V), ("Q_out", Q_out))]
+    if sides[2][1] not in (0, Hkv) or sides[3][1] != H:
+        raise ValueError("V must have the heads of K, Q_out those of Q")
+    caches = [(_ptr(t), *(_steps(t) if t is not None else (0, 0, 0))) for t in (K_cache, V_cache)]
+    _check(_lib.lemo_qk_rotate_step(*sides[0][0], *sides[1][0], *sides[2][0], B, S, H, Hkv, d, F32 if dtype == torch.float32 else BF16, _ptr(lengths),
+                                    _ptr(inv_freq), rot, float(amplitude), int(norm), _ptr(w_q), _ptr(w_k), float(eps), flags, *sides[3][0], *caches[0],
+                                    *caches[1], _stream()), "lemo_qk_rotate_step")
+    return Q_out
+
+
+# --------------------------------------------------------------------------------- dropout into the residual rows
+
+def _generator(rng: torch.Tensor):
+    if rng.dtype not in (torch.int64, torch.uint64) or tuple(rng.shape) != (2,) or not rng.is_contiguous():
+        raise ValueError("rng must be contiguous int64 [2]: seed, stream")
+
+
+def lemo_dropout_add(Y: torch.Tensor, R: torch.Tensor, kept_idx: Optional[torch.Tensor], rng: torch.Tensor, p: float, site: int = 0) -> torch.Tensor:
+    """In place: R[kept_idx[m],:] += dropout(Y[m,:]).  Y [M,C], R [S,C]; rng int64 [2] on the GPU (seed, stream), site: which dropout of the step."""
+    _here(Y, R, kept_idx, rng)
+    _generator(rng)
+    M, S, C, ldy, _, ldr = _norm_args(Y, R, kept_idx, None, None, None, None, None)
+    _check(_lib.lemo_dropout_add(_ptr(Y), ldy, _ptr(R), ldr, S, _ptr(kept_idx), M, float(p), _ptr(rng), int(site) & (2 ** 64 - 1), C, _dt(R), _stream()),
+           "lemo_dropout_add")
+    return R
+
+
+def lemo_dropout_add_grad(dR: torch.Tensor, kept_idx: Optional[torch.Tensor], rng: torch.Tensor, p: float, site: int = 0,
+                          dY: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dY[m,:] = the gradient of lemo_dropout_add's Y from dR [S,C], with the same rng, p and site -> [M,C].  kept_idx None: plain dropout of dR's rows
+    (dY may then be dR)."""
+    _here(dR, kept_idx, rng, dY)
+    _generator(rng)
+    M, S, C, _, _, lddr = _norm_args(None, dR, kept_idx, None, None, None, None, None)
+    if dY is None:
+        dY = torch.empty((M, C), dtype=dR.dtype, device=dR.device)
+    elif dY.dim() == 2 and kept_idx is None:
+        M = dY.shape[0]
+    lddy = _rows_of(dY, M, C, dR.dtype, "dY")
+    _check(_lib.lemo_dropout_add_grad(_ptr(dR), lddr, S, _ptr(kept_idx), M, float(p), _ptr(rng), int(site) & (2 ** 64 - 1), _ptr(dY), lddy, C, _dt(dR),
+                                      _stream()), "lemo_dropout_add_grad")
+    return dY
