@@ -579,6 +579,45 @@ int lemo_dropout_add(const void* Y, int64_t ldy, void* R, int64_t ldr, int64_t S
 int lemo_dropout_add_grad(const void* dR, int64_t lddr, int64_t S, const int32_t* kept_idx, int64_t M, double p, const uint64_t* rng, uint64_t site,
                           void* dY, int64_t lddy, int32_t C, lemo_dtype_t dt, void* stream);
 
+/*
+ * Cross entropy over a vocabulary from hidden rows and the head's weight (what Sec. 4.4's segment-based peak cutting is there for: the logits are
+ * never stored as a whole).  The rows are read in place, as the selective-load GEMM reads them:
+ *
+ *     x[m, v] = sum_c X[kept_idx[m], c] * W[v, c]      u = softcap > 0 ? softcap * tanh(x / softcap) : x      lse[m] = log sum_v exp(u[m, v])
+ *     loss[m] = lse - (1 - smoothing) * u[m, labels[m]] - smoothing * mean_v u[m, v] + z_weight * lse^2
+ *
+ *   X [S, C] row stride ldx;  W [V, C] row stride ldw;  kept_idx [M] int32 rows of X in [0, S) (not checked on the device; a row may be named more than
+ *   once), or NULL for rows 0..M-1 (then M <= S);  labels [M] int32: a row whose label lies outside [0, V) does not count: its loss is 0.
+ *   loss, lse [M] float (natural logarithm; lse is there for every row);  total [4] float or NULL: sum of the losses, number of rows that count, their
+ *   mean, and 1 / number -- 0, 0, 0, 0 where none counts; the last is what the gradient of the mean takes.
+ *   workspace: lemo_vocab_loss_workspace_bytes() bytes, 256-byte aligned.  M == 0: total is written, nothing else.
+ *   One token: M = 1; -loss is its logarithm of probability.
+ *
+ * lemo_vocab_loss_grad: from dloss, the gradients of the losses (dloss_stride 1: [M]; 0: one value for all rows, e.g. total + 3), and lse as the forward
+ *   call left it:
+ *     G[m, v] = dloss[m] * (exp(u - lse) * (1 + 2 z_weight lse) - (1 - smoothing) [v = label] - smoothing / V) * (1 - (u / softcap)^2)
+ *     dX[m, c] = sum_v G[m, v] * W[v, c]          dW[v, c] = sum_m G[m, v] * X[kept_idx[m], c]
+ *   dX [M, C] row stride lddx (row m is that of token kept_idx[m]: lemo_scatter_grad puts it back), dW [V, C] row stride lddw, both of dtype dt,
+ *   overwritten; either may be NULL (a head that is not trained, a first layer).  Rows that do not count get zeros in dX and add nothing to dW, whatever
+ *   their rows of X hold.
+ *   The vocabulary is worked through `piece` columns at a time (0: this library's choice, about 256 MB of G; rounded up to 64).
+ *   workspace: lemo_vocab_loss_grad_workspace_bytes() bytes for the same piece, 256-byte aligned: a piece of G, and binary32 sums of dX.
+ *   M == 0 writes zeros to dW.
+ *
+ * Sums in binary32 (of the losses in 64 bits), over the whole vocabulary and all rows before they are rounded once; in bf16 G is rounded to bf16 for
+ * the two products.  No atomics: the same bits on every run.  What is not finite in a row of X spoils that row's results, and if it counts dW; in W, all.
+ * Supported: bf16 and fp32; C % 8 == 0 (bf16) / % 4 (fp32), any V <= 2^21, M <= 2^22; X, W, dX, dW follow the 16-byte rule, pitches below 8 MiB (dX in
+ * bf16: any); X with a row more spanning less than 4 GiB - 4096, a fp32 dX less than 4 GiB.  Results overlap neither operands nor each other.
+ */
+int lemo_vocab_loss_workspace_bytes(int64_t M, int32_t C, int32_t V, lemo_dtype_t dt, size_t* bytes);
+int lemo_vocab_loss(const void* X, int64_t S, int64_t ldx, const int32_t* kept_idx, int64_t M, const void* W, int64_t ldw, int32_t C, int32_t V,
+                    lemo_dtype_t dt, const int32_t* labels, float softcap, float smoothing, float z_weight, float* loss, float* lse, float* total,
+                    void* workspace, size_t workspace_bytes, void* stream);
+int lemo_vocab_loss_grad_workspace_bytes(int64_t M, int32_t C, int32_t V, int64_t ldw, lemo_dtype_t dt, int32_t piece, size_t* bytes);
+int lemo_vocab_loss_grad(const float* dloss, int64_t dloss_stride, const void* X, int64_t S, int64_t ldx, const int32_t* kept_idx, int64_t M, const void* W,
+                         int64_t ldw, int32_t C, int32_t V, lemo_dtype_t dt, const int32_t* labels, const float* lse, float softcap, float smoothing,
+                         float z_weight, void* dX, int64_t lddx, void* dW, int64_t lddw, int32_t piece, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

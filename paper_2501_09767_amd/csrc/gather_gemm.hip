@@ -4,6 +4,8 @@
 //
 // This file holds the launches and the choice of the output tiles; the kernels are gather_gemm_large.hip (256 x 256, bf16),
 // gather_gemm_mid.hip (256, 192, 128 or 64 x 128, bf16) and gather_gemm_small.hip (64 x 64; binary32).
+#include <cmath>
+
 #include "gather_gemm.hpp"
 
 namespace lemo {
@@ -37,15 +39,22 @@ namespace lemo {
 // faster they still serve.
 struct GgPlan { int head_cols; GgTile head, rest; };
 struct GgFit { GgTile tile; int rows, cols; double a, b, c[2], d, e; };
+static constexpr GgFit along[] = {{GG_T256, 256, 256, 6.43, 1.405, {1.004, 0.998}, 0.347, 5.76}, {GG_T256x128, 256, 128, 4.76, 0.812, {0.735, 0.655}, 0.129, 5.19},
+                                  {GG_T192x128, 192, 128, 4.36, 0.673, {0.617, 0.573}, 0.091, 4.24}, {GG_T128, 128, 128, 3.62, 0.529, {0.498, 0.461}, 0.068, 3.01},
+                                  {GG_T64x128, 64, 128, 3.19, 0.388, {0.359, 0.307}, 0.040, 1.78}, {GG_T64, 64, 64, 4.59, 0.226, {0.223, 0.207}, 0.012, 1.27}};
+static constexpr GgFit mixed[] = {{GG_T256, 256, 256, 8.34, 1.429, {0.919, 1.011}, 0.472, 11.79}, {GG_T256x128, 256, 128, 6.15, 0.819, {0.658, 0.701}, 0.178, 7.01},
+                                  {GG_T192x128, 192, 128, 4.82, 0.672, {0.583, 0.600}, 0.087, 6.43}, {GG_T128, 128, 128, 4.71, 0.534, {0.486, 0.542}, 0.040, 3.94},
+                                  {GG_T64x128, 64, 128, 3.86, 0.409, {0.404, 0.411}, 0.008, 2.24}, {GG_T64, 64, 64, 4.45, 0.272, {0.264, 0.156}, 0.017, 1.33}};
+static constexpr GgFit across[] = {{GG_T256, 256, 256, 5.6, 1.51, {1.16, 1.16}, 0.14, 7.1}, {GG_T256x128, 256, 128, 5.0, 0.94, {0.75, 0.75}, 0.13, 5.0},
+                                   {GG_T128, 128, 128, 3.2, 0.59, {0.56, 0.56}, 0.02, 3.6}, {GG_T64, 64, 64, 4.4, 0.18, {0.17, 0.17}, 0.30, 4.2}};
+// time of n tiles over k slabs
+static double gg_time(const GgFit& f, double n, double k) {
+    const double full = (double)(long long)(n / 256), part = n / 256 - full;
+    return f.a + full * (f.b * k + f.e) + (part == 0 ? 0. : (f.c[full > 0] + f.d * part) * k + f.e * part);
+}
+static double gg_tiles(const GgFit& f, long long M, long long cols) { return (double)((M + f.rows - 1) / f.rows) * (double)((cols + f.cols - 1) / f.cols); }
+
 static GgPlan gg_plan(long long M, int N, int K, int layout, lemo_dtype_t dt) {
-    static constexpr GgFit along[] = {{GG_T256, 256, 256, 6.43, 1.405, {1.004, 0.998}, 0.347, 5.76}, {GG_T256x128, 256, 128, 4.76, 0.812, {0.735, 0.655}, 0.129, 5.19},
-                                      {GG_T192x128, 192, 128, 4.36, 0.673, {0.617, 0.573}, 0.091, 4.24}, {GG_T128, 128, 128, 3.62, 0.529, {0.498, 0.461}, 0.068, 3.01},
-                                      {GG_T64x128, 64, 128, 3.19, 0.388, {0.359, 0.307}, 0.040, 1.78}, {GG_T64, 64, 64, 4.59, 0.226, {0.223, 0.207}, 0.012, 1.27}};
-    static constexpr GgFit mixed[] = {{GG_T256, 256, 256, 8.34, 1.429, {0.919, 1.011}, 0.472, 11.79}, {GG_T256x128, 256, 128, 6.15, 0.819, {0.658, 0.701}, 0.178, 7.01},
-                                      {GG_T192x128, 192, 128, 4.82, 0.672, {0.583, 0.600}, 0.087, 6.43}, {GG_T128, 128, 128, 4.71, 0.534, {0.486, 0.542}, 0.040, 3.94},
-                                      {GG_T64x128, 64, 128, 3.86, 0.409, {0.404, 0.411}, 0.008, 2.24}, {GG_T64, 64, 64, 4.45, 0.272, {0.264, 0.156}, 0.017, 1.33}};
-    static constexpr GgFit across[] = {{GG_T256, 256, 256, 5.6, 1.51, {1.16, 1.16}, 0.14, 7.1}, {GG_T256x128, 256, 128, 5.0, 0.94, {0.75, 0.75}, 0.13, 5.0},
-                                       {GG_T128, 128, 128, 3.2, 0.59, {0.56, 0.56}, 0.02, 3.6}, {GG_T64, 64, 64, 4.4, 0.18, {0.17, 0.17}, 0.30, 4.2}};
     if (dt == LEMO_F32) {
         const double n128 = (double)((M + 127) / 128) * (double)(((long long)N + 127) / 128);
         return {0, GG_T128, n128 <= 192 ? GG_T64 : GG_T128};
@@ -54,11 +63,7 @@ static GgPlan gg_plan(long long M, int N, int K, int layout, lemo_dtype_t dt) {
     const int kinds = layout == GG_TN ? 4 : 6, heads = kinds / 2;  // heads: the kinds that may come before another one
     const double meets = layout == GG_TN ? 0. : 2.;                // the second launch starts as the first one ends
     const double k = K / 64.;
-    auto time = [&](const GgFit& f, long long cols) {
-        const double n = (double)((M + f.rows - 1) / f.rows) * (double)((cols + f.cols - 1) / f.cols);
-        const double full = (double)(long long)(n / 256), part = n / 256 - full;
-        return f.a + full * (f.b * k + f.e) + (part == 0 ? 0. : (f.c[full > 0] + f.d * part) * k + f.e * part);
-    };
+    auto time = [&](const GgFit& f, long long cols) { return gg_time(f, gg_tiles(f, M, cols), k); };
     GgPlan best{0, GG_T256, GG_T256};
     double least = time(fits[0], N);
     for (int t = 1; t < kinds; ++t)
@@ -70,6 +75,24 @@ static GgPlan gg_plan(long long M, int N, int K, int layout, lemo_dtype_t dt) {
         for (int t = h + 1; t < kinds; ++t) {
             const double both = time(fits[h], cols) + time(fits[t], N - cols) - meets;
             if (both < least) { least = both; best = {(int)cols, fits[h].tile, fits[t].tile}; }
+        }
+    }
+    return best;
+}
+
+// The kind of eight-wave tiles for a product as a whole, and into how many parts of the contraction it is cut where a part costs `split_us`
+// (X W^T: into one).
+GgTile gg_choose_tile(long long M, int N, int K, int layout, int most_splits, double split_us, int* splits) {
+    const GgFit* fits = layout == GG_NN ? mixed : along;
+    GgTile best = GG_T256;
+    double least = INFINITY;
+    for (int t = 0; t < 5; ++t) {
+        if (fits[t].tile == GG_T192x128) continue;
+        for (int s = 1; s <= most_splits; s *= 2) {
+            const int k = (K + s * 64 - 1) / (s * 64);  // slabs of a part
+            if (s > 1 && (long long)k * (s - 1) * 64 >= K) break;
+            const double us = gg_time(fits[t], gg_tiles(fits[t], M, N) * s, k) + s * split_us;
+            if (us < least) { least = us; best = fits[t].tile; *splits = s; }
         }
     }
     return best;

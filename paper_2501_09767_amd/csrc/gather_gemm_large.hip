@@ -21,26 +21,13 @@
 //   weight grad.   8192 x 8192 x 8192: 800 / 987;   9856 x 11008 x 4096: 688 / 869;   3280 x 11008 x 4096: 278 / 357
 // Tried: four waves of 128 x 128 in this scheme (the compiler moves the 256 accumulators about: 987); counters in LDS, written
 // ahead of the wait, in the barriers' place (793).
-#include "gather_gemm_regions.hpp"
+#include "gather_gemm_tiles.hpp"
 
 namespace lemo {
 
-constexpr int LG_BM = 256, LG_BN = 256;
-constexpr int LG_STAGE = 2 * RG_BYTES;   // regions: rows (columns of the output) 0-127, 128-255
-constexpr int LG_OPER = 2 * LG_STAGE;    // two stages of A, then two of B: 64 KB, the reach of an LDS read's immediate offset
-constexpr int LG_TOK = 2 * LG_OPER;      // (GG_TN) token rings
-constexpr int LG_EP = LG_BN * 2 + 16;    // epilogue: LDS pitch of a row of bf16, ...
-constexpr int LG_EPF = LG_BN * 4 + 16;   // ... of binary32 (128 rows at a time)
-constexpr int LG_WN = 4;                 // waves along the columns
-constexpr int LG_TA = 4, LG_TB = 2;      // 16-row tiles of a wave per half of A, of B
-constexpr int LG_LDS_EPI = LG_BM * LG_EP > 128 * LG_EPF ? LG_BM * LG_EP : 128 * LG_EPF;
-constexpr int LG_LDS = LG_TOK + RG_TOK > LG_LDS_EPI ? LG_TOK + RG_TOK : LG_LDS_EPI;
-static_assert(LG_LDS <= 160 * 1024, "a workgroup's LDS");
-
 template <bool ADD, int LAYOUT>
 __global__ __launch_bounds__(RG_THREADS, 1) void gather_gemm_large_kernel(GgParams p) {
-    constexpr bool A_KMAJOR = LAYOUT == GG_TN, B_KMAJOR = LAYOUT != GG_NT;
-    constexpr int TA = LG_TA, TB = LG_TB, NL = RG_NLD;
+    constexpr int TA = LG_TA, TB = LG_TB;
     extern __shared__ __attribute__((aligned(16))) char smem[];
 
     int tm, tn;
@@ -51,131 +38,8 @@ __global__ __launch_bounds__(RG_THREADS, 1) void gather_gemm_large_kernel(GgPara
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / LG_WN, wn = wave % LG_WN;
     const int l16 = lane & 15, quad = lane >> 4;
-    using Loads = RgLoads<LAYOUT, 4, 4>;
-    using Slab = typename Loads::Slab;
-    Loads ld(p, m0, n0, tid, smem + LG_TOK + wave * 1024);
-    const int nk = ld.nk;
-    const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_offset_of(smem) + wave * 1024);
-    auto load_a = [&](const Slab& s, int kt, int r, int i) { ld.load_a(s, 2 * r + i, lds0 + (kt & 1) * LG_STAGE); };
-    auto load_b = [&](const Slab& s, int kt, int r, int i) { ld.load_b(s, 2 * r + i, lds0 + LG_OPER + (kt & 1) * LG_STAGE); };
-
     f32x4 acc[2][TA][2][TB];  // [half of A][tile][half of B][tile]
-#pragma unroll
-    for (int a = 0; a < 2; ++a)
-#pragma unroll
-        for (int i = 0; i < TA; ++i)
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int j = 0; j < TB; ++j) acc[a][i][b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // fragments: the current half of A, both halves of B
-    u32x4 fa[2][TA], fb[2][2][TB];
-    auto read_a = [&](int st, int r, int c, int i) { fa[c][i] = rg_fragment(smem + st * LG_STAGE + r * RG_BYTES, A_KMAJOR, wm * TA + i, c, lane); };
-    auto read_b = [&](int st, int r, int c, int j) { fb[r][c][j] = rg_fragment(smem + LG_OPER + st * LG_STAGE + r * RG_BYTES, B_KMAJOR, wn * TB + j, c, lane); };
-
-    constexpr int NM = 2 * TA * TB;  // MFMAs of a quarter
-    // One quarter of a slab: the MFMAs of (half AH of A) x (half BH of B), `mem(q, c, i, j)` behind MFMA q, which is of chunk c
-    // and tile (i, j).  The source order is the issue order.
-    auto quarter = [&](auto ah, auto bh, bool by_columns, auto mem) {
-        constexpr int AH = decltype(ah)::value, BH = decltype(bh)::value;
-#pragma unroll
-        for (int q = 0; q < NM; ++q) {  // the tiles back and forth, row by row or column by column: neighbours share a fragment
-            const int c = q / (TA * TB), w = q % (TA * TB), u = by_columns ? w / TA : w / TB, v = by_columns ? w % TA : w % TB;
-            const int back = by_columns ? TA - 1 - v : TB - 1 - v, t = u & 1 ? back : v, i = by_columns ? t : u, j = by_columns ? u : t;
-            __builtin_amdgcn_sched_barrier(0);
-            rg_mma(acc[AH][i][BH][j], fa[c][i], fb[BH][c][j]);
-            mem(q, c, i, j);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-    using I0 = std::integral_constant<int, 0>;
-    using I1 = std::integral_constant<int, 1>;
-    auto load_region = [&](const Slab& s, int kt, bool a, int r) {
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            if (a) load_a(s, kt, r, i); else load_b(s, kt, r, i);
-        }
-    };
-
-    // What would have been asked for in the halves before: {B 0} {A 0, B 1} of slab 0, {A 1 of 0, B 1 of 1}, {A 0, B 0 of 1}
-    if constexpr (LAYOUT == GG_TN) {
-        for (int kt = 0; kt < 4; ++kt) ld.issue_tokens(kt, lane);
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-        asm volatile("" ::: "memory");
-    }
-    {
-        const Slab s0 = ld.slab(0), s1 = ld.slab(1);
-        ld.read_tokens(0);
-        load_region(s0, 0, false, 0);
-        load_region(s0, 0, true, 0);
-        load_region(s0, 0, false, 1);
-        load_region(s0, 0, true, 1);
-        ld.read_tokens(1);
-        load_region(s1, 1, false, 1);
-        load_region(s1, 1, true, 0);
-        load_region(s1, 1, false, 0);
-        ld.read_tokens(2);
-    }
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(5 * NL));
-    rg_barrier();
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-#pragma unroll
-        for (int j = 0; j < TB; ++j) read_b(0, 0, c, j);
-#pragma unroll
-        for (int i = 0; i < TA; ++i) read_a(0, 0, c, i);
-    }
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(3 * NL));
-    __builtin_amdgcn_s_waitcnt(LGKMCNT0);
-
-    // Waves of one SIMD do not take turns: one of them goes first (X W^T 752 -> 742 us at 8192^3, the gradients no change)
-    if constexpr (LAYOUT == GG_NT)
-        if (wave < RG_WAVES / 2) __builtin_amdgcn_s_setprio(1);
-    // Slab kt, kt & 1 == PAR.  Halves of a slab begin with a barrier, before which every wave has seen to it that the regions
-    // read in this half have landed (its own part: all loads but the last IN_FLIGHT, which complete in order) and that it
-    // has read what this half's loads overwrite: all but the fragments read in the quarter before.
-    constexpr int IN_FLIGHT = 3 * NL;
-    auto slab = [&](int kt, auto par_tag) {
-        constexpr int PAR = decltype(par_tag)::value, F = PAR, L = PAR ^ 1;
-        using IF = std::integral_constant<int, F>;
-        using IL = std::integral_constant<int, L>;
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm(IN_FLIGHT));
-        __builtin_amdgcn_s_waitcnt(lgkmcnt_imm(A_KMAJOR ? 15 : 2 * TA));
-        rg_barrier();
-        const Slab s1 = ld.slab(kt + 1), s2 = ld.slab(kt + 2);
-        quarter(I0{}, IF{}, false, [&](int q, int c, int i, int j) {
-            if (q < 2 * TB) read_b(PAR, L, q / TB, q % TB);
-            if (q < 2 * NL) {
-                if (q < NL) load_a(s1, PAR ^ 1, 1, q); else load_b(s2, PAR, F, q - NL);
-            }
-        });
-        quarter(I0{}, IL{}, false, [&](int q, int c, int i, int j) {
-            if (q % TB == TB - 1) read_a(PAR, 1, c, i);
-        });
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm(IN_FLIGHT));
-        rg_barrier();
-        ld.issue_tokens(kt + 4, lane);
-        quarter(I1{}, IL{}, true, [&](int q, int c, int i, int j) {
-            if (q % TA == TA - 1) read_b(PAR ^ 1, L, c, j);
-            if (q < 2 * NL) {
-                if (q < NL) load_a(s2, PAR, 0, q); else load_b(s2, PAR, L, q - NL);
-            }
-        });
-        ld.read_tokens(kt + 3);
-        quarter(I1{}, IF{}, false, [&](int q, int c, int i, int j) {
-            if (q % TB == TB - 1) read_a(PAR ^ 1, 0, c, i);
-        });
-    };
-    int kt = 0;
-    for (; kt + 1 < nk; kt += 2) {
-        slab(kt, I0{});
-        slab(kt + 1, I1{});
-    }
-    if (kt < nk) slab(kt, I0{});
-    if constexpr (LAYOUT == GG_NT) __builtin_amdgcn_s_setprio(0);
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // requests past the end write (zeros) to the stages, too
-    __builtin_amdgcn_s_waitcnt(LGKMCNT0);
-    __syncthreads();
+    lg_product<LAYOUT>(p, m0, n0, smem, acc);
 
     // Epilogue, through LDS: whole rows of 16-byte pieces, 8 consecutive columns per lane.  In-place add: binary32, half of the tile
     // at a time, what the rows hold already asked for ahead through a range-checked descriptor (rows that are not to be written get

@@ -16,27 +16,14 @@
 //   128 x 128  M = 256, N = 11008, K = 4096: 42;  M = 768, N = 3072, K = 768: 9.4
 //   64 x 128   M = 128, N = 11008, K = 4096: 32 (128 x 128: 42);  M = 500, N = K = 4096 30 (37);  M = 408, N = 3072, K = 768 8.0 (9.7)
 // (128 x 64 does as well as 64 x 128.  128 x 96 gained 7 % in X W^T where 64 x 128 loses, M = 256, N = 11008; it is not built: B's rows are loaded 64 at a time.)
-#include "gather_gemm_regions.hpp"
+#include "gather_gemm_tiles.hpp"
 
 namespace lemo {
-
-template <int LAYOUT, int UA> struct MdGeo {               // UA: the tile's rows / 64
-    static constexpr int BM = 64 * UA, BN = 128;
-    static constexpr int A_BYTES = BM * RG_KB, STAGE = A_BYTES + RG_BYTES;  // A's rows, then B's region
-    static constexpr int TOKENS = LAYOUT == GG_TN ? RG_TOK : 0;
-    static constexpr int NS = UA == 4 ? 3 : 4;             // stages
-    static constexpr int TOK = NS * STAGE;                 // (GG_TN) token rings
-    static constexpr int EP = BN * 4 + 16;                 // epilogue: LDS pitch of a row of floats
-    static constexpr int LDS_LOOP = TOK + TOKENS, LDS_EPI = BM * EP;
-    static constexpr int LDS = LDS_LOOP > LDS_EPI ? LDS_LOOP : LDS_EPI;
-    static_assert(LDS <= 160 * 1024, "a workgroup's LDS");
-};
 
 template <bool ADD, int LAYOUT, int UA>
 __global__ __launch_bounds__(RG_THREADS, 1) void gather_gemm_mid_kernel(GgParams p) {
     using G = MdGeo<LAYOUT, UA>;
-    constexpr bool A_KMAJOR = LAYOUT == GG_TN, B_KMAJOR = LAYOUT != GG_NT;
-    constexpr int TA = UA, TB = 4, NS = G::NS;  // 16-row tiles of a wave of A, of B
+    constexpr int TA = UA, TB = MD_TB;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     int tm, tn;
     if (!gg_tile(blockIdx.x, p.tiles_m, p.tiles_n, UA <= 2 ? 16 / UA : 4, tm, tn)) return;
@@ -45,96 +32,9 @@ __global__ __launch_bounds__(RG_THREADS, 1) void gather_gemm_mid_kernel(GgParams
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave >> 1, wn = wave & 1;
-    // 16-row tile i of the wave, among the tile's: contraction-major rows come in regions of 128, of which a wave takes 32
-    auto a_tile = [&](int i) { return A_KMAJOR ? i / 2 * 8 + wm * 2 + i % 2 : wm * TA + i; };
-    using Loads = RgLoads<LAYOUT, UA, 2>;
-    Loads ld(p, m0, n0, tid, smem + G::TOK + wave * 1024);
-    const int nk = ld.nk;
-    const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_offset_of(smem) + wave * 1024);
-    constexpr int LOADS = UA + 2, BATCH = LOADS + (LAYOUT == GG_TN ? 1 : 0);
-    constexpr int AHEAD = NS - 1;  // (GG_TN) the indices of a slab are asked for this many slabs ahead of its rows
-    auto load = [&](const typename Loads::Slab& s, unsigned stage, int k) {  // load k of a slab
-        if (k < UA) ld.load_a(s, k, stage);
-        else ld.load_b(s, k - UA, stage + G::A_BYTES);
-    };
-
+    auto a_tile = [&](int i) { return md_a_tile<LAYOUT, UA>(wm, i); };
     f32x4 acc[TA][TB];
-#pragma unroll
-    for (int i = 0; i < TA; ++i)
-#pragma unroll
-        for (int j = 0; j < TB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    u32x4 fa[2][2][TA], fb[2][2][TB];  // fragments of two slabs
-    constexpr int NF = 2 * (TA + TB);
-    auto read = [&](auto set_tag, const char* stage, int f) {  // fragment f of a slab: B's, then A's
-        constexpr int SET = decltype(set_tag)::value;
-        if (f < 2 * TB) { fb[SET][f / TB][f % TB] = rg_fragment(stage + G::A_BYTES, B_KMAJOR, wn * TB + f % TB, f / TB, lane); return; }
-        f -= 2 * TB;
-        const int c = f / TA, t = a_tile(f % TA);
-        fa[SET][c][f % TA] = A_KMAJOR ? rg_fragment(stage + t / 8 * RG_BYTES, true, t % 8, c, lane) : rg_fragment(stage, false, t, c, lane);
-    };
-
-    if constexpr (LAYOUT == GG_TN) {
-        for (int kt = 0; kt < 4; ++kt) ld.issue_tokens(kt, lane);
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-        asm volatile("" ::: "memory");
-    }
-    // (the batches as the loop issues them: a slab's rows, then the indices of the slab AHEAD, into the entry of a slab that is done)
-#pragma unroll
-    for (int kt = 0; kt < NS; ++kt) {
-        const typename Loads::Slab s = ld.slab(kt);
-        ld.read_tokens(kt);
-#pragma unroll
-        for (int k = 0; k < LOADS; ++k) load(s, lds0 + kt * G::STAGE, k);
-        if constexpr (LAYOUT == GG_TN) {
-            __builtin_amdgcn_s_waitcnt(LGKMCNT0);
-            asm volatile("" ::: "memory");
-            ld.issue_tokens(kt + AHEAD, lane);
-        }
-    }
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm((NS - 1) * BATCH));
-    rg_barrier();
-#pragma unroll
-    for (int f = 0; f < NF; ++f) read(std::integral_constant<int, 0>{}, smem, f);
-
-    constexpr int NM = 2 * TA * TB;
-    int st = 0;  // stage of slab kt
-    // Slab kt (kt & 1 == PAR), its fragments in set PAR.  Behind the barrier slab kt + 1 has landed (all batches but the last
-    // NS - 2) and stage st is free; the source order is the issue order, neighbouring MFMAs share a fragment.
-    auto step = [&](int kt, auto par_tag) {
-        constexpr int PAR = decltype(par_tag)::value;
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm((NS - 2) * BATCH));
-        __builtin_amdgcn_s_waitcnt(LGKMCNT0);
-        rg_barrier();
-        const typename Loads::Slab s = ld.slab(kt + NS);
-        const int nxt = st + 1 == NS ? 0 : st + 1;
-        const char* next = smem + nxt * G::STAGE;
-        const unsigned free_stage = lds0 + st * G::STAGE;
-        if constexpr (LAYOUT == GG_TN) ld.read_tokens(kt + NS);
-#pragma unroll
-        for (int q = 0; q < NM; ++q) {
-            const int c = q / (TA * TB), w = q % (TA * TB), i = w / TB, j = i & 1 ? TB - 1 - w % TB : w % TB;
-            __builtin_amdgcn_sched_barrier(0);
-            rg_mma(acc[i][j], fa[PAR][c][i], fb[PAR][c][j]);
-#pragma unroll
-            for (int f = q * NF / (NM * 3 / 4); f < (q + 1) * NF / (NM * 3 / 4); ++f)
-                if (f < NF) read(std::integral_constant<int, PAR ^ 1>{}, next, f);
-#pragma unroll
-            for (int k = q * LOADS / (NM / 2); k < (q + 1) * LOADS / (NM / 2); ++k)
-                if (k < LOADS) load(s, free_stage, k);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if constexpr (LAYOUT == GG_TN) ld.issue_tokens(kt + NS + AHEAD, lane);
-        st = nxt;
-    };
-    int kt = 0;
-    for (; kt + 1 < nk; kt += 2) {
-        step(kt, std::integral_constant<int, 0>{});
-        step(kt + 1, std::integral_constant<int, 1>{});
-    }
-    if (kt < nk) step(kt, std::integral_constant<int, 0>{});
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // requests past the end write (zeros) to the stages, too
-    __builtin_amdgcn_s_waitcnt(LGKMCNT0);
-    __syncthreads();
+    md_product<LAYOUT, UA>(p, m0, n0, smem, acc);
 
     // Epilogue, through LDS as binary32: whole rows of 16-byte pieces, 8 consecutive columns per lane, one rounding.  In-place add:
     // what the rows hold is asked for ahead (rows that are not to be written get an offset past the descriptor's end).

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void gather_transpose_kernel(const uint32_t* _
     }
 }
 
-static int launch_transpose(const void* in, long long ld_in, const int* idx, long long M, long long Mpad, int ncols, void* out, hipStream_t st) {
+int launch_transpose(const void* in, long long ld_in, const int* idx, long long M, long long Mpad, int ncols, void* out, hipStream_t st) {
     constexpr int TC = 16 * 4;
     hipLaunchKernelGGL(gather_transpose_kernel, dim3((unsigned)(Mpad / 64), (unsigned)((ncols + TC - 1) / TC)), dim3(256), 0, st,
                        static_cast<const uint32_t*>(in), ld_in, idx, (int)M, ncols, static_cast<uint32_t*>(out), Mpad);

@@ -1,0 +1,364 @@
+// Cross entropy over a vocabulary from hidden rows and the head's weight, and its gradients; the logits are never stored as a whole.
+//
+//   x = X[idx] W^T,  u = softcap tanh(x / softcap) or x,  lse = log sum exp u
+//   loss = lse - (1 - s) u[label] - s mean(u) + z lse^2            0 for rows without a label in [0, V)
+//   G = dloss (exp(u - lse) (1 + 2 z lse) - (1 - s) [label] - s / V) (1 - (u / softcap)^2)      dX = G W      dW = G^T X[idx]
+//
+// Forward: one pass over the tiles of the product (vocab_loss_tiles.hip), which leave (maximum, sum of exponentials) a row and tile; the tiles' parts are
+// joined in their order by a kernel here, and the rows' losses added by another, in 64 bits.  Gradients: the vocabulary in pieces; of a piece its
+// logits once more, turned into G, then its rows of dW (finished: every token is in them) and its part of dX, which is added up in
+// binary32 over the pieces and rounded once.  No atomics: the same bits on every run.
+//
+// What bounds it: the matrix cores, 2 M C V products forward and 6 in the gradients.  Keeping G of the whole vocabulary would save a
+// piece's tail and the additions to dX, and is what the operator is there to avoid.
+//
+// binary32: the products are the selective-load GEMM's, a piece at a time in both directions, with the softmax in kernels of its own between them; dX takes the
+// weight's piece transposed, since that GEMM wants both operands along the contraction.
+#include <algorithm>
+
+#include "vocab_softmax.hpp"
+#include "row_pieces.hpp"
+
+namespace lemo {
+
+constexpr int VL_THREADS = 256;
+constexpr long long VL_ROWS = 16384;  // rows of a forward launch: bounds what the tiles leave
+
+// ---- rows --------------------------------------------------------------------------------------------
+
+// Joins the parts of a row: `per` rows a workgroup, VL_THREADS / per threads a row, each a part in so many; then those in their order.
+__global__ __launch_bounds__(VL_THREADS) void vocab_join_kernel(VocabRule rule, const float2* parts, const float* sums, const float* picked, const int* labels,
+                                                                long long M, int n, int per, float* loss, float* lse) {
+    __shared__ float lds[3][VL_THREADS];
+    const int threads = VL_THREADS / per, mine = threadIdx.x / per;
+    const long long m = (long long)blockIdx.x * per + threadIdx.x % per;
+    float top = -INFINITY, sum = 0.f, all = 0.f;
+    if (m < M) {
+#pragma unroll 4
+        for (int t = mine; t < n; t += threads) {
+            const float2 v = parts[(long long)t * M + m];
+            vocab_join(top, sum, v.x, v.y);
+            if (sums) all += sums[(long long)t * M + m];
+        }
+    }
+    lds[0][threadIdx.x] = top;
+    lds[1][threadIdx.x] = sum;
+    lds[2][threadIdx.x] = all;
+    __syncthreads();
+    if (mine || m >= M) return;
+    for (int t = 1; t < threads; ++t) {
+        vocab_join(top, sum, lds[0][t * per + threadIdx.x], lds[1][t * per + threadIdx.x]);
+        all += lds[2][t * per + threadIdx.x];
+    }
+    const float total = top + logf(sum);
+    lse[m] = total;
+    if (!loss) return;
+    const int label = labels[m];
+    const bool counts = label >= 0 && label < rule.V;
+    float v = fmaf(rule.z * total, total, total);
+    if (counts) v -= rule.hit * picked[m];
+    if (sums) v -= rule.all * all;
+    loss[m] = counts ? v : 0.f;
+}
+
+// sum, number, mean and 1 / number of the rows that count
+__global__ __launch_bounds__(1024) void vocab_total_kernel(const float* loss, const int* labels, long long M, int V, float* total) {
+    __shared__ double sums[16];
+    __shared__ int counts[16];
+    double sum = 0.;
+    long long n = 0;
+    for (long long m = threadIdx.x; m < M; m += 1024) {
+        sum += (double)loss[m];
+        n += labels[m] >= 0 && labels[m] < V;
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        sum += __shfl_xor(sum, s);
+        n += __shfl_xor(n, s);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        sums[threadIdx.x >> 6] = sum;
+        counts[threadIdx.x >> 6] = (int)n;
+    }
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < 16; ++w) {
+        sum += sums[w];
+        n += counts[w];
+    }
+    total[0] = (float)sum;
+    total[1] = (float)n;
+    total[2] = n ? (float)(sum / (double)n) : 0.f;
+    total[3] = n ? (float)(1. / (double)n) : 0.f;
+}
+
+// What the gradient's products take of the rows: their losses' gradients side by side, and for the weight's gradient the rows of X, those without a
+// label replaced by one past X's end, which the loads' range check turns into zeros whatever such a row holds.  Row M is one more of those:
+// the last row of G a product reads is then one of zeros, whose last piece of columns may end in the operand's middle.
+__global__ __launch_bounds__(VL_THREADS) void vocab_rows_kernel(const float* dloss, long long stride, const int* labels, const int* idx, long long M, long long S,
+                                                                int V, float* weight, int* rows) {
+    const long long m = (long long)blockIdx.x * VL_THREADS + threadIdx.x;
+    if (m > M) return;
+    const bool counts = m < M && labels[m] >= 0 && labels[m] < V;
+    rows[m] = (int)(!counts ? S : idx ? (long long)idx[m] : m);
+    if (m < M) weight[m] = counts ? dloss[m * stride] : 0.f;
+}
+
+// dX = the sum of the planes, rounded once.  A thread has eight columns of a row.
+__global__ __launch_bounds__(VL_THREADS) void vocab_planes_kernel(const float* planes, int n, long long M, int C, void* dX, long long lddx, long long first) {
+    const long long per_row = C / 8, i = (first + blockIdx.x) * VL_THREADS + threadIdx.x;
+    const long long m = i / per_row;
+    if (m >= M) return;
+    const int c = (int)(i - m * per_row) * 8;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < n; ++s) {
+        const f32x4* const at = reinterpret_cast<const f32x4*>(planes + ((long long)s * M + m) * C + c);
+        const f32x4 lo = at[0], hi = at[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] += lo[e]; v[e + 4] += hi[e]; }
+    }
+    row_store<bf16_t>(dX, m * lddx + c, RowPiece<bf16_t>::put(v));
+}
+
+// ---- binary32: a piece's logits in memory -----------------------------------------------------------
+
+// A workgroup a row: its part of the statistics, as a tile leaves it
+__global__ __launch_bounds__(VL_THREADS) void vocab_stats_f32_kernel(VocabRule rule, const float* x, long long ldx, int N, int v0, const int* labels, long long M,
+                                                                     float2* parts, float* sums, float* picked, long long first) {
+    __shared__ float lds[3][VL_THREADS / 64];
+    const long long m = first + blockIdx.x;
+    const float* const row = x + m * ldx;
+    const bool capped = rule.softcap > 0.f;
+    const float inv_cap = capped ? 1.f / rule.softcap : 0.f;
+    const unsigned label = (unsigned)labels[m] - (unsigned)v0;
+    float top = -INFINITY, sum = 0.f, all = 0.f;
+    for (int n = threadIdx.x; n < N; n += VL_THREADS) {
+        const float u = capped ? vocab_cap(row[n], rule.softcap, inv_cap) : row[n];
+        if ((unsigned)n == label) picked[m] = u;
+        const float t = fmaxf(top, u);
+        sum = sum * vocab_scale(top, t) + vocab_scale(u, t);
+        top = t;
+        all += u;
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        vocab_join(top, sum, __shfl_xor(top, s), __shfl_xor(sum, s));
+        all += __shfl_xor(all, s);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        lds[0][threadIdx.x >> 6] = top;
+        lds[1][threadIdx.x >> 6] = sum;
+        lds[2][threadIdx.x >> 6] = all;
+    }
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < VL_THREADS / 64; ++w) {
+        vocab_join(top, sum, lds[0][w], lds[1][w]);
+        all += lds[2][w];
+    }
+    parts[m] = make_float2(top, sum);
+    if (sums) sums[m] = all;
+}
+
+// logits -> G in place, and zeros in the columns from N up to a multiple of 64
+__global__ __launch_bounds__(VL_THREADS) void vocab_probs_f32_kernel(VocabRule rule, float* x, long long ldx, int N, int v0, const int* labels, const float* lse,
+                                                                     const float* weight, long long first) {
+    const long long m = first + blockIdx.x;
+    float* const row = x + m * ldx;
+    const bool capped = rule.softcap > 0.f;
+    const float inv_cap = capped ? 1.f / rule.softcap : 0.f;
+    const VocabRow of = vocab_row(rule, lse[m], weight[m], labels[m]);
+    for (int n = threadIdx.x; n < (N + 63) / 64 * 64; n += VL_THREADS) {
+        const float u = n < N ? capped ? vocab_cap(row[n], rule.softcap, inv_cap) : row[n] : 0.f;
+        row[n] = n < N ? vocab_grad(rule, of, u, v0 + n, inv_cap) : 0.f;
+    }
+}
+
+// ---- launches ------------------------------------------------------------------------------------------
+
+static size_t vl_round(size_t v) { return (v + 255) / 256 * 256; }
+static long long vl_pitch(int piece) { return (piece + 63) / 64 * 64; }
+
+// Columns at a time.  A piece costs what its launches leave idle and, of dX, 8 bytes for each of M C elements; G of a piece costs memory, 256 MB here, which also
+// is what the last-level cache holds.
+static int vl_choice(long long M, int V, int esz) {
+    const long long most = std::max<long long>(8192, (256ll << 20) / (std::max<long long>(M, 1) * esz) / 1024 * 1024);
+    const long long n = (V + most - 1) / most;
+    return (int)((V + n - 1) / n + 255) / 256 * 256;
+}
+
+int vocab_piece(long long M, int C, int V, long long ldw, int wanted, lemo_dtype_t dt) {
+    const long long esz = dt == LEMO_BF16 ? 2 : 4, span = (1ll << 31) - 1;
+    long long piece = wanted > 0 ? (std::min(wanted, V) + 63) / 64 * 64ll : vl_choice(M, V, (int)esz);
+    piece = std::min(piece, vl_pitch(V));
+    piece = std::min(piece, span / (ldw * esz) / 64 * 64);       // the piece's rows of W, and
+    piece = std::min(piece, span / ((M + 1) * esz) / 64 * 64);   // G lie within 32-bit offsets,
+    piece = std::min(piece, ((8ll << 20) / esz - 64) / 64 * 64); // G's pitch within a load's
+    return piece < 64 ? 0 : (int)piece;
+}
+
+// forward: what the tiles, or binary32's pieces, leave
+struct LossSpace { float2* parts; float* sums; float* picked; float* logits; long long rows; int piece; size_t bytes; };
+static LossSpace loss_space(long long M, int C, int V, lemo_dtype_t dt, void* base) {
+    LossSpace s{};
+    s.rows = std::min(M, VL_ROWS);
+    s.piece = dt == LEMO_F32 ? std::min<int>(vl_choice(s.rows, V, 4), (int)vl_pitch(V)) : 0;
+    const size_t n = dt == LEMO_F32 ? (size_t)((V + s.piece - 1) / s.piece) : (size_t)(V + 127) / 128;
+    char* at = static_cast<char*>(base);
+    auto take = [&](size_t bytes) {
+        char* const here = at + s.bytes;
+        s.bytes += vl_round(bytes);
+        return here;
+    };
+    s.parts = reinterpret_cast<float2*>(take(n * s.rows * sizeof(float2)));
+    s.sums = reinterpret_cast<float*>(take(n * s.rows * sizeof(float)));
+    s.picked = reinterpret_cast<float*>(take(s.rows * sizeof(float)));
+    if (dt == LEMO_F32) s.logits = reinterpret_cast<float*>(take((size_t)s.rows * s.piece * sizeof(float)));
+    return s;
+}
+size_t vocab_loss_workspace(long long M, int C, int V, lemo_dtype_t dt) { return M > 0 ? loss_space(M, C, V, dt, nullptr).bytes : 0; }
+
+int prepare_vocab_loss(lemo_dtype_t dt) { return dt == LEMO_BF16 ? prepare_vocab_tiles() : prepare_gather_gemm_small(dt, false, GG_NT); }
+int prepare_vocab_grad(lemo_dtype_t dt) {
+    const int rc = prepare_vocab_loss(dt) ?: prepare_gather_gemm_dw(dt);
+    return rc || dt == LEMO_BF16 ? rc : prepare_gather_gemm_small(dt, true, GG_NT);
+}
+
+static unsigned vl_span(long long rows, long long ld, long long cols, int esz) { return (unsigned)(((rows - 1) * ld + cols) * esz); }
+
+int launch_vocab_loss(const VocabLossParams& p, lemo_dtype_t dt, hipStream_t st) {
+    int rc = prepare_vocab_loss(dt);
+    if (rc) return rc;
+    const int V = p.rule.V;
+    const LossSpace s = loss_space(p.M, p.C, V, dt, p.workspace);
+    float* const sums = p.rule.all != 0.f ? s.sums : nullptr;
+    for (long long m0 = 0; m0 < p.M; m0 += VL_ROWS) {
+        const long long M = std::min(VL_ROWS, p.M - m0);
+        const int* const idx = p.idx ? p.idx + m0 : nullptr;
+        const int esz = dt == LEMO_BF16 ? 2 : 4;
+        const char* const X = static_cast<const char*>(p.X) + (p.idx ? 0 : m0 * p.ldx * esz);  // (without a list the rows of X themselves move on)
+        const long long S = p.idx ? p.S : p.S - m0;
+        int n;
+        if (dt == LEMO_BF16) {
+            VocabTileParams t{};
+            t.A = X; t.B = p.W; t.idx = idx; t.lda = p.ldx; t.ldb = p.ldw; t.M = M; t.K = p.C; t.N = V;
+            t.a_bytes = vl_span(S, p.ldx, p.C, 2);
+            t.rule = p.rule; t.labels = p.labels + m0; t.parts = s.parts; t.sums = sums; t.picked = s.picked;
+            int one = 1;
+            const GgTile tile = gg_choose_tile(M, V, p.C, GG_NT, 1, 0., &one);
+            n = (V + vocab_tile_cols(tile) - 1) / vocab_tile_cols(tile);
+            rc = launch_vocab_tiles(t, VOCAB_STATS, tile, st);
+        } else {
+            n = 0;
+            for (int v0 = 0; v0 < V && rc == 0; v0 += s.piece, ++n) {
+                const int N = std::min(s.piece, V - v0);
+                rc = launch_gather_gemm(X, S, p.ldx, idx, M, static_cast<const float*>(p.W) + v0 * p.ldw, p.ldw, nullptr, s.logits, s.piece, p.C, N, dt, st);
+                if (rc) break;
+                rc = launch_in_turns(M, VL_THREADS, [&](long long first, unsigned count) {
+                    hipLaunchKernelGGL(vocab_stats_f32_kernel, dim3(count), dim3(VL_THREADS), 0, st, p.rule, s.logits, (long long)s.piece, N, v0, p.labels + m0, M,
+                                       s.parts + n * M, sums ? sums + n * M : nullptr, s.picked, first);
+                });
+            }
+        }
+        if (rc) return rc;
+        const int per = M >= 4096 ? 32 : 4;  // few rows: more threads a row, whose parts are as many as the vocabulary's tiles
+        hipLaunchKernelGGL(vocab_join_kernel, dim3((unsigned)((M + per - 1) / per)), dim3(VL_THREADS), 0, st, p.rule, s.parts, sums, s.picked, p.labels + m0, M, n, per,
+                           p.loss ? p.loss + m0 : nullptr, p.lse + m0);
+        rc = (int)hipGetLastError();
+        if (rc) return rc;
+    }
+    if (!p.total) return 0;
+    hipLaunchKernelGGL(vocab_total_kernel, dim3(1), dim3(1024), 0, st, p.loss, p.labels, p.M, V, p.total);
+    return (int)hipGetLastError();
+}
+
+// gradient: rows, G, and for dX the planes (bf16) or the weight's piece transposed (binary32)
+struct GradSpace { float* weight; int* rows; char* G; float* aside; long long ldg; GgTile tile; int splits, k_split; size_t bytes; };
+static GradSpace grad_space(long long M, int C, int V, int piece, lemo_dtype_t dt, void* base) {
+    GradSpace s{};
+    const int esz = dt == LEMO_BF16 ? 2 : 4;
+    s.ldg = vl_pitch(piece);
+    char* at = static_cast<char*>(base);
+    auto take = [&](size_t bytes) {
+        char* const here = at + s.bytes;
+        s.bytes += vl_round(bytes);
+        return here;
+    };
+    s.weight = reinterpret_cast<float*>(take((size_t)M * sizeof(float)));
+    s.rows = reinterpret_cast<int*>(take((size_t)(M + 1) * sizeof(int)));
+    s.G = take((size_t)(M + 1) * s.ldg * esz);
+    if (dt == LEMO_BF16) {
+        // a plane is written and read once for every piece: 8 bytes an element, at 4 TB/s
+        s.tile = gg_choose_tile(M, C, std::min(piece, V), GG_NN, 32, (double)M * C * 8e-6 / 4., &s.splits);
+        const int k = std::min(piece, V);
+        s.k_split = (k + s.splits * 64 - 1) / (s.splits * 64) * 64;
+        s.aside = reinterpret_cast<float*>(take((size_t)s.splits * M * C * sizeof(float)));
+    } else {
+        s.aside = reinterpret_cast<float*>(take((size_t)C * s.ldg * sizeof(float)));
+    }
+    return s;
+}
+size_t vocab_grad_workspace(long long M, int C, int V, int piece, lemo_dtype_t dt) { return M > 0 ? grad_space(M, C, V, piece, dt, nullptr).bytes : 0; }
+
+int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st) {
+    int rc = prepare_vocab_grad(dt);
+    if (rc) return rc;
+    const int V = p.rule.V, C = p.C, esz = dt == LEMO_BF16 ? 2 : 4;
+    if (p.M == 0) return p.dW ? launch_zero_matrix(p.dW, p.lddw, C, V, dt, st) : 0;
+    if (!p.dX && !p.dW) return 0;
+    const GradSpace s = grad_space(p.M, C, V, p.piece, dt, p.workspace);
+    hipLaunchKernelGGL(vocab_rows_kernel, dim3((unsigned)(p.M / VL_THREADS + 1)), dim3(VL_THREADS), 0, st, p.dloss, p.dloss_stride, p.labels, p.idx, p.M, p.S, V,
+                       s.weight, s.rows);
+    rc = (int)hipGetLastError();
+    if (rc) return rc;
+    const int e16 = 16 / esz;
+    if (V % e16) rc = launch_zero_matrix(s.G + p.M * s.ldg * esz, s.ldg, (int)s.ldg, 1, dt, st);  // (columns past the vocabulary: see vocab_rows_kernel)
+    if (rc) return rc;
+    for (int v0 = 0; v0 < V; v0 += p.piece) {
+        const int N = std::min(p.piece, V - v0), N16 = (N + e16 - 1) / e16 * e16;
+        const char* const W = static_cast<const char*>(p.W) + v0 * p.ldw * esz;
+        if (dt == LEMO_BF16) {
+            VocabTileParams t{};
+            t.A = p.X; t.B = W; t.idx = p.idx; t.lda = p.ldx; t.ldb = p.ldw; t.M = p.M; t.K = C; t.N = N;
+            t.a_bytes = vl_span(p.S, p.ldx, C, 2);
+            t.rule = p.rule; t.labels = p.labels; t.v0 = v0; t.lse = p.lse; t.weight = s.weight; t.G = s.G; t.ldg = s.ldg;
+            int one = 1;
+            rc = launch_vocab_tiles(t, VOCAB_PROBS, gg_choose_tile(p.M, N, C, GG_NT, 1, 0., &one), st);
+        } else {
+            rc = launch_gather_gemm(p.X, p.S, p.ldx, p.idx, p.M, W, p.ldw, nullptr, s.G, s.ldg, C, N, dt, st);
+            if (rc) return rc;
+            rc = launch_in_turns(p.M, VL_THREADS, [&](long long first, unsigned count) {
+                hipLaunchKernelGGL(vocab_probs_f32_kernel, dim3(count), dim3(VL_THREADS), 0, st, p.rule, reinterpret_cast<float*>(s.G), s.ldg, N, v0, p.labels, p.lse,
+                                   s.weight, first);
+            });
+        }
+        if (rc) return rc;
+        if (p.dW) {
+            rc = launch_gather_gemm_dw_direct(s.G, s.ldg, p.X, p.S, p.ldx, s.rows, p.M + (N % e16 != 0), static_cast<char*>(p.dW) + v0 * p.lddw * esz, p.lddw, C, N,
+                                              dt, st);
+            if (rc) return rc;
+        }
+        if (!p.dX) continue;
+        if (dt == LEMO_BF16) {
+            VocabTileParams t{};
+            t.A = s.G; t.B = W; t.lda = s.ldg; t.ldb = p.ldw; t.M = p.M; t.K = N; t.N = C;
+            t.a_bytes = vl_span(p.M, s.ldg, N16, 2);
+            t.planes = s.aside; t.k_split = s.k_split; t.add = v0 > 0;
+            t.splits = (N + s.k_split - 1) / s.k_split;  // (the last piece may be shorter: its parts that are empty leave their planes as they are)
+            rc = launch_vocab_tiles(t, VOCAB_PLANES, s.tile, st);
+        } else {
+            const long long pad = vl_pitch(N);
+            rc = launch_transpose(W, p.ldw, nullptr, N, pad, C, s.aside, st);
+            if (rc) return rc;
+            rc = v0 == 0 ? launch_gather_gemm(s.G, p.M, s.ldg, nullptr, p.M, s.aside, pad, nullptr, p.dX, p.lddx, N16, C, dt, st)
+                         : launch_gather_gemm_add(s.G, p.M, s.ldg, nullptr, p.M, s.aside, pad, nullptr, p.dX, p.lddx, p.M, nullptr, N16, C, dt, st);
+        }
+        if (rc) return rc;
+    }
+    if (!p.dX || dt == LEMO_F32) return 0;
+    return launch_in_turns((p.M * (C / 8) + VL_THREADS - 1) / VL_THREADS, VL_THREADS, [&](long long first, unsigned count) {
+        hipLaunchKernelGGL(vocab_planes_kernel, dim3(count), dim3(VL_THREADS), 0, st, s.aside, s.splits, p.M, C, p.dX, p.lddx, first);
+    });
+}
+
+}  // namespace lemo

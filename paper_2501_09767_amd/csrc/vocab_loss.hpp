@@ -1,0 +1,67 @@
+// Parameter blocks and launchers of the loss over a vocabulary (vocab_loss.hip, vocab_loss_tiles.hip).
+#pragma once
+#include "gather_gemm.hpp"
+
+namespace lemo {
+
+// What turns logits into losses: u = softcap tanh(x / softcap) (0: u = x), hit = 1 - smoothing, all = smoothing / V.
+struct VocabRule {
+    float softcap, hit, all, z;
+    int V;
+};
+
+// A product of the rows with (a piece of) the head's weight and what is done with a tile of it.  GgParams: A = X [S, C], idx = the kept rows, B = the piece's
+// first row of W, M, N = the piece's columns, K = C; for the planes A = G, B = W (contraction-major), K = the piece's columns, N = C.
+struct VocabTileParams : GgParams {
+    VocabRule rule;
+    const int* labels;     // [M]
+    int v0;                // the piece's first column in the vocabulary
+    float2* parts;         // statistics: [tiles_n][M] maximum, sum of exponentials
+    float* sums;           // statistics: [tiles_n][M] sums of the logits, or null (no smoothing)
+    float* picked;         // statistics: [M] the labels' logits
+    const float* lse;      // probabilities: [M]
+    const float* weight;   // probabilities: [M] gradients of the losses
+    void* G;               // probabilities: [M, ldg] bf16, columns from N up to a multiple of 8 are zeros
+    long long ldg;
+    float* planes;         // planes: [splits][M][N]
+    int splits, k_split;   // planes: of the contraction, and its length of each (a multiple of 64)
+    int add;               // planes: to what they hold
+};
+enum { VOCAB_STATS, VOCAB_PROBS, VOCAB_PLANES };
+int prepare_vocab_tiles();
+int launch_vocab_tiles(VocabTileParams p, int what, GgTile tile, hipStream_t st);
+// tiles of a launch of one kind along the columns
+int vocab_tile_cols(GgTile tile);
+
+struct VocabLossParams {
+    const void *X, *W;
+    const int *idx, *labels;
+    long long S, ldx, ldw, M;
+    int C;
+    VocabRule rule;
+    float *loss, *lse, *total;  // loss, total: or null
+    void* workspace;
+};
+struct VocabGradParams {
+    const void *X, *W;
+    const int *idx, *labels;
+    long long S, ldx, ldw, M;
+    int C;
+    VocabRule rule;
+    const float *lse, *dloss;
+    long long dloss_stride;
+    void *dX, *dW;  // or null
+    long long lddx, lddw;
+    int piece;
+    void* workspace;
+};
+int prepare_vocab_loss(lemo_dtype_t dt);
+int prepare_vocab_grad(lemo_dtype_t dt);
+size_t vocab_loss_workspace(long long M, int C, int V, lemo_dtype_t dt);
+int launch_vocab_loss(const VocabLossParams& p, lemo_dtype_t dt, hipStream_t st);
+// columns of a piece for a wanted number of them (0: this library's choice); 0: no piece fits the operands' 32-bit offsets
+int vocab_piece(long long M, int C, int V, long long ldw, int wanted, lemo_dtype_t dt);
+size_t vocab_grad_workspace(long long M, int C, int V, int piece, lemo_dtype_t dt);
+int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st);
+
+}  // namespace lemo

@@ -1,0 +1,228 @@
+// The products of the loss over a vocabulary (bf16), on the main loops of the selective-load GEMM, with what is done to a tile while it is still in
+// registers:
+//
+//   statistics      x = X[idx] W^T: of every row of a tile its largest logit, the sum of exponentials against that, the sum of logits (smoothed
+//                   labels) and the label's logit.  8 to 12 bytes a row leave the tile in the place of 512.
+//   probabilities   the same product again, turned into the gradient of the logits with the row's log-sum-exp: G, bf16, one piece of the
+//                   vocabulary at a time.  bf16 because the two products that follow take it so: off by 2^-9 of each element, at random.
+//   planes          dX = G W over the piece's columns, in binary32: a piece adds to what the pieces before left, and where the
+//                   output has few tiles the contraction is split, with a plane for each part; a kernel of its own rounds their sum once.
+//
+// What bounds it: the matrix cores, as in gather_gemm_large.hip; the epilogues read no memory but a few bytes a row.
+#include "gather_gemm_tiles.hpp"
+#include "vocab_softmax.hpp"
+
+namespace lemo {
+
+// A tile kind: UA = 0 the 256 x 256 tile, otherwise 64 UA x 128.  A lane holds ROWS rows (one of each 16-row tile of its wave) by 4 x 4 columns.
+template <int LAYOUT, int UA> struct VocabTile {
+    static constexpr bool LARGE = UA == 0;
+    static constexpr int BM = LARGE ? LG_BM : 64 * UA, BN = LARGE ? LG_BN : 128;
+    static constexpr int ROWS = LARGE ? 2 * LG_TA : UA, ACROSS = LARGE ? LG_WN : 2;  // ACROSS: waves along the columns
+    static constexpr int PITCH = BN * 2 + 16;                                         // of a row of bf16 in LDS
+    static constexpr int LDS_LOOP = LARGE ? LG_LDS : MdGeo<LAYOUT, LARGE ? 1 : UA>::LDS;
+    static constexpr int LDS = LDS_LOOP > BM * PITCH ? LDS_LOOP : BM * PITCH;
+    static constexpr int GROUP = LARGE ? 4 : UA <= 2 ? 16 / UA : 4;  // tile rows walked together
+    using Acc = std::conditional_t<LARGE, f32x4[2][LG_TA][2][LG_TB], f32x4[LARGE ? 1 : UA][MD_TB]>;
+    static_assert(LDS <= 160 * 1024 && ACROSS * BM * 12 <= LDS, "a workgroup's LDS");
+
+    __device__ static __forceinline__ void product(const GgParams& p, long long m0, int n0, char* smem, Acc& acc) {
+        if constexpr (LARGE) lg_product<LAYOUT>(p, m0, n0, smem, acc);
+        else md_product<LAYOUT, UA>(p, m0, n0, smem, acc);
+    }
+    __device__ static __forceinline__ f32x4& at(Acc& acc, int i, int j) {
+        if constexpr (LARGE) return acc[i / LG_TA][i % LG_TA][j / LG_TB][j % LG_TB];
+        else return acc[i][j];
+    }
+    __device__ static __forceinline__ int across(int wave) { return LARGE ? wave % LG_WN : wave & 1; }
+    __device__ static __forceinline__ int row(int wave, int lane, int i) {
+        if constexpr (LARGE) return i / LG_TA * 128 + (wave / LG_WN * LG_TA + i % LG_TA) * 16 + (lane & 15);
+        else return md_a_tile<LAYOUT, LARGE ? 1 : UA>(wave >> 1, i) * 16 + (lane & 15);
+    }
+    __device__ static __forceinline__ int col(int wave, int lane, int j) {  // the first of four
+        if constexpr (LARGE) return j / LG_TB * 128 + (wave % LG_WN * LG_TB + j % LG_TB) * 16 + (lane >> 4) * 4;
+        else return ((wave & 1) * MD_TB + j) * 16 + (lane >> 4) * 4;
+    }
+};
+
+// the lanes of a row: lane, lane ^ 16, lane ^ 32, lane ^ 48
+__device__ __forceinline__ float row_lanes_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float row_lanes_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+template <int WHAT, int UA>
+__global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTileParams p) {
+    constexpr int LAYOUT = WHAT == VOCAB_PLANES ? GG_NN : GG_NT;
+    using Tile = VocabTile<LAYOUT, UA>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int tm, tn, block = blockIdx.x, split = 0;
+    GgParams q = p;
+    if constexpr (WHAT == VOCAB_PLANES) {
+        const int each = (p.tiles_m * p.tiles_n + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
+        split = block / each;
+        block -= split * each;
+        const int k0 = split * p.k_split;  // (host: below the contraction's length for every split)
+        q.A = static_cast<const bf16_t*>(p.A) + k0;
+        q.B = static_cast<const bf16_t*>(p.B) + (long long)k0 * p.ldb;
+        q.K = min(p.k_split, p.K - k0);
+        q.a_bytes = p.a_bytes - (unsigned)k0 * 2u;
+    }
+    if (!gg_tile(block, p.tiles_m, p.tiles_n, Tile::GROUP, tm, tn)) return;
+    const long long m0 = (long long)tm * Tile::BM;
+    const int n0 = tn * Tile::BN;
+    typename Tile::Acc acc;
+    Tile::product(q, m0, n0, smem, acc);
+
+    if constexpr (WHAT == VOCAB_PLANES) {
+        float* const plane = p.planes + (long long)split * p.M * p.N;
+#pragma unroll
+        for (int i = 0; i < Tile::ROWS; ++i) {
+            const long long m = m0 + Tile::row(wave, lane, i);
+            if (m >= p.M) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int n = n0 + Tile::col(wave, lane, j);
+                if (n >= p.N) continue;  // (N is a multiple of 8)
+                f32x4* const to = reinterpret_cast<f32x4*>(plane + m * p.N + n);
+                f32x4 v = Tile::at(acc, i, j);
+                if (p.add) v += *to;
+                *to = v;
+            }
+        }
+        return;
+    }
+    const bool whole = n0 + Tile::BN <= p.N, capped = p.rule.softcap > 0.f;
+    const float inv_cap = capped ? 1.f / p.rule.softcap : 0.f;
+    if (capped) {
+#pragma unroll
+        for (int i = 0; i < Tile::ROWS; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) Tile::at(acc, i, j)[r] = vocab_cap(Tile::at(acc, i, j)[r], p.rule.softcap, inv_cap);
+    }
+    if constexpr (WHAT == VOCAB_STATS) {
+        float* const red = reinterpret_cast<float*>(smem);  // [3][ACROSS][BM]: maxima, sums of exponentials, sums
+#pragma unroll
+        for (int i = 0; i < Tile::ROWS; ++i) {
+            const int row = Tile::row(wave, lane, i);
+            const long long m = min(m0 + row, p.M - 1);
+            const unsigned label = (unsigned)p.labels[m] - (unsigned)(p.v0 + n0);  // column in the tile (a label outside the vocabulary is none of those below N)
+            float top = -INFINITY, sum = 0.f, all = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f32x4& v = Tile::at(acc, i, j);
+                const int c = Tile::col(wave, lane, j);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (!whole && n0 + c + r >= p.N) v[r] = -INFINITY;
+                    else if ((unsigned)(c + r) == label) p.picked[m] = v[r];
+                    top = fmaxf(top, v[r]);
+                }
+            }
+            top = row_lanes_max(top);
+            const float base = top == -INFINITY ? 0.f : top * LOG2E;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(Tile::at(acc, i, j)[r], LOG2E, -base));
+            sum = row_lanes_sum(sum);
+            if (p.sums) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) all += whole || n0 + Tile::col(wave, lane, j) + r < p.N ? Tile::at(acc, i, j)[r] : 0.f;
+                all = row_lanes_sum(all);
+            }
+            if (lane < 16) {
+                float* const to = red + Tile::across(wave) * Tile::BM + row;
+                to[0] = top;
+                to[Tile::ACROSS * Tile::BM] = sum;
+                to[2 * Tile::ACROSS * Tile::BM] = all;
+            }
+        }
+        __syncthreads();
+        const int row = tid;
+        if (row < Tile::BM && m0 + row < p.M) {
+            float top = red[row], sum = red[Tile::ACROSS * Tile::BM + row], all = red[2 * Tile::ACROSS * Tile::BM + row];
+#pragma unroll
+            for (int w = 1; w < Tile::ACROSS; ++w) {
+                const float* const from = red + w * Tile::BM + row;
+                vocab_join(top, sum, from[0], from[Tile::ACROSS * Tile::BM]);
+                all += from[2 * Tile::ACROSS * Tile::BM];
+            }
+            const long long to = (long long)tn * p.M + m0 + row;
+            p.parts[to] = make_float2(top, sum);
+            if (p.sums) p.sums[to] = all;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < Tile::ROWS; ++i) {
+            const int row = Tile::row(wave, lane, i);
+            const long long m = min(m0 + row, p.M - 1);
+            const VocabRow of = vocab_row(p.rule, p.lse[m], p.weight[m], p.labels[m]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int c = Tile::col(wave, lane, j);
+                float g[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    g[r] = vocab_grad(p.rule, of, Tile::at(acc, i, j)[r], p.v0 + n0 + c + r, inv_cap);
+                    if (!whole && n0 + c + r >= p.N) g[r] = 0.f;
+                }
+                *reinterpret_cast<uint2*>(smem + row * Tile::PITCH + c * 2) = make_uint2(pack_bf16x2_hw(g[0], g[1]), pack_bf16x2_hw(g[2], g[3]));
+            }
+        }
+        __syncthreads();
+        constexpr int LPR = Tile::BN / 8, RPP = 64 / LPR, OWN = Tile::BM / RG_WAVES;  // lanes of a row, rows at a time, rows of a wave
+        const int c = lane % LPR * 8;
+        if (n0 + c >= p.N) return;
+#pragma unroll 4
+        for (int k = 0; k < OWN / RPP; ++k) {
+            const int row = wave * OWN + k * RPP + lane / LPR;
+            if (m0 + row >= p.M) continue;
+            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.G) + (m0 + row) * p.ldg + n0 + c) = *reinterpret_cast<const u32x4*>(smem + row * Tile::PITCH + c * 2);
+        }
+    }
+}
+
+template <int WHAT, int UA> constexpr LdsLimit vocab_limit() {
+    return {reinterpret_cast<const void*>(&vocab_tile_kernel<WHAT, UA>), VocabTile<WHAT == VOCAB_PLANES ? GG_NN : GG_NT, UA>::LDS};
+}
+template <int WHAT> static int prepare_what() {
+    static const int err = raise_lds_limits({vocab_limit<WHAT, 0>(), vocab_limit<WHAT, 1>(), vocab_limit<WHAT, 2>(), vocab_limit<WHAT, 4>()});
+    return err;
+}
+int prepare_vocab_tiles() { return first_error(prepare_what<VOCAB_STATS>, prepare_what<VOCAB_PROBS>, prepare_what<VOCAB_PLANES>); }
+
+int vocab_tile_cols(GgTile tile) { return tile == GG_T256 ? 256 : 128; }
+
+template <int WHAT, int UA> static int launch_one(VocabTileParams p, hipStream_t st) {
+    using Tile = VocabTile<WHAT == VOCAB_PLANES ? GG_NN : GG_NT, UA>;
+    p.tiles_m = (int)((p.M + Tile::BM - 1) / Tile::BM);
+    p.tiles_n = (p.N + Tile::BN - 1) / Tile::BN;
+    const long long blocks = ((long long)p.tiles_m * p.tiles_n + NUM_XCD - 1) / NUM_XCD * NUM_XCD * (WHAT == VOCAB_PLANES ? p.splits : 1);
+    if (blocks * RG_THREADS >= 1ll << 32) return (int)hipErrorInvalidValue;  // (the callers' pieces are far below)
+    hipLaunchKernelGGL((vocab_tile_kernel<WHAT, UA>), dim3((unsigned)blocks), dim3(RG_THREADS), Tile::LDS, st, p);
+    return (int)hipGetLastError();
+}
+template <int WHAT> static int launch_what(const VocabTileParams& p, GgTile tile, hipStream_t st) {
+    switch (tile) {
+        case GG_T256: return launch_one<WHAT, 0>(p, st);
+        case GG_T256x128: return launch_one<WHAT, 4>(p, st);
+        case GG_T128: return launch_one<WHAT, 2>(p, st);
+        default: return launch_one<WHAT, 1>(p, st);
+    }
+}
+int launch_vocab_tiles(VocabTileParams p, int what, GgTile tile, hipStream_t st) {
+    return what == VOCAB_STATS ? launch_what<VOCAB_STATS>(p, tile, st) : what == VOCAB_PROBS ? launch_what<VOCAB_PROBS>(p, tile, st) : launch_what<VOCAB_PLANES>(p, tile, st);
+}
+
+}  // namespace lemo

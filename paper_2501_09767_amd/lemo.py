@@ -36,7 +36,8 @@ EXPORTS = ("lemo_strerror", "lemo_keep_k", "lemo_kept_count", "lemo_score_worksp
            "lemo_block_attention_grad_workspace_bytes", "lemo_block_attention_grad", "lemo_block_means_step", "lemo_select_blocks_step",
            "lemo_block_attention_step_workspace_bytes", "lemo_block_attention_step",
            "lemo_qk_rotate", "lemo_qk_rotate_grad_workspace_bytes", "lemo_qk_rotate_grad", "lemo_qk_rotate_step",
-           "lemo_dropout_add", "lemo_dropout_add_grad")
+           "lemo_dropout_add", "lemo_dropout_add_grad",
+           "lemo_vocab_loss_workspace_bytes", "lemo_vocab_loss", "lemo_vocab_loss_grad_workspace_bytes", "lemo_vocab_loss_grad")
 
 
 class LemoError(RuntimeError):
@@ -122,7 +123,9 @@ def _load() -> ctypes.CDLL:
                        ("qk_rotate", "pll" "pll" "l" "iiii" "plpi" "fi" "pp" "fu" "pll" "pll" "p"), ("qk_rotate_grad_workspace_bytes", "liiiius"),
                        ("qk_rotate_grad", "pll" "pll" "pll" "pll" "l" "iiii" "plpi" "fi" "pp" "fu" "pll" "pll" "pp" "pzp"),
                        ("qk_rotate_step", "pll" "pll" "pll" "il" "iiii" "ppi" "fi" "pp" "fu" "pll" "plll" "plll" "p"),
-                       ("dropout_add", "plpll" "pl" "dpq" "ii" "p"), ("dropout_add_grad", "pll" "pl" "dpq" "pl" "ii" "p")):
+                       ("dropout_add", "plpll" "pl" "dpq" "ii" "p"), ("dropout_add_grad", "pll" "pl" "dpq" "pl" "ii" "p"),
+                       ("vocab_loss_workspace_bytes", "liiis"), ("vocab_loss", "pllpl" "pl" "iii" "p" "fff" "ppp" "pzp"),
+                       ("vocab_loss_grad_workspace_bytes", "liiliis"), ("vocab_loss_grad", "pl" "pllpl" "pl" "iii" "pp" "fff" "plpl" "i" "pzp")):
         fn = getattr(lib, "lemo_" + name)
         fn.restype = ctypes.c_int
         fn.argtypes = [kinds[k] for k in args]
@@ -1132,3 +1135,61 @@ def lemo_dropout_add_grad(dR: torch.Tensor, kept_idx: Optional[torch.Tensor], rn
     _check(_lib.lemo_dropout_add_grad(_ptr(dR), lddr, S, _ptr(kept_idx), M, float(p), _ptr(rng), int(site) & (2 ** 64 - 1), _ptr(dY), lddy, C, _dt(dR),
                                       _stream()), "lemo_dropout_add_grad")
     return dY
+
+
+# --------------------------------------------------------------------------------- the loss over a vocabulary
+
+class VocabLoss(NamedTuple):
+    loss: torch.Tensor   # [M] float32, 0 for rows that do not count
+    lse: torch.Tensor    # [M] float32, what the gradient takes
+    total: torch.Tensor  # [4] float32: sum, number of rows that count, mean, 1 / number
+
+
+def _head(X, kept_idx, W, labels):
+    """S, C, M, V and the row strides of the loss's operands."""
+    if X.dim() != 2 or W.dim() != 2 or X.shape[1] != W.shape[1] or X.dtype != W.dtype or any(t.stride(1) != 1 and t.shape[1] > 1 for t in (X, W)):
+        raise ValueError("X must be [S,C], W [V,C], same dtype, rows contiguous")
+    _dt(X)
+    S, C = X.shape
+    M = labels.numel()
+    _index(labels, M, "labels")
+    _index(kept_idx, M, "kept_idx")
+    return S, C, M, W.shape[0], X.stride(0) if S > 1 else C, W.stride(0) if W.shape[0] > 1 else C
+
+
+def lemo_vocab_loss(X: torch.Tensor, kept_idx: Optional[torch.Tensor], W: torch.Tensor, labels: torch.Tensor, *, softcap: float = 0.0, smoothing: float = 0.0,
+                    z_weight: float = 0.0, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> VocabLoss:
+    """Cross entropy of the kept rows of X [S,C] over the vocabulary of W [V,C], labels [M] int32 (outside [0,V): the row does not count)."""
+    _here(X, kept_idx, W, labels, loss, lse, total, workspace)
+    S, C, M, V, ldx, ldw = _head(X, kept_idx, W, labels)
+    loss = _filled(loss, (M,), torch.float32, X.device, "loss")
+    lse = _filled(lse, (M,), torch.float32, X.device, "lse")
+    total = _filled(total, (4,), torch.float32, X.device, "total")
+    workspace, size = _scratch(workspace, _bytes("lemo_vocab_loss_workspace_bytes", M, C, V, _dt(X)), X.device)
+    _check(_lib.lemo_vocab_loss(_ptr(X), S, ldx, _ptr(kept_idx), M, _ptr(W), ldw, C, V, _dt(X), _ptr(labels), float(softcap), float(smoothing), float(z_weight),
+                                _ptr(loss), _ptr(lse), _ptr(total), _ptr(workspace), size, _stream()), "lemo_vocab_loss")
+    return VocabLoss(loss, lse, total)
+
+
+def lemo_vocab_loss_grad(dloss: torch.Tensor, X: torch.Tensor, kept_idx: Optional[torch.Tensor], W: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor, *,
+                         softcap: float = 0.0, smoothing: float = 0.0, z_weight: float = 0.0, want_dX: bool = True, want_dW: bool = True,
+                         dX: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None, piece: int = 0, workspace: Optional[torch.Tensor] = None):
+    """Gradients of lemo_vocab_loss from dloss [M], or one value for all rows [1] (the mean's: total[3:]) -> (dX [M,C], dW [V,C]), either None if not
+    wanted.  piece: columns of the vocabulary at a time."""
+    _here(dloss, X, kept_idx, W, labels, lse, dX, dW, workspace)
+    S, C, M, V, ldx, ldw = _head(X, kept_idx, W, labels)
+    if dloss.dtype != torch.float32 or dloss.dim() != 1 or dloss.numel() not in (1, M) or not dloss.is_contiguous():
+        raise ValueError("dloss must be contiguous float32 [M] or [1]")
+    _filled(lse, (M,), torch.float32, None, "lse")
+    if want_dX and dX is None:
+        dX = torch.empty((M, C), dtype=X.dtype, device=X.device)
+    if want_dW and dW is None:
+        dW = torch.empty((V, C), dtype=X.dtype, device=X.device)
+    dX, dW = dX if want_dX else None, dW if want_dW else None
+    lddx, lddw = _rows_of(dX, M, C, X.dtype, "dX"), _rows_of(dW, V, C, X.dtype, "dW")
+    workspace, size = _scratch(workspace, _bytes("lemo_vocab_loss_grad_workspace_bytes", M, C, V, ldw, _dt(X), int(piece)), X.device)
+    _check(_lib.lemo_vocab_loss_grad(_ptr(dloss), 1 if dloss.numel() == M else 0, _ptr(X), S, ldx, _ptr(kept_idx), M, _ptr(W), ldw, C, V, _dt(X), _ptr(labels),
+                                     _ptr(lse), float(softcap), float(smoothing), float(z_weight), _ptr(dX), lddx, _ptr(dW), lddw, int(piece), _ptr(workspace),
+                                     size, _stream()), "lemo_vocab_loss_grad")
+    return dX, dW
