@@ -81,12 +81,12 @@ static GgPlan gg_plan(long long M, int N, int K, int layout, lemo_dtype_t dt) {
 }
 
 // The kind of eight-wave tiles for a product as a whole, and into how many parts of the contraction it is cut where a part costs `split_us`
-// (X W^T: into one).
+// (one part where `most_splits` is 1).
 GgTile gg_choose_tile(long long M, int N, int K, int layout, int most_splits, double split_us, int* splits) {
-    const GgFit* fits = layout == GG_NN ? mixed : along;
+    const GgFit* fits = layout == GG_NN ? mixed : layout == GG_NT ? along : across;
     GgTile best = GG_T256;
     double least = INFINITY;
-    for (int t = 0; t < 5; ++t) {
+    for (int t = 0; fits[t].tile != GG_T64; ++t) {
         if (fits[t].tile == GG_T192x128) continue;
         for (int s = 1; s <= most_splits; s *= 2) {
             const int k = (K + s * 64 - 1) / (s * 64);  // slabs of a part

@@ -59,6 +59,6 @@ int prepare_gather_gemm_small(lemo_dtype_t dt, bool add, int layout);
 int launch_gather_gemm_large(const GgParams& p, bool add, int layout, hipStream_t st);               // GG_T256, bf16
 int launch_gather_gemm_mid(const GgParams& p, bool add, int layout, GgTile tile, hipStream_t st);    // the kinds of 128 columns, bf16
 int launch_gather_gemm_small(const GgParams& p, lemo_dtype_t dt, bool add, int layout, GgTile tile, hipStream_t st);
-GgTile gg_choose_tile(long long M, int N, int K, int layout, int most_splits, double split_us, int* splits);  // GG_NT, GG_NN, bf16
+GgTile gg_choose_tile(long long M, int N, int K, int layout, int most_splits, double split_us, int* splits);  // bf16
 
 }  // namespace lemo

@@ -92,30 +92,43 @@ __global__ __launch_bounds__(1024) void vocab_total_kernel(const float* loss, co
     total[3] = n ? (float)(1. / (double)n) : 0.f;
 }
 
-// What the gradient's products take of the rows: their losses' gradients side by side, and for the weight's gradient the rows of X, those without a
-// label replaced by one past X's end, which the loads' range check turns into zeros whatever such a row holds.  Row M is one more of those:
-// the last row of G a product reads is then one of zeros, whose last piece of columns may end in the operand's middle.
-__global__ __launch_bounds__(VL_THREADS) void vocab_rows_kernel(const float* dloss, long long stride, const int* labels, const int* idx, long long M, long long S,
-                                                                int V, float* weight, int* rows) {
-    const long long m = (long long)blockIdx.x * VL_THREADS + threadIdx.x;
-    if (m > M) return;
-    const bool counts = m < M && labels[m] >= 0 && labels[m] < V;
-    rows[m] = (int)(!counts ? S : idx ? (long long)idx[m] : m);
-    if (m < M) weight[m] = counts ? dloss[m * stride] : 0.f;
+// What the gradient's products take of the rows: their losses' gradients side by side (ones, where one gradient for all is left out of G), and for the
+// weight's gradient the rows of X, those without a label replaced by one past X's end, which the loads' range check turns into zeros
+// whatever such a row holds.  Row M is one more of those, and of zeros in G where `zeros` is given: the last row of G a product reads is then
+// one of zeros, whose last piece of columns may end in the operand's middle.
+__global__ __launch_bounds__(VL_THREADS) void vocab_rows_kernel(const float* dloss, long long stride, int ones, const int* labels, const int* idx, long long M,
+                                                                long long S, int V, float* weight, int* rows, u32x4* zeros, long long pieces) {
+    const long long at = (long long)blockIdx.x * VL_THREADS + threadIdx.x, all = (long long)gridDim.x * VL_THREADS;
+    for (long long m = at; m <= M; m += all) {
+        const bool counts = m < M && labels[m] >= 0 && labels[m] < V;
+        rows[m] = (int)(!counts ? S : idx ? (long long)idx[m] : m);
+        if (m < M) weight[m] = !counts ? 0.f : ones ? 1.f : dloss[m * stride];
+    }
+    if (zeros)
+        for (long long i = at; i < pieces; i += all) zeros[i] = u32x4{0u, 0u, 0u, 0u};
 }
 
-// dX = the sum of the planes, rounded once.  A thread has eight columns of a row.
-__global__ __launch_bounds__(VL_THREADS) void vocab_planes_kernel(const float* planes, int n, long long M, int C, void* dX, long long lddx, long long first) {
+// dX = the sum of the planes and the label's row of W times what G's rounding has left of its element, times the gradient that was left out of G,
+// rounded once.  A thread has eight columns of a row.
+__global__ __launch_bounds__(VL_THREADS) void vocab_planes_kernel(const float* planes, int n, const float* rest, const float* scale, const int* labels, int V,
+                                                                  const void* W, long long ldw, long long M, int C, void* dX, long long lddx, long long first) {
     const long long per_row = C / 8, i = (first + blockIdx.x) * VL_THREADS + threadIdx.x;
     const long long m = i / per_row;
     if (m >= M) return;
-    const int c = (int)(i - m * per_row) * 8;
+    const int c = (int)(i - m * per_row) * 8, label = labels[m];
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < n; ++s) {
-        const f32x4* const at = reinterpret_cast<const f32x4*>(planes + ((long long)s * M + m) * C + c);
-        const f32x4 lo = at[0], hi = at[1];
+    if (label >= 0 && label < V) {
+        const float left = rest[m], by = scale ? *scale : 1.f;
+        float w[8];
+        RowPiece<bf16_t>::get(row_load<bf16_t>(W, label * ldw + c), w);
+        for (int s = 0; s < n; ++s) {
+            const f32x4* const at = reinterpret_cast<const f32x4*>(planes + ((long long)s * M + m) * C + c);
+            const f32x4 lo = at[0], hi = at[1];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { v[e] += lo[e]; v[e + 4] += hi[e]; }
+            for (int e = 0; e < 4; ++e) { v[e] += lo[e]; v[e + 4] += hi[e]; }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(left, w[e], v[e]) * by;
     }
     row_store<bf16_t>(dX, m * lddx + c, RowPiece<bf16_t>::put(v));
 }
@@ -220,8 +233,9 @@ size_t vocab_loss_workspace(long long M, int C, int V, lemo_dtype_t dt) { return
 
 int prepare_vocab_loss(lemo_dtype_t dt) { return dt == LEMO_BF16 ? prepare_vocab_tiles() : prepare_gather_gemm_small(dt, false, GG_NT); }
 int prepare_vocab_grad(lemo_dtype_t dt) {
-    const int rc = prepare_vocab_loss(dt) ?: prepare_gather_gemm_dw(dt);
-    return rc || dt == LEMO_BF16 ? rc : prepare_gather_gemm_small(dt, true, GG_NT);
+    if (dt == LEMO_BF16) return prepare_vocab_tiles();
+    const int rc = first_error([&] { return prepare_vocab_loss(dt); }, [&] { return prepare_gather_gemm_dw(dt); });
+    return rc ? rc : prepare_gather_gemm_small(dt, true, GG_NT);
 }
 
 static unsigned vl_span(long long rows, long long ld, long long cols, int esz) { return (unsigned)(((rows - 1) * ld + cols) * esz); }
@@ -273,7 +287,7 @@ int launch_vocab_loss(const VocabLossParams& p, lemo_dtype_t dt, hipStream_t st)
 }
 
 // gradient: rows, G, and for dX the planes (bf16) or the weight's piece transposed (binary32)
-struct GradSpace { float* weight; int* rows; char* G; float* aside; long long ldg; GgTile tile; int splits, k_split; size_t bytes; };
+struct GradSpace { float *weight, *rest; int* rows; char* G; float* aside; long long ldg; GgTile tile; int splits, k_split; size_t bytes; };
 static GradSpace grad_space(long long M, int C, int V, int piece, lemo_dtype_t dt, void* base) {
     GradSpace s{};
     const int esz = dt == LEMO_BF16 ? 2 : 4;
@@ -285,6 +299,7 @@ static GradSpace grad_space(long long M, int C, int V, int piece, lemo_dtype_t d
         return here;
     };
     s.weight = reinterpret_cast<float*>(take((size_t)M * sizeof(float)));
+    s.rest = reinterpret_cast<float*>(take((size_t)M * sizeof(float)));
     s.rows = reinterpret_cast<int*>(take((size_t)(M + 1) * sizeof(int)));
     s.G = take((size_t)(M + 1) * s.ldg * esz);
     if (dt == LEMO_BF16) {
@@ -300,6 +315,55 @@ static GradSpace grad_space(long long M, int C, int V, int piece, lemo_dtype_t d
 }
 size_t vocab_grad_workspace(long long M, int C, int V, int piece, lemo_dtype_t dt) { return M > 0 ? grad_space(M, C, V, piece, dt, nullptr).bytes : 0; }
 
+// bf16: one piece.  W: its first row.
+static int grad_piece_bf16(const VocabGradParams& p, const GradSpace& s, int v0, int N, const void* W, hipStream_t st) {
+    int one = 1;
+    VocabTileParams t{};
+    t.A = p.X; t.B = W; t.idx = p.idx; t.lda = p.ldx; t.ldb = p.ldw; t.M = p.M; t.K = p.C; t.N = N;
+    t.a_bytes = vl_span(p.S, p.ldx, p.C, 2);
+    t.rule = p.rule; t.labels = p.labels; t.v0 = v0; t.lse = p.lse; t.weight = s.weight; t.rest = s.rest; t.G = s.G; t.ldg = s.ldg;
+    int rc = launch_vocab_tiles(t, VOCAB_PROBS, gg_choose_tile(p.M, N, p.C, GG_NT, 1, 0., &one), st);
+    if (rc) return rc;
+    if (p.dW) {
+        VocabTileParams g{};
+        g.A = s.G; g.B = p.X; g.idx = s.rows; g.lda = s.ldg; g.ldb = p.ldx; g.M = N; g.N = p.C;
+        g.K = (int)p.M + (N % 8 != 0);
+        g.Y = static_cast<char*>(p.dW) + v0 * p.lddw * 2; g.ldy = p.lddw;
+        g.b_bytes = vl_span(p.S, p.ldx, p.C, 2);
+        g.scale = p.dloss_stride == 0 ? p.dloss : nullptr;
+        rc = launch_vocab_tiles(g, VOCAB_WEIGHT, gg_choose_tile(N, p.C, g.K, GG_TN, 1, 0., &one), st);
+        if (rc) return rc;
+    }
+    if (!p.dX) return 0;
+    VocabTileParams x{};
+    x.A = s.G; x.B = W; x.lda = s.ldg; x.ldb = p.ldw; x.M = p.M; x.K = N; x.N = p.C;
+    x.a_bytes = vl_span(p.M, s.ldg, (N + 7) / 8 * 8, 2);
+    x.planes = s.aside; x.k_split = s.k_split; x.add = v0 > 0;
+    x.splits = (N + s.k_split - 1) / s.k_split;  // (the last piece may be shorter: its parts that are empty leave their planes as they are)
+    return launch_vocab_tiles(x, VOCAB_PLANES, s.tile, st);
+}
+
+static int grad_piece_f32(const VocabGradParams& p, const GradSpace& s, int v0, int N, const float* W, hipStream_t st) {
+    const int N4 = (N + 3) / 4 * 4;
+    float* const G = reinterpret_cast<float*>(s.G);
+    int rc = launch_gather_gemm(p.X, p.S, p.ldx, p.idx, p.M, W, p.ldw, nullptr, G, s.ldg, p.C, N, LEMO_F32, st);
+    if (rc) return rc;
+    rc = launch_in_turns(p.M, VL_THREADS, [&](long long first, unsigned count) {
+        hipLaunchKernelGGL(vocab_probs_f32_kernel, dim3(count), dim3(VL_THREADS), 0, st, p.rule, G, s.ldg, N, v0, p.labels, p.lse, s.weight, first);
+    });
+    if (rc) return rc;
+    if (p.dW) {
+        rc = launch_gather_gemm_dw_direct(G, s.ldg, p.X, p.S, p.ldx, s.rows, p.M + (N % 4 != 0), static_cast<float*>(p.dW) + v0 * p.lddw, p.lddw, p.C, N, LEMO_F32, st);
+        if (rc) return rc;
+    }
+    if (!p.dX) return 0;
+    const long long pad = vl_pitch(N);
+    rc = launch_transpose(W, p.ldw, nullptr, N, pad, p.C, s.aside, st);
+    if (rc) return rc;
+    if (v0 == 0) return launch_gather_gemm(G, p.M, s.ldg, nullptr, p.M, s.aside, pad, nullptr, p.dX, p.lddx, N4, p.C, LEMO_F32, st);
+    return launch_gather_gemm_add(G, p.M, s.ldg, nullptr, p.M, s.aside, pad, nullptr, p.dX, p.lddx, p.M, nullptr, N4, p.C, LEMO_F32, st);
+}
+
 int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st) {
     int rc = prepare_vocab_grad(dt);
     if (rc) return rc;
@@ -307,57 +371,21 @@ int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st)
     if (p.M == 0) return p.dW ? launch_zero_matrix(p.dW, p.lddw, C, V, dt, st) : 0;
     if (!p.dX && !p.dW) return 0;
     const GradSpace s = grad_space(p.M, C, V, p.piece, dt, p.workspace);
-    hipLaunchKernelGGL(vocab_rows_kernel, dim3((unsigned)(p.M / VL_THREADS + 1)), dim3(VL_THREADS), 0, st, p.dloss, p.dloss_stride, p.labels, p.idx, p.M, p.S, V,
-                       s.weight, s.rows);
+    const bool shared = p.dloss_stride == 0 && dt == LEMO_BF16;
+    const long long zeros = V % (16 / esz) ? s.ldg * esz / 16 : 0;
+    const unsigned blocks = (unsigned)std::max<long long>(p.M / VL_THREADS + 1, std::min<long long>(64, (zeros + VL_THREADS - 1) / VL_THREADS));
+    hipLaunchKernelGGL(vocab_rows_kernel, dim3(blocks), dim3(VL_THREADS), 0, st, p.dloss, p.dloss_stride, (int)shared, p.labels, p.idx, p.M, p.S, V, s.weight, s.rows,
+                       zeros ? reinterpret_cast<u32x4*>(s.G + p.M * s.ldg * esz) : nullptr, zeros);
     rc = (int)hipGetLastError();
-    if (rc) return rc;
-    const int e16 = 16 / esz;
-    if (V % e16) rc = launch_zero_matrix(s.G + p.M * s.ldg * esz, s.ldg, (int)s.ldg, 1, dt, st);  // (columns past the vocabulary: see vocab_rows_kernel)
-    if (rc) return rc;
-    for (int v0 = 0; v0 < V; v0 += p.piece) {
-        const int N = std::min(p.piece, V - v0), N16 = (N + e16 - 1) / e16 * e16;
+    for (int v0 = 0; v0 < V && rc == 0; v0 += p.piece) {
+        const int N = std::min(p.piece, V - v0);
         const char* const W = static_cast<const char*>(p.W) + v0 * p.ldw * esz;
-        if (dt == LEMO_BF16) {
-            VocabTileParams t{};
-            t.A = p.X; t.B = W; t.idx = p.idx; t.lda = p.ldx; t.ldb = p.ldw; t.M = p.M; t.K = C; t.N = N;
-            t.a_bytes = vl_span(p.S, p.ldx, C, 2);
-            t.rule = p.rule; t.labels = p.labels; t.v0 = v0; t.lse = p.lse; t.weight = s.weight; t.G = s.G; t.ldg = s.ldg;
-            int one = 1;
-            rc = launch_vocab_tiles(t, VOCAB_PROBS, gg_choose_tile(p.M, N, C, GG_NT, 1, 0., &one), st);
-        } else {
-            rc = launch_gather_gemm(p.X, p.S, p.ldx, p.idx, p.M, W, p.ldw, nullptr, s.G, s.ldg, C, N, dt, st);
-            if (rc) return rc;
-            rc = launch_in_turns(p.M, VL_THREADS, [&](long long first, unsigned count) {
-                hipLaunchKernelGGL(vocab_probs_f32_kernel, dim3(count), dim3(VL_THREADS), 0, st, p.rule, reinterpret_cast<float*>(s.G), s.ldg, N, v0, p.labels, p.lse,
-                                   s.weight, first);
-            });
-        }
-        if (rc) return rc;
-        if (p.dW) {
-            rc = launch_gather_gemm_dw_direct(s.G, s.ldg, p.X, p.S, p.ldx, s.rows, p.M + (N % e16 != 0), static_cast<char*>(p.dW) + v0 * p.lddw * esz, p.lddw, C, N,
-                                              dt, st);
-            if (rc) return rc;
-        }
-        if (!p.dX) continue;
-        if (dt == LEMO_BF16) {
-            VocabTileParams t{};
-            t.A = s.G; t.B = W; t.lda = s.ldg; t.ldb = p.ldw; t.M = p.M; t.K = N; t.N = C;
-            t.a_bytes = vl_span(p.M, s.ldg, N16, 2);
-            t.planes = s.aside; t.k_split = s.k_split; t.add = v0 > 0;
-            t.splits = (N + s.k_split - 1) / s.k_split;  // (the last piece may be shorter: its parts that are empty leave their planes as they are)
-            rc = launch_vocab_tiles(t, VOCAB_PLANES, s.tile, st);
-        } else {
-            const long long pad = vl_pitch(N);
-            rc = launch_transpose(W, p.ldw, nullptr, N, pad, C, s.aside, st);
-            if (rc) return rc;
-            rc = v0 == 0 ? launch_gather_gemm(s.G, p.M, s.ldg, nullptr, p.M, s.aside, pad, nullptr, p.dX, p.lddx, N16, C, dt, st)
-                         : launch_gather_gemm_add(s.G, p.M, s.ldg, nullptr, p.M, s.aside, pad, nullptr, p.dX, p.lddx, p.M, nullptr, N16, C, dt, st);
-        }
-        if (rc) return rc;
+        rc = dt == LEMO_BF16 ? grad_piece_bf16(p, s, v0, N, W, st) : grad_piece_f32(p, s, v0, N, reinterpret_cast<const float*>(W), st);
     }
-    if (!p.dX || dt == LEMO_F32) return 0;
+    if (rc || !p.dX || dt == LEMO_F32) return rc;
     return launch_in_turns((p.M * (C / 8) + VL_THREADS - 1) / VL_THREADS, VL_THREADS, [&](long long first, unsigned count) {
-        hipLaunchKernelGGL(vocab_planes_kernel, dim3(count), dim3(VL_THREADS), 0, st, s.aside, s.splits, p.M, C, p.dX, p.lddx, first);
+        hipLaunchKernelGGL(vocab_planes_kernel, dim3(count), dim3(VL_THREADS), 0, st, s.aside, s.splits, s.rest, shared ? p.dloss : nullptr, p.labels, V, p.W, p.ldw, p.M, C,
+                           p.dX, p.lddx, first);
     });
 }
 

@@ -11,7 +11,8 @@ struct VocabRule {
 };
 
 // A product of the rows with (a piece of) the head's weight and what is done with a tile of it.  GgParams: A = X [S, C], idx = the kept rows, B = the piece's
-// first row of W, M, N = the piece's columns, K = C; for the planes A = G, B = W (contraction-major), K = the piece's columns, N = C.
+// first row of W, M, N = the piece's columns, K = C; for the planes A = G, B = W (contraction-major), K = the piece's columns, N = C; for the weight's
+// gradient A = G, B = X (both contraction-major, X's rows by idx), M = the piece's columns, N = C, K = rows.
 struct VocabTileParams : GgParams {
     VocabRule rule;
     const int* labels;     // [M]
@@ -21,13 +22,15 @@ struct VocabTileParams : GgParams {
     float* picked;         // statistics: [M] the labels' logits
     const float* lse;      // probabilities: [M]
     const float* weight;   // probabilities: [M] gradients of the losses
+    float* rest;           // probabilities: [M] what rounding the label's element has left
     void* G;               // probabilities: [M, ldg] bf16, columns from N up to a multiple of 8 are zeros
     long long ldg;
     float* planes;         // planes: [splits][M][N]
     int splits, k_split;   // planes: of the contraction, and its length of each (a multiple of 64)
     int add;               // planes: to what they hold
+    const float* scale;    // the weight's gradient: a factor for all of it, or null
 };
-enum { VOCAB_STATS, VOCAB_PROBS, VOCAB_PLANES };
+enum { VOCAB_STATS, VOCAB_PROBS, VOCAB_PLANES, VOCAB_WEIGHT };
 int prepare_vocab_tiles();
 int launch_vocab_tiles(VocabTileParams p, int what, GgTile tile, hipStream_t st);
 // tiles of a launch of one kind along the columns

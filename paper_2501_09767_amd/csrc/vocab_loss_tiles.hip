@@ -5,8 +5,12 @@
 //                   labels) and the label's logit.  8 to 12 bytes a row leave the tile in the place of 512.
 //   probabilities   the same product again, turned into the gradient of the logits with the row's log-sum-exp: G, bf16, one piece of the
 //                   vocabulary at a time.  bf16 because the two products that follow take it so: off by 2^-9 of each element, at random.
+//                   The largest error is that of the label's element, whose rest dX gets back (vocab_planes_kernel); and one
+//                   gradient for all losses is left out of G and multiplied into the results instead, since its rounding would be the same
+//                   relative error in every label's element (4096 rows, 131072 words, mean: dX and dW 3.0e-3 from 64 bits, so 1.9e-3; their own store alone 1.7e-3).
 //   planes          dX = G W over the piece's columns, in binary32: a piece adds to what the pieces before left, and where the
 //                   output has few tiles the contraction is split, with a plane for each part; a kernel of its own rounds their sum once.
+//   the weight's    dW = G^T X[idx], the piece's rows, times what was left out of G, rounded once.
 //
 // What bounds it: the matrix cores, as in gather_gemm_large.hip; the epilogues read no memory but a few bytes a row.
 #include "gather_gemm_tiles.hpp"
@@ -55,9 +59,24 @@ __device__ __forceinline__ float row_lanes_sum(float v) {
     return v + __shfl_xor(v, 32);
 }
 
+constexpr int vocab_layout(int what) { return what == VOCAB_PLANES ? GG_NN : what == VOCAB_WEIGHT ? GG_TN : GG_NT; }
+
+// rows of bf16 in LDS -> rows of a matrix, whose columns below `cols` (a multiple of 8) are written
+template <typename Tile> __device__ __forceinline__ void store_rows(const char* smem, int wave, int lane, void* to, long long ld, long long m0, long long M, int n0, int cols) {
+    constexpr int LPR = Tile::BN / 8, RPP = 64 / LPR, OWN = Tile::BM / RG_WAVES;  // lanes of a row, rows at a time, rows of a wave
+    const int c = lane % LPR * 8;
+    if (n0 + c >= cols) return;
+#pragma unroll 4
+    for (int k = 0; k < OWN / RPP; ++k) {
+        const int row = wave * OWN + k * RPP + lane / LPR;
+        if (m0 + row >= M) continue;
+        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(to) + (m0 + row) * ld + n0 + c) = *reinterpret_cast<const u32x4*>(smem + row * Tile::PITCH + c * 2);
+    }
+}
+
 template <int WHAT, int UA>
 __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTileParams p) {
-    constexpr int LAYOUT = WHAT == VOCAB_PLANES ? GG_NN : GG_NT;
+    constexpr int LAYOUT = vocab_layout(WHAT);
     using Tile = VocabTile<LAYOUT, UA>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -96,6 +115,20 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
                 *to = v;
             }
         }
+        return;
+    }
+    if constexpr (WHAT == VOCAB_WEIGHT) {
+        const float scale = p.scale ? *p.scale : 1.f;
+#pragma unroll
+        for (int i = 0; i < Tile::ROWS; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 v = Tile::at(acc, i, j) * scale;
+                *reinterpret_cast<uint2*>(smem + Tile::row(wave, lane, i) * Tile::PITCH + Tile::col(wave, lane, j) * 2) =
+                    make_uint2(pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3]));
+            }
+        __syncthreads();
+        store_rows<Tile>(smem, wave, lane, p.Y, p.ldy, m0, p.M, n0, p.N);
         return;
     }
     const bool whole = n0 + Tile::BN <= p.N, capped = p.rule.softcap > 0.f;
@@ -177,35 +210,37 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
                     g[r] = vocab_grad(p.rule, of, Tile::at(acc, i, j)[r], p.v0 + n0 + c + r, inv_cap);
                     if (!whole && n0 + c + r >= p.N) g[r] = 0.f;
                 }
-                *reinterpret_cast<uint2*>(smem + row * Tile::PITCH + c * 2) = make_uint2(pack_bf16x2_hw(g[0], g[1]), pack_bf16x2_hw(g[2], g[3]));
+                const uint2 stored = make_uint2(pack_bf16x2_hw(g[0], g[1]), pack_bf16x2_hw(g[2], g[3]));
+                *reinterpret_cast<uint2*>(smem + row * Tile::PITCH + c * 2) = stored;
+                const unsigned label = (unsigned)of.label - (unsigned)(p.v0 + n0 + c);  // (a column past the piece is no label of this piece's: below)
+                if (label < 4u && (whole || n0 + c + (int)label < p.N)) {
+                    const uint32_t two = label < 2 ? stored.x : stored.y;
+                    const float left = label < 2 ? label ? g[1] : g[0] : label & 1 ? g[3] : g[2];
+                    p.rest[m] = left - (label & 1 ? bf16hi_to_f32(two) : bf16lo_to_f32(two));
+                }
             }
         }
         __syncthreads();
-        constexpr int LPR = Tile::BN / 8, RPP = 64 / LPR, OWN = Tile::BM / RG_WAVES;  // lanes of a row, rows at a time, rows of a wave
-        const int c = lane % LPR * 8;
-        if (n0 + c >= p.N) return;
-#pragma unroll 4
-        for (int k = 0; k < OWN / RPP; ++k) {
-            const int row = wave * OWN + k * RPP + lane / LPR;
-            if (m0 + row >= p.M) continue;
-            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.G) + (m0 + row) * p.ldg + n0 + c) = *reinterpret_cast<const u32x4*>(smem + row * Tile::PITCH + c * 2);
-        }
+        store_rows<Tile>(smem, wave, lane, p.G, p.ldg, m0, p.M, n0, (p.N + 7) & ~7);
     }
 }
 
-template <int WHAT, int UA> constexpr LdsLimit vocab_limit() {
-    return {reinterpret_cast<const void*>(&vocab_tile_kernel<WHAT, UA>), VocabTile<WHAT == VOCAB_PLANES ? GG_NN : GG_NT, UA>::LDS};
-}
+template <int WHAT, int UA> constexpr LdsLimit vocab_limit() { return {reinterpret_cast<const void*>(&vocab_tile_kernel<WHAT, UA>), VocabTile<vocab_layout(WHAT), UA>::LDS}; }
 template <int WHAT> static int prepare_what() {
-    static const int err = raise_lds_limits({vocab_limit<WHAT, 0>(), vocab_limit<WHAT, 1>(), vocab_limit<WHAT, 2>(), vocab_limit<WHAT, 4>()});
+    static const int err = [] {
+        if constexpr (WHAT == VOCAB_WEIGHT) return raise_lds_limits({vocab_limit<WHAT, 0>(), vocab_limit<WHAT, 2>(), vocab_limit<WHAT, 4>()});
+        else return raise_lds_limits({vocab_limit<WHAT, 0>(), vocab_limit<WHAT, 1>(), vocab_limit<WHAT, 2>(), vocab_limit<WHAT, 4>()});
+    }();
     return err;
 }
-int prepare_vocab_tiles() { return first_error(prepare_what<VOCAB_STATS>, prepare_what<VOCAB_PROBS>, prepare_what<VOCAB_PLANES>); }
+int prepare_vocab_tiles() {
+    return first_error(prepare_what<VOCAB_STATS>, prepare_what<VOCAB_PROBS>, prepare_what<VOCAB_PLANES>, prepare_what<VOCAB_WEIGHT>);
+}
 
 int vocab_tile_cols(GgTile tile) { return tile == GG_T256 ? 256 : 128; }
 
 template <int WHAT, int UA> static int launch_one(VocabTileParams p, hipStream_t st) {
-    using Tile = VocabTile<WHAT == VOCAB_PLANES ? GG_NN : GG_NT, UA>;
+    using Tile = VocabTile<vocab_layout(WHAT), UA>;
     p.tiles_m = (int)((p.M + Tile::BM - 1) / Tile::BM);
     p.tiles_n = (p.N + Tile::BN - 1) / Tile::BN;
     const long long blocks = ((long long)p.tiles_m * p.tiles_n + NUM_XCD - 1) / NUM_XCD * NUM_XCD * (WHAT == VOCAB_PLANES ? p.splits : 1);
@@ -218,11 +253,18 @@ template <int WHAT> static int launch_what(const VocabTileParams& p, GgTile tile
         case GG_T256: return launch_one<WHAT, 0>(p, st);
         case GG_T256x128: return launch_one<WHAT, 4>(p, st);
         case GG_T128: return launch_one<WHAT, 2>(p, st);
-        default: return launch_one<WHAT, 1>(p, st);
+        default:
+            if constexpr (WHAT == VOCAB_WEIGHT) return (int)hipErrorInvalidValue;  // (contraction-major rows come in whole regions)
+            else return launch_one<WHAT, 1>(p, st);
     }
 }
 int launch_vocab_tiles(VocabTileParams p, int what, GgTile tile, hipStream_t st) {
-    return what == VOCAB_STATS ? launch_what<VOCAB_STATS>(p, tile, st) : what == VOCAB_PROBS ? launch_what<VOCAB_PROBS>(p, tile, st) : launch_what<VOCAB_PLANES>(p, tile, st);
+    switch (what) {
+        case VOCAB_STATS: return launch_what<VOCAB_STATS>(p, tile, st);
+        case VOCAB_PROBS: return launch_what<VOCAB_PROBS>(p, tile, st);
+        case VOCAB_PLANES: return launch_what<VOCAB_PLANES>(p, tile, st);
+        default: return launch_what<VOCAB_WEIGHT>(p, tile, st);
+    }
 }
 
 }  // namespace lemo

@@ -28,7 +28,9 @@ __device__ __forceinline__ void vocab_join(float& top, float& sum, float top2, f
 // Gradient of a row's logit u (capped) at column v: what the row's probabilities and label leave, times the gradient of its loss.
 struct VocabRow { float neg_lse2, factor, weight; int label; bool counts; };
 __device__ __forceinline__ VocabRow vocab_row(const VocabRule& r, float lse, float weight, int label) {
-    return {-lse * LOG2E, fmaf(2.f * r.z, lse, 1.f), weight, label, label >= 0 && label < r.V};
+    // what rounding lse log2(e) leaves would be an error of all of the row's probabilities: it goes into their factor (lse 10, binary32: 6e-7 of them)
+    const float neg = -lse * LOG2E, left = fmaf(-lse, LOG2E, -neg);
+    return {neg, fmaf(2.f * r.z, lse, 1.f) * fmaf(left, 0.6931471805599453f, 1.f), weight, label, label >= 0 && label < r.V};
 }
 __device__ __forceinline__ float vocab_grad(const VocabRule& r, const VocabRow& row, float u, int v, float inv_cap) {
     float g = fmaf(__builtin_amdgcn_exp2f(fmaf(u, LOG2E, row.neg_lse2)), row.factor, -r.all);
