@@ -35,6 +35,13 @@ struct GgParams {
     unsigned a_bytes, b_bytes, y_bytes;  // spans of the whole operands (b_bytes: GG_TN; y_bytes: in-place add)
 };
 
+// The same with the contraction cut into parts of k_part (a multiple of a slab): part `b / blocks` of workgroup b, whose sums go to a matrix of its own, `plane`
+// elements behind the one before (X W^T, the large binary32 tiles).
+struct GgPartParams : GgParams {
+    int k_part, blocks;
+    long long plane;
+};
+
 // Tile of workgroup b: die b % 8 takes a contiguous run of tiles in grouped order (group_m tile rows at a time, column
 // by column), so the tiles resident on one die share rows of both operands through its L2.  False: nothing to do.
 __device__ __forceinline__ bool gg_tile(int b, int tiles_m, int tiles_n, int group_m, int& tm, int& tn) {
@@ -60,5 +67,8 @@ int launch_gather_gemm_large(const GgParams& p, bool add, int layout, hipStream_
 int launch_gather_gemm_mid(const GgParams& p, bool add, int layout, GgTile tile, hipStream_t st);    // the kinds of 128 columns, bf16
 int launch_gather_gemm_small(const GgParams& p, lemo_dtype_t dt, bool add, int layout, GgTile tile, hipStream_t st);
 GgTile gg_choose_tile(long long M, int N, int K, int layout, int most_splits, double split_us, int* splits);  // bf16
+// Y (+)= A . B^T over parts of the contraction, the planes of Y M * N apart with rows of N: binary32, 128 x 128 tiles
+int launch_gather_gemm_parts(const GgParams& p, bool add, int parts, int k_part, hipStream_t st);
+int prepare_gather_gemm_parts();
 
 }  // namespace lemo

@@ -57,8 +57,8 @@ template <int GW, int ESZ, int WT, int E = 32> struct SgGeo {
 };
 
 // SPLIT: products from three-part splits
-template <typename T, bool ADD, int LAYOUT, int GW, int WT, bool SPLIT, int E = 32>
-__global__ __launch_bounds__(SG_THREADS, GW == 4 ? 2 : 1) void gather_gemm_small_kernel(GgParams p) {
+template <typename T, bool ADD, int LAYOUT, int GW, int WT, bool SPLIT, int E = 32, typename P = GgParams>
+__global__ __launch_bounds__(SG_THREADS, GW == 4 ? 2 : 1) void gather_gemm_small_kernel(P p) {
     constexpr bool A_KMAJOR = LAYOUT == GG_TN, B_KMAJOR = LAYOUT != GG_NT;
     constexpr int ESZ = (int)sizeof(T);
     static_assert(ESZ == 4 || (WT == 2 && GW == 1), "the 16-bit transposing read is laid out for 64 x 64 tiles");
@@ -68,8 +68,18 @@ __global__ __launch_bounds__(SG_THREADS, GW == 4 ? 2 : 1) void gather_gemm_small
     constexpr int GROUPS = G::GROUPS, NLD = G::NLD;
     extern __shared__ __attribute__((aligned(16))) char smem[];
 
-    int tm, tn;
-    if (!gg_tile(blockIdx.x, p.tiles_m, p.tiles_n, 8, tm, tn)) return;
+    int tm, tn, block = blockIdx.x;
+    if constexpr (std::is_same_v<P, GgPartParams>) {
+        static_assert(LAYOUT == GG_NT, "parts of the contraction: rows of both operands run along it");
+        const int part = block / p.blocks, k0 = part * p.k_part;  // (host: below K for every part)
+        block -= part * p.blocks;
+        p.A = static_cast<const T*>(p.A) + k0;
+        p.B = static_cast<const T*>(p.B) + k0;
+        p.Y = static_cast<T*>(p.Y) + part * p.plane;
+        p.K = min(p.k_part, p.K - k0);
+        p.a_bytes -= (unsigned)k0 * ESZ;
+    }
+    if (!gg_tile(block, p.tiles_m, p.tiles_n, 8, tm, tn)) return;
     const long long m0 = (long long)tm * G::BM;
     const int n0 = tn * G::BN;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
@@ -653,6 +663,27 @@ static int prepare_small_form(bool add, int layout) {
     if constexpr (sizeof(T) == 2)
         if (layout == GG_NN) return prepare_small<T, true, GG_NN>();
     return add ? prepare_small<T, true, GG_NT>() : prepare_small<T, false, GG_NT>();
+}
+
+template <bool ADD> static int launch_parts(GgPartParams p, int parts, hipStream_t st) {
+    using G = SgGeo<4, 4, 2>;
+    p.tiles_m = (int)((p.M + G::BM - 1) / G::BM);
+    p.tiles_n = (p.N + G::BN - 1) / G::BN;
+    p.blocks = (p.tiles_m * p.tiles_n + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
+    hipLaunchKernelGGL((gather_gemm_small_kernel<float, ADD, GG_NT, 4, 2, true, 32, GgPartParams>), dim3((unsigned)(p.blocks * parts)), dim3(SG_THREADS), G::LDS, st, p);
+    return (int)hipGetLastError();
+}
+int launch_gather_gemm_parts(const GgParams& p, bool add, int parts, int k_part, hipStream_t st) {
+    GgPartParams q;
+    static_cast<GgParams&>(q) = p;
+    q.k_part = k_part;
+    q.plane = p.M * p.N;
+    return add ? launch_parts<true>(q, parts, st) : launch_parts<false>(q, parts, st);
+}
+int prepare_gather_gemm_parts() {
+    static const int err = raise_lds_limits({{reinterpret_cast<const void*>(&gather_gemm_small_kernel<float, false, GG_NT, 4, 2, true, 32, GgPartParams>), SgGeo<4, 4, 2>::LDS},
+                                             {reinterpret_cast<const void*>(&gather_gemm_small_kernel<float, true, GG_NT, 4, 2, true, 32, GgPartParams>), SgGeo<4, 4, 2>::LDS}});
+    return err;
 }
 
 int prepare_gather_gemm_small(lemo_dtype_t dt, bool add, int layout) {

@@ -13,7 +13,7 @@
 // piece's tail and the additions to dX, and is what the operator is there to avoid.
 //
 // binary32: the products are the selective-load GEMM's, a piece at a time in both directions, with the softmax in kernels of its own between them; dX takes the
-// weight's piece transposed, since that GEMM wants both operands along the contraction.
+// weight's piece transposed, since that GEMM wants both operands along the contraction, and cuts that into parts like bf16's.
 #include <algorithm>
 
 #include "vocab_softmax.hpp"
@@ -108,34 +108,44 @@ __global__ __launch_bounds__(VL_THREADS) void vocab_rows_kernel(const float* dlo
         for (long long i = at; i < pieces; i += all) zeros[i] = u32x4{0u, 0u, 0u, 0u};
 }
 
-// dX = the sum of the planes and the label's row of W times what G's rounding has left of its element, times the gradient that was left out of G,
-// rounded once.  A thread has eight columns of a row.
+// dX = the sum of the planes, rounded once; in bf16 with the label's row of W times what G's rounding has left of its element, and times the gradient
+// that was left out of G.  A thread has 16 bytes of a row.
+template <typename T>
 __global__ __launch_bounds__(VL_THREADS) void vocab_planes_kernel(const float* planes, int n, const float* rest, const float* scale, const int* labels, int V,
                                                                   const void* W, long long ldw, long long M, int C, void* dX, long long lddx, long long first) {
-    const long long per_row = C / 8, i = (first + blockIdx.x) * VL_THREADS + threadIdx.x;
+    constexpr int E = RowPiece<T>::E;
+    const long long per_row = C / E, i = (first + blockIdx.x) * VL_THREADS + threadIdx.x;
     const long long m = i / per_row;
     if (m >= M) return;
-    const int c = (int)(i - m * per_row) * 8, label = labels[m];
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int c = (int)(i - m * per_row) * E, label = labels[m];
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = 0.f;
     if (label >= 0 && label < V) {
-        const float left = rest[m], by = scale ? *scale : 1.f;
-        float w[8];
-        RowPiece<bf16_t>::get(row_load<bf16_t>(W, label * ldw + c), w);
+#pragma unroll 4
         for (int s = 0; s < n; ++s) {
             const f32x4* const at = reinterpret_cast<const f32x4*>(planes + ((long long)s * M + m) * C + c);
-            const f32x4 lo = at[0], hi = at[1];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { v[e] += lo[e]; v[e + 4] += hi[e]; }
+            for (int h = 0; h < E / 4; ++h) {
+                const f32x4 x = at[h];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[h * 4 + e] += x[e];
+            }
         }
+        if constexpr (E == 8) {
+            const float left = rest[m], by = scale ? *scale : 1.f;
+            float w[E];
+            RowPiece<T>::get(row_load<T>(W, label * ldw + c), w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fmaf(left, w[e], v[e]) * by;
+            for (int e = 0; e < E; ++e) v[e] = fmaf(left, w[e], v[e]) * by;
+        }
     }
-    row_store<bf16_t>(dX, m * lddx + c, RowPiece<bf16_t>::put(v));
+    row_store<T>(dX, m * lddx + c, RowPiece<T>::put(v));
 }
 
 // ---- binary32: a piece's logits in memory -----------------------------------------------------------
 
-// A workgroup a row: its part of the statistics, as a tile leaves it
+// A workgroup a row (16-byte aligned): its part of the statistics, as a tile leaves it
 __global__ __launch_bounds__(VL_THREADS) void vocab_stats_f32_kernel(VocabRule rule, const float* x, long long ldx, int N, int v0, const int* labels, long long M,
                                                                      float2* parts, float* sums, float* picked, long long first) {
     __shared__ float lds[3][VL_THREADS / 64];
@@ -145,13 +155,22 @@ __global__ __launch_bounds__(VL_THREADS) void vocab_stats_f32_kernel(VocabRule r
     const float inv_cap = capped ? 1.f / rule.softcap : 0.f;
     const unsigned label = (unsigned)labels[m] - (unsigned)v0;
     float top = -INFINITY, sum = 0.f, all = 0.f;
-    for (int n = threadIdx.x; n < N; n += VL_THREADS) {
-        const float u = capped ? vocab_cap(row[n], rule.softcap, inv_cap) : row[n];
-        if ((unsigned)n == label) picked[m] = u;
-        const float t = fmaxf(top, u);
-        sum = sum * vocab_scale(top, t) + vocab_scale(u, t);
+    for (int n = threadIdx.x * 4; n < N; n += VL_THREADS * 4) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(row + n);  // (the pitch is a multiple of 64: what lies behind the row is there, and not used)
+        float u[4], t = top;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            u[e] = n + e >= N ? -INFINITY : capped ? vocab_cap(v[e], rule.softcap, inv_cap) : v[e];
+            if (n + e < N && (unsigned)(n + e) == label) picked[m] = u[e];
+            t = fmaxf(t, u[e]);
+        }
+        sum *= vocab_scale(top, t);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sum += vocab_scale(u[e], t);
+            all += n + e < N ? u[e] : 0.f;
+        }
         top = t;
-        all += u;
     }
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
@@ -181,9 +200,15 @@ __global__ __launch_bounds__(VL_THREADS) void vocab_probs_f32_kernel(VocabRule r
     const bool capped = rule.softcap > 0.f;
     const float inv_cap = capped ? 1.f / rule.softcap : 0.f;
     const VocabRow of = vocab_row(rule, lse[m], weight[m], labels[m]);
-    for (int n = threadIdx.x; n < (N + 63) / 64 * 64; n += VL_THREADS) {
-        const float u = n < N ? capped ? vocab_cap(row[n], rule.softcap, inv_cap) : row[n] : 0.f;
-        row[n] = n < N ? vocab_grad(rule, of, u, v0 + n, inv_cap) : 0.f;
+    for (int n = threadIdx.x * 4; n < (N + 63) / 64 * 64; n += VL_THREADS * 4) {
+        f32x4* const at = reinterpret_cast<f32x4*>(row + n);
+        f32x4 v = *at;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float u = capped ? vocab_cap(v[e], rule.softcap, inv_cap) : v[e];
+            v[e] = n + e < N ? vocab_grad(rule, of, u, v0 + n + e, inv_cap) : 0.f;
+        }
+        *at = v;
     }
 }
 
@@ -235,7 +260,7 @@ int prepare_vocab_loss(lemo_dtype_t dt) { return dt == LEMO_BF16 ? prepare_vocab
 int prepare_vocab_grad(lemo_dtype_t dt) {
     if (dt == LEMO_BF16) return prepare_vocab_tiles();
     const int rc = first_error([&] { return prepare_vocab_loss(dt); }, [&] { return prepare_gather_gemm_dw(dt); });
-    return rc ? rc : prepare_gather_gemm_small(dt, true, GG_NT);
+    return rc ? rc : prepare_gather_gemm_parts();
 }
 
 static unsigned vl_span(long long rows, long long ld, long long cols, int esz) { return (unsigned)(((rows - 1) * ld + cols) * esz); }
@@ -286,8 +311,24 @@ int launch_vocab_loss(const VocabLossParams& p, lemo_dtype_t dt, hipStream_t st)
     return (int)hipGetLastError();
 }
 
-// gradient: rows, G, and for dX the planes (bf16) or the weight's piece transposed (binary32)
-struct GradSpace { float *weight, *rest; int* rows; char* G; float* aside; long long ldg; GgTile tile; int splits, k_split; size_t bytes; };
+// binary32: into how many parts dX's contraction is cut.  128 x 128 tiles, two a CU: a round of 512 of them takes 0.104 us for each element of the contraction (161
+// TFLOP/s), one of up to 256 0.06; a plane 8 bytes an element at 4 TB/s.  (M = 777, 768 columns, V = 50001: 32 x 32 tiles without parts 700 us)
+static int f32_splits(long long M, int C, int K, int* k_part) {
+    const long long tiles = (M + 127) / 128 * ((C + 127) / 128);
+    int best = 1;
+    double least = INFINITY;
+    for (int s = 1; s <= 64 && s * 64 <= std::max(K, 64); ++s) {
+        const int k = (K + s * 64 - 1) / (s * 64) * 64;
+        if ((long long)k * (s - 1) >= K) continue;
+        const long long n = tiles * s, left = n % 512;
+        const double us = (double)k * ((double)(n / 512) * 0.104 + (left == 0 ? 0. : left <= 256 ? 0.06 : 0.104)) + s * (double)M * C * 8e-6 / 4.;
+        if (us < least) { least = us; best = s; *k_part = k; }
+    }
+    return best;
+}
+
+// gradient: rows, G, dX's planes, and in binary32 the weight's piece transposed
+struct GradSpace { float *weight, *rest; int* rows; char* G; float *planes, *turned; long long ldg; GgTile tile; int splits, k_split; size_t bytes; };
 static GradSpace grad_space(long long M, int C, int V, int piece, lemo_dtype_t dt, void* base) {
     GradSpace s{};
     const int esz = dt == LEMO_BF16 ? 2 : 4;
@@ -307,10 +348,11 @@ static GradSpace grad_space(long long M, int C, int V, int piece, lemo_dtype_t d
         s.tile = gg_choose_tile(M, C, std::min(piece, V), GG_NN, 32, (double)M * C * 8e-6 / 4., &s.splits);
         const int k = std::min(piece, V);
         s.k_split = (k + s.splits * 64 - 1) / (s.splits * 64) * 64;
-        s.aside = reinterpret_cast<float*>(take((size_t)s.splits * M * C * sizeof(float)));
     } else {
-        s.aside = reinterpret_cast<float*>(take((size_t)C * s.ldg * sizeof(float)));
+        s.splits = f32_splits(M, C, std::min(piece, V), &s.k_split);
+        s.turned = reinterpret_cast<float*>(take((size_t)C * s.ldg * sizeof(float)));
     }
+    s.planes = reinterpret_cast<float*>(take((size_t)s.splits * M * C * sizeof(float)));
     return s;
 }
 size_t vocab_grad_workspace(long long M, int C, int V, int piece, lemo_dtype_t dt) { return M > 0 ? grad_space(M, C, V, piece, dt, nullptr).bytes : 0; }
@@ -338,7 +380,7 @@ static int grad_piece_bf16(const VocabGradParams& p, const GradSpace& s, int v0,
     VocabTileParams x{};
     x.A = s.G; x.B = W; x.lda = s.ldg; x.ldb = p.ldw; x.M = p.M; x.K = N; x.N = p.C;
     x.a_bytes = vl_span(p.M, s.ldg, (N + 7) / 8 * 8, 2);
-    x.planes = s.aside; x.k_split = s.k_split; x.add = v0 > 0;
+    x.planes = s.planes; x.k_split = s.k_split; x.add = v0 > 0;
     x.splits = (N + s.k_split - 1) / s.k_split;  // (the last piece may be shorter: its parts that are empty leave their planes as they are)
     return launch_vocab_tiles(x, VOCAB_PLANES, s.tile, st);
 }
@@ -358,10 +400,13 @@ static int grad_piece_f32(const VocabGradParams& p, const GradSpace& s, int v0, 
     }
     if (!p.dX) return 0;
     const long long pad = vl_pitch(N);
-    rc = launch_transpose(W, p.ldw, nullptr, N, pad, p.C, s.aside, st);
+    rc = launch_transpose(W, p.ldw, nullptr, N, pad, p.C, s.turned, st);
     if (rc) return rc;
-    if (v0 == 0) return launch_gather_gemm(G, p.M, s.ldg, nullptr, p.M, s.aside, pad, nullptr, p.dX, p.lddx, N4, p.C, LEMO_F32, st);
-    return launch_gather_gemm_add(G, p.M, s.ldg, nullptr, p.M, s.aside, pad, nullptr, p.dX, p.lddx, p.M, nullptr, N4, p.C, LEMO_F32, st);
+    GgParams x{};
+    x.A = G; x.B = s.turned; x.Y = s.planes; x.lda = s.ldg; x.ldb = pad; x.ldy = p.C; x.M = p.M; x.out_rows = p.M; x.K = N4; x.N = p.C;
+    x.a_bytes = vl_span(p.M, s.ldg, N4, 4);
+    x.y_bytes = vl_span(p.M, p.C, p.C, 4);
+    return launch_gather_gemm_parts(x, v0 > 0, (N4 + s.k_split - 1) / s.k_split, s.k_split, st);
 }
 
 int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st) {
@@ -382,11 +427,14 @@ int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st)
         const char* const W = static_cast<const char*>(p.W) + v0 * p.ldw * esz;
         rc = dt == LEMO_BF16 ? grad_piece_bf16(p, s, v0, N, W, st) : grad_piece_f32(p, s, v0, N, reinterpret_cast<const float*>(W), st);
     }
-    if (rc || !p.dX || dt == LEMO_F32) return rc;
-    return launch_in_turns((p.M * (C / 8) + VL_THREADS - 1) / VL_THREADS, VL_THREADS, [&](long long first, unsigned count) {
-        hipLaunchKernelGGL(vocab_planes_kernel, dim3(count), dim3(VL_THREADS), 0, st, s.aside, s.splits, s.rest, shared ? p.dloss : nullptr, p.labels, V, p.W, p.ldw, p.M, C,
-                           p.dX, p.lddx, first);
-    });
+    if (rc || !p.dX) return rc;
+    auto planes = [&](auto kernel, int e) {
+        return launch_in_turns((p.M * (C / e) + VL_THREADS - 1) / VL_THREADS, VL_THREADS, [&](long long first, unsigned count) {
+            hipLaunchKernelGGL(kernel, dim3(count), dim3(VL_THREADS), 0, st, s.planes, s.splits, s.rest, shared ? p.dloss : nullptr, p.labels, V, p.W, p.ldw, p.M, C, p.dX,
+                               p.lddx, first);
+        });
+    };
+    return dt == LEMO_BF16 ? planes(vocab_planes_kernel<bf16_t>, 8) : planes(vocab_planes_kernel<float>, 4);
 }
 
 }  // namespace lemo
