@@ -529,6 +529,213 @@ PyObject* block_attention_step(PyObject* const* a) {  // Q K V lengths blocks b 
     }, {O});
 }
 
+// queries or keys of the calls on heads, or none
+struct Side { const at::Tensor* t; void* p; int64_t ts, hs; int32_t heads; };
+Side side(PyObject* o, const Place& here) {
+    if (o == Py_None) return {nullptr, nullptr, 0, 0, 0};
+    const at::Tensor& t = here.at(heads(o));
+    return {&t, t.data_ptr(), t.stride(0), t.stride(1), size32(t.size(1))};
+}
+// a result like `s`: the caller's, or a new one in `keep`
+Side like(const Side& s, PyObject* o, const Place& here, at::Tensor& keep) {
+    if (!s.t) {
+        need(o == Py_None);
+        return s;
+    }
+    keep = o == Py_None ? at::empty(s.t->sizes(), here.options.dtype(s.t->scalar_type())) : here.at(heads(o));
+    need(keep.sizes() == s.t->sizes() && keep.scalar_type() == s.t->scalar_type());
+    return {&keep, keep.data_ptr(), keep.stride(0), keep.stride(1), s.heads};
+}
+struct Rotation { int64_t M; int32_t d, rot, flags; lemo_dtype_t dt; at::ScalarType type; const float* freq; const void *wq, *wk; const at::Tensor *tq, *tk; };
+Rotation rotation(const Side& q, const Side& k, PyObject* freq, PyObject* wq, PyObject* wk, int32_t norm, int32_t flags, const Place& here) {
+    need(q.t || k.t);
+    const at::Tensor& one = q.t ? *q.t : *k.t;
+    Rotation r{one.size(0), size32(one.size(2)), 0, flags, dtype(one), one.scalar_type(), nullptr, nullptr, nullptr, nullptr, nullptr};
+    need(!q.t || !k.t || (k.t->size(0) == r.M && k.t->size(2) == r.d && k.t->scalar_type() == r.type));
+    if (freq != Py_None) {
+        const at::Tensor& t = here.at(tensor(freq, 1));
+        need(t.scalar_type() == at::kFloat && t.is_contiguous() && t.size(0) < (1 << 20));
+        r.freq = static_cast<const float*>(t.data_ptr());
+        r.rot = 2 * (int32_t)t.size(0);
+    }
+    auto weight = [&](PyObject* o, const Side& of, const void*& p, const at::Tensor*& t) {
+        if (o == Py_None) return;
+        need(THPVariable_CheckExact(o) && of.t && norm != LEMO_NORM_NONE);
+        const int64_t dims = THPVariable_Unpack(o).dim();
+        t = &here.at(tensor(o, dims));
+        need((dims == 1 || (dims == 2 && t->size(0) == of.heads)) && t->size(dims - 1) == r.d && t->scalar_type() == r.type && t->is_contiguous());
+        p = t->data_ptr();
+    };
+    weight(wq, q, r.wq, r.tq);
+    weight(wk, k, r.wk, r.tk);
+    need(!r.tq || !r.tk || r.tq->dim() == r.tk->dim());
+    if ((r.tq && r.tq->dim() == 2) || (r.tk && r.tk->dim() == 2)) r.flags |= LEMO_WEIGHTS_PER_HEAD;
+    return r;
+}
+const int32_t* positions_of(PyObject* o, const Place& here, int64_t M) {
+    const at::Tensor* t = index(o);
+    need(!t || (t->numel() == M && here.at(*t).defined()));
+    return rows(t);
+}
+
+PyObject* qk_rotate(PyObject* const* a) {  // Q K inv_freq positions pos_start norm w_q w_k eps amplitude flags Q_out K_out
+    const Place here;
+    const Side q = side(a[0], here), k = side(a[1], here);
+    const int64_t start = whole(a[4]);
+    const int32_t norm = whole32(a[5]);
+    const float eps = real(a[8]), amplitude = real(a[9]);
+    const Rotation r = rotation(q, k, a[2], a[6], a[7], norm, whole32(a[10]), here);
+    const int32_t* pos = positions_of(a[3], here, r.M);
+    at::Tensor Q, K;
+    const Side qo = like(q, a[11], here, Q), ko = like(k, a[12], here, K);
+    return call_for([=] {
+        return lemo_qk_rotate(q.p, q.ts, q.hs, k.p, k.ts, k.hs, r.M, q.heads, k.heads, r.d, r.dt, pos, start, r.freq, r.rot, amplitude, norm, r.wq, r.wk, eps, (uint32_t)r.flags,
+                              qo.p, qo.ts, qo.hs, ko.p, ko.ts, ko.hs, here.stream);
+    }, {Q, K});
+}
+
+PyObject* qk_rotate_grad(PyObject* const* a) {  // dQ_out dK_out Q K inv_freq positions pos_start norm w_q w_k eps amplitude flags dQ dK weights workspace
+    const Place here;
+    const Side gq = side(a[0], here), gk = side(a[1], here);
+    const int64_t start = whole(a[6]);
+    const int32_t norm = whole32(a[7]);
+    const float eps = real(a[10]), amplitude = real(a[11]);
+    const Rotation r = rotation(gq, gk, a[4], a[8], a[9], norm, whole32(a[12]), here);
+    const int32_t* pos = positions_of(a[5], here, r.M);
+    need(PyBool_Check(a[15]));
+    const bool sums = a[15] == Py_True && (r.tq || r.tk);
+    auto operand = [&](PyObject* o, const Side& g) {
+        if (norm == LEMO_NORM_NONE) return Side{nullptr, nullptr, 0, 0, 0};
+        const Side x = side(o, here);
+        need((x.t != nullptr) == (g.t != nullptr) && (!x.t || (x.t->sizes() == g.t->sizes() && x.t->scalar_type() == g.t->scalar_type())));
+        return x;
+    };
+    const Side q = operand(a[2], gq), k = operand(a[3], gk);
+    at::Tensor Q, K, keep;
+    const Side dq = like(gq, a[13], here, Q), dk = like(gk, a[14], here, K);
+    const at::Tensor wq = here.fresh(sums && r.tq, r.tq ? r.tq->sizes() : at::IntArrayRef{}, at::kFloat), wk = here.fresh(sums && r.tk, r.tk ? r.tk->sizes() : at::IntArrayRef{}, at::kFloat);
+    size_t bytes = 0;
+    need(!sums || lemo_qk_rotate_grad_workspace_bytes(r.M, gq.heads, gk.heads, r.d, r.dt, (uint32_t)r.flags, &bytes) == LEMO_OK);
+    const Bytes ws = here.scratch(a[16], bytes, keep);
+    void *sq = address(wq), *sk = address(wk);
+    return call_for([=] {
+        return lemo_qk_rotate_grad(gq.p, gq.ts, gq.hs, gk.p, gk.ts, gk.hs, q.p, q.ts, q.hs, k.p, k.ts, k.hs, r.M, gq.heads, gk.heads, r.d, r.dt, pos, start, r.freq, r.rot, amplitude,
+                                   norm, r.wq, r.wk, eps, (uint32_t)r.flags, dq.p, dq.ts, dq.hs, dk.p, dk.ts, dk.hs, (float*)sq, (float*)sk, ws.p, ws.n, here.stream);
+    }, {Q, K, wq, wk});
+}
+
+PyObject* qk_rotate_step(PyObject* const* a) {  // Q K V K_cache V_cache lengths inv_freq norm w_q w_k eps amplitude flags Q_out
+    const Place here;
+    const Side q = side(a[0], here), k = side(a[1], here), v = side(a[2], here);
+    const int32_t norm = whole32(a[7]);
+    const float eps = real(a[10]), amplitude = real(a[11]);
+    const Rotation r = rotation(q, k, a[6], a[8], a[9], norm, whole32(a[12]), here);
+    need(q.t && k.t && (v.t != nullptr) == (a[4] != Py_None));
+    const at::Tensor& kc = cache(a[3], here);
+    const at::Tensor& vc = v.t ? cache(a[4], here) : kc;
+    need(kc.size(0) == r.M && kc.size(2) == k.heads && kc.size(3) == r.d && kc.scalar_type() == r.type && vc.sizes() == kc.sizes() && vc.scalar_type() == r.type);
+    need(!v.t || (v.t->sizes() == k.t->sizes() && v.t->scalar_type() == r.type));
+    const int32_t* len = sequence_lengths(a[5], here, r.M);
+    const int32_t B = size32(r.M);
+    at::Tensor Q;
+    const Side qo = like(q, a[13], here, Q);
+    void *kp = kc.data_ptr(), *vp = v.t ? vc.data_ptr() : nullptr;
+    const int64_t S = kc.size(1), k0 = kc.stride(0), k1 = kc.stride(1), k2 = kc.stride(2), v0 = vc.stride(0), v1 = vc.stride(1), v2 = vc.stride(2);
+    return call_for([=] {
+        return lemo_qk_rotate_step(q.p, q.ts, q.hs, k.p, k.ts, k.hs, v.p, v.ts, v.hs, B, S, q.heads, k.heads, r.d, r.dt, len, r.freq, r.rot, amplitude, norm, r.wq, r.wk, eps,
+                                   (uint32_t)r.flags, qo.p, qo.ts, qo.hs, kp, k0, k1, k2, vp, v0, v1, v2, here.stream);
+    }, {Q});
+}
+
+double real64(PyObject* o) {
+    need(PyFloat_CheckExact(o));
+    return PyFloat_AS_DOUBLE(o);
+}
+const uint64_t* generator(PyObject* o, const Place& here) {
+    const at::Tensor& t = here.at(tensor(o, 1));
+    need((t.scalar_type() == at::kLong || t.scalar_type() == at::kUInt64) && t.size(0) == 2 && t.is_contiguous());
+    return static_cast<const uint64_t*>(t.data_ptr());
+}
+
+PyObject* dropout_add(PyObject* const* a) {  // Y R kept rng p site
+    const Place here;
+    const at::Tensor &Y = here.at(matrix(a[0])), &R = here.at(matrix(a[1]));
+    const lemo_dtype_t dt = dtype(R);
+    const int64_t M = Y.size(0), S = R.size(0), site = whole(a[5]), ldy = Y.stride(0), ldr = R.stride(0);
+    const int32_t C = size32(R.size(1));
+    need(Y.size(1) == C && Y.scalar_type() == R.scalar_type());
+    const int32_t* ki = positions_of(a[2], here, M);
+    const uint64_t* rng = generator(a[3], here);
+    const double p = real64(a[4]);
+    void *y = Y.data_ptr(), *r = R.data_ptr();
+    return call([=] { return lemo_dropout_add(y, ldy, r, ldr, S, ki, M, p, rng, (uint64_t)site, C, dt, here.stream); });
+}
+
+PyObject* dropout_add_grad(PyObject* const* a) {  // dR kept rng p site dY
+    const Place here;
+    const at::Tensor& R = here.at(matrix(a[0]));
+    const lemo_dtype_t dt = dtype(R);
+    const at::Tensor* kept = index(a[1]);
+    const int64_t S = R.size(0), site = whole(a[4]), ldr = R.stride(0), C = R.size(1);
+    need(kept || a[5] == Py_None || THPVariable_CheckExact(a[5]));
+    const int64_t M = kept ? here.at(*kept).numel() : a[5] == Py_None ? S : matrix(a[5]).size(0);
+    const at::Tensor* given = maybe_matrix(a[5], here, M, C, R.scalar_type());
+    const uint64_t* rng = generator(a[2], here);
+    const double p = real64(a[3]);
+    const at::Tensor Y = given ? *given : here.fresh(true, {M, C}, R.scalar_type());
+    void *y = Y.data_ptr(), *r = R.data_ptr();
+    const int64_t ldy = Y.stride(0);
+    const int32_t c = size32(C), *ki = rows(kept);
+    return call_for([=] { return lemo_dropout_add_grad(r, ldr, S, ki, M, p, rng, (uint64_t)site, y, ldy, c, dt, here.stream); }, {Y});
+}
+
+struct Head { int64_t S, M, ldx, ldw; int32_t C, V; lemo_dtype_t dt; at::ScalarType type; void *X, *W; const int32_t *kept, *labels; };
+Head head(PyObject* x, PyObject* k, PyObject* w, PyObject* l, const Place& here) {
+    const at::Tensor &X = here.at(matrix(x)), &W = here.at(matrix(w)), &labels = here.at(tensor(l, 1));
+    need(X.size(1) == W.size(1) && X.scalar_type() == W.scalar_type() && labels.scalar_type() == at::kInt && labels.is_contiguous());
+    const int64_t M = labels.numel();
+    return {X.size(0), M, X.stride(0), W.stride(0), size32(X.size(1)), size32(W.size(0)), dtype(X), X.scalar_type(), X.data_ptr(), W.data_ptr(), positions_of(k, here, M),
+            static_cast<const int32_t*>(labels.data_ptr())};
+}
+
+PyObject* vocab_loss(PyObject* const* a) {  // X kept W labels softcap smoothing z_weight loss lse total workspace
+    const Place here;
+    const Head h = head(a[0], a[1], a[2], a[3], here);
+    const float cap = real(a[4]), s = real(a[5]), z = real(a[6]);
+    const at::Tensor loss = here.result(a[7], {h.M}, at::kFloat), lse = here.result(a[8], {h.M}, at::kFloat), total = here.result(a[9], {4}, at::kFloat);
+    size_t bytes = 0;
+    need(lemo_vocab_loss_workspace_bytes(h.M, h.C, h.V, h.dt, &bytes) == LEMO_OK);
+    at::Tensor keep;
+    const Bytes ws = here.scratch(a[10], bytes, keep);
+    void *l0 = loss.data_ptr(), *l1 = lse.data_ptr(), *l2 = total.data_ptr();
+    return call_for([=] {
+        return lemo_vocab_loss(h.X, h.S, h.ldx, h.kept, h.M, h.W, h.ldw, h.C, h.V, h.dt, h.labels, cap, s, z, (float*)l0, (float*)l1, (float*)l2, ws.p, ws.n, here.stream);
+    }, {loss, lse, total});
+}
+
+PyObject* vocab_loss_grad(PyObject* const* a) {  // dloss X kept W labels lse softcap smoothing z_weight want_dX want_dW dX dW piece workspace
+    const Place here;
+    const Head h = head(a[1], a[2], a[3], a[4], here);
+    const at::Tensor &dloss = here.at(tensor(a[0], 1)), &lse = here.at(tensor(a[5], 1));
+    need(dloss.scalar_type() == at::kFloat && dloss.is_contiguous() && (dloss.numel() == 1 || dloss.numel() == h.M));
+    need(lse.scalar_type() == at::kFloat && lse.is_contiguous() && lse.numel() == h.M && PyBool_Check(a[9]) && PyBool_Check(a[10]));
+    const float cap = real(a[6]), s = real(a[7]), z = real(a[8]);
+    const bool x = a[9] == Py_True, w = a[10] == Py_True;
+    const int32_t piece = whole32(a[13]);
+    const at::Tensor *gx = x ? maybe_matrix(a[11], here, h.M, h.C, h.type) : nullptr, *gw = w ? maybe_matrix(a[12], here, h.V, h.C, h.type) : nullptr;
+    const at::Tensor dX = gx ? *gx : here.fresh(x, {h.M, h.C}, h.type), dW = gw ? *gw : here.fresh(w, {h.V, h.C}, h.type);
+    size_t bytes = 0;
+    need(lemo_vocab_loss_grad_workspace_bytes(h.M, h.C, h.V, h.ldw, h.dt, piece, &bytes) == LEMO_OK);
+    at::Tensor keep;
+    const Bytes ws = here.scratch(a[14], bytes, keep);
+    void *g = dloss.data_ptr(), *l = lse.data_ptr(), *px = address(dX), *pw = address(dW);
+    const int64_t gs = dloss.numel() == h.M, lddx = x ? dX.stride(0) : h.C, lddw = w ? dW.stride(0) : h.C;
+    return call_for([=] {
+        return lemo_vocab_loss_grad((const float*)g, gs, h.X, h.S, h.ldx, h.kept, h.M, h.W, h.ldw, h.C, h.V, h.dt, h.labels, (const float*)l, cap, s, z, px, lddx, pw, lddw, piece,
+                                    ws.p, ws.n, here.stream);
+    }, {dX, dW});
+}
+
 PyObject* set_stream_source(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 2) {
         PyErr_SetString(PyExc_TypeError, "set_stream_source(current_device, raw_stream)");
@@ -544,6 +751,8 @@ PyMethodDef methods[] = {LEMO_FAST(score_segments, 9), LEMO_FAST(select_topk, 4)
                          LEMO_FAST(gather_gemm_add, 7), LEMO_FAST(gather_gemm_dx, 4), LEMO_FAST(gather_gemm_dw, 5), LEMO_FAST(scatter_grad, 4),
                          LEMO_FAST(norm_residual, 16), LEMO_FAST(norm_residual_grad, 19), LEMO_FAST(block_means, 3), LEMO_FAST(select_blocks, 9),
                          LEMO_FAST(block_attention, 12), LEMO_FAST(block_attention_grad, 16), LEMO_FAST(select_blocks_step, 7), LEMO_FAST(block_attention_step, 9),
+                         LEMO_FAST(qk_rotate, 13), LEMO_FAST(qk_rotate_grad, 17), LEMO_FAST(qk_rotate_step, 14), LEMO_FAST(dropout_add, 6), LEMO_FAST(dropout_add_grad, 6),
+                         LEMO_FAST(vocab_loss, 11), LEMO_FAST(vocab_loss_grad, 15),
                          {"set_stream_source", (PyCFunction)(void*)set_stream_source, METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "lemo_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

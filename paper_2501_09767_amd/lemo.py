@@ -1036,6 +1036,10 @@ def lemo_qk_rotate(Q: Optional[torch.Tensor], K: Optional[torch.Tensor], inv_fre
                    amplitude: float = 1.0, flags: int = 0, Q_out: Optional[torch.Tensor] = None, K_out: Optional[torch.Tensor] = None):
     """Norm of every head of Q [M,H,d] and K [M,H_kv,d], and rotation by positions [M] int32 (0 ... M-1 if not given) + pos_start, inv_freq
     [rot/2] float32 -> (Q_out, K_out).  Weights [d], or [heads,d].  Q or K may be None; a result may be its operand."""
+    done = _native.qk_rotate(Q, K, inv_freq, positions, pos_start, norm, w_q, w_k, eps, amplitude, flags, Q_out, K_out)
+    if done is not None:
+        _check(done[0], "lemo_qk_rotate")
+        return done[1], done[2]
     _here(Q, K, inv_freq, positions, w_q, w_k, Q_out, K_out)
     M, d, H, Hkv, dtype, rot, flags = _rotate_sizes(Q, K, inv_freq, norm, w_q, w_k, flags)
     _index(positions, M, "positions")
@@ -1056,6 +1060,10 @@ def lemo_qk_rotate_grad(dQ_out: Optional[torch.Tensor], dK_out: Optional[torch.T
                         workspace: Optional[torch.Tensor] = None) -> RotateGrads:
     """Gradients of lemo_qk_rotate, Q and K as it took them (with NORM_NONE they may be None).  dQ may be dQ_out, dK dK_out; weights=False leaves out
     those of w_q and w_k."""
+    done = _native.qk_rotate_grad(dQ_out, dK_out, Q, K, inv_freq, positions, pos_start, norm, w_q, w_k, eps, amplitude, flags, dQ, dK, weights, workspace)
+    if done is not None:
+        _check(done[0], "lemo_qk_rotate_grad")
+        return RotateGrads(*done[1:])
     _here(dQ_out, dK_out, Q, K, inv_freq, positions, w_q, w_k, dQ, dK, workspace)
     M, d, H, Hkv, dtype, rot, flags = _rotate_sizes(dQ_out, dK_out, inv_freq, norm, w_q, w_k, flags)
     _index(positions, M, "positions")
@@ -1081,6 +1089,10 @@ def lemo_qk_rotate_step(Q: torch.Tensor, K: torch.Tensor, V: Optional[torch.Tens
                         Q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The newest token of each sequence, at position lengths - 1: Q [B,H,d] -> Q_out; K, V [B,H_kv,d] go to their rows of the caches
     [B,S_max,H_kv,d] in place."""
+    done = _native.qk_rotate_step(Q, K, V, K_cache, V_cache, lengths, inv_freq, norm, w_q, w_k, eps, amplitude, flags, Q_out)
+    if done is not None:
+        _check(done[0], "lemo_qk_rotate_step")
+        return done[1]
     _here(Q, K, V, K_cache, V_cache, lengths, inv_freq, w_q, w_k, Q_out)
     B, d, H, Hkv, dtype, rot, flags = _rotate_sizes(Q, K, inv_freq, norm, w_q, w_k, flags)
     _lengths(lengths, B)
@@ -1112,6 +1124,10 @@ def _generator(rng: torch.Tensor):
 
 def lemo_dropout_add(Y: torch.Tensor, R: torch.Tensor, kept_idx: Optional[torch.Tensor], rng: torch.Tensor, p: float, site: int = 0) -> torch.Tensor:
     """In place: R[kept_idx[m],:] += dropout(Y[m,:]).  Y [M,C], R [S,C]; rng int64 [2] on the GPU (seed, stream), site: which dropout of the step."""
+    rc = _native.dropout_add(Y, R, kept_idx, rng, p, site)
+    if rc is not None:
+        _check(rc, "lemo_dropout_add")
+        return R
     _here(Y, R, kept_idx, rng)
     _generator(rng)
     M, S, C, ldy, _, ldr = _norm_args(Y, R, kept_idx, None, None, None, None, None)
@@ -1124,6 +1140,10 @@ def lemo_dropout_add_grad(dR: torch.Tensor, kept_idx: Optional[torch.Tensor], rn
                           dY: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dY[m,:] = the gradient of lemo_dropout_add's Y from dR [S,C], with the same rng, p and site -> [M,C].  kept_idx None: plain dropout of dR's rows
     (dY may then be dR)."""
+    done = _native.dropout_add_grad(dR, kept_idx, rng, p, site, dY)
+    if done is not None:
+        _check(done[0], "lemo_dropout_add_grad")
+        return done[1]
     _here(dR, kept_idx, rng, dY)
     _generator(rng)
     M, S, C, _, _, lddr = _norm_args(None, dR, kept_idx, None, None, None, None, None)
@@ -1161,6 +1181,10 @@ def lemo_vocab_loss(X: torch.Tensor, kept_idx: Optional[torch.Tensor], W: torch.
                     z_weight: float = 0.0, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None,
                     workspace: Optional[torch.Tensor] = None) -> VocabLoss:
     """Cross entropy of the kept rows of X [S,C] over the vocabulary of W [V,C], labels [M] int32 (outside [0,V): the row does not count)."""
+    done = _native.vocab_loss(X, kept_idx, W, labels, softcap, smoothing, z_weight, loss, lse, total, workspace)
+    if done is not None:
+        _check(done[0], "lemo_vocab_loss")
+        return VocabLoss(*done[1:])
     _here(X, kept_idx, W, labels, loss, lse, total, workspace)
     S, C, M, V, ldx, ldw = _head(X, kept_idx, W, labels)
     loss = _filled(loss, (M,), torch.float32, X.device, "loss")
@@ -1177,6 +1201,10 @@ def lemo_vocab_loss_grad(dloss: torch.Tensor, X: torch.Tensor, kept_idx: Optiona
                          dX: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None, piece: int = 0, workspace: Optional[torch.Tensor] = None):
     """Gradients of lemo_vocab_loss from dloss [M], or one value for all rows [1] (the mean's: total[3:]) -> (dX [M,C], dW [V,C]), either None if not
     wanted.  piece: columns of the vocabulary at a time."""
+    done = _native.vocab_loss_grad(dloss, X, kept_idx, W, labels, lse, softcap, smoothing, z_weight, want_dX, want_dW, dX, dW, piece, workspace)
+    if done is not None:
+        _check(done[0], "lemo_vocab_loss_grad")
+        return done[1], done[2]
     _here(dloss, X, kept_idx, W, labels, lse, dX, dW, workspace)
     S, C, M, V, ldx, ldw = _head(X, kept_idx, W, labels)
     if dloss.dtype != torch.float32 or dloss.dim() != 1 or dloss.numel() not in (1, M) or not dloss.is_contiguous():
