@@ -26,42 +26,75 @@ constexpr long long VL_ROWS = 16384;  // rows of a forward launch: bounds what t
 
 // ---- rows --------------------------------------------------------------------------------------------
 
-// Joins the parts of a row: `per` rows a workgroup, VL_THREADS / per threads a row, each a part in so many; then those in their order.
+// sum, number, mean and 1 / number of the rows that count
+__device__ __forceinline__ void write_total(double sum, long long n, float* total) {
+    total[0] = (float)sum;
+    total[1] = (float)n;
+    total[2] = n ? (float)(sum / (double)n) : 0.f;
+    total[3] = n ? (float)(1. / (double)n) : 0.f;
+}
+
+// Joins the parts of a row: `per` rows a workgroup (a power of two up to 64), VL_THREADS / per threads a row, each a part in so many; then the threads of a
+// wave, then the waves.  One workgroup for all rows: the losses' sum, too (total; a launch less).
 __global__ __launch_bounds__(VL_THREADS) void vocab_join_kernel(VocabRule rule, const float2* parts, const float* sums, const float* picked, const int* labels,
-                                                                long long M, int n, int per, float* loss, float* lse) {
-    __shared__ float lds[3][VL_THREADS];
+                                                                long long M, int n, int per, float* loss, float* lse, float* total) {
+    constexpr int WAVES = VL_THREADS / 64;
+    __shared__ float lds[3][WAVES][64];
+    __shared__ float losses[64];
     const int threads = VL_THREADS / per, mine = threadIdx.x / per;
     const long long m = (long long)blockIdx.x * per + threadIdx.x % per;
     float top = -INFINITY, sum = 0.f, all = 0.f;
     if (m < M) {
-#pragma unroll 4
+#pragma unroll 8
         for (int t = mine; t < n; t += threads) {
             const float2 v = parts[(long long)t * M + m];
             vocab_join(top, sum, v.x, v.y);
             if (sums) all += sums[(long long)t * M + m];
         }
     }
-    lds[0][threadIdx.x] = top;
-    lds[1][threadIdx.x] = sum;
-    lds[2][threadIdx.x] = all;
-    __syncthreads();
-    if (mine || m >= M) return;
-    for (int t = 1; t < threads; ++t) {
-        vocab_join(top, sum, lds[0][t * per + threadIdx.x], lds[1][t * per + threadIdx.x]);
-        all += lds[2][t * per + threadIdx.x];
+    for (int s = per; s < 64; s <<= 1) {
+        const float top2 = __shfl_xor(top, s), sum2 = __shfl_xor(sum, s);
+        vocab_join(top, sum, top2, sum2);
+        all += __shfl_xor(all, s);
     }
-    const float total = top + logf(sum);
-    lse[m] = total;
-    if (!loss) return;
-    const int label = labels[m];
-    const bool counts = label >= 0 && label < rule.V;
-    float v = fmaf(rule.z * total, total, total);
-    if (counts) v -= rule.hit * picked[m];
-    if (sums) v -= rule.all * all;
-    loss[m] = counts ? v : 0.f;
+    const int lane = threadIdx.x & 63;
+    if (lane < per) {
+        lds[0][threadIdx.x >> 6][lane] = top;
+        lds[1][threadIdx.x >> 6][lane] = sum;
+        lds[2][threadIdx.x >> 6][lane] = all;
+    }
+    __syncthreads();
+    if (threadIdx.x < per) {
+        for (int w = 1; w < WAVES; ++w) {
+            vocab_join(top, sum, lds[0][w][lane], lds[1][w][lane]);
+            all += lds[2][w][lane];
+        }
+        float v = 0.f;
+        if (m < M) {
+            const float whole = top + logf(sum);
+            lse[m] = whole;
+            const int label = labels[m];
+            if (label >= 0 && label < rule.V) {
+                v = fmaf(rule.z * whole, whole, whole) - rule.hit * picked[m];
+                if (sums) v -= rule.all * all;
+            }
+            loss[m] = v;
+        }
+        losses[threadIdx.x] = v;
+    }
+    if (!total) return;
+    __syncthreads();
+    if (threadIdx.x) return;
+    double of = 0.;
+    long long counted = 0;
+    for (long long i = 0; i < M; ++i) {
+        of += (double)losses[i];
+        counted += labels[i] >= 0 && labels[i] < rule.V;
+    }
+    write_total(of, counted, total);
 }
 
-// sum, number, mean and 1 / number of the rows that count
+// the same of many rows
 __global__ __launch_bounds__(1024) void vocab_total_kernel(const float* loss, const int* labels, long long M, int V, float* total) {
     __shared__ double sums[16];
     __shared__ int counts[16];
@@ -86,10 +119,7 @@ __global__ __launch_bounds__(1024) void vocab_total_kernel(const float* loss, co
         sum += sums[w];
         n += counts[w];
     }
-    total[0] = (float)sum;
-    total[1] = (float)n;
-    total[2] = n ? (float)(sum / (double)n) : 0.f;
-    total[3] = n ? (float)(1. / (double)n) : 0.f;
+    write_total(sum, n, total);
 }
 
 // What the gradient's products take of the rows: their losses' gradients side by side (ones, where one gradient for all is left out of G), and for the
@@ -300,13 +330,14 @@ int launch_vocab_loss(const VocabLossParams& p, lemo_dtype_t dt, hipStream_t st)
             }
         }
         if (rc) return rc;
-        const int per = M >= 4096 ? 32 : 4;  // few rows: more threads a row, whose parts are as many as the vocabulary's tiles
+        // few rows: more threads a row, whose parts are as many as the vocabulary's tiles; up to 16: one workgroup
+        const int per = M >= 4096 ? 32 : p.M <= 16 ? 16 : 4;
         hipLaunchKernelGGL(vocab_join_kernel, dim3((unsigned)((M + per - 1) / per)), dim3(VL_THREADS), 0, st, p.rule, s.parts, sums, s.picked, p.labels + m0, M, n, per,
-                           p.loss ? p.loss + m0 : nullptr, p.lse + m0);
+                           p.loss + m0, p.lse + m0, p.M <= 16 ? p.total : nullptr);
         rc = (int)hipGetLastError();
         if (rc) return rc;
     }
-    if (!p.total) return 0;
+    if (!p.total || (p.M > 0 && p.M <= 16)) return 0;
     hipLaunchKernelGGL(vocab_total_kernel, dim3(1), dim3(1024), 0, st, p.loss, p.labels, p.M, V, p.total);
     return (int)hipGetLastError();
 }

@@ -42,7 +42,7 @@ struct VocabLossParams {
     long long S, ldx, ldw, M;
     int C;
     VocabRule rule;
-    float *loss, *lse, *total;  // loss, total: or null
+    float *loss, *lse, *total;  // total: or null
     void* workspace;
 };
 struct VocabGradParams {
