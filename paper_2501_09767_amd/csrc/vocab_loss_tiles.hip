@@ -49,14 +49,24 @@ template <int LAYOUT, int UA> struct VocabTile {
     }
 };
 
-// the lanes of a row: lane, lane ^ 16, lane ^ 32, lane ^ 48
+// Over the lanes of a row: lane, lane ^ 16, lane ^ 32, lane ^ 48.  The swaps leave a lane's value and its partner's in two registers.
+__device__ __forceinline__ float2 swapped32(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float2 swapped16(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 __device__ __forceinline__ float row_lanes_max(float v) {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    const float2 a = swapped32(v);
+    const float2 b = swapped16(fmaxf(a.x, a.y));
+    return fmaxf(b.x, b.y);
 }
 __device__ __forceinline__ float row_lanes_sum(float v) {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    const float2 a = swapped32(v);
+    const float2 b = swapped16(a.x + a.y);
+    return b.x + b.y;
 }
 
 constexpr int vocab_layout(int what) { return what == VOCAB_PLANES ? GG_NN : what == VOCAB_WEIGHT ? GG_TN : GG_NT; }
@@ -143,30 +153,43 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
     }
     if constexpr (WHAT == VOCAB_STATS) {
         float* const red = reinterpret_cast<float*>(smem);  // [3][ACROSS][BM]: maxima, sums of exponentials, sums
+        int labels[Tile::ROWS];
+#pragma unroll
+        for (int i = 0; i < Tile::ROWS; ++i) labels[i] = p.labels[min(m0 + Tile::row(wave, lane, i), p.M - 1)];
 #pragma unroll
         for (int i = 0; i < Tile::ROWS; ++i) {
             const int row = Tile::row(wave, lane, i);
             const long long m = min(m0 + row, p.M - 1);
-            const unsigned label = (unsigned)p.labels[m] - (unsigned)(p.v0 + n0);  // column in the tile (a label outside the vocabulary is none of those below N)
-            float top = -INFINITY, sum = 0.f, all = 0.f;
+            float top = -INFINITY, sum, all = 0.f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 f32x4& v = Tile::at(acc, i, j);
-                const int c = Tile::col(wave, lane, j);
+                if (!whole) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (!whole && n0 + c + r >= p.N) v[r] = -INFINITY;
-                    else if ((unsigned)(c + r) == label) p.picked[m] = v[r];
-                    top = fmaxf(top, v[r]);
+                    for (int r = 0; r < 4; ++r)
+                        if (n0 + Tile::col(wave, lane, j) + r >= p.N) v[r] = -INFINITY;
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, v[r]);
+            }
+            // the label's logit: few tiles hold one (a label outside the vocabulary is no column below N)
+            const unsigned label = (unsigned)labels[i] - (unsigned)(p.v0 + n0);
+            if (__any(label < (unsigned)min(Tile::BN, p.N - n0))) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned at = label - (unsigned)Tile::col(wave, lane, j);
+                    const f32x4 v = Tile::at(acc, i, j);
+                    if (at < 4u && label < (unsigned)(p.N - n0)) p.picked[m] = at < 2 ? at ? v[1] : v[0] : at == 2 ? v[2] : v[3];
                 }
             }
             top = row_lanes_max(top);
             const float base = top == -INFINITY ? 0.f : top * LOG2E;
+            f32x4 some = {0.f, 0.f, 0.f, 0.f};  // (four chains of additions)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(Tile::at(acc, i, j)[r], LOG2E, -base));
-            sum = row_lanes_sum(sum);
+                for (int r = 0; r < 4; ++r) some[r] += __builtin_amdgcn_exp2f(fmaf(Tile::at(acc, i, j)[r], LOG2E, -base));
+            sum = row_lanes_sum((some[0] + some[1]) + (some[2] + some[3]));
             if (p.sums) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -196,11 +219,17 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
             if (p.sums) p.sums[to] = all;
         }
     } else {
+        VocabRow rows[Tile::ROWS];
+#pragma unroll
+        for (int i = 0; i < Tile::ROWS; ++i) {
+            const long long m = min(m0 + Tile::row(wave, lane, i), p.M - 1);
+            rows[i] = vocab_row(p.rule, p.lse[m], p.weight[m], p.labels[m]);
+        }
 #pragma unroll
         for (int i = 0; i < Tile::ROWS; ++i) {
             const int row = Tile::row(wave, lane, i);
             const long long m = min(m0 + row, p.M - 1);
-            const VocabRow of = vocab_row(p.rule, p.lse[m], p.weight[m], p.labels[m]);
+            const VocabRow of = rows[i];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int c = Tile::col(wave, lane, j);
