@@ -18,7 +18,7 @@
 
 namespace lemo {
 
-constexpr int RT_THREADS = 256;
+constexpr int RT_THREADS = 256, RT_MOST = 16;  // RT_MOST: tokens of a workgroup
 
 // Sum over the LANES neighbouring lanes of a head, the same bits in all of them.
 template <int LANES> __device__ __forceinline__ float head_sum(float v) {
@@ -89,7 +89,7 @@ template <int E, int LANES> __device__ __forceinline__ float head_norm(float (&x
 template <typename T, int D>
 __global__ __launch_bounds__(RT_THREADS) void qk_rotate_kernel(RotateParams p) {
     constexpr int E = RowPiece<T>::E, LANES = D / (2 * E);
-    __shared__ float2 table[4 * D / 2];
+    __shared__ float2 table[RT_MOST * D / 2];
     const int rp = p.rot / (2 * E), angles = rp * E;
     const long long block = p.first + blockIdx.x;
     const long long m0 = block / p.slots * p.tokens;
@@ -150,22 +150,22 @@ __global__ __launch_bounds__(RT_THREADS) void qk_rotate_kernel(RotateParams p) {
     }
 }
 
-// A workgroup's RT_THREADS / LANES places are heads, or where there are fewer heads than places, `teams` tokens by the heads.  It walks
-// the tokens in steps of the grid, RT_TOKENS a team at a time: the sums over the tokens stay with the lane that owns a channel.
-constexpr int RT_TOKENS = 4, RT_TEAMS = 8;
+// A workgroup's RT_THREADS / LANES places are `own` heads by `teams` tokens.  It walks the tokens in steps of the grid: the sums over the tokens
+// stay with the lane that owns a channel.  One token at a time, and four waves a SIMD instead (8192 tokens, 32 / 32 heads of 128: four tokens
+// ahead on two waves 95 us, one on three 100, on four 83; 32768 tokens, 32 / 8 heads 218 / 233 / 198: 5.1 TB/s).
+constexpr int RT_TEAMS = 8;
 template <typename T, int D>
-__global__ __launch_bounds__(RT_THREADS) void qk_rotate_grad_kernel(RotateGradParams p, int chunks, int teams) {
+__global__ __launch_bounds__(RT_THREADS, 4) void qk_rotate_grad_kernel(RotateGradParams p, int chunks, int own, int teams) {
     constexpr int E = RowPiece<T>::E, LANES = D / (2 * E), PLACES = RT_THREADS / LANES;
     constexpr float INV = 1.f / D;
     constexpr int MOST = PLACES < RT_TEAMS ? PLACES : RT_TEAMS;
-    __shared__ float2 table[RT_TOKENS * MOST * D / 2];
+    __shared__ float2 table[MOST * D / 2];
     __shared__ float sums[PLACES][D];
     const int rp = p.rot / (2 * E), angles = rp * E;
     const int chunk = blockIdx.x % chunks, walker = blockIdx.x / chunks, walkers = gridDim.x / chunks;
     const int heads = p.side[0].heads + p.side[1].heads;
     const int place = threadIdx.x / LANES, j = threadIdx.x % LANES;
-    const int team = teams > 1 ? place / heads : 0;  // (teams > 1: all heads in one workgroup)
-    const int head = chunk * PLACES + place - team * heads;
+    const int team = place / own, head = chunk * own + place - team * own;
     const bool live = head < heads && team < teams;
     const bool keys = head >= p.side[0].heads;
     const int h = keys ? head - p.side[0].heads : head;
@@ -181,64 +181,55 @@ __global__ __launch_bounds__(RT_THREADS) void qk_rotate_grad_kernel(RotateGradPa
         RowPiece<T>::get(row_load<T>(s.w, (long long)h * s.w_hs + c0), w0);
         RowPiece<T>::get(row_load<T>(s.w, (long long)h * s.w_hs + c1), w1);
     }
-    const int step = RT_TOKENS * teams;
-    for (long long m0 = (long long)walker * step; m0 < p.M; m0 += (long long)walkers * step) {
-        const int tokens = (int)min((long long)step, p.M - m0);
-        u32x4 x[RT_TOKENS][2], g[RT_TOKENS][2];
-#pragma unroll
-        for (int i = 0; i < RT_TOKENS; ++i) {
-            const int t = i * teams + team;
-            if (!live || t >= tokens) continue;
-            const long long m = m0 + t;
-            g[i][0] = row_load<T>(dY, m * dy_ts + h * dy_hs + c0);
-            g[i][1] = row_load<T>(dY, m * dy_ts + h * dy_hs + c1);
+    for (long long m0 = (long long)walker * teams; m0 < p.M; m0 += (long long)walkers * teams) {
+        const int tokens = (int)min((long long)teams, p.M - m0);
+        const bool there = live && team < tokens;
+        const long long m = m0 + team;
+        u32x4 x[2], g[2];
+        if (there) {
+            g[0] = row_load<T>(dY, m * dy_ts + h * dy_hs + c0);
+            g[1] = row_load<T>(dY, m * dy_ts + h * dy_hs + c1);
             if (p.norm != LEMO_NORM_NONE) {
-                x[i][0] = row_load<T>(s.X, m * s.x_ts + h * s.x_hs + c0);
-                x[i][1] = row_load<T>(s.X, m * s.x_ts + h * s.x_hs + c1);
+                x[0] = row_load<T>(s.X, m * s.x_ts + h * s.x_hs + c0);
+                x[1] = row_load<T>(s.X, m * s.x_ts + h * s.x_hs + c1);
             }
         }
         __syncthreads();  // the table of the tokens before has been read
         for (int r = threadIdx.x; r < tokens * angles; r += RT_THREADS) {
             const int t = r / angles;
-            const long long m = m0 + t;
-            table[r] = turn_of<E>(p.inv_freq, p.pos_start + (p.positions ? (long long)p.positions[m] : m), r - t * angles, rp, p.pairs, p.amplitude);
+            table[r] = turn_of<E>(p.inv_freq, p.pos_start + (p.positions ? (long long)p.positions[m0 + t] : m0 + t), r - t * angles, rp, p.pairs, p.amplitude);
         }
         __syncthreads();
+        if (!there) continue;
+        float t0[E], t1[E];
+        RowPiece<T>::get(g[0], t0);
+        RowPiece<T>::get(g[1], t1);
+        if (j < rp) turn<E, -1>(t0, t1, table + team * angles + j, rp, p.pairs);
+        if (p.norm != LEMO_NORM_NONE) {
+            float x0[E], x1[E];
+            RowPiece<T>::get(x[0], x0);
+            RowPiece<T>::get(x[1], x1);
+            const float rstd = head_norm<E, LANES>(x0, x1, p.norm, p.eps);
+            float both = 0.f, alone = 0.f;
 #pragma unroll
-        for (int i = 0; i < RT_TOKENS; ++i) {
-            const int t = i * teams + team;
-            if (!live || t >= tokens) continue;
-            const long long to = (m0 + t) * s.y_ts + h * s.y_hs;
-            float t0[E], t1[E];
-            RowPiece<T>::get(g[i][0], t0);
-            RowPiece<T>::get(g[i][1], t1);
-            if (j < rp) turn<E, -1>(t0, t1, table + t * angles + j, rp, p.pairs);
-            if (p.norm != LEMO_NORM_NONE) {
-                float x0[E], x1[E];
-                RowPiece<T>::get(x[i][0], x0);
-                RowPiece<T>::get(x[i][1], x1);
-                const float rstd = head_norm<E, LANES>(x0, x1, p.norm, p.eps);
-                float both = 0.f, alone = 0.f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    dw0[e] = fmaf(t0[e], x0[e], dw0[e]);
-                    dw1[e] = fmaf(t1[e], x1[e], dw1[e]);
-                    t0[e] *= w0[e];
-                    t1[e] *= w1[e];
-                    both = fmaf(t0[e], x0[e], fmaf(t1[e], x1[e], both));
-                    alone += t0[e] + t1[e];
-                }
-                both = head_sum<LANES>(both) * INV;
-                alone = p.norm == LEMO_NORM_LAYER ? head_sum<LANES>(alone) * INV : 0.f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    t0[e] = (t0[e] - fmaf(x0[e], both, alone)) * rstd;
-                    t1[e] = (t1[e] - fmaf(x1[e], both, alone)) * rstd;
-                }
+            for (int e = 0; e < E; ++e) {
+                dw0[e] = fmaf(t0[e], x0[e], dw0[e]);
+                dw1[e] = fmaf(t1[e], x1[e], dw1[e]);
+                t0[e] *= w0[e];
+                t1[e] *= w1[e];
+                both = fmaf(t0[e], x0[e], fmaf(t1[e], x1[e], both));
+                alone += t0[e] + t1[e];
             }
-            row_store<T>(s.Y, to + c0, RowPiece<T>::put(t0));
-            row_store<T>(s.Y, to + c1, RowPiece<T>::put(t1));
+            both = head_sum<LANES>(both) * INV;
+            alone = p.norm == LEMO_NORM_LAYER ? head_sum<LANES>(alone) * INV : 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                t0[e] = (t0[e] - fmaf(x0[e], both, alone)) * rstd;
+                t1[e] = (t1[e] - fmaf(x1[e], both, alone)) * rstd;
+            }
         }
+        row_store<T>(s.Y, m * s.y_ts + h * s.y_hs + c0, RowPiece<T>::put(t0));
+        row_store<T>(s.Y, m * s.y_ts + h * s.y_hs + c1, RowPiece<T>::put(t1));
     }
     if (!p.sums) return;
     // a channel's sums of the workgroup's places, in their order: of a head's teams, or of all queries and of all keys
@@ -248,21 +239,21 @@ __global__ __launch_bounds__(RT_THREADS) void qk_rotate_grad_kernel(RotateGradPa
         sums[place][c1 + e] = live ? dw1[e] : 0.f;
     }
     __syncthreads();
-    const int here = min(heads - chunk * PLACES, PLACES);  // heads of this workgroup
+    const int here = min(heads - chunk * own, own);  // heads of this workgroup
     if (p.per_head) {
         for (int c = threadIdx.x; c < here * D; c += RT_THREADS) {
             float v = 0.f;
-            for (int t = 0; t < teams; ++t) v += sums[t * heads + c / D][c % D];
-            p.parts[((long long)walker * heads + chunk * PLACES) * D + c] = v;
+            for (int t = 0; t < teams; ++t) v += sums[t * own + c / D][c % D];
+            p.parts[((long long)walker * heads + chunk * own) * D + c] = v;
         }
         return;
     }
     for (int c = threadIdx.x; c < 2 * D; c += RT_THREADS) {
-        const int queries = min(max(p.side[0].heads - chunk * PLACES, 0), here);
+        const int queries = min(max(p.side[0].heads - chunk * own, 0), here);
         const int first = c < D ? 0 : queries, last = c < D ? queries : here;
         float v = 0.f;
         for (int t = 0; t < teams; ++t)
-            for (int i = first; i < last; ++i) v += sums[t * heads + i][c % D];
+            for (int i = first; i < last; ++i) v += sums[t * own + i][c % D];
         p.parts[(long long)blockIdx.x * 2 * D + c] = v;
     }
 }
@@ -286,9 +277,12 @@ __global__ __launch_bounds__(RT_THREADS) void rotate_sums_kernel(const float* pa
 template <typename T, int D> static int launch_rotate(RotateParams p, hipStream_t st) {
     constexpr int HEADS = RT_THREADS / (D / (2 * RowPiece<T>::E));
     const int heads = p.side[0].heads + p.side[1].heads + p.side[2].heads;
-    // four tokens a workgroup share the work of their angles' table; few tokens are spread over as many workgroups as have a pass each
-    p.tokens = p.M >= 2048 ? 4 : 1;
-    p.slots = p.M >= 2048 ? 1 : (heads + HEADS - 1) / HEADS;
+    // A workgroup has the tokens that give its threads two passes at least, or one; few tokens are spread over as many workgroups as have a pass
+    // each.  8192 tokens, 32 / 32 heads of 128: 4 tokens 57 us, 2 55, 1 54 (5.0 TB/s);  4 / 4 heads of 64: 4 tokens 7.9, 2 9.3, 1 13.6.
+    const long long lanes = (long long)heads * (D / (2 * RowPiece<T>::E));
+    const bool many = p.M * lanes >= 1 << 18;
+    p.tokens = many ? (int)std::min<long long>(RT_MOST, std::max<long long>(1, 2 * RT_THREADS / lanes)) : 1;
+    p.slots = many ? 1 : (heads + HEADS - 1) / HEADS;
     const long long blocks = (p.M + p.tokens - 1) / p.tokens * p.slots;
     return launch_in_turns(blocks, RT_THREADS, [&](long long first, unsigned count) {
         p.first = first;
@@ -301,14 +295,24 @@ int launch_qk_rotate(RotateParams p, lemo_dtype_t dt, hipStream_t st) {
     return p.d == 64 ? launch_rotate<float, 64>(p, st) : launch_rotate<float, 128>(p, st);
 }
 
-// How the gradient's workgroups share the work: `chunks` of the heads, `teams` of tokens in one, `walkers` over the tokens
-struct RotateGrid { int chunks, teams, walkers; };
+// How the gradient's workgroups share the work: `chunks` of `own` heads each, `teams` of tokens in one, `walkers` over the tokens.  The fewest chunks that leave
+// a tenth of the places empty at most, or fewest empty ones (32768 tokens, 32 / 8 heads of 128: 2 chunks of 32 and 8 heads 266 us, 4 of 10 by 3 tokens 218).
+struct RotateGrid { int chunks, own, teams, walkers; };
 static RotateGrid rotate_grid(int64_t M, int heads, int d, lemo_dtype_t dt) {
     const int places = RT_THREADS / (d / (dt == LEMO_BF16 ? 16 : 8));
-    RotateGrid g;
-    g.chunks = (heads + places - 1) / places;
-    g.teams = std::min(RT_TEAMS, std::max(1, places / heads));
-    const int64_t steps = (M + RT_TOKENS * g.teams - 1) / (RT_TOKENS * g.teams);
+    RotateGrid g{};
+    double most = 0.;
+    for (int c = 1; c <= heads && most < 0.9; ++c) {
+        const int own = (heads + c - 1) / c, chunks = (heads + own - 1) / own;
+        if (own > places) continue;
+        const int teams = std::min(RT_TEAMS, places / own);
+        const double used = (double)heads * teams / ((double)chunks * places);
+        if (used > most) {
+            most = used;
+            g = {chunks, own, teams, 0};
+        }
+    }
+    const int64_t steps = (M + g.teams - 1) / g.teams;
     g.walkers = (int)std::max<int64_t>(1, std::min<int64_t>(steps, std::max(64, 1024 / g.chunks)));
     return g;
 }
@@ -319,7 +323,7 @@ size_t qk_rotate_grad_parts(int64_t M, int heads, int d, lemo_dtype_t dt, bool p
 }
 
 template <typename T, int D> static int launch_rotate_grad(const RotateGradParams& p, RotateGrid g, hipStream_t st) {
-    hipLaunchKernelGGL((qk_rotate_grad_kernel<T, D>), dim3((unsigned)(g.chunks * g.walkers)), dim3(RT_THREADS), 0, st, p, g.chunks, g.teams);
+    hipLaunchKernelGGL((qk_rotate_grad_kernel<T, D>), dim3((unsigned)(g.chunks * g.walkers)), dim3(RT_THREADS), 0, st, p, g.chunks, g.own, g.teams);
     return (int)hipGetLastError();
 }
 
