@@ -15,7 +15,9 @@
  * of the selective-load GEMM (lemo_gather_gemm_dx, lemo_gather_gemm_dw).  Then what a layer has around and instead of
  * these: the norms, gate and residual scale between two blocks, on the kept rows in place (lemo_norm_residual), and attention over
  * key blocks that a cheap score selects for each query (lemo_block_means, lemo_select_blocks, lemo_block_attention), both with
- * their gradients, the latter also for single tokens over caches (lemo_*_step).
+ * their gradients, the latter also for single tokens over caches (lemo_*_step).  And what a fine-tuning step has before the scoring
+ * and at its end, with gradients: norms and rotation of queries and keys (lemo_qk_rotate, also for single tokens), dropout into the residual
+ * rows (lemo_dropout_add), and the loss over a vocabulary without its logits (lemo_vocab_loss).
  *
  * Conventions shared by every call
  *   - Pointers are DEVICE pointers unless the comment says "host".  The caller owns every buffer;
@@ -601,12 +603,12 @@ int lemo_dropout_add_grad(const void* dR, int64_t lddr, int64_t S, const int32_t
  *   overwritten; either may be NULL (a head that is not trained, a first layer).  Rows that do not count get zeros in dX and add nothing to dW, whatever
  *   their rows of X hold.
  *   The vocabulary is worked through `piece` columns at a time (0: this library's choice, about 256 MB of G; rounded up to 64).
- *   workspace: lemo_vocab_loss_grad_workspace_bytes() bytes for the same piece, 256-byte aligned: a piece of G, and binary32 sums of dX.
+ *   workspace: lemo_vocab_loss_grad_workspace_bytes() bytes for the same piece and ldw, 256-byte aligned: a piece of G, and binary32 sums of dX.
  *   M == 0 writes zeros to dW.
  *
  * Sums in binary32 (of the losses in 64 bits), over the whole vocabulary and all rows before they are rounded once; in bf16 G is rounded to bf16 for
  * the two products.  No atomics: the same bits on every run.  What is not finite in a row of X spoils that row's results, and if it counts dW; in W, all.
- * Supported: bf16 and fp32; C % 8 == 0 (bf16) / % 4 (fp32), any V <= 2^21, M <= 2^22; X, W, dX, dW follow the 16-byte rule, pitches below 8 MiB (dX:
+ * Supported: bf16 and fp32; C % 8 == 0 (bf16) / % 4 (fp32), C <= 65536, any V <= 2^21, M <= 2^22; X, W, dX, dW follow the 16-byte rule, pitches below 8 MiB (dX:
  * any); X with a row more spanning less than 4 GiB - 4096; fp32: M * C * 4 below 4 GiB.  Results overlap neither operands nor each other.
  */
 int lemo_vocab_loss_workspace_bytes(int64_t M, int32_t C, int32_t V, lemo_dtype_t dt, size_t* bytes);

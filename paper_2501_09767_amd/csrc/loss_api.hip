@@ -9,16 +9,16 @@ using namespace lemo;
 namespace {
 
 constexpr int64_t MOST_ROWS = (int64_t)1 << 22;
-constexpr int32_t MOST_WORDS = 1 << 21;
+constexpr int32_t MOST_WORDS = 1 << 21, MOST_WIDTH = 1 << 16;  // (launches below 2^32 threads)
 
 int check_sizes(int64_t M, int32_t C, int32_t V, lemo_dtype_t dt) {
     if (!valid_dtype(dt)) return LEMO_ERR_DTYPE;
     if (M < 0 || C <= 0 || V <= 0) return LEMO_ERR_SHAPE;
-    return M > MOST_ROWS || V > MOST_WORDS || C % elems_per_16B(dt) ? LEMO_ERR_UNSUPPORTED : LEMO_OK;
+    return M > MOST_ROWS || V > MOST_WORDS || C > MOST_WIDTH || C % elems_per_16B(dt) ? LEMO_ERR_UNSUPPORTED : LEMO_OK;
 }
 
 bool valid_rule(float softcap, float smoothing, float z_weight) {
-    return std::isfinite(softcap) && softcap >= 0.f && smoothing >= 0.f && smoothing <= 1.f && std::isfinite(z_weight);
+    return std::isfinite(softcap) && softcap >= 0.f && (softcap == 0.f || std::isfinite(1.f / softcap)) && smoothing >= 0.f && smoothing <= 1.f && std::isfinite(z_weight);
 }
 VocabRule rule_of(float softcap, float smoothing, float z_weight, int32_t V) { return {softcap, 1.f - smoothing, smoothing / (float)V, z_weight, V}; }
 

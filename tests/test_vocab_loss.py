@@ -326,9 +326,9 @@ def test_argument_errors():
               wsb=1 << 24, stream=None)
     f = lambda **kw: lib.lemo_vocab_loss(*[dict(ok, **kw)[k] for k in names])  # noqa: E731
     assert f(dt=7) == -3 and f(X=None) == -1 and f(W=None) == -1 and f(labels=None) == -1 and f(loss=None) == -1 and f(lse=None) == -1 and f(ws=None) == -1
-    assert f(cap=-1.0) == -2 and f(cap=math.inf) == -2 and f(s=-0.1) == -2 and f(s=1.5) == -2 and f(s=math.nan) == -2 and f(z=math.nan) == -2
+    assert f(cap=-1.0) == -2 and f(cap=math.inf) == -2 and f(cap=1e-40) == -2 and f(s=-0.1) == -2 and f(s=1.5) == -2 and f(s=math.nan) == -2 and f(z=math.nan) == -2
     assert f(S=0) == -2 and f(M=-1) == -2 and f(idx=None, M=101) == -2 and f(ldx=56) == -2 and f(ldw=32) == -2 and f(V=0) == -2
-    assert f(C=60) == -6 and f(ldx=2 ** 22) == -6 and f(S=2 ** 25) == -6 and f(V=2 ** 21 + 1) == -6
+    assert f(C=60) == -6 and f(ldx=2 ** 22) == -6 and f(S=2 ** 25) == -6 and f(V=2 ** 21 + 1) == -6 and f(C=65544, ldx=65544, ldw=65544) == -6
     assert f(X=P[0] + 8) == -5 and f(W=P[2] + 2) == -5 and f(ldx=68) == -5 and f(labels=P[3] + 2) == -5 and f(total=P[6] + 1) == -5 and f(ws=P[7] + 16) == -5
     assert f(wsb=64) == -4
     need = lib.lemo_vocab_loss_grad_workspace_bytes
