@@ -609,7 +609,7 @@ int lemo_dropout_add_grad(const void* dR, int64_t lddr, int64_t S, const int32_t
  * Sums in binary32 (of the losses in 64 bits), over the whole vocabulary and all rows before they are rounded once; in bf16 G is rounded to bf16 for
  * the two products.  No atomics: the same bits on every run.  What is not finite in a row of X spoils that row's results, and if it counts dW; in W, all.
  * Supported: bf16 and fp32; C % 8 == 0 (bf16) / % 4 (fp32), C <= 65536, any V <= 2^21, M <= 2^22; X, W, dX, dW follow the 16-byte rule, pitches below 8 MiB (dX:
- * any); X with a row more spanning less than 4 GiB - 4096; fp32: M * C * 4 below 4 GiB.  Results overlap neither operands nor each other.
+ * any); X with a row more spanning less than 4 GiB - 4096; fp32: (M + 63) * C * 4 below 4 GiB.  Results overlap neither operands nor each other.
  */
 int lemo_vocab_loss_workspace_bytes(int64_t M, int32_t C, int32_t V, lemo_dtype_t dt, size_t* bytes);
 int lemo_vocab_loss(const void* X, int64_t S, int64_t ldx, const int32_t* kept_idx, int64_t M, const void* W, int64_t ldw, int32_t C, int32_t V,

@@ -36,7 +36,7 @@ struct GgParams {
 };
 
 // The same with the contraction cut into parts of k_part (a multiple of a slab): part `b / blocks` of workgroup b, whose sums go to a matrix of its own, `plane`
-// elements behind the one before (X W^T, the large binary32 tiles).
+// elements behind the one before (GG_NT, or GG_TN without a list; the large binary32 tiles).
 struct GgPartParams : GgParams {
     int k_part, blocks;
     long long plane;
@@ -68,7 +68,7 @@ int launch_gather_gemm_mid(const GgParams& p, bool add, int layout, GgTile tile,
 int launch_gather_gemm_small(const GgParams& p, lemo_dtype_t dt, bool add, int layout, GgTile tile, hipStream_t st);
 GgTile gg_choose_tile(long long M, int N, int K, int layout, int most_splits, double split_us, int* splits);  // bf16
 // Y (+)= A . B^T over parts of the contraction, the planes of Y M * N apart with rows of N: binary32, 128 x 128 tiles
-int launch_gather_gemm_parts(const GgParams& p, bool add, int parts, int k_part, hipStream_t st);
+int launch_gather_gemm_parts(const GgParams& p, bool add, int layout, int parts, int k_part, hipStream_t st);
 int prepare_gather_gemm_parts();
 
 }  // namespace lemo

@@ -70,14 +70,15 @@ __global__ __launch_bounds__(SG_THREADS, GW == 4 ? 2 : 1) void gather_gemm_small
 
     int tm, tn, block = blockIdx.x;
     if constexpr (std::is_same_v<P, GgPartParams>) {
-        static_assert(LAYOUT == GG_NT, "parts of the contraction: rows of both operands run along it");
+        static_assert(LAYOUT != GG_NN, "both operands along the contraction, or neither");
         const int part = block / p.blocks, k0 = part * p.k_part;  // (host: below K for every part)
         block -= part * p.blocks;
-        p.A = static_cast<const T*>(p.A) + k0;
-        p.B = static_cast<const T*>(p.B) + k0;
+        p.A = static_cast<const T*>(p.A) + (A_KMAJOR ? k0 * p.lda : k0);
+        p.B = static_cast<const T*>(p.B) + (A_KMAJOR ? k0 * p.ldb : k0);
         p.Y = static_cast<T*>(p.Y) + part * p.plane;
         p.K = min(p.k_part, p.K - k0);
-        p.a_bytes -= (unsigned)k0 * ESZ;
+        if (A_KMAJOR) p.b_bytes -= (unsigned)k0 * (unsigned)p.ldb * ESZ;
+        else p.a_bytes -= (unsigned)k0 * ESZ;
     }
     if (!gg_tile(block, p.tiles_m, p.tiles_n, 8, tm, tn)) return;
     const long long m0 = (long long)tm * G::BM;
@@ -665,24 +666,27 @@ static int prepare_small_form(bool add, int layout) {
     return add ? prepare_small<T, true, GG_NT>() : prepare_small<T, false, GG_NT>();
 }
 
-template <bool ADD> static int launch_parts(GgPartParams p, int parts, hipStream_t st) {
+template <bool ADD, int LAYOUT> static int launch_parts(GgPartParams p, int parts, hipStream_t st) {
     using G = SgGeo<4, 4, 2>;
     p.tiles_m = (int)((p.M + G::BM - 1) / G::BM);
     p.tiles_n = (p.N + G::BN - 1) / G::BN;
     p.blocks = (p.tiles_m * p.tiles_n + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
-    hipLaunchKernelGGL((gather_gemm_small_kernel<float, ADD, GG_NT, 4, 2, true, 32, GgPartParams>), dim3((unsigned)(p.blocks * parts)), dim3(SG_THREADS), G::LDS, st, p);
+    hipLaunchKernelGGL((gather_gemm_small_kernel<float, ADD, LAYOUT, 4, 2, true, 32, GgPartParams>), dim3((unsigned)(p.blocks * parts)), dim3(SG_THREADS), G::LDS, st, p);
     return (int)hipGetLastError();
 }
-int launch_gather_gemm_parts(const GgParams& p, bool add, int parts, int k_part, hipStream_t st) {
+int launch_gather_gemm_parts(const GgParams& p, bool add, int layout, int parts, int k_part, hipStream_t st) {
     GgPartParams q;
     static_cast<GgParams&>(q) = p;
     q.k_part = k_part;
     q.plane = p.M * p.N;
-    return add ? launch_parts<true>(q, parts, st) : launch_parts<false>(q, parts, st);
+    if (layout == GG_TN) return add ? launch_parts<true, GG_TN>(q, parts, st) : launch_parts<false, GG_TN>(q, parts, st);
+    return add ? launch_parts<true, GG_NT>(q, parts, st) : launch_parts<false, GG_NT>(q, parts, st);
+}
+template <bool ADD, int LAYOUT> constexpr LdsLimit parts_limit() {
+    return {reinterpret_cast<const void*>(&gather_gemm_small_kernel<float, ADD, LAYOUT, 4, 2, true, 32, GgPartParams>), SgGeo<4, 4, 2>::LDS};
 }
 int prepare_gather_gemm_parts() {
-    static const int err = raise_lds_limits({{reinterpret_cast<const void*>(&gather_gemm_small_kernel<float, false, GG_NT, 4, 2, true, 32, GgPartParams>), SgGeo<4, 4, 2>::LDS},
-                                             {reinterpret_cast<const void*>(&gather_gemm_small_kernel<float, true, GG_NT, 4, 2, true, 32, GgPartParams>), SgGeo<4, 4, 2>::LDS}});
+    static const int err = raise_lds_limits({parts_limit<false, GG_NT>(), parts_limit<true, GG_NT>(), parts_limit<false, GG_TN>(), parts_limit<true, GG_TN>()});
     return err;
 }
 

@@ -90,7 +90,7 @@ int lemo_vocab_loss_grad(const float* dloss, int64_t dloss_stride, const void* X
     if ((dX && lddx < C) || (dW && lddw < C)) return LEMO_ERR_SHAPE;
     if (!aligned16(dX) || !aligned16(dW) || (dX && lddx % e16) || (dW && lddw % e16)) return LEMO_ERR_ALIGN;
     if (dW && lddw * esz >= (int64_t)1 << 23) return LEMO_ERR_UNSUPPORTED;
-    if (dX && dt == LEMO_F32 && M * C * esz >= (int64_t)1 << 32) return LEMO_ERR_UNSUPPORTED;  // (a plane's 32-bit offsets)
+    if (dX && dt == LEMO_F32 && (M + 63) * C * esz >= (int64_t)1 << 32) return LEMO_ERR_UNSUPPORTED;  // (a plane's 32-bit offsets)
     int cols = 0;
     if (M > 0) {
         rc = check_operands(X, S, ldx, kept_idx, M, W, ldw, C, dt, labels);

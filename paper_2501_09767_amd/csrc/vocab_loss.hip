@@ -12,8 +12,9 @@
 // What bounds it: the matrix cores, 2 M C V products forward and 6 in the gradients.  Keeping G of the whole vocabulary would save a
 // piece's tail and the additions to dX, and is what the operator is there to avoid.
 //
-// binary32: the products are the selective-load GEMM's, a piece at a time in both directions, with the softmax in kernels of its own between them; dX takes the
-// weight's piece transposed, since that GEMM wants both operands along the contraction, and cuts that into parts like bf16's.
+// binary32: the products are the selective-load GEMM's, a piece at a time in both directions, with the softmax in kernels of its own between them.  For dX
+// that GEMM wants both operands along the contraction, or neither: the smaller of G and the weight's piece is transposed, and the contraction cut into
+// parts like bf16's.
 #include <algorithm>
 
 #include "vocab_softmax.hpp"
@@ -122,26 +123,10 @@ __global__ __launch_bounds__(1024) void vocab_total_kernel(const float* loss, co
     write_total(sum, n, total);
 }
 
-// What the gradient's products take of the rows: their losses' gradients side by side (ones, where one gradient for all is left out of G), and for the
-// weight's gradient the rows of X, those without a label replaced by one past X's end, which the loads' range check turns into zeros
-// whatever such a row holds.  Row M is one more of those, and of zeros in G where `zeros` is given: the last row of G a product reads is then
-// one of zeros, whose last piece of columns may end in the operand's middle.
-__global__ __launch_bounds__(VL_THREADS) void vocab_rows_kernel(const float* dloss, long long stride, int ones, const int* labels, const int* idx, long long M,
-                                                                long long S, int V, float* weight, int* rows, u32x4* zeros, long long pieces) {
-    const long long at = (long long)blockIdx.x * VL_THREADS + threadIdx.x, all = (long long)gridDim.x * VL_THREADS;
-    for (long long m = at; m <= M; m += all) {
-        const bool counts = m < M && labels[m] >= 0 && labels[m] < V;
-        rows[m] = (int)(!counts ? S : idx ? (long long)idx[m] : m);
-        if (m < M) weight[m] = !counts ? 0.f : ones ? 1.f : dloss[m * stride];
-    }
-    if (zeros)
-        for (long long i = at; i < pieces; i += all) zeros[i] = u32x4{0u, 0u, 0u, 0u};
-}
-
 // dX = the sum of the planes, rounded once; in bf16 with the label's row of W times what G's rounding has left of its element, and times the gradient
 // that was left out of G.  A thread has 16 bytes of a row.
 template <typename T>
-__global__ __launch_bounds__(VL_THREADS) void vocab_planes_kernel(const float* planes, int n, const float* rest, const float* scale, const int* labels, int V,
+__global__ __launch_bounds__(VL_THREADS) void vocab_planes_kernel(const float* planes, long long plane, int n, const float* rest, const float* scale, const int* labels, int V,
                                                                   const void* W, long long ldw, long long M, int C, void* dX, long long lddx, long long first) {
     constexpr int E = RowPiece<T>::E;
     const long long per_row = C / E, i = (first + blockIdx.x) * VL_THREADS + threadIdx.x;
@@ -154,7 +139,7 @@ __global__ __launch_bounds__(VL_THREADS) void vocab_planes_kernel(const float* p
     if (label >= 0 && label < V) {
 #pragma unroll 4
         for (int s = 0; s < n; ++s) {
-            const f32x4* const at = reinterpret_cast<const f32x4*>(planes + ((long long)s * M + m) * C + c);
+            const f32x4* const at = reinterpret_cast<const f32x4*>(planes + s * plane + m * C + c);
 #pragma unroll
             for (int h = 0; h < E / 4; ++h) {
                 const f32x4 x = at[h];
@@ -223,13 +208,18 @@ __global__ __launch_bounds__(VL_THREADS) void vocab_stats_f32_kernel(VocabRule r
 }
 
 // logits -> G in place, and zeros in the columns from N up to a multiple of 64
-__global__ __launch_bounds__(VL_THREADS) void vocab_probs_f32_kernel(VocabRule rule, float* x, long long ldx, int N, int v0, const int* labels, const float* lse,
-                                                                     const float* weight, long long first) {
+__global__ __launch_bounds__(VL_THREADS) void vocab_probs_f32_kernel(VocabRule rule, VocabSide side, float* x, long long ldx, int N, int v0, const int* labels,
+                                                                     const float* lse, const int* idx, long long M, long long first) {
     const long long m = first + blockIdx.x;
+    if (side.rows) {
+        if (threadIdx.x == 0) vocab_list_row(rule, side, labels, idx, m, M);
+        if (side.zero_row && m == M - 1)
+            for (int n = threadIdx.x * 4; n < N; n += VL_THREADS * 4) *reinterpret_cast<f32x4*>(x + M * ldx + n) = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     float* const row = x + m * ldx;
     const bool capped = rule.softcap > 0.f;
     const float inv_cap = capped ? 1.f / rule.softcap : 0.f;
-    const VocabRow of = vocab_row(rule, lse[m], weight[m], labels[m]);
+    const VocabRow of = vocab_row_of(rule, side, lse, labels, m);
     for (int n = threadIdx.x * 4; n < (N + 63) / 64 * 64; n += VL_THREADS * 4) {
         f32x4* const at = reinterpret_cast<f32x4*>(row + n);
         f32x4 v = *at;
@@ -295,6 +285,17 @@ int prepare_vocab_grad(lemo_dtype_t dt) {
 
 static unsigned vl_span(long long rows, long long ld, long long cols, int esz) { return (unsigned)(((rows - 1) * ld + cols) * esz); }
 
+// binary32.  Up to 32 rows are one row of 32 x 32 tiles, on which the weight passes at memory's rate; 128 x 128 tiles would multiply by 96 rows of nothing
+// (16 rows, 4096 columns, 131072 words: 663 us).
+static int launch_logits_f32(const void* X, long long S, long long ldx, const int* idx, long long M, const void* W, long long ldw, float* Y, long long ldy, int C, int N,
+                             hipStream_t st) {
+    if (M > 32) return launch_gather_gemm(X, S, ldx, idx, M, W, ldw, nullptr, Y, ldy, C, N, LEMO_F32, st);
+    GgParams t{};
+    t.A = X; t.B = W; t.Y = Y; t.idx = idx; t.lda = ldx; t.ldb = ldw; t.ldy = ldy; t.M = M; t.K = C; t.N = N;
+    t.a_bytes = vl_span(S, ldx, C, 4);
+    return launch_gather_gemm_small(t, LEMO_F32, false, GG_NT, GG_T64, st);
+}
+
 int launch_vocab_loss(const VocabLossParams& p, lemo_dtype_t dt, hipStream_t st) {
     int rc = prepare_vocab_loss(dt);
     if (rc) return rc;
@@ -321,7 +322,7 @@ int launch_vocab_loss(const VocabLossParams& p, lemo_dtype_t dt, hipStream_t st)
             n = 0;
             for (int v0 = 0; v0 < V && rc == 0; v0 += s.piece, ++n) {
                 const int N = std::min(s.piece, V - v0);
-                rc = launch_gather_gemm(X, S, p.ldx, idx, M, static_cast<const float*>(p.W) + v0 * p.ldw, p.ldw, nullptr, s.logits, s.piece, p.C, N, dt, st);
+                rc = launch_logits_f32(X, S, p.ldx, idx, M, static_cast<const float*>(p.W) + v0 * p.ldw, p.ldw, s.logits, s.piece, p.C, N, st);
                 if (rc) break;
                 rc = launch_in_turns(M, VL_THREADS, [&](long long first, unsigned count) {
                     hipLaunchKernelGGL(vocab_stats_f32_kernel, dim3(count), dim3(VL_THREADS), 0, st, p.rule, s.logits, (long long)s.piece, N, v0, p.labels + m0, M,
@@ -358,10 +359,11 @@ static int f32_splits(long long M, int C, int K, int* k_part) {
     return best;
 }
 
-// gradient: rows, G, dX's planes, and in binary32 the weight's piece transposed
-struct GradSpace { float *weight, *rest; int* rows; char* G; float *planes, *turned; long long ldg; GgTile tile; int splits, k_split; size_t bytes; };
+// gradient: rows, G, dX's planes, and in binary32 what is transposed: G, with rows of `rows` to a multiple of 64, or the weight's piece
+struct GradSpace { float* rest; int* rows; char* G; float *planes, *turned; long long ldg, plane_rows; bool turn_G; GgTile tile; int splits, k_split; size_t bytes; };
 static GradSpace grad_space(long long M, int C, int V, int piece, lemo_dtype_t dt, void* base) {
     GradSpace s{};
+    s.plane_rows = M;
     const int esz = dt == LEMO_BF16 ? 2 : 4;
     s.ldg = vl_pitch(piece);
     char* at = static_cast<char*>(base);
@@ -370,7 +372,6 @@ static GradSpace grad_space(long long M, int C, int V, int piece, lemo_dtype_t d
         s.bytes += vl_round(bytes);
         return here;
     };
-    s.weight = reinterpret_cast<float*>(take((size_t)M * sizeof(float)));
     s.rest = reinterpret_cast<float*>(take((size_t)M * sizeof(float)));
     s.rows = reinterpret_cast<int*>(take((size_t)(M + 1) * sizeof(int)));
     s.G = take((size_t)(M + 1) * s.ldg * esz);
@@ -381,20 +382,22 @@ static GradSpace grad_space(long long M, int C, int V, int piece, lemo_dtype_t d
         s.k_split = (k + s.splits * 64 - 1) / (s.splits * 64) * 64;
     } else {
         s.splits = f32_splits(M, C, std::min(piece, V), &s.k_split);
-        s.turned = reinterpret_cast<float*>(take((size_t)C * s.ldg * sizeof(float)));
+        s.turn_G = M < C;
+        if (s.turn_G) s.plane_rows = (M + 63) / 64 * 64;
+        s.turned = reinterpret_cast<float*>(take((size_t)(s.turn_G ? s.plane_rows : C) * s.ldg * sizeof(float)));
     }
-    s.planes = reinterpret_cast<float*>(take((size_t)s.splits * M * C * sizeof(float)));
+    s.planes = reinterpret_cast<float*>(take((size_t)s.splits * s.plane_rows * C * sizeof(float)));
     return s;
 }
 size_t vocab_grad_workspace(long long M, int C, int V, int piece, lemo_dtype_t dt) { return M > 0 ? grad_space(M, C, V, piece, dt, nullptr).bytes : 0; }
 
 // bf16: one piece.  W: its first row.
-static int grad_piece_bf16(const VocabGradParams& p, const GradSpace& s, int v0, int N, const void* W, hipStream_t st) {
+static int grad_piece_bf16(const VocabGradParams& p, const GradSpace& s, const VocabSide& side, int v0, int N, const void* W, hipStream_t st) {
     int one = 1;
     VocabTileParams t{};
     t.A = p.X; t.B = W; t.idx = p.idx; t.lda = p.ldx; t.ldb = p.ldw; t.M = p.M; t.K = p.C; t.N = N;
     t.a_bytes = vl_span(p.S, p.ldx, p.C, 2);
-    t.rule = p.rule; t.labels = p.labels; t.v0 = v0; t.lse = p.lse; t.weight = s.weight; t.rest = s.rest; t.G = s.G; t.ldg = s.ldg;
+    t.rule = p.rule; t.labels = p.labels; t.v0 = v0; t.lse = p.lse; t.side = side; t.rest = s.rest; t.G = s.G; t.ldg = s.ldg;
     int rc = launch_vocab_tiles(t, VOCAB_PROBS, gg_choose_tile(p.M, N, p.C, GG_NT, 1, 0., &one), st);
     if (rc) return rc;
     if (p.dW) {
@@ -416,13 +419,13 @@ static int grad_piece_bf16(const VocabGradParams& p, const GradSpace& s, int v0,
     return launch_vocab_tiles(x, VOCAB_PLANES, s.tile, st);
 }
 
-static int grad_piece_f32(const VocabGradParams& p, const GradSpace& s, int v0, int N, const float* W, hipStream_t st) {
+static int grad_piece_f32(const VocabGradParams& p, const GradSpace& s, const VocabSide& side, int v0, int N, const float* W, hipStream_t st) {
     const int N4 = (N + 3) / 4 * 4;
     float* const G = reinterpret_cast<float*>(s.G);
-    int rc = launch_gather_gemm(p.X, p.S, p.ldx, p.idx, p.M, W, p.ldw, nullptr, G, s.ldg, p.C, N, LEMO_F32, st);
+    int rc = launch_logits_f32(p.X, p.S, p.ldx, p.idx, p.M, W, p.ldw, G, s.ldg, p.C, N, st);
     if (rc) return rc;
     rc = launch_in_turns(p.M, VL_THREADS, [&](long long first, unsigned count) {
-        hipLaunchKernelGGL(vocab_probs_f32_kernel, dim3(count), dim3(VL_THREADS), 0, st, p.rule, G, s.ldg, N, v0, p.labels, p.lse, s.weight, first);
+        hipLaunchKernelGGL(vocab_probs_f32_kernel, dim3(count), dim3(VL_THREADS), 0, st, p.rule, side, G, s.ldg, N, v0, p.labels, p.lse, p.idx, p.M, first);
     });
     if (rc) return rc;
     if (p.dW) {
@@ -430,14 +433,21 @@ static int grad_piece_f32(const VocabGradParams& p, const GradSpace& s, int v0, 
         if (rc) return rc;
     }
     if (!p.dX) return 0;
-    const long long pad = vl_pitch(N);
-    rc = launch_transpose(W, p.ldw, nullptr, N, pad, p.C, s.turned, st);
-    if (rc) return rc;
     GgParams x{};
-    x.A = G; x.B = s.turned; x.Y = s.planes; x.lda = s.ldg; x.ldb = pad; x.ldy = p.C; x.M = p.M; x.out_rows = p.M; x.K = N4; x.N = p.C;
-    x.a_bytes = vl_span(p.M, s.ldg, N4, 4);
-    x.y_bytes = vl_span(p.M, p.C, p.C, 4);
-    return launch_gather_gemm_parts(x, v0 > 0, (N4 + s.k_split - 1) / s.k_split, s.k_split, st);
+    x.Y = s.planes; x.ldy = p.C; x.M = x.out_rows = s.plane_rows; x.N = p.C;
+    x.y_bytes = vl_span(s.plane_rows, p.C, p.C, 4);
+    if (s.turn_G) {  // G^T [N, plane_rows], zeros behind M, and W as it lies
+        rc = launch_transpose(G, s.ldg, nullptr, p.M, s.plane_rows, N4, s.turned, st);
+        x.A = s.turned; x.B = W; x.lda = s.plane_rows; x.ldb = p.ldw; x.K = N;
+        x.b_bytes = vl_span(N, p.ldw, p.C, 4);
+    } else {
+        const long long pad = vl_pitch(N);
+        rc = launch_transpose(W, p.ldw, nullptr, N, pad, p.C, s.turned, st);
+        x.A = G; x.B = s.turned; x.lda = s.ldg; x.ldb = pad; x.K = N4;
+        x.a_bytes = vl_span(p.M, s.ldg, N4, 4);
+    }
+    if (rc) return rc;
+    return launch_gather_gemm_parts(x, v0 > 0, s.turn_G ? GG_TN : GG_NT, (x.K + s.k_split - 1) / s.k_split, s.k_split, st);
 }
 
 int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st) {
@@ -448,20 +458,17 @@ int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st)
     if (!p.dX && !p.dW) return 0;
     const GradSpace s = grad_space(p.M, C, V, p.piece, dt, p.workspace);
     const bool shared = p.dloss_stride == 0 && dt == LEMO_BF16;
-    const long long zeros = V % (16 / esz) ? s.ldg * esz / 16 : 0;
-    const unsigned blocks = (unsigned)std::max<long long>(p.M / VL_THREADS + 1, std::min<long long>(64, (zeros + VL_THREADS - 1) / VL_THREADS));
-    hipLaunchKernelGGL(vocab_rows_kernel, dim3(blocks), dim3(VL_THREADS), 0, st, p.dloss, p.dloss_stride, (int)shared, p.labels, p.idx, p.M, p.S, V, s.weight, s.rows,
-                       zeros ? reinterpret_cast<u32x4*>(s.G + p.M * s.ldg * esz) : nullptr, zeros);
-    rc = (int)hipGetLastError();
+    VocabSide side{p.dloss, p.dloss_stride, (int)shared, s.rows, (int)p.S, V % (16 / esz) != 0};
     for (int v0 = 0; v0 < V && rc == 0; v0 += p.piece) {
         const int N = std::min(p.piece, V - v0);
         const char* const W = static_cast<const char*>(p.W) + v0 * p.ldw * esz;
-        rc = dt == LEMO_BF16 ? grad_piece_bf16(p, s, v0, N, W, st) : grad_piece_f32(p, s, v0, N, reinterpret_cast<const float*>(W), st);
+        rc = dt == LEMO_BF16 ? grad_piece_bf16(p, s, side, v0, N, W, st) : grad_piece_f32(p, s, side, v0, N, reinterpret_cast<const float*>(W), st);
+        side.rows = nullptr;
     }
     if (rc || !p.dX) return rc;
     auto planes = [&](auto kernel, int e) {
         return launch_in_turns((p.M * (C / e) + VL_THREADS - 1) / VL_THREADS, VL_THREADS, [&](long long first, unsigned count) {
-            hipLaunchKernelGGL(kernel, dim3(count), dim3(VL_THREADS), 0, st, s.planes, s.splits, s.rest, shared ? p.dloss : nullptr, p.labels, V, p.W, p.ldw, p.M, C, p.dX,
+            hipLaunchKernelGGL(kernel, dim3(count), dim3(VL_THREADS), 0, st, s.planes, s.plane_rows * C, s.splits, s.rest, shared ? p.dloss : nullptr, p.labels, V, p.W, p.ldw, p.M, C, p.dX,
                                p.lddx, first);
         });
     };

@@ -10,6 +10,18 @@ struct VocabRule {
     int V;
 };
 
+// What the kernels that form G do beside it, for the products that follow: `rows` [M + 1], the rows of X for the weight's gradient, those without a label
+// replaced by `past`, one past X's end, which the loads' range check turns into zeros whatever such a row holds.  Entry M is one more of those, and
+// row M of G zeros where the vocabulary does not fill whole pieces of 16 bytes (zero_row): the last row of G that a product reads is then one of
+// zeros, whose last piece of columns may end in the operand's middle.
+struct VocabSide {
+    const float* dloss;  // gradients of the losses
+    long long stride;
+    int ones;            // 1 in their place: one gradient for all, which is left out of G
+    int* rows;           // or null: not the first piece
+    int past, zero_row;
+};
+
 // A product of the rows with (a piece of) the head's weight and what is done with a tile of it.  GgParams: A = X [S, C], idx = the kept rows, B = the piece's
 // first row of W, M, N = the piece's columns, K = C; for the planes A = G, B = W (contraction-major), K = the piece's columns, N = C; for the weight's
 // gradient A = G, B = X (both contraction-major, X's rows by idx), M = the piece's columns, N = C, K = rows.
@@ -21,7 +33,7 @@ struct VocabTileParams : GgParams {
     float* sums;           // statistics: [tiles_n][M] sums of the logits, or null (no smoothing)
     float* picked;         // statistics: [M] the labels' logits
     const float* lse;      // probabilities: [M]
-    const float* weight;   // probabilities: [M] gradients of the losses
+    VocabSide side;        // probabilities
     float* rest;           // probabilities: [M] what rounding the label's element has left
     void* G;               // probabilities: [M, ldg] bf16, columns from N up to a multiple of 8 are zeros
     long long ldg;

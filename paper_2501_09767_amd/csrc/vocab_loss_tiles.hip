@@ -219,11 +219,16 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
             if (p.sums) p.sums[to] = all;
         }
     } else {
+        if (p.side.rows) {
+            if (tn == 0 && tid < Tile::BM && m0 + tid < p.M) vocab_list_row(p.rule, p.side, p.labels, p.idx, m0 + tid, p.M);
+            if (p.side.zero_row && tm == p.tiles_m - 1 && tid < Tile::BN / 8 && n0 + tid * 8 < p.N)
+                *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.G) + p.M * p.ldg + n0 + tid * 8) = u32x4{0u, 0u, 0u, 0u};
+        }
         VocabRow rows[Tile::ROWS];
 #pragma unroll
         for (int i = 0; i < Tile::ROWS; ++i) {
             const long long m = min(m0 + Tile::row(wave, lane, i), p.M - 1);
-            rows[i] = vocab_row(p.rule, p.lse[m], p.weight[m], p.labels[m]);
+            rows[i] = vocab_row_of(p.rule, p.side, p.lse, p.labels, m);
         }
 #pragma unroll
         for (int i = 0; i < Tile::ROWS; ++i) {

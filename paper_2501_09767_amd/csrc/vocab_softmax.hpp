@@ -32,6 +32,17 @@ __device__ __forceinline__ VocabRow vocab_row(const VocabRule& r, float lse, flo
     const float neg = -lse * LOG2E, left = fmaf(-lse, LOG2E, -neg);
     return {neg, fmaf(2.f * r.z, lse, 1.f) * fmaf(left, 0.6931471805599453f, 1.f), weight, label, label >= 0 && label < r.V};
 }
+// row m of M (idx: of X, or null)
+__device__ __forceinline__ VocabRow vocab_row_of(const VocabRule& r, const VocabSide& side, const float* lse, const int* labels, long long m) {
+    const int label = labels[m];
+    const bool counts = label >= 0 && label < r.V;
+    return vocab_row(r, lse[m], !counts ? 0.f : side.ones ? 1.f : side.dloss[m * side.stride], label);
+}
+__device__ __forceinline__ void vocab_list_row(const VocabRule& r, const VocabSide& side, const int* labels, const int* idx, long long m, long long M) {
+    const int label = labels[m];
+    side.rows[m] = label >= 0 && label < r.V ? idx ? idx[m] : (int)m : side.past;
+    if (m == M - 1) side.rows[M] = side.past;
+}
 __device__ __forceinline__ float vocab_grad(const VocabRule& r, const VocabRow& row, float u, int v, float inv_cap) {
     float g = fmaf(__builtin_amdgcn_exp2f(fmaf(u, LOG2E, row.neg_lse2)), row.factor, -r.all);
     g = v == row.label ? g - r.hit : g;
