@@ -24,6 +24,7 @@ namespace lemo {
 
 constexpr int VL_THREADS = 256;
 constexpr long long VL_ROWS = 16384;  // rows of a forward launch: bounds what the tiles leave
+constexpr int VL_CHUNK = 8192;        // (binary32) columns of a workgroup: few long rows fill the machine, too
 
 // ---- rows --------------------------------------------------------------------------------------------
 
@@ -160,17 +161,18 @@ __global__ __launch_bounds__(VL_THREADS) void vocab_planes_kernel(const float* p
 
 // ---- binary32: a piece's logits in memory -----------------------------------------------------------
 
-// A workgroup a row (16-byte aligned): its part of the statistics, as a tile leaves it
-__global__ __launch_bounds__(VL_THREADS) void vocab_stats_f32_kernel(VocabRule rule, const float* x, long long ldx, int N, int v0, const int* labels, long long M,
-                                                                     float2* parts, float* sums, float* picked, long long first) {
+// A workgroup a chunk of a row (16-byte aligned): its part of the statistics, as a tile leaves it
+__global__ __launch_bounds__(VL_THREADS) void vocab_stats_f32_kernel(VocabRule rule, const float* x, long long ldx, int N, int chunks, int v0, const int* labels,
+                                                                     long long M, float2* parts, float* sums, float* picked, long long first) {
     __shared__ float lds[3][VL_THREADS / 64];
-    const long long m = first + blockIdx.x;
+    const long long block = first + blockIdx.x, m = block / chunks;
+    const int chunk = (int)(block - m * chunks), end = min(N, (chunk + 1) * VL_CHUNK);
     const float* const row = x + m * ldx;
     const bool capped = rule.softcap > 0.f;
     const float inv_cap = capped ? 1.f / rule.softcap : 0.f;
     const unsigned label = (unsigned)labels[m] - (unsigned)v0;
     float top = -INFINITY, sum = 0.f, all = 0.f;
-    for (int n = threadIdx.x * 4; n < N; n += VL_THREADS * 4) {
+    for (int n = chunk * VL_CHUNK + threadIdx.x * 4; n < end; n += VL_THREADS * 4) {
         const f32x4 v = *reinterpret_cast<const f32x4*>(row + n);  // (the pitch is a multiple of 64: what lies behind the row is there, and not used)
         float u[4], t = top;
 #pragma unroll
@@ -203,15 +205,16 @@ __global__ __launch_bounds__(VL_THREADS) void vocab_stats_f32_kernel(VocabRule r
         vocab_join(top, sum, lds[0][w], lds[1][w]);
         all += lds[2][w];
     }
-    parts[m] = make_float2(top, sum);
-    if (sums) sums[m] = all;
+    parts[chunk * M + m] = make_float2(top, sum);
+    if (sums) sums[chunk * M + m] = all;
 }
 
 // logits -> G in place, and zeros in the columns from N up to a multiple of 64
-__global__ __launch_bounds__(VL_THREADS) void vocab_probs_f32_kernel(VocabRule rule, VocabSide side, float* x, long long ldx, int N, int v0, const int* labels,
-                                                                     const float* lse, const int* idx, long long M, long long first) {
-    const long long m = first + blockIdx.x;
-    if (side.rows) {
+__global__ __launch_bounds__(VL_THREADS) void vocab_probs_f32_kernel(VocabRule rule, VocabSide side, float* x, long long ldx, int N, int chunks, int v0,
+                                                                     const int* labels, const float* lse, const int* idx, long long M, long long first) {
+    const long long block = first + blockIdx.x, m = block / chunks;
+    const int chunk = (int)(block - m * chunks), end = min((N + 63) / 64 * 64, (chunk + 1) * VL_CHUNK);
+    if (side.rows && chunk == 0) {
         if (threadIdx.x == 0) vocab_list_row(rule, side, labels, idx, m, M);
         if (side.zero_row && m == M - 1)
             for (int n = threadIdx.x * 4; n < N; n += VL_THREADS * 4) *reinterpret_cast<f32x4*>(x + M * ldx + n) = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -220,7 +223,7 @@ __global__ __launch_bounds__(VL_THREADS) void vocab_probs_f32_kernel(VocabRule r
     const bool capped = rule.softcap > 0.f;
     const float inv_cap = capped ? 1.f / rule.softcap : 0.f;
     const VocabRow of = vocab_row_of(rule, side, lse, labels, m);
-    for (int n = threadIdx.x * 4; n < (N + 63) / 64 * 64; n += VL_THREADS * 4) {
+    for (int n = chunk * VL_CHUNK + threadIdx.x * 4; n < end; n += VL_THREADS * 4) {
         f32x4* const at = reinterpret_cast<f32x4*>(row + n);
         f32x4 v = *at;
 #pragma unroll
@@ -237,6 +240,8 @@ __global__ __launch_bounds__(VL_THREADS) void vocab_probs_f32_kernel(VocabRule r
 static size_t vl_round(size_t v) { return (v + 255) / 256 * 256; }
 static long long vl_pitch(int piece) { return (piece + 63) / 64 * 64; }
 
+static int vl_chunks(int N) { return (N + VL_CHUNK - 1) / VL_CHUNK; }
+
 // Columns at a time.  A piece costs what its launches leave idle and, of dX, 8 bytes for each of M C elements; G of a piece costs memory, 256 MB here, which also
 // is what the last-level cache holds.
 static int vl_choice(long long M, int V, int esz) {
@@ -252,7 +257,9 @@ int vocab_piece(long long M, int C, int V, long long ldw, int wanted, lemo_dtype
     piece = std::min(piece, span / (ldw * esz) / 64 * 64);       // the piece's rows of W, and
     piece = std::min(piece, span / ((M + 1) * esz) / 64 * 64);   // G lie within 32-bit offsets,
     piece = std::min(piece, ((8ll << 20) / esz - 64) / 64 * 64); // G's pitch within a load's
-    return piece < 64 ? 0 : (int)piece;
+    if (piece < 64) return 0;
+    if (wanted == 0) piece = std::min(piece, vl_pitch((int)((V + (V + piece - 1) / piece - 1) / ((V + piece - 1) / piece))));  // no small rest
+    return (int)piece;
 }
 
 // forward: what the tiles, or binary32's pieces, leave
@@ -261,7 +268,7 @@ static LossSpace loss_space(long long M, int C, int V, lemo_dtype_t dt, void* ba
     LossSpace s{};
     s.rows = std::min(M, VL_ROWS);
     s.piece = dt == LEMO_F32 ? std::min<int>(vl_choice(s.rows, V, 4), (int)vl_pitch(V)) : 0;
-    const size_t n = dt == LEMO_F32 ? (size_t)((V + s.piece - 1) / s.piece) : (size_t)(V + 127) / 128;
+    const size_t n = dt == LEMO_F32 ? (size_t)((V + s.piece - 1) / s.piece) * vl_chunks(s.piece) : (size_t)(V + 127) / 128;
     char* at = static_cast<char*>(base);
     auto take = [&](size_t bytes) {
         char* const here = at + s.bytes;
@@ -320,14 +327,15 @@ int launch_vocab_loss(const VocabLossParams& p, lemo_dtype_t dt, hipStream_t st)
             rc = launch_vocab_tiles(t, VOCAB_STATS, tile, st);
         } else {
             n = 0;
-            for (int v0 = 0; v0 < V && rc == 0; v0 += s.piece, ++n) {
-                const int N = std::min(s.piece, V - v0);
+            for (int v0 = 0; v0 < V && rc == 0; v0 += s.piece) {
+                const int N = std::min(s.piece, V - v0), chunks = vl_chunks(N);
                 rc = launch_logits_f32(X, S, p.ldx, idx, M, static_cast<const float*>(p.W) + v0 * p.ldw, p.ldw, s.logits, s.piece, p.C, N, st);
                 if (rc) break;
-                rc = launch_in_turns(M, VL_THREADS, [&](long long first, unsigned count) {
-                    hipLaunchKernelGGL(vocab_stats_f32_kernel, dim3(count), dim3(VL_THREADS), 0, st, p.rule, s.logits, (long long)s.piece, N, v0, p.labels + m0, M,
-                                       s.parts + n * M, sums ? sums + n * M : nullptr, s.picked, first);
+                rc = launch_in_turns(M * chunks, VL_THREADS, [&](long long first, unsigned count) {
+                    hipLaunchKernelGGL(vocab_stats_f32_kernel, dim3(count), dim3(VL_THREADS), 0, st, p.rule, s.logits, (long long)s.piece, N, chunks, v0, p.labels + m0,
+                                       M, s.parts + n * M, sums ? sums + n * M : nullptr, s.picked, first);
                 });
+                n += chunks;
             }
         }
         if (rc) return rc;
@@ -424,8 +432,9 @@ static int grad_piece_f32(const VocabGradParams& p, const GradSpace& s, const Vo
     float* const G = reinterpret_cast<float*>(s.G);
     int rc = launch_logits_f32(p.X, p.S, p.ldx, p.idx, p.M, W, p.ldw, G, s.ldg, p.C, N, st);
     if (rc) return rc;
-    rc = launch_in_turns(p.M, VL_THREADS, [&](long long first, unsigned count) {
-        hipLaunchKernelGGL(vocab_probs_f32_kernel, dim3(count), dim3(VL_THREADS), 0, st, p.rule, side, G, s.ldg, N, v0, p.labels, p.lse, p.idx, p.M, first);
+    const int chunks = vl_chunks(N);  // (a multiple of 64 columns each: what fills up the last 64 belongs to the last)
+    rc = launch_in_turns(p.M * chunks, VL_THREADS, [&](long long first, unsigned count) {
+        hipLaunchKernelGGL(vocab_probs_f32_kernel, dim3(count), dim3(VL_THREADS), 0, st, p.rule, side, G, s.ldg, N, chunks, v0, p.labels, p.lse, p.idx, p.M, first);
     });
     if (rc) return rc;
     if (p.dW) {
