@@ -35,26 +35,43 @@ struct GgParams {
     unsigned a_bytes, b_bytes, y_bytes;  // spans of the whole operands (b_bytes: GG_TN; y_bytes: in-place add)
 };
 
-// The same with the contraction cut into parts of k_part (a multiple of a slab): part `b / blocks` of workgroup b, whose sums go to a matrix of its own, `plane`
-// elements behind the one before (GG_NT, or GG_TN without a list; the large binary32 tiles).
+// The same with the contraction cut into parts of k_part (a multiple of a slab), whose sums go to matrices of their own, `plane` elements apart
+// (GG_NT, or GG_TN without a list; the large binary32 tiles).
 struct GgPartParams : GgParams {
-    int k_part, blocks;
+    int k_part, parts;
     long long plane;
 };
 
-// Tile of workgroup b: die b % 8 takes a contiguous run of tiles in grouped order (group_m tile rows at a time, column
-// by column), so the tiles resident on one die share rows of both operands through its L2.  False: nothing to do.
-__device__ __forceinline__ bool gg_tile(int b, int tiles_m, int tiles_n, int group_m, int& tm, int& tn) {
-    const int total = tiles_m * tiles_n;
-    const int per_xcd = (total + NUM_XCD - 1) / NUM_XCD;
-    const int tile = (b % NUM_XCD) * per_xcd + b / NUM_XCD;
-    if (b / NUM_XCD >= per_xcd || tile >= total) return false;
+// Place of tile `tile` in grouped order: group_m tile rows at a time, column by column.
+__device__ __forceinline__ void gg_place(int tile, int tiles_m, int tiles_n, int group_m, int& tm, int& tn) {
     const int group = tile / (group_m * tiles_n);
     const int first_m = group * group_m;
     const int rows_in_group = min(group_m, tiles_m - first_m);
     const int within = tile - group * group_m * tiles_n;
     tm = first_m + within % rows_in_group;
     tn = within / rows_in_group;
+}
+
+// Tile of workgroup b: die b % 8 takes a contiguous run of tiles in grouped order, so the tiles resident on one die share rows of both operands
+// through its L2.  False: nothing to do.
+__device__ __forceinline__ bool gg_tile(int b, int tiles_m, int tiles_n, int group_m, int& tm, int& tn) {
+    const int total = tiles_m * tiles_n;
+    const int per_xcd = (total + NUM_XCD - 1) / NUM_XCD;
+    const int tile = (b % NUM_XCD) * per_xcd + b / NUM_XCD;
+    if (b / NUM_XCD >= per_xcd || tile >= total) return false;
+    gg_place(tile, tiles_m, tiles_n, group_m, tm, tn);
+    return true;
+}
+
+// The same over parts of the contraction, part by part: a die has few parts, whose rows of both operands pass through its L2 once.  (Every part on all dies, 777 rows, 768
+// columns, 50001 of the contraction, binary32: 500 us, so 375.)
+__device__ __forceinline__ bool gg_part_tile(int b, int parts, int tiles_m, int tiles_n, int group_m, int& part, int& tm, int& tn) {
+    const int tiles = tiles_m * tiles_n, total = tiles * parts;
+    const int per_xcd = (total + NUM_XCD - 1) / NUM_XCD;
+    const int item = (b % NUM_XCD) * per_xcd + b / NUM_XCD;
+    if (b / NUM_XCD >= per_xcd || item >= total) return false;
+    part = item / tiles;
+    gg_place(item - part * tiles, tiles_m, tiles_n, group_m, tm, tn);
     return true;
 }
 

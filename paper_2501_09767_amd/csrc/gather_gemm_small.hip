@@ -68,19 +68,21 @@ __global__ __launch_bounds__(SG_THREADS, GW == 4 ? 2 : 1) void gather_gemm_small
     constexpr int GROUPS = G::GROUPS, NLD = G::NLD;
     extern __shared__ __attribute__((aligned(16))) char smem[];
 
-    int tm, tn, block = blockIdx.x;
+    int tm, tn;
     if constexpr (std::is_same_v<P, GgPartParams>) {
         static_assert(LAYOUT != GG_NN, "both operands along the contraction, or neither");
-        const int part = block / p.blocks, k0 = part * p.k_part;  // (host: below K for every part)
-        block -= part * p.blocks;
+        int part;
+        if (!gg_part_tile(blockIdx.x, p.parts, p.tiles_m, p.tiles_n, 8, part, tm, tn)) return;
+        const int k0 = part * p.k_part;  // (host: below K for every part)
         p.A = static_cast<const T*>(p.A) + (A_KMAJOR ? k0 * p.lda : k0);
         p.B = static_cast<const T*>(p.B) + (A_KMAJOR ? k0 * p.ldb : k0);
         p.Y = static_cast<T*>(p.Y) + part * p.plane;
         p.K = min(p.k_part, p.K - k0);
         if (A_KMAJOR) p.b_bytes -= (unsigned)k0 * (unsigned)p.ldb * ESZ;
         else p.a_bytes -= (unsigned)k0 * ESZ;
+    } else {
+        if (!gg_tile(blockIdx.x, p.tiles_m, p.tiles_n, 8, tm, tn)) return;
     }
-    if (!gg_tile(block, p.tiles_m, p.tiles_n, 8, tm, tn)) return;
     const long long m0 = (long long)tm * G::BM;
     const int n0 = tn * G::BN;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
@@ -670,8 +672,9 @@ template <bool ADD, int LAYOUT> static int launch_parts(GgPartParams p, int part
     using G = SgGeo<4, 4, 2>;
     p.tiles_m = (int)((p.M + G::BM - 1) / G::BM);
     p.tiles_n = (p.N + G::BN - 1) / G::BN;
-    p.blocks = (p.tiles_m * p.tiles_n + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
-    hipLaunchKernelGGL((gather_gemm_small_kernel<float, ADD, LAYOUT, 4, 2, true, 32, GgPartParams>), dim3((unsigned)(p.blocks * parts)), dim3(SG_THREADS), G::LDS, st, p);
+    p.parts = parts;
+    const unsigned blocks = (unsigned)((p.tiles_m * p.tiles_n * parts + NUM_XCD - 1) / NUM_XCD * NUM_XCD);
+    hipLaunchKernelGGL((gather_gemm_small_kernel<float, ADD, LAYOUT, 4, 2, true, 32, GgPartParams>), dim3(blocks), dim3(SG_THREADS), G::LDS, st, p);
     return (int)hipGetLastError();
 }
 int launch_gather_gemm_parts(const GgParams& p, bool add, int layout, int parts, int k_part, hipStream_t st) {

@@ -91,19 +91,18 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int tm, tn, block = blockIdx.x, split = 0;
+    int tm, tn, split = 0;
     GgParams q = p;
     if constexpr (WHAT == VOCAB_PLANES) {
-        const int each = (p.tiles_m * p.tiles_n + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
-        split = block / each;
-        block -= split * each;
+        if (!gg_part_tile(blockIdx.x, p.splits, p.tiles_m, p.tiles_n, Tile::GROUP, split, tm, tn)) return;
         const int k0 = split * p.k_split;  // (host: below the contraction's length for every split)
         q.A = static_cast<const bf16_t*>(p.A) + k0;
         q.B = static_cast<const bf16_t*>(p.B) + (long long)k0 * p.ldb;
         q.K = min(p.k_split, p.K - k0);
         q.a_bytes = p.a_bytes - (unsigned)k0 * 2u;
+    } else {
+        if (!gg_tile(blockIdx.x, p.tiles_m, p.tiles_n, Tile::GROUP, tm, tn)) return;
     }
-    if (!gg_tile(block, p.tiles_m, p.tiles_n, Tile::GROUP, tm, tn)) return;
     const long long m0 = (long long)tm * Tile::BM;
     const int n0 = tn * Tile::BN;
     typename Tile::Acc acc;
@@ -277,7 +276,7 @@ template <int WHAT, int UA> static int launch_one(VocabTileParams p, hipStream_t
     using Tile = VocabTile<vocab_layout(WHAT), UA>;
     p.tiles_m = (int)((p.M + Tile::BM - 1) / Tile::BM);
     p.tiles_n = (p.N + Tile::BN - 1) / Tile::BN;
-    const long long blocks = ((long long)p.tiles_m * p.tiles_n + NUM_XCD - 1) / NUM_XCD * NUM_XCD * (WHAT == VOCAB_PLANES ? p.splits : 1);
+    const long long blocks = ((long long)p.tiles_m * p.tiles_n * (WHAT == VOCAB_PLANES ? p.splits : 1) + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
     if (blocks * RG_THREADS >= 1ll << 32) return (int)hipErrorInvalidValue;  // (the callers' pieces are far below)
     hipLaunchKernelGGL((vocab_tile_kernel<WHAT, UA>), dim3((unsigned)blocks), dim3(RG_THREADS), Tile::LDS, st, p);
     return (int)hipGetLastError();
