@@ -229,7 +229,7 @@ __global__ __launch_bounds__(VL_THREADS) void vocab_probs_f32_kernel(VocabRule r
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float u = capped ? vocab_cap(v[e], rule.softcap, inv_cap) : v[e];
-            v[e] = n + e < N ? vocab_grad(rule, of, u, v0 + n + e, inv_cap) : 0.f;
+            v[e] = n + e < N && of.counts ? vocab_grad(rule, of, u, v0 + n + e == of.label, inv_cap) : 0.f;
         }
         *at = v;
     }

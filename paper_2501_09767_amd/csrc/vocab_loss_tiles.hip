@@ -234,22 +234,36 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
             const int row = Tile::row(wave, lane, i);
             const long long m = min(m0 + row, p.M - 1);
             const VocabRow of = rows[i];
+            const uint32_t mask = of.counts ? ~0u : 0u;
+            char* const to = smem + row * Tile::PITCH;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int c = Tile::col(wave, lane, j);
                 float g[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    g[r] = vocab_grad(p.rule, of, Tile::at(acc, i, j)[r], p.v0 + n0 + c + r, inv_cap);
-                    if (!whole && n0 + c + r >= p.N) g[r] = 0.f;
+                for (int r = 0; r < 4; ++r) g[r] = vocab_share(of, Tile::at(acc, i, j)[r]);
+                if (capped) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) g[r] = vocab_slope(p.rule, g[r], Tile::at(acc, i, j)[r], inv_cap);
                 }
-                const uint2 stored = make_uint2(pack_bf16x2_hw(g[0], g[1]), pack_bf16x2_hw(g[2], g[3]));
-                *reinterpret_cast<uint2*>(smem + row * Tile::PITCH + c * 2) = stored;
-                const unsigned label = (unsigned)of.label - (unsigned)(p.v0 + n0 + c);  // (a column past the piece is no label of this piece's: below)
-                if (label < 4u && (whole || n0 + c + (int)label < p.N)) {
-                    const uint32_t two = label < 2 ? stored.x : stored.y;
-                    const float left = label < 2 ? label ? g[1] : g[0] : label & 1 ? g[3] : g[2];
-                    p.rest[m] = left - (label & 1 ? bf16hi_to_f32(two) : bf16lo_to_f32(two));
+                if (!whole) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) g[r] = n0 + c + r < p.N ? g[r] : 0.f;
+                }
+                *reinterpret_cast<uint2*>(to + c * 2) = make_uint2(pack_bf16x2_hw(g[0], g[1]) & mask, pack_bf16x2_hw(g[2], g[3]) & mask);
+            }
+            // the label's element, over what the lane has just written there: few tiles hold one
+            const unsigned label = (unsigned)of.label - (unsigned)(p.v0 + n0);
+            if (__any(label < (unsigned)min(Tile::BN, p.N - n0))) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned at = label - (unsigned)Tile::col(wave, lane, j);
+                    if (at >= 4u || label >= (unsigned)(p.N - n0)) continue;
+                    const f32x4 v = Tile::at(acc, i, j);
+                    const float g = vocab_grad(p.rule, of, at < 2 ? at ? v[1] : v[0] : at == 2 ? v[2] : v[3], true, inv_cap);
+                    const uint32_t stored = pack_bf16x2_hw(g, 0.f);
+                    *reinterpret_cast<uint16_t*>(to + label * 2) = (uint16_t)stored;
+                    p.rest[m] = g - bf16lo_to_f32(stored);
                 }
             }
         }

@@ -25,32 +25,32 @@ __device__ __forceinline__ void vocab_join(float& top, float& sum, float top2, f
     top = t;
 }
 
-// Gradient of a row's logit u (capped) at column v: what the row's probabilities and label leave, times the gradient of its loss.
-struct VocabRow { float neg_lse2, factor, weight; int label; bool counts; };
-__device__ __forceinline__ VocabRow vocab_row(const VocabRule& r, float lse, float weight, int label) {
-    // what rounding lse log2(e) leaves would be an error of all of the row's probabilities: it goes into their factor (lse 10, binary32: 6e-7 of them)
-    const float neg = -lse * LOG2E, left = fmaf(-lse, LOG2E, -neg);
-    return {neg, fmaf(2.f * r.z, lse, 1.f) * fmaf(left, 0.6931471805599453f, 1.f), weight, label, label >= 0 && label < r.V};
-}
-// row m of M (idx: of X, or null)
+// What the gradient of a row's logits takes of the row: the probabilities' factor, smoothing's share and the label's, all times the gradient of its loss.
+struct VocabRow { float neg_lse2, factor, all, hit; int label; bool counts; };
+// row m
 __device__ __forceinline__ VocabRow vocab_row_of(const VocabRule& r, const VocabSide& side, const float* lse, const int* labels, long long m) {
     const int label = labels[m];
     const bool counts = label >= 0 && label < r.V;
-    return vocab_row(r, lse[m], !counts ? 0.f : side.ones ? 1.f : side.dloss[m * side.stride], label);
+    const float weight = !counts ? 0.f : side.ones ? 1.f : side.dloss[m * side.stride];
+    // what rounding lse log2(e) leaves would be an error of all of the row's probabilities: it goes into their factor (lse 10, binary32: 6e-7 of them)
+    const float neg = -lse[m] * LOG2E, left = fmaf(-lse[m], LOG2E, -neg);
+    return {neg, weight * fmaf(2.f * r.z, lse[m], 1.f) * fmaf(left, 0.6931471805599453f, 1.f), weight * r.all, weight * r.hit, label, counts};
+}
+// Gradient of its logit u (capped) at a column that is not its label's, and at its label's.  A row that does not count may hold anything: what comes of it is
+// replaced by zeros.
+__device__ __forceinline__ float vocab_slope(const VocabRule& r, float g, float u, float inv_cap) {
+    const float t = u * inv_cap;
+    return r.softcap > 0.f ? g * fmaf(-t, t, 1.f) : g;
+}
+__device__ __forceinline__ float vocab_share(const VocabRow& row, float u) { return fmaf(__builtin_amdgcn_exp2f(fmaf(u, LOG2E, row.neg_lse2)), row.factor, -row.all); }
+__device__ __forceinline__ float vocab_grad(const VocabRule& r, const VocabRow& row, float u, bool hit, float inv_cap) {
+    const float g = vocab_share(row, u);
+    return vocab_slope(r, hit ? g - row.hit : g, u, inv_cap);
 }
 __device__ __forceinline__ void vocab_list_row(const VocabRule& r, const VocabSide& side, const int* labels, const int* idx, long long m, long long M) {
     const int label = labels[m];
     side.rows[m] = label >= 0 && label < r.V ? idx ? idx[m] : (int)m : side.past;
     if (m == M - 1) side.rows[M] = side.past;
-}
-__device__ __forceinline__ float vocab_grad(const VocabRule& r, const VocabRow& row, float u, int v, float inv_cap) {
-    float g = fmaf(__builtin_amdgcn_exp2f(fmaf(u, LOG2E, row.neg_lse2)), row.factor, -r.all);
-    g = v == row.label ? g - r.hit : g;
-    if (r.softcap > 0.f) {
-        const float t = u * inv_cap;
-        g *= fmaf(-t, t, 1.f);
-    }
-    return row.counts ? g * row.weight : 0.f;  // (chosen: a row without a label may hold anything)
 }
 
 }  // namespace lemo
