@@ -127,8 +127,8 @@ __global__ __launch_bounds__(1024) void vocab_total_kernel(const float* loss, co
 // dX = the sum of the planes, rounded once; in bf16 with the label's row of W times what G's rounding has left of its element, and times the gradient
 // that was left out of G.  A thread has 16 bytes of a row.
 template <typename T>
-__global__ __launch_bounds__(VL_THREADS) void vocab_planes_kernel(const float* planes, long long plane, int n, const float* rest, const float* scale, const int* labels, int V,
-                                                                  const void* W, long long ldw, long long M, int C, void* dX, long long lddx, long long first) {
+__global__ __launch_bounds__(VL_THREADS) void vocab_planes_kernel(const float* planes, long long plane, int n, const float* rest, const float* scale, float scale_by,
+                                                                  const int* labels, int V, const void* W, long long ldw, long long M, int C, void* dX, long long lddx, long long first) {
     constexpr int E = RowPiece<T>::E;
     const long long per_row = C / E, i = (first + blockIdx.x) * VL_THREADS + threadIdx.x;
     const long long m = i / per_row;
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(VL_THREADS) void vocab_planes_kernel(const float* p
             }
         }
         if constexpr (E == 8) {
-            const float left = rest[m], by = scale ? *scale : 1.f;
+            const float left = rest[m], by = scale ? *scale * scale_by : 1.f;
             float w[E];
             RowPiece<T>::get(row_load<T>(W, label * ldw + c), w);
 #pragma unroll
@@ -414,7 +414,7 @@ static int grad_piece_bf16(const VocabGradParams& p, const GradSpace& s, const V
         g.K = (int)p.M + (N % 8 != 0);
         g.Y = static_cast<char*>(p.dW) + v0 * p.lddw * 2; g.ldy = p.lddw;
         g.b_bytes = vl_span(p.S, p.ldx, p.C, 2);
-        g.scale = p.dloss_stride == 0 ? p.dloss : nullptr;
+        if (side.uniform != 0.f) g.scale = p.dloss, g.scale_by = 1.f / side.uniform;
         rc = launch_vocab_tiles(g, VOCAB_WEIGHT, gg_choose_tile(N, p.C, g.K, GG_TN, 1, 0., &one), st);
         if (rc) return rc;
     }
@@ -467,7 +467,7 @@ int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st)
     if (!p.dX && !p.dW) return 0;
     const GradSpace s = grad_space(p.M, C, V, p.piece, dt, p.workspace);
     const bool shared = p.dloss_stride == 0 && dt == LEMO_BF16;
-    VocabSide side{p.dloss, p.dloss_stride, (int)shared, s.rows, (int)p.S, V % (16 / esz) != 0};
+    VocabSide side{p.dloss, p.dloss_stride, !shared ? 0.f : p.rule.hit > 0.f ? 1.f / p.rule.hit : 1.f, s.rows, (int)p.S, V % (16 / esz) != 0};
     for (int v0 = 0; v0 < V && rc == 0; v0 += p.piece) {
         const int N = std::min(p.piece, V - v0);
         const char* const W = static_cast<const char*>(p.W) + v0 * p.ldw * esz;
@@ -477,8 +477,8 @@ int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st)
     if (rc || !p.dX) return rc;
     auto planes = [&](auto kernel, int e) {
         return launch_in_turns((p.M * (C / e) + VL_THREADS - 1) / VL_THREADS, VL_THREADS, [&](long long first, unsigned count) {
-            hipLaunchKernelGGL(kernel, dim3(count), dim3(VL_THREADS), 0, st, s.planes, s.plane_rows * C, s.splits, s.rest, shared ? p.dloss : nullptr, p.labels, V, p.W, p.ldw, p.M, C, p.dX,
-                               p.lddx, first);
+            hipLaunchKernelGGL(kernel, dim3(count), dim3(VL_THREADS), 0, st, s.planes, s.plane_rows * C, s.splits, s.rest, shared ? p.dloss : nullptr,
+                               shared ? 1.f / side.uniform : 1.f, p.labels, V, p.W, p.ldw, p.M, C, p.dX, p.lddx, first);
         });
     };
     return dt == LEMO_BF16 ? planes(vocab_planes_kernel<bf16_t>, 8) : planes(vocab_planes_kernel<float>, 4);

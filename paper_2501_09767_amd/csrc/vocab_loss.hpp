@@ -10,14 +10,17 @@ struct VocabRule {
     int V;
 };
 
-// What the kernels that form G do beside it, for the products that follow: `rows` [M + 1], the rows of X for the weight's gradient, those without a label
-// replaced by `past`, one past X's end, which the loads' range check turns into zeros whatever such a row holds.  Entry M is one more of those, and
-// row M of G zeros where the vocabulary does not fill whole pieces of 16 bytes (zero_row): the last row of G that a product reads is then one of
-// zeros, whose last piece of columns may end in the operand's middle.
+// What the kernels that form G do beside it, for the products that follow.
+//   rows [M + 1]   the rows of X for the weight's gradient, those without a label replaced by `past`, one past X's end, which the loads' range check
+//             turns into zeros whatever such a row holds.  Entry M is one more of those, and row M of G zeros where the vocabulary does not fill
+//             whole pieces of 16 bytes (zero_row): the last row of G that a product reads is then one of zeros, whose last piece of columns may
+//             end in the operand's middle.
+//   uniform   one gradient for all losses: G is formed for gradients of `uniform` each (1 / (1 - smoothing), which makes the label's share 1), the rest is
+//             multiplied into the results.  0: gradients of their own.
 struct VocabSide {
     const float* dloss;  // gradients of the losses
     long long stride;
-    int ones;            // 1 in their place: one gradient for all, which is left out of G
+    float uniform;
     int* rows;           // or null: not the first piece
     int past, zero_row;
 };
@@ -40,7 +43,8 @@ struct VocabTileParams : GgParams {
     float* planes;         // planes: [splits][M][N]
     int splits, k_split;   // planes: of the contraction, and its length of each (a multiple of 64)
     int add;               // planes: to what they hold
-    const float* scale;    // the weight's gradient: a factor for all of it, or null
+    const float* scale;    // the weight's gradient: a factor for all of it, times scale_by, or null
+    float scale_by;
 };
 enum { VOCAB_STATS, VOCAB_PROBS, VOCAB_PLANES, VOCAB_WEIGHT };
 int prepare_vocab_tiles();

@@ -7,7 +7,7 @@
 //                   vocabulary at a time.  bf16 because the two products that follow take it so: off by 2^-9 of each element, at random.
 //                   The largest error is that of the label's element, whose rest dX gets back (vocab_planes_kernel); and one
 //                   gradient for all losses is left out of G and multiplied into the results instead, since its rounding would be the same
-//                   relative error in every label's element (4096 rows, 131072 words, mean: dX and dW 3.0e-3 from 64 bits, so 1.9e-3; their own store alone 1.7e-3).
+//                   relative error in every label's element (4096 rows, 131072 words, mean: dX and dW 3.0e-3 from 64 bits, so 1.8e-3; their own store alone 1.7e-3).
 //   planes          dX = G W over the piece's columns, in binary32: a piece adds to what the pieces before left, and where the
 //                   output has few tiles the contraction is split, with a plane for each part; a kernel of its own rounds their sum once.
 //   the weight's    dW = G^T X[idx], the piece's rows, times what was left out of G, rounded once.
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
         return;
     }
     if constexpr (WHAT == VOCAB_WEIGHT) {
-        const float scale = p.scale ? *p.scale : 1.f;
+        const float scale = p.scale ? *p.scale * p.scale_by : 1.f;
 #pragma unroll
         for (int i = 0; i < Tile::ROWS; ++i)
 #pragma unroll

@@ -31,7 +31,7 @@ struct VocabRow { float neg_lse2, factor, all, hit; int label; bool counts; };
 __device__ __forceinline__ VocabRow vocab_row_of(const VocabRule& r, const VocabSide& side, const float* lse, const int* labels, long long m) {
     const int label = labels[m];
     const bool counts = label >= 0 && label < r.V;
-    const float weight = !counts ? 0.f : side.ones ? 1.f : side.dloss[m * side.stride];
+    const float weight = !counts ? 0.f : side.uniform != 0.f ? side.uniform : side.dloss[m * side.stride];
     // what rounding lse log2(e) leaves would be an error of all of the row's probabilities: it goes into their factor (lse 10, binary32: 6e-7 of them)
     const float neg = -lse[m] * LOG2E, left = fmaf(-lse[m], LOG2E, -neg);
     return {neg, weight * fmaf(2.f * r.z, lse[m], 1.f) * fmaf(left, 0.6931471805599453f, 1.f), weight * r.all, weight * r.hit, label, counts};
