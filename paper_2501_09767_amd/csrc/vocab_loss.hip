@@ -9,8 +9,10 @@
 // logits once more, turned into G, then its rows of dW (finished: every token is in them) and its part of dX, which is added up in
 // binary32 over the pieces and rounded once.  No atomics: the same bits on every run.
 //
-// What bounds it: the matrix cores, 2 M C V products forward and 6 in the gradients.  Keeping G of the whole vocabulary would save a
-// piece's tail and the additions to dX, and is what the operator is there to avoid.
+// What bounds it: the matrix cores, 2 M C V products forward and 6 in the gradients (8192 rows of 4096, 131072 words, bf16: loss 6.1 ms, 1.43 PFLOP/s; 777 rows
+// of 768, 50001 words, binary32: gradients 1.21 ms, 148 TFLOP/s of a library product's 154); with few rows the weight's bytes (16 rows of 4096,
+// 32000 words, bf16: loss 61 us = 4.3 TB/s).  Keeping G of the whole vocabulary would save a piece's tail and the additions to dX, and is what
+// the operator is there to avoid.
 //
 // binary32: the products are the selective-load GEMM's, a piece at a time in both directions, with the softmax in kernels of its own between them.  For dX
 // that GEMM wants both operands along the contraction, or neither: the smaller of G and the weight's piece is transposed, and the contraction cut into

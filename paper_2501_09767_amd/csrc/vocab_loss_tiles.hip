@@ -12,7 +12,9 @@
 //                   output has few tiles the contraction is split, with a plane for each part; a kernel of its own rounds their sum once.
 //   the weight's    dW = G^T X[idx], the piece's rows, times what was left out of G, rounded once.
 //
-// What bounds it: the matrix cores, as in gather_gemm_large.hip; the epilogues read no memory but a few bytes a row.
+// What bounds it: the matrix cores, as in gather_gemm_large.hip; the epilogues read no memory but a few bytes a row.  8192 rows, 4096 columns, 131072 words:
+// statistics 6.1 ms, 1.43 PFLOP/s, matrix cores busy for 74 % of the cycles; the gradients of 4096 rows 9.7 ms, 1.36 (probabilities 66 %, planes 72 %,
+// the weight's 64 %).  Narrow rows are few slabs a tile, whose first loads and epilogue nothing overlaps: 256 columns take twice the products' time.
 #include "gather_gemm_tiles.hpp"
 #include "vocab_softmax.hpp"
 
