@@ -34,13 +34,13 @@ PEAK_HBM_GBS = 8000.0       # MI355X HBM3E, published
 # The figures belong to the kernel sources they were measured on: "sources" is sources_digest() at that time, and the
 # bench reports traffic as null when the sources have changed since.
 MEASURED_TRAFFIC_BYTES = {
-    "sources": "27cec1cbc9c1582b",
-    "C5:rowstats": 2549091643, "C5:colsum": 2679616646, "C5:head_mean_select": 8650907,
-    "C5:gather_gemm": 1687178573, "C5:scatter": 242879169,
+    "sources": "42cfba904c2210cb",
+    "C5:rowstats": 2546315861, "C5:colsum": 2689182037, "C5:head_mean_select": 8651435,
+    "C5:gather_gemm": 1686823125, "C5:scatter": 242889557,
 }
 
 
-HOT_PATH_SOURCES = ("lemo_common.hpp", "score.hip", "score_sweeps.hpp", "select.hip", "gather_gemm.hpp", "gather_gemm.hip", "gather_gemm_large.hip", "gather_gemm_mid.hip", "gather_gemm_regions.hpp", "gather_gemm_small.hip", "scatter.hip")
+HOT_PATH_SOURCES = ("lemo_common.hpp", "score.hip", "score_sweeps.hpp", "select.hip", "gather_gemm.hpp", "gather_gemm.hip", "gather_gemm_large.hip", "gather_gemm_mid.hip", "gather_gemm_regions.hpp", "gather_gemm_small.hip", "gather_gemm_tiles.hpp", "scatter.hip")
 
 
 def sources_digest() -> str:
