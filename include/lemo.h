@@ -532,7 +532,7 @@ int lemo_block_attention_step(const void* Q, const void* K, const void* V, int32
  *   its caches.  Other rows of the caches are not touched.
  *
  * binary32 arithmetic, one rounding at the store; no atomics: the same bits on every run.  What is not finite in a head spoils that head's
- * row only (and the sums over the tokens).  M == 0 is a no-op.  Results overlap neither operands, but as said, nor each other.
+ * row only (and the sums over the tokens).  M == 0 is a no-op.  Results overlap neither operands, but as said, nor each other, nor their rows one another (LEMO_ERR_SHAPE).
  * Supported: d in {64, 128}, bf16 and fp32; rot <= d, a multiple of 16 (bf16) / 8 (fp32); H + H_kv <= 65535, M < 2^31; positions and
  * pos_start of magnitude below 2^31.
  */

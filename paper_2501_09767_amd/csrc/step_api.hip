@@ -1,5 +1,7 @@
 // Host side of the norms and rotation of queries and keys and of dropout (lemo.h): argument validation and kernel launches only.
+#include <algorithm>
 #include <cmath>
+#include <utility>
 
 #include "api_checks.hpp"
 #include "dropout.hpp"
@@ -17,11 +19,18 @@ int check_heads(const void* p, int64_t ts, int64_t hs, int32_t heads, int e16) {
     return aligned16(p) && ts % e16 == 0 && hs % e16 == 0 ? LEMO_OK : LEMO_ERR_ALIGN;
 }
 
-// the same for a result, whose rows and heads do not lie on each other
-int check_result(const void* p, int64_t ts, int64_t hs, int64_t M, int32_t heads, int32_t d, int e16) {
+// the same for a result, whose rows do not lie on each other: of its dimensions, from the shortest stride on, each steps over what those before it span
+int check_result(const void* p, int64_t ts, int64_t hs, int64_t M, int32_t heads, int32_t d, int e16, int64_t seqs = 1, int64_t ss = 0) {
     const int rc = check_heads(p, ts, hs, heads, e16);
     if (rc != LEMO_OK || heads == 0) return rc;
-    return (M > 1 && ts < d) || (heads > 1 && hs < d) ? LEMO_ERR_SHAPE : LEMO_OK;
+    std::pair<int64_t, int64_t> dims[3] = {{ts, M}, {hs, heads}, {ss, seqs}};
+    std::sort(dims, dims + 3);
+    __int128 span = d;
+    for (const auto& [stride, n] : dims) {
+        if (n > 1 && stride < span) return LEMO_ERR_SHAPE;
+        if (n > 1) span += (__int128)(n - 1) * stride;
+    }
+    return LEMO_OK;
 }
 
 // what the three calls on heads share
@@ -168,11 +177,11 @@ int lemo_qk_rotate_step(const void* Q, int64_t q_tok_stride, int64_t q_head_stri
     rc = check_heads(Q, q_tok_stride, q_head_stride, H, e16);
     if (rc == LEMO_OK) rc = check_result(Q_out, qo_tok_stride, qo_head_stride, B, H, d, e16);
     if (rc == LEMO_OK) rc = check_heads(K, k_tok_stride, k_head_stride, H_kv, e16);
-    if (rc == LEMO_OK) rc = check_result(K_cache, kc_tok_stride, kc_head_stride, S_max, H_kv, d, e16);
+    if (rc == LEMO_OK) rc = check_result(K_cache, kc_tok_stride, kc_head_stride, S_max, H_kv, d, e16, B, kc_seq_stride);
     if (rc == LEMO_OK) rc = check_heads(V, v_tok_stride, v_head_stride, H_v, e16);
-    if (rc == LEMO_OK) rc = check_result(V_cache, vc_tok_stride, vc_head_stride, S_max, H_v, d, e16);
+    if (rc == LEMO_OK) rc = check_result(V_cache, vc_tok_stride, vc_head_stride, S_max, H_v, d, e16, B, vc_seq_stride);
     if (rc != LEMO_OK) return rc;
-    if ((H_kv > 0 && kc_seq_stride < (B > 1 ? d : 0)) || (H_v > 0 && vc_seq_stride < (B > 1 ? d : 0))) return LEMO_ERR_SHAPE;
+    if ((H_kv > 0 && kc_seq_stride < 0) || (H_v > 0 && vc_seq_stride < 0)) return LEMO_ERR_SHAPE;
     if ((H_kv > 0 && kc_seq_stride % e16) || (H_v > 0 && vc_seq_stride % e16) || (reinterpret_cast<uintptr_t>(lengths) & 3u)) return LEMO_ERR_ALIGN;
     RotateParams p{};
     p.side[0] = side(Q, q_tok_stride, q_head_stride, Q_out, qo_tok_stride, qo_head_stride, H, w_q, norm, d, flags);

@@ -321,6 +321,26 @@ def test_argument_errors():
     assert f(B=0) == 0
 
 
+def test_results_whose_rows_lie_on_each_other_are_refused():
+    """Refused on the host, in whatever order the dimensions lie; what is not refused for its strides is for the positions' or lengths' address, looked at after them."""
+    from paper_2501_09767_amd import lemo
+    lib = lemo._lib
+    A = 0x10000
+
+    def rotate(M, H, ts, hs):  # (heads of queries only)
+        return lib.lemo_qk_rotate(A, 4096, 128, None, 0, 0, M, H, 0, 128, 1, A + 2, 0, A, 128, 1.0, 1, None, None, 1e-6, 0, A, ts, hs, None, 0, 0, None)
+
+    def step(B, S, H, seq, tok, head):  # (heads of keys only)
+        return lib.lemo_qk_rotate_step(None, 0, 0, A, 4096, 128, None, 0, 0, B, S, 0, H, 128, 1, A + 2, A, 128, 1.0, 1, None, None, 1e-6, 0, None, 0, 0, A, seq, tok, head,
+                                       None, 0, 0, 0, None)
+    assert rotate(10, 4, 512, 128) == -5 and rotate(10, 4, 128, 1280) == -5 and rotate(1, 4, 0, 128) == -5 and rotate(10, 1, 128, 0) == -5
+    for ts, hs in ((128, 128), (384, 128), (128, 1152), (512, 0), (0, 1280), (504, 128)):
+        assert rotate(10, 4, ts, hs) == -2, (ts, hs)
+    assert step(3, 100, 2, 25600, 256, 128) == -5 and step(3, 100, 2, 256, 768, 128) == -5 and step(3, 100, 2, 25600, 128, 12800) == -5 and step(1, 100, 2, 0, 256, 128) == -5
+    for seq, tok, head in ((256, 256, 128), (25472, 256, 128), (128, 256, 128), (256, 512, 128), (25600, 256, 0), (2 ** 62, 2 ** 62, 128)):
+        assert step(3, 100, 2, seq, tok, head) == -2, (seq, tok, head)
+
+
 def test_binding_refuses_tensors_that_do_not_fit(lemo):
     with pytest.raises(ValueError):
         lemo.lemo_qk_rotate(torch.zeros(2, 1, 64), None, None)  # not on the GPU
