@@ -20,8 +20,18 @@ static_assert(LG_LDS <= 160 * 1024, "a workgroup's LDS");
 
 // The product of a 256 x 256 tile at row m0, column n0: acc[a][i][b][j][r] is row a*128 + (wm*TA + i)*16 + lane % 16, column
 // b*128 + (wn*TB + j)*16 + 4*(lane / 16) + r of the tile, wm = wave / LG_WN, wn = wave % LG_WN.  At the end nothing is on its way to LDS, and everyone is done with it.
-template <int LAYOUT>
-__device__ __forceinline__ void lg_product(const GgParams& p, long long m0, int n0, char* smem, f32x4 (&acc)[2][LG_TA][2][LG_TB]) {
+//
+// With a run that has MORE tiles (its first at m0, n0): what is asked for ahead in a tile's last slabs is the next tile's, run.next(), on its way while run.done(acc)
+// does with the tile what is to be done; it leaves the stages alone, returns with all loads landed for everyone, and says whether there is another tile.
+struct LgOne {
+    static constexpr bool MORE = false;
+    template <class Loads> __device__ __forceinline__ int slabs(const Loads& ld) const { return ld.nk; }
+    template <class Loads> __device__ __forceinline__ typename Loads::Slab slab(const Loads& ld, int kt) const { return ld.slab(kt); }
+};
+template <int LAYOUT, class Run = LgOne>
+__device__ __forceinline__ void lg_product(const GgParams& p, long long m0, int n0, char* smem, f32x4 (&acc)[2][LG_TA][2][LG_TB], Run&& run = {}) {
+    constexpr bool MORE = std::remove_reference_t<Run>::MORE;
+    static_assert(!MORE || LAYOUT == GG_NT, "runs of tiles along the contraction");
     constexpr bool A_KMAJOR = LAYOUT == GG_TN, B_KMAJOR = LAYOUT != GG_NT;
     constexpr int TA = LG_TA, TB = LG_TB, NL = RG_NLD;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -30,23 +40,41 @@ __device__ __forceinline__ void lg_product(const GgParams& p, long long m0, int 
     using Loads = RgLoads<LAYOUT, 4, 4>;
     using Slab = typename Loads::Slab;
     Loads ld(p, m0, n0, tid, smem + LG_TOK + wave * 1024);
-    const int nk = ld.nk;
+    const int nk = run.slabs(ld);  // (MORE: an even number)
     const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_offset_of(smem) + wave * 1024);
     auto load_a = [&](const Slab& s, int kt, int r, int i) { ld.load_a(s, 2 * r + i, lds0 + (kt & 1) * LG_STAGE); };
     auto load_b = [&](const Slab& s, int kt, int r, int i) { ld.load_b(s, 2 * r + i, lds0 + LG_OPER + (kt & 1) * LG_STAGE); };
 
+    auto clear = [&] {
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+        for (int a = 0; a < 2; ++a)
 #pragma unroll
-        for (int i = 0; i < TA; ++i)
+            for (int i = 0; i < TA; ++i)
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int j = 0; j < TB; ++j) acc[a][i][b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int j = 0; j < TB; ++j) acc[a][i][b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+    clear();
     // fragments: the current half of A, both halves of B
     u32x4 fa[2][TA], fb[2][2][TB];
-    auto read_a = [&](int st, int r, int c, int i) { fa[c][i] = rg_fragment(smem + st * LG_STAGE + r * RG_BYTES, A_KMAJOR, wm * TA + i, c, lane); };
-    auto read_b = [&](int st, int r, int c, int j) { fb[r][c][j] = rg_fragment(smem + LG_OPER + st * LG_STAGE + r * RG_BYTES, B_KMAJOR, wn * TB + j, c, lane); };
+    unsigned at[2][2];  // (MORE) places of a chunk's first fragments of A, of B, which the compiler would otherwise add up for each read
+    if constexpr (MORE) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            at[0][c] = rg_place(wm * TA, c, lane);
+            at[1][c] = LG_OPER + rg_place(wn * TB, c, lane);
+            asm volatile("" : "+v"(at[0][c]), "+v"(at[1][c]));
+        }
+    }
+    auto read_a = [&](int st, int r, int c, int i) {
+        if constexpr (MORE) fa[c][i] = *reinterpret_cast<const u32x4*>(smem + at[0][c] + (st * LG_STAGE + r * RG_BYTES + i * 16 * RG_KB));
+        else fa[c][i] = rg_fragment(smem + st * LG_STAGE + r * RG_BYTES, A_KMAJOR, wm * TA + i, c, lane);
+    };
+    auto read_b = [&](int st, int r, int c, int j) {
+        if constexpr (MORE) fb[r][c][j] = *reinterpret_cast<const u32x4*>(smem + at[1][c] + (st * LG_STAGE + r * RG_BYTES + j * 16 * RG_KB));
+        else fb[r][c][j] = rg_fragment(smem + LG_OPER + st * LG_STAGE + r * RG_BYTES, B_KMAJOR, wn * TB + j, c, lane);
+    };
 
     constexpr int NM = 2 * TA * TB;  // MFMAs of a quarter
     // One quarter of a slab: the MFMAs of (half AH of A) x (half BH of B), `mem(q, c, i, j)` behind MFMA q, which is of chunk c
@@ -79,7 +107,7 @@ __device__ __forceinline__ void lg_product(const GgParams& p, long long m0, int 
         asm volatile("" ::: "memory");
     }
     {
-        const Slab s0 = ld.slab(0), s1 = ld.slab(1);
+        const Slab s0 = run.slab(ld, 0), s1 = run.slab(ld, 1);
         ld.read_tokens(0);
         load_region(s0, 0, false, 0);
         load_region(s0, 0, true, 0);
@@ -93,31 +121,37 @@ __device__ __forceinline__ void lg_product(const GgParams& p, long long m0, int 
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(5 * NL));
     rg_barrier();
+    auto first_fragments = [&] {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < 2; ++c) {
 #pragma unroll
-        for (int j = 0; j < TB; ++j) read_b(0, 0, c, j);
+            for (int j = 0; j < TB; ++j) read_b(0, 0, c, j);
 #pragma unroll
-        for (int i = 0; i < TA; ++i) read_a(0, 0, c, i);
-    }
+            for (int i = 0; i < TA; ++i) read_a(0, 0, c, i);
+        }
+    };
+    first_fragments();
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(3 * NL));
     __builtin_amdgcn_s_waitcnt(LGKMCNT0);
 
     // Waves of one SIMD do not take turns: one of them goes first (X W^T 752 -> 742 us at 8192^3, the gradients no change)
-    if constexpr (LAYOUT == GG_NT)
-        if (wave < RG_WAVES / 2) __builtin_amdgcn_s_setprio(1);
+    auto go_first = [&] {
+        if constexpr (LAYOUT == GG_NT)
+            if (wave < RG_WAVES / 2) __builtin_amdgcn_s_setprio(1);
+    };
+    go_first();
     // Slab kt, kt & 1 == PAR.  Halves of a slab begin with a barrier, before which every wave has seen to it that the regions
     // read in this half have landed (its own part: all loads but the last IN_FLIGHT, which complete in order) and that it
     // has read what this half's loads overwrite: all but the fragments read in the quarter before.
     constexpr int IN_FLIGHT = 3 * NL;
-    auto slab = [&](int kt, auto par_tag) {
+    auto slab = [&](int kt, auto par_tag, auto one_ahead, auto two_ahead) {
         constexpr int PAR = decltype(par_tag)::value, F = PAR, L = PAR ^ 1;
         using IF = std::integral_constant<int, F>;
         using IL = std::integral_constant<int, L>;
         __builtin_amdgcn_s_waitcnt(vmcnt_imm(IN_FLIGHT));
         __builtin_amdgcn_s_waitcnt(lgkmcnt_imm(A_KMAJOR ? 15 : 2 * TA));
         rg_barrier();
-        const Slab s1 = ld.slab(kt + 1), s2 = ld.slab(kt + 2);
+        const Slab s1 = one_ahead(), s2 = two_ahead();
         quarter(I0{}, IF{}, false, [&](int q, int c, int i, int j) {
             if (q < 2 * TB) read_b(PAR, L, q / TB, q % TB);
             if (q < 2 * NL) {
@@ -141,13 +175,29 @@ __device__ __forceinline__ void lg_product(const GgParams& p, long long m0, int 
             if (q % TB == TB - 1) read_a(PAR ^ 1, 0, c, i);
         });
     };
-    int kt = 0;
-    for (; kt + 1 < nk; kt += 2) {
-        slab(kt, I0{});
-        slab(kt + 1, I1{});
+    auto pair = [&](int kt) {
+        slab(kt, I0{}, [&] { return run.slab(ld, kt + 1); }, [&] { return run.slab(ld, kt + 2); });
+        slab(kt + 1, I1{}, [&] { return run.slab(ld, kt + 2); }, [&] { return run.slab(ld, kt + 3); });
+    };
+    if constexpr (MORE) {
+        for (;;) {
+            for (int kt = 0; kt + 2 < nk; kt += 2) pair(kt);
+            slab(nk - 2, I0{}, [&] { return run.slab(ld, nk - 1); }, [&] { return run.next(ld, 0); });
+            slab(nk - 1, I1{}, [&] { return run.next(ld, 0); }, [&] { return run.next(ld, 1); });
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_s_waitcnt(LGKMCNT0);  // (the next slab's fragments, read again below: the registers are wanted meanwhile)
+            if (!run.done(acc)) break;
+            clear();
+            first_fragments();
+            __builtin_amdgcn_s_waitcnt(LGKMCNT0);
+            go_first();
+        }
+    } else {
+        int kt = 0;
+        for (; kt + 1 < nk; kt += 2) pair(kt);
+        if (kt < nk) slab(kt, I0{}, [&] { return run.slab(ld, kt + 1); }, [&] { return run.slab(ld, kt + 2); });
+        if constexpr (LAYOUT == GG_NT) __builtin_amdgcn_s_setprio(0);
     }
-    if (kt < nk) slab(kt, I0{});
-    if constexpr (LAYOUT == GG_NT) __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // requests past the end write (zeros) to the stages, too
     __builtin_amdgcn_s_waitcnt(LGKMCNT0);
     __syncthreads();

@@ -86,6 +86,89 @@ template <typename Tile> __device__ __forceinline__ void store_rows(const char* 
     }
 }
 
+// softcap, in place
+template <typename Tile> __device__ __forceinline__ void cap_tile(const VocabRule& rule, typename Tile::Acc& acc) {
+    if (rule.softcap <= 0.f) return;
+    const float inv_cap = 1.f / rule.softcap;
+#pragma unroll
+    for (int i = 0; i < Tile::ROWS; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) Tile::at(acc, i, j)[r] = vocab_cap(Tile::at(acc, i, j)[r], rule.softcap, inv_cap);
+}
+
+// The statistics of tile (m0, column tile tn).  labels(row, i) of the rows of a lane; red [3][ACROSS][BM] in LDS: maxima, sums of exponentials, sums.
+template <typename Tile, class Labels>
+__device__ __forceinline__ void tile_stats(const VocabTileParams& p, typename Tile::Acc& acc, Labels&& labels, float* red, int tid, long long m0, int tn) {
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n0 = tn * Tile::BN;
+    const bool whole = n0 + Tile::BN <= p.N;
+    cap_tile<Tile>(p.rule, acc);
+#pragma unroll
+    for (int i = 0; i < Tile::ROWS; ++i) {
+        const int row = Tile::row(wave, lane, i);
+        const long long m = min(m0 + row, p.M - 1);
+        float top = -INFINITY, sum, all = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f32x4& v = Tile::at(acc, i, j);
+            if (!whole) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (n0 + Tile::col(wave, lane, j) + r >= p.N) v[r] = -INFINITY;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, v[r]);
+        }
+        // the label's logit: few tiles hold one (a label outside the vocabulary is no column below N)
+        const unsigned label = (unsigned)labels(row, i) - (unsigned)(p.v0 + n0);
+        if (__any(label < (unsigned)min(Tile::BN, p.N - n0))) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned at = label - (unsigned)Tile::col(wave, lane, j);
+                const f32x4 v = Tile::at(acc, i, j);
+                if (at < 4u && label < (unsigned)(p.N - n0)) p.picked[m] = at < 2 ? at ? v[1] : v[0] : at == 2 ? v[2] : v[3];
+            }
+        }
+        top = row_lanes_max(top);
+        const float base = top == -INFINITY ? 0.f : top * LOG2E;
+        f32x4 some = {0.f, 0.f, 0.f, 0.f};  // (four chains of additions)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) some[r] += __builtin_amdgcn_exp2f(fmaf(Tile::at(acc, i, j)[r], LOG2E, -base));
+        sum = row_lanes_sum((some[0] + some[1]) + (some[2] + some[3]));
+        if (p.sums) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) all += whole || n0 + Tile::col(wave, lane, j) + r < p.N ? Tile::at(acc, i, j)[r] : 0.f;
+            all = row_lanes_sum(all);
+        }
+        if (lane < 16) {
+            float* const to = red + Tile::across(wave) * Tile::BM + row;
+            to[0] = top;
+            to[Tile::ACROSS * Tile::BM] = sum;
+            to[2 * Tile::ACROSS * Tile::BM] = all;
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // (in a run: the next tile's first slabs)
+    __syncthreads();
+    const int row = tid;
+    if (row < Tile::BM && m0 + row < p.M) {
+        float top = red[row], sum = red[Tile::ACROSS * Tile::BM + row], all = red[2 * Tile::ACROSS * Tile::BM + row];
+#pragma unroll
+        for (int w = 1; w < Tile::ACROSS; ++w) {
+            const float* const from = red + w * Tile::BM + row;
+            vocab_join(top, sum, from[0], from[Tile::ACROSS * Tile::BM]);
+            all += from[2 * Tile::ACROSS * Tile::BM];
+        }
+        const long long to = (long long)tn * p.M + m0 + row;
+        p.parts[to] = make_float2(top, sum);
+        if (p.sums) p.sums[to] = all;
+    }
+}
+
 template <int WHAT, int UA>
 __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTileParams p) {
     constexpr int LAYOUT = vocab_layout(WHAT);
@@ -142,84 +225,17 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
         store_rows<Tile>(smem, wave, lane, p.Y, p.ldy, m0, p.M, n0, p.N);
         return;
     }
-    const bool whole = n0 + Tile::BN <= p.N, capped = p.rule.softcap > 0.f;
-    const float inv_cap = capped ? 1.f / p.rule.softcap : 0.f;
-    if (capped) {
-#pragma unroll
-        for (int i = 0; i < Tile::ROWS; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) Tile::at(acc, i, j)[r] = vocab_cap(Tile::at(acc, i, j)[r], p.rule.softcap, inv_cap);
-    }
     if constexpr (WHAT == VOCAB_STATS) {
-        float* const red = reinterpret_cast<float*>(smem);  // [3][ACROSS][BM]: maxima, sums of exponentials, sums
         int labels[Tile::ROWS];
 #pragma unroll
         for (int i = 0; i < Tile::ROWS; ++i) labels[i] = p.labels[min(m0 + Tile::row(wave, lane, i), p.M - 1)];
-#pragma unroll
-        for (int i = 0; i < Tile::ROWS; ++i) {
-            const int row = Tile::row(wave, lane, i);
-            const long long m = min(m0 + row, p.M - 1);
-            float top = -INFINITY, sum, all = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                f32x4& v = Tile::at(acc, i, j);
-                if (!whole) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (n0 + Tile::col(wave, lane, j) + r >= p.N) v[r] = -INFINITY;
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) top = fmaxf(top, v[r]);
-            }
-            // the label's logit: few tiles hold one (a label outside the vocabulary is no column below N)
-            const unsigned label = (unsigned)labels[i] - (unsigned)(p.v0 + n0);
-            if (__any(label < (unsigned)min(Tile::BN, p.N - n0))) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const unsigned at = label - (unsigned)Tile::col(wave, lane, j);
-                    const f32x4 v = Tile::at(acc, i, j);
-                    if (at < 4u && label < (unsigned)(p.N - n0)) p.picked[m] = at < 2 ? at ? v[1] : v[0] : at == 2 ? v[2] : v[3];
-                }
-            }
-            top = row_lanes_max(top);
-            const float base = top == -INFINITY ? 0.f : top * LOG2E;
-            f32x4 some = {0.f, 0.f, 0.f, 0.f};  // (four chains of additions)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) some[r] += __builtin_amdgcn_exp2f(fmaf(Tile::at(acc, i, j)[r], LOG2E, -base));
-            sum = row_lanes_sum((some[0] + some[1]) + (some[2] + some[3]));
-            if (p.sums) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) all += whole || n0 + Tile::col(wave, lane, j) + r < p.N ? Tile::at(acc, i, j)[r] : 0.f;
-                all = row_lanes_sum(all);
-            }
-            if (lane < 16) {
-                float* const to = red + Tile::across(wave) * Tile::BM + row;
-                to[0] = top;
-                to[Tile::ACROSS * Tile::BM] = sum;
-                to[2 * Tile::ACROSS * Tile::BM] = all;
-            }
-        }
-        __syncthreads();
-        const int row = tid;
-        if (row < Tile::BM && m0 + row < p.M) {
-            float top = red[row], sum = red[Tile::ACROSS * Tile::BM + row], all = red[2 * Tile::ACROSS * Tile::BM + row];
-#pragma unroll
-            for (int w = 1; w < Tile::ACROSS; ++w) {
-                const float* const from = red + w * Tile::BM + row;
-                vocab_join(top, sum, from[0], from[Tile::ACROSS * Tile::BM]);
-                all += from[2 * Tile::ACROSS * Tile::BM];
-            }
-            const long long to = (long long)tn * p.M + m0 + row;
-            p.parts[to] = make_float2(top, sum);
-            if (p.sums) p.sums[to] = all;
-        }
-    } else {
+        tile_stats<Tile>(p, acc, [&](int, int i) { return labels[i]; }, reinterpret_cast<float*>(smem), tid, m0, tn);
+        return;
+    }
+    const bool whole = n0 + Tile::BN <= p.N, capped = p.rule.softcap > 0.f;
+    const float inv_cap = capped ? 1.f / p.rule.softcap : 0.f;
+    cap_tile<Tile>(p.rule, acc);
+    if constexpr (WHAT == VOCAB_PROBS) {
         if (p.side.rows) {
             if (tn == 0 && tid < Tile::BM && m0 + tid < p.M) vocab_list_row(p.rule, p.side, p.labels, p.idx, m0 + tid, p.M);
             if (p.side.zero_row && tm == p.tiles_m - 1 && tid < Tile::BN / 8 && n0 + tid * 8 < p.N)
@@ -274,10 +290,90 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
     }
 }
 
+// Statistics of 256 x 256 tiles by 256 workgroups, each for runs of tiles of the same rows: a tile's first slabs are on their way during the statistics of the one
+// before.  A die has a part of the tiles in grouped order, four rows of tiles by a range of columns at a time (or two, or one), whose columns go round its
+// workgroups: at any time four of them read the same columns and eight the same rows.  4096 rows, 131072 words: 256 columns 376 -> 303 us, 512 555 -> 471, 1024 918 -> 856;
+// wide rows have little to hide and their workgroups fall out of step (2048 columns as long either way, 4096 3 % longer), and one tile a workgroup
+// has no next (300 rows of 512, 32000 words 25.4, so 25.8).
+constexpr int VR_WIDEST = 1536;
+constexpr int VR_GRID = 256, VR_PER_XCD = VR_GRID / NUM_XCD, VR_RED = LG_TOK, VR_LABELS = VR_RED + 3 * LG_WN * LG_BM * 4, VR_LDS = VR_LABELS + LG_BM * 4;
+static_assert(VR_LDS <= 160 * 1024, "a workgroup's LDS");
+using VrTile = VocabTile<GG_NT, 0>;
+struct StatsRun {
+    static constexpr bool MORE = true;
+    const VocabTileParams& p;
+    char* smem;
+    long long m0;
+    int tn, step, end;  // column tiles
+    u32x4 b[2];         // descriptors of this tile's columns and of the next one's
+    __device__ __forceinline__ StatsRun(const VocabTileParams& p, char* smem, long long m0, int tn, int step, int end) : p(p), smem(smem), m0(m0), tn(tn), step(step), end(end) {
+        b[0] = columns(tn);
+        b[1] = columns(tn + step);
+    }
+    __device__ __forceinline__ u32x4 columns(int t) const {
+        const int n0 = min(t, p.tiles_n - 1) * LG_BN;
+        u32x4 r = raw_rsrc(static_cast<const bf16_t*>(p.B) + (long long)n0 * p.ldb, (unsigned)(min(LG_BN, p.N - n0) - 1) * (unsigned)p.ldb * 2 + (unsigned)p.K * 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = __builtin_amdgcn_readfirstlane(r[e]);
+        return r;
+    }
+    template <class Loads> __device__ __forceinline__ int slabs(const Loads& ld) const { return (ld.nk + 1) / 2 * 2; }
+    template <class Loads> __device__ __forceinline__ typename Loads::Slab slab(const Loads& ld, int kt) const { return of(ld, kt, b[0], true); }
+    template <class Loads> __device__ __forceinline__ typename Loads::Slab next(const Loads& ld, int kt) const { return of(ld, kt, b[1], tn + step < end); }
+    template <class Loads> __device__ __forceinline__ typename Loads::Slab of(const Loads& ld, int kt, u32x4 columns, bool some) const {
+        typename Loads::Slab s;
+        s.soff = min(kt, ld.nk - 1) * RG_KB;  // (a slab behind the contraction: offsets at the descriptors' sizes or past them, zeros)
+        s.in_k = some && ld.kpos < ld.K * 2 - kt * RG_KB;
+        s.a = raw_rsrc(ld.a_base, ld.a_size);
+        s.b = columns;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            s.a[e] = __builtin_amdgcn_readfirstlane(s.a[e]);
+            s.b[e] = __builtin_amdgcn_readfirstlane(s.b[e]);
+        }
+        return s;
+    }
+    __device__ __forceinline__ bool done(VrTile::Acc& acc) {
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));  // (what comes of it is not kept in registers through the products)
+        const int* const labels = reinterpret_cast<const int*>(smem + VR_LABELS);
+        tile_stats<VrTile>(p, acc, [&](int row, int) { return labels[row]; }, reinterpret_cast<float*>(smem + VR_RED), tid, m0, tn);
+        tn += step;
+        b[0] = b[1];
+        b[1] = columns(tn + step);
+        return tn < end;
+    }
+};
+__global__ __launch_bounds__(RG_THREADS, 1) void vocab_stats_run_kernel(VocabTileParams p) {
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int xcd = blockIdx.x % NUM_XCD, w = blockIdx.x / NUM_XCD;
+    const long long total = (long long)p.tiles_m * p.tiles_n, from = total * xcd / NUM_XCD, to = total * (xcd + 1) / NUM_XCD;
+    long long before = 0;  // tiles of the groups before
+    for (int g = 0, rows; g < p.tiles_m; g += rows) {
+        rows = p.tiles_m - g >= 4 ? 4 : p.tiles_m - g >= 2 ? 2 : 1;
+        const int first = (int)min(max(from - before, 0ll) / rows, (long long)p.tiles_n), last = (int)min(max(to - before, 0ll) / rows, (long long)p.tiles_n);
+        before += (long long)rows * p.tiles_n;
+        const int step = VR_PER_XCD / rows, start = first + w / rows;
+        if (start >= last) continue;
+        const long long m0 = (long long)(g + w % rows) * LG_BM;
+        if (threadIdx.x < LG_BM) reinterpret_cast<int*>(smem + VR_LABELS)[threadIdx.x] = p.labels[min(m0 + (int)threadIdx.x, p.M - 1)];  // (seen by all after the products' barriers)
+        VrTile::Acc acc;
+        lg_product<GG_NT>(p, m0, start * LG_BN, smem, acc, StatsRun(p, smem, m0, start, step, last));
+    }
+}
+static int launch_stats_run(VocabTileParams p, hipStream_t st) {
+    p.tiles_m = (int)((p.M + LG_BM - 1) / LG_BM);
+    p.tiles_n = (p.N + LG_BN - 1) / LG_BN;
+    hipLaunchKernelGGL(vocab_stats_run_kernel, dim3(VR_GRID), dim3(RG_THREADS), VR_LDS, st, p);
+    return (int)hipGetLastError();
+}
+
 template <int WHAT, int UA> constexpr LdsLimit vocab_limit() { return {reinterpret_cast<const void*>(&vocab_tile_kernel<WHAT, UA>), VocabTile<vocab_layout(WHAT), UA>::LDS}; }
 template <int WHAT> static int prepare_what() {
     static const int err = [] {
-        if constexpr (WHAT == VOCAB_WEIGHT) return raise_lds_limits({vocab_limit<WHAT, 0>(), vocab_limit<WHAT, 2>(), vocab_limit<WHAT, 4>()});
+        if constexpr (WHAT == VOCAB_STATS)
+            return raise_lds_limits({{reinterpret_cast<const void*>(&vocab_stats_run_kernel), VR_LDS}, vocab_limit<WHAT, 0>(), vocab_limit<WHAT, 1>(), vocab_limit<WHAT, 2>(), vocab_limit<WHAT, 4>()});
+        else if constexpr (WHAT == VOCAB_WEIGHT) return raise_lds_limits({vocab_limit<WHAT, 0>(), vocab_limit<WHAT, 2>(), vocab_limit<WHAT, 4>()});
         else return raise_lds_limits({vocab_limit<WHAT, 0>(), vocab_limit<WHAT, 1>(), vocab_limit<WHAT, 2>(), vocab_limit<WHAT, 4>()});
     }();
     return err;
@@ -299,7 +395,11 @@ template <int WHAT, int UA> static int launch_one(VocabTileParams p, hipStream_t
 }
 template <int WHAT> static int launch_what(const VocabTileParams& p, GgTile tile, hipStream_t st) {
     switch (tile) {
-        case GG_T256: return launch_one<WHAT, 0>(p, st);
+        case GG_T256:
+            if constexpr (WHAT == VOCAB_STATS) {
+                if (p.K <= VR_WIDEST && (p.M + LG_BM - 1) / LG_BM * ((p.N + LG_BN - 1) / LG_BN) > VR_GRID) return launch_stats_run(p, st);
+            }
+            return launch_one<WHAT, 0>(p, st);
         case GG_T256x128: return launch_one<WHAT, 4>(p, st);
         case GG_T128: return launch_one<WHAT, 2>(p, st);
         default:

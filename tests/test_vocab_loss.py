@@ -240,6 +240,28 @@ def test_more_rows_than_a_launch_takes(lemo, kept):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("case", [  # M, C, V, kept, softcap, smoothing: rows of tiles in groups of 4, 2 and 1; one slab, odd numbers of slabs, a partial one; a last column tile cut short
+    (1700, 136, 11000, True, 5.0, 0.1), (900, 8, 33001, False, 0.0, 0.0), (1000, 1536, 17001, True, 0.0, 0.2), (300, 64, 40000, False, 0.0, 0.0), (2305, 264, 9999, True, 0.0, 0.0),
+    (256, 192, 70000, False, 30.0, 0.0)])
+def test_runs_of_tiles(lemo, case):
+    """More tiles of 256 x 256 than CUs, rows of up to 1536 columns: workgroups go from tile to tile."""
+    print(case, flush=True)
+    M, C, V, kept, cap, s = case
+    X, W, labels, idx, w = (t.cuda() if t is not None else None for t in inputs(torch.bfloat16, M, M + 50, C, V, kept, 21))
+    labels[-3:] = torch.tensor([0, V - 1, V // 256 * 256], dtype=torch.int32)
+    want = reference((X[idx.long()] if kept else X[:M]).double(), W.double(), labels, cap, s, 1e-3, w.double(), 2.0 ** -8)
+    want = {name: (value.cpu(), bound.cpu()) for name, (value, bound) in want.items()}
+    got = lemo.lemo_vocab_loss(X, idx, W, labels, softcap=cap, smoothing=s, z_weight=1e-3)
+    check("loss", got.loss, want["loss"])
+    check("lse", got.lse, want["lse"])
+    dX, dW = lemo.lemo_vocab_loss_grad(w, X, idx, W, labels, got.lse, softcap=cap, smoothing=s, z_weight=1e-3)
+    check("dX", dX, want["dX"])
+    check("dW", dW, want["dW"])
+    again = lemo.lemo_vocab_loss(X, idx, W, labels, softcap=cap, smoothing=s, z_weight=1e-3)
+    assert torch.equal(again.loss, got.loss) and torch.equal(again.lse, got.lse)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_the_largest_vocabulary_and_offsets_past_32_bits(lemo, dtype):
     """V = 2^21 rows of W (and dW) 4 KB or more apart: past 4 GiB."""
