@@ -34,9 +34,9 @@ PEAK_HBM_GBS = 8000.0       # MI355X HBM3E, published
 # The figures belong to the kernel sources they were measured on: "sources" is sources_digest() at that time, and the
 # bench reports traffic as null when the sources have changed since.
 MEASURED_TRAFFIC_BYTES = {
-    "sources": "42cfba904c2210cb",
-    "C5:rowstats": 2546315861, "C5:colsum": 2689182037, "C5:head_mean_select": 8651435,
-    "C5:gather_gemm": 1686823125, "C5:scatter": 242889557,
+    "sources": "0914a3c1133ef777",
+    "C5:rowstats": 2543534336, "C5:colsum": 2712394795, "C5:head_mean_select": 8651435,
+    "C5:gather_gemm": 1686967595, "C5:scatter": 242890581,
 }
 
 

@@ -118,13 +118,9 @@ template <int LAYOUT, int UA, int UB> struct RgLoads {  // the tile's rows of A,
 
 // MFMA operands (16 x 16 x 32): a lane holds row lane % 16 of a 16-row tile, elements 8 (lane / 16) .. + 7 of a chunk of 32.
 // Fragment of tile t of a region, chunk c of the slab; the transposing read: see gather_gemm.hpp.
-__device__ __forceinline__ int rg_place(int t, int c, int lane) {  // in a region of rows along the contraction
-    const int l16 = lane & 15, quad = lane >> 4;
-    return t * 16 * RG_KB + l16 * RG_KB + (((4 * c + quad) ^ ((l16 >> 1) & 7)) << 4);
-}
 __device__ __forceinline__ u32x4 rg_fragment(const char* region, bool kmajor, int t, int c, int lane) {
     const int l16 = lane & 15, quad = lane >> 4;
-    if (!kmajor) return *reinterpret_cast<const u32x4*>(region + rg_place(t, c, lane));
+    if (!kmajor) return *reinterpret_cast<const u32x4*>(region + t * 16 * RG_KB + l16 * RG_KB + (((4 * c + quad) ^ ((l16 >> 1) & 7)) << 4));
     const int row = 8 * quad + (l16 >> 2);
     const char* at = region + row * 256 + (lane & 1) * 8 + c * 32 * 256 + (((t * 2 + ((lane & 3) >> 1)) ^ rg_kswz(row)) << 4);
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at));

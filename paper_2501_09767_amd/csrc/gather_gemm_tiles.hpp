@@ -27,6 +27,7 @@ struct LgOne {
     static constexpr bool MORE = false;
     template <class Loads> __device__ __forceinline__ int slabs(const Loads& ld) const { return ld.nk; }
     template <class Loads> __device__ __forceinline__ typename Loads::Slab slab(const Loads& ld, int kt) const { return ld.slab(kt); }
+    template <class Loads> __device__ typename Loads::Slab next(const Loads& ld, int kt) const;  // (there is none)
 };
 template <int LAYOUT, class Run = LgOne>
 __device__ __forceinline__ void lg_product(const GgParams& p, long long m0, int n0, char* smem, f32x4 (&acc)[2][LG_TA][2][LG_TB], Run&& run = {}) {
@@ -62,8 +63,9 @@ __device__ __forceinline__ void lg_product(const GgParams& p, long long m0, int 
     if constexpr (MORE) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            at[0][c] = rg_place(wm * TA, c, lane);
-            at[1][c] = LG_OPER + rg_place(wn * TB, c, lane);
+            const int row = lane & 15, piece = (4 * c + (lane >> 4)) ^ ((row >> 1) & 7);  // as rg_fragment finds them
+            at[0][c] = (wm * TA * 16 + row) * RG_KB + piece * 16;
+            at[1][c] = LG_OPER + (wn * TB * 16 + row) * RG_KB + piece * 16;
             asm volatile("" : "+v"(at[0][c]), "+v"(at[1][c]));
         }
     }
@@ -121,16 +123,13 @@ __device__ __forceinline__ void lg_product(const GgParams& p, long long m0, int 
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(5 * NL));
     rg_barrier();
-    auto first_fragments = [&] {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < 2; ++c) {
 #pragma unroll
-            for (int j = 0; j < TB; ++j) read_b(0, 0, c, j);
+        for (int j = 0; j < TB; ++j) read_b(0, 0, c, j);
 #pragma unroll
-            for (int i = 0; i < TA; ++i) read_a(0, 0, c, i);
-        }
-    };
-    first_fragments();
+        for (int i = 0; i < TA; ++i) read_a(0, 0, c, i);
+    }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(3 * NL));
     __builtin_amdgcn_s_waitcnt(LGKMCNT0);
 
@@ -144,14 +143,18 @@ __device__ __forceinline__ void lg_product(const GgParams& p, long long m0, int 
     // read in this half have landed (its own part: all loads but the last IN_FLIGHT, which complete in order) and that it
     // has read what this half's loads overwrite: all but the fragments read in the quarter before.
     constexpr int IN_FLIGHT = 3 * NL;
-    auto slab = [&](int kt, auto par_tag, auto one_ahead, auto two_ahead) {
+    auto ahead = [&](int kt, auto next_tag) {  // slab kt, or of the next tile
+        if constexpr (decltype(next_tag)::value < 0) return run.slab(ld, kt);
+        else return run.next(ld, decltype(next_tag)::value);
+    };
+    auto slab = [&](int kt, auto par_tag, auto next1, auto next2) {
         constexpr int PAR = decltype(par_tag)::value, F = PAR, L = PAR ^ 1;
         using IF = std::integral_constant<int, F>;
         using IL = std::integral_constant<int, L>;
         __builtin_amdgcn_s_waitcnt(vmcnt_imm(IN_FLIGHT));
         __builtin_amdgcn_s_waitcnt(lgkmcnt_imm(A_KMAJOR ? 15 : 2 * TA));
         rg_barrier();
-        const Slab s1 = one_ahead(), s2 = two_ahead();
+        const Slab s1 = ahead(kt + 1, next1), s2 = ahead(kt + 2, next2);
         quarter(I0{}, IF{}, false, [&](int q, int c, int i, int j) {
             if (q < 2 * TB) read_b(PAR, L, q / TB, q % TB);
             if (q < 2 * NL) {
@@ -175,27 +178,36 @@ __device__ __forceinline__ void lg_product(const GgParams& p, long long m0, int 
             if (q % TB == TB - 1) read_a(PAR ^ 1, 0, c, i);
         });
     };
-    auto pair = [&](int kt) {
-        slab(kt, I0{}, [&] { return run.slab(ld, kt + 1); }, [&] { return run.slab(ld, kt + 2); });
-        slab(kt + 1, I1{}, [&] { return run.slab(ld, kt + 2); }, [&] { return run.slab(ld, kt + 3); });
-    };
+    using Own = std::integral_constant<int, -1>;
     if constexpr (MORE) {
         for (;;) {
-            for (int kt = 0; kt + 2 < nk; kt += 2) pair(kt);
-            slab(nk - 2, I0{}, [&] { return run.slab(ld, nk - 1); }, [&] { return run.next(ld, 0); });
-            slab(nk - 1, I1{}, [&] { return run.next(ld, 0); }, [&] { return run.next(ld, 1); });
+            for (int kt = 0; kt + 2 < nk; kt += 2) {
+                slab(kt, I0{}, Own{}, Own{});
+                slab(kt + 1, I1{}, Own{}, Own{});
+            }
+            slab(nk - 2, I0{}, Own{}, I0{});
+            slab(nk - 1, I1{}, I0{}, I1{});
             __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_s_waitcnt(LGKMCNT0);  // (the next slab's fragments, read again below: the registers are wanted meanwhile)
             if (!run.done(acc)) break;
             clear();
-            first_fragments();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {  // (as above; in one function for both places the single tile's kernel spilled registers)
+#pragma unroll
+                for (int j = 0; j < TB; ++j) read_b(0, 0, c, j);
+#pragma unroll
+                for (int i = 0; i < TA; ++i) read_a(0, 0, c, i);
+            }
             __builtin_amdgcn_s_waitcnt(LGKMCNT0);
             go_first();
         }
     } else {
         int kt = 0;
-        for (; kt + 1 < nk; kt += 2) pair(kt);
-        if (kt < nk) slab(kt, I0{}, [&] { return run.slab(ld, kt + 1); }, [&] { return run.slab(ld, kt + 2); });
+        for (; kt + 1 < nk; kt += 2) {
+            slab(kt, I0{}, Own{}, Own{});
+            slab(kt + 1, I1{}, Own{}, Own{});
+        }
+        if (kt < nk) slab(kt, I0{}, Own{}, Own{});
         if constexpr (LAYOUT == GG_NT) __builtin_amdgcn_s_setprio(0);
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // requests past the end write (zeros) to the stages, too
