@@ -468,7 +468,7 @@ int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st)
     if (p.M == 0) return p.dW ? launch_zero_matrix(p.dW, p.lddw, C, V, dt, st) : 0;
     if (!p.dX && !p.dW) return 0;
     const GradSpace s = grad_space(p.M, C, V, p.piece, dt, p.workspace);
-    const bool shared = p.dloss_stride == 0 && dt == LEMO_BF16;
+    const bool shared = (p.dloss_stride == 0 || p.M == 1) && dt == LEMO_BF16;
     VocabSide side{p.dloss, p.dloss_stride, !shared ? 0.f : p.rule.hit > 0.f ? 1.f / p.rule.hit : 1.f, s.rows, (int)p.S, V % (16 / esz) != 0};
     for (int v0 = 0; v0 < V && rc == 0; v0 += p.piece) {
         const int N = std::min(p.piece, V - v0);

@@ -241,7 +241,7 @@ def test_more_rows_than_a_launch_takes(lemo, kept):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("case", [  # M, C, V, kept, softcap, smoothing: rows of tiles in groups of 4, 2 and 1; one slab, odd numbers of slabs, a partial one; a last column tile cut short
-    (1700, 136, 11000, True, 5.0, 0.1), (900, 8, 33001, False, 0.0, 0.0), (1000, 1536, 17001, True, 0.0, 0.2), (300, 64, 40000, False, 0.0, 0.0), (2305, 264, 9999, True, 0.0, 0.0),
+    (1700, 136, 11000, True, 5.0, 0.1), (900, 8, 33001, False, 0.0, 0.0), (1000, 1536, 32001, True, 0.0, 0.2), (300, 64, 40000, False, 0.0, 0.0), (2305, 264, 9999, True, 0.0, 0.0),
     (256, 192, 70000, False, 30.0, 0.0)])
 def test_runs_of_tiles(lemo, case):
     """More tiles of 256 x 256 than CUs, rows of up to 1536 columns: workgroups go from tile to tile."""
