@@ -570,6 +570,7 @@ Rotation rotation(const Side& q, const Side& k, PyObject* freq, PyObject* wq, Py
     weight(wk, k, r.wk, r.tk);
     need(!r.tq || !r.tk || r.tq->dim() == r.tk->dim());
     if ((r.tq && r.tq->dim() == 2) || (r.tk && r.tk->dim() == 2)) r.flags |= LEMO_WEIGHTS_PER_HEAD;
+    need(!(flags & LEMO_WEIGHTS_PER_HEAD) || ((!r.tq || r.tq->dim() == 2) && (!r.tk || r.tk->dim() == 2)));  // (shared ones are no [heads, d])
     return r;
 }
 const int32_t* positions_of(PyObject* o, const Place& here, int64_t M) {

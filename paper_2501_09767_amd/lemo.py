@@ -1018,6 +1018,8 @@ def _rotate_sizes(Q, K, inv_freq, norm, w_q, w_k, flags):
             raise ValueError("w_q and w_k must both be [d] or both [heads,d]")
         per_head = w.dim() == 2
         _filled(w, (heads, d) if per_head else (d,), one.dtype, None, name)
+    if int(flags) & WEIGHTS_PER_HEAD and per_head is False:  # (the kernels would go past the end of shared ones)
+        raise ValueError("WEIGHTS_PER_HEAD is for weights [heads,d]")
     if inv_freq is not None and (inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous()):
         raise ValueError("inv_freq must be contiguous float32 [rot / 2]")
     return M, d, H, Hkv, one.dtype, 0 if inv_freq is None else 2 * inv_freq.numel(), int(flags) | (WEIGHTS_PER_HEAD if per_head else 0)
