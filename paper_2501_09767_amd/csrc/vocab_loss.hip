@@ -416,7 +416,10 @@ static int grad_piece_bf16(const VocabGradParams& p, const GradSpace& s, const V
         g.K = (int)p.M + (N % 8 != 0);
         g.Y = static_cast<char*>(p.dW) + v0 * p.lddw * 2; g.ldy = p.lddw;
         g.b_bytes = vl_span(p.S, p.ldx, p.C, 2);
-        if (side.uniform != 0.f) g.scale = p.dloss, g.scale_by = 1.f / side.uniform;
+        if (side.uniform != 0.f) {
+            g.scale = p.dloss; g.scale_by = 1.f / side.uniform;
+            g.labels = p.labels; g.n_labels = p.M; g.rule = p.rule;
+        }
         rc = launch_vocab_tiles(g, VOCAB_WEIGHT, gg_choose_tile(N, p.C, g.K, GG_TN, 1, 0., &one), st);
         if (rc) return rc;
     }

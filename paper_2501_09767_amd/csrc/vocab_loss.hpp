@@ -45,6 +45,7 @@ struct VocabTileParams : GgParams {
     int add;               // planes: to what they hold
     const float* scale;    // the weight's gradient: a factor for all of it, times scale_by, or null
     float scale_by;
+    long long n_labels;    // the weight's gradient with such a factor: rows, whose labels say whether any counts
 };
 enum { VOCAB_STATS, VOCAB_PROBS, VOCAB_PLANES, VOCAB_WEIGHT };
 int prepare_vocab_tiles();

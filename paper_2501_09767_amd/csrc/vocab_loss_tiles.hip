@@ -212,7 +212,17 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
         return;
     }
     if constexpr (WHAT == VOCAB_WEIGHT) {
-        const float scale = p.scale ? *p.scale * p.scale_by : 1.f;
+        float scale = p.scale ? *p.scale * p.scale_by : 1.f;
+        if (!isfinite(scale)) {  // (the same in all threads)  Where no row counts, nothing is added, whatever their gradient holds
+            int* const some = reinterpret_cast<int*>(smem);
+            if (tid == 0) *some = 0;
+            __syncthreads();
+            for (long long m = tid; m < p.n_labels; m += RG_THREADS)
+                if (p.labels[m] >= 0 && p.labels[m] < p.rule.V) *some = 1;
+            __syncthreads();
+            if (*some == 0) scale = 0.f;
+            __syncthreads();
+        }
 #pragma unroll
         for (int i = 0; i < Tile::ROWS; ++i)
 #pragma unroll
