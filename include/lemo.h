@@ -607,7 +607,7 @@ int lemo_dropout_add_grad(const void* dR, int64_t lddr, int64_t S, const int32_t
  *   M == 0 writes zeros to dW.
  *
  * Sums in binary32 (of the losses in 64 bits), over the whole vocabulary and all rows before they are rounded once; in bf16 G is rounded to bf16 for
- * the two products.  No atomics: the same bits on every run.  What is not finite in a row of X spoils that row's results, and if it counts dW; in W, all.
+ * the two products (the label's element in dX, and up to 32 rows in dW, have what that leaves added).  No atomics: the same bits on every run.  What is not finite in a row of X spoils that row's results, and if it counts dW; in W, all.
  * Supported: bf16 and fp32; C % 8 == 0 (bf16) / % 4 (fp32), C <= 65536, any V <= 2^21, M <= 2^22; X, W, dX, dW follow the 16-byte rule, pitches below 8 MiB (dX:
  * any); X with a row more spanning less than 4 GiB - 4096; fp32: (M + 63) * C * 4 below 4 GiB.  Results overlap neither operands nor each other.
  */

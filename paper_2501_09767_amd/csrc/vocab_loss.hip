@@ -252,12 +252,18 @@ static int vl_choice(long long M, int V, int esz) {
     return (int)((V + n - 1) / n + 255) / 256 * 256;
 }
 
+// Parts of G's elements (bf16).  Rounded once, the label's element of a row is as far off as the store of the results it makes, and the weight's gradient of few rows has no
+// mean of many such roundings (1 to 32 rows of 1024, 8000 words, gradients of their own: dW 2.1e-3 to 2.4e-3 from 64 bits on the mean of draws, up to 3.9e-3; in two parts
+// 1.6e-3 to 1.7e-3, as its store alone).  Both parts within the slab that the contraction is padded to: 16 rows of 4096, 131072 words 688 -> 707 us, one row 679 -> 676;  16 rows
+// of 1024, 8000 words 28.0 -> 28.5.  More rows in two parts would be products of twice the length.
+static int vl_parts(long long M, int V, lemo_dtype_t dt) { return dt == LEMO_BF16 && 2 * M + (V % 8 != 0) <= 64 ? 2 : 1; }
+
 int vocab_piece(long long M, int C, int V, long long ldw, int wanted, lemo_dtype_t dt) {
     const long long esz = dt == LEMO_BF16 ? 2 : 4, span = (1ll << 31) - 1;
     long long piece = wanted > 0 ? (std::min(wanted, V) + 63) / 64 * 64ll : vl_choice(M, V, (int)esz);
     piece = std::min(piece, vl_pitch(V));
     piece = std::min(piece, span / (ldw * esz) / 64 * 64);       // the piece's rows of W, and
-    piece = std::min(piece, span / ((M + 1) * esz) / 64 * 64);   // G lie within 32-bit offsets,
+    piece = std::min(piece, span / ((vl_parts(M, V, dt) * M + 1) * esz) / 64 * 64);  // G lie within 32-bit offsets,
     piece = std::min(piece, ((8ll << 20) / esz - 64) / 64 * 64); // G's pitch within a load's
     if (piece < 64) return 0;
     if (wanted == 0) piece = std::min(piece, vl_pitch((int)((V + (V + piece - 1) / piece - 1) / ((V + piece - 1) / piece))));  // no small rest
@@ -370,12 +376,13 @@ static int f32_splits(long long M, int C, int K, int* k_part) {
 }
 
 // gradient: rows, G, dX's planes, and in binary32 what is transposed: G, with rows of `rows` to a multiple of 64, or the weight's piece
-struct GradSpace { float* rest; int* rows; char* G; float *planes, *turned; long long ldg, plane_rows; bool turn_G; GgTile tile; int splits, k_split; size_t bytes; };
+struct GradSpace { float* rest; int* rows; char* G; float *planes, *turned; long long ldg, plane_rows; bool turn_G; GgTile tile; int parts, splits, k_split; size_t bytes; };
 static GradSpace grad_space(long long M, int C, int V, int piece, lemo_dtype_t dt, void* base) {
     GradSpace s{};
     s.plane_rows = M;
     const int esz = dt == LEMO_BF16 ? 2 : 4;
     s.ldg = vl_pitch(piece);
+    s.parts = vl_parts(M, V, dt);
     char* at = static_cast<char*>(base);
     auto take = [&](size_t bytes) {
         char* const here = at + s.bytes;
@@ -383,8 +390,8 @@ static GradSpace grad_space(long long M, int C, int V, int piece, lemo_dtype_t d
         return here;
     };
     s.rest = reinterpret_cast<float*>(take((size_t)M * sizeof(float)));
-    s.rows = reinterpret_cast<int*>(take((size_t)(M + 1) * sizeof(int)));
-    s.G = take((size_t)(M + 1) * s.ldg * esz);
+    s.rows = reinterpret_cast<int*>(take((size_t)(s.parts * M + 1) * sizeof(int)));
+    s.G = take((size_t)(s.parts * M + 1) * s.ldg * esz);
     if (dt == LEMO_BF16) {
         // a plane is written and read once for every piece: 8 bytes an element, at 4 TB/s
         s.tile = gg_choose_tile(M, C, std::min(piece, V), GG_NN, 32, (double)M * C * 8e-6 / 4., &s.splits);
@@ -408,12 +415,13 @@ static int grad_piece_bf16(const VocabGradParams& p, const GradSpace& s, const V
     t.A = p.X; t.B = W; t.idx = p.idx; t.lda = p.ldx; t.ldb = p.ldw; t.M = p.M; t.K = p.C; t.N = N;
     t.a_bytes = vl_span(p.S, p.ldx, p.C, 2);
     t.rule = p.rule; t.labels = p.labels; t.v0 = v0; t.lse = p.lse; t.side = side; t.rest = s.rest; t.G = s.G; t.ldg = s.ldg;
-    int rc = launch_vocab_tiles(t, VOCAB_PROBS, gg_choose_tile(p.M, N, p.C, GG_NT, 1, 0., &one), st);
+    const GgTile tile = side.parts == 2 ? GG_T64x128 : gg_choose_tile(p.M, N, p.C, GG_NT, 1, 0., &one);  // (the same for so few rows, and the kernel that has parts)
+    int rc = launch_vocab_tiles(t, VOCAB_PROBS, tile, st);
     if (rc) return rc;
     if (p.dW) {
         VocabTileParams g{};
         g.A = s.G; g.B = p.X; g.idx = s.rows; g.lda = s.ldg; g.ldb = p.ldx; g.M = N; g.N = p.C;
-        g.K = (int)p.M + (N % 8 != 0);
+        g.K = side.parts * (int)p.M + (N % 8 != 0);
         g.Y = static_cast<char*>(p.dW) + v0 * p.lddw * 2; g.ldy = p.lddw;
         g.b_bytes = vl_span(p.S, p.ldx, p.C, 2);
         if (side.uniform != 0.f) {
@@ -471,8 +479,8 @@ int launch_vocab_grad(const VocabGradParams& p, lemo_dtype_t dt, hipStream_t st)
     if (p.M == 0) return p.dW ? launch_zero_matrix(p.dW, p.lddw, C, V, dt, st) : 0;
     if (!p.dX && !p.dW) return 0;
     const GradSpace s = grad_space(p.M, C, V, p.piece, dt, p.workspace);
-    const bool shared = (p.dloss_stride == 0 || p.M == 1) && dt == LEMO_BF16;
-    VocabSide side{p.dloss, p.dloss_stride, !shared ? 0.f : p.rule.hit > 0.f ? 1.f / p.rule.hit : 1.f, s.rows, (int)p.S, V % (16 / esz) != 0};
+    const bool shared = p.dloss_stride == 0 && dt == LEMO_BF16;
+    VocabSide side{p.dloss, p.dloss_stride, !shared ? 0.f : p.rule.hit > 0.f ? 1.f / p.rule.hit : 1.f, s.rows, (int)p.S, V % (16 / esz) != 0, p.dW ? s.parts : 1};
     for (int v0 = 0; v0 < V && rc == 0; v0 += p.piece) {
         const int N = std::min(p.piece, V - v0);
         const char* const W = static_cast<const char*>(p.W) + v0 * p.ldw * esz;

@@ -11,8 +11,10 @@ struct VocabRule {
 };
 
 // What the kernels that form G do beside it, for the products that follow.
-//   rows [M + 1]   the rows of X for the weight's gradient, those without a label replaced by `past`, one past X's end, which the loads' range check
-//             turns into zeros whatever such a row holds.  Entry M is one more of those, and row M of G zeros where the vocabulary does not fill
+//   parts     2: behind the M rows of G stand M more, of what rounding the first has left, which meet the same rows of X in the weight's gradient.  Where both
+//             fit the one slab that its contraction is padded to, so at no product's cost; bf16 only.
+//   rows [parts M + 1]   the rows of X for the weight's gradient, those without a label replaced by `past`, one past X's end, which the loads' range check
+//             turns into zeros whatever such a row holds.  Entry parts M is one more of those, and row parts M of G zeros where the vocabulary does not fill
 //             whole pieces of 16 bytes (zero_row): the last row of G that a product reads is then one of zeros, whose last piece of columns may
 //             end in the operand's middle.
 //   uniform   one gradient for all losses: G is formed for gradients of `uniform` each (1 / (1 - smoothing), which makes the label's share 1), the rest is
@@ -22,7 +24,7 @@ struct VocabSide {
     long long stride;
     float uniform;
     int* rows;           // or null: not the first piece
-    int past, zero_row;
+    int past, zero_row, parts;
 };
 
 // A product of the rows with (a piece of) the head's weight and what is done with a tile of it.  GgParams: A = X [S, C], idx = the kept rows, B = the piece's

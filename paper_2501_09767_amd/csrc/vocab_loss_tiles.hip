@@ -8,6 +8,7 @@
 //                   The largest error is that of the label's element, whose rest dX gets back (vocab_planes_kernel); and one
 //                   gradient for all losses is left out of G and multiplied into the results instead, since its rounding would be the same
 //                   relative error in every label's element (4096 rows, 131072 words, mean: dX and dW 3.0e-3 from 64 bits, so 1.8e-3; their own store alone 1.7e-3).
+//                   Up to 32 rows stand in G in two parts for dW, which few rows' labels would otherwise leave as far off again as its store.
 //   planes          dX = G W over the piece's columns, in binary32: a piece adds to what the pieces before left, and where the
 //                   output has few tiles the contraction is split, with a plane for each part; a kernel of its own rounds their sum once.
 //   the weight's    dW = G^T X[idx], the piece's rows, times what was left out of G, rounded once.
@@ -73,16 +74,18 @@ __device__ __forceinline__ float row_lanes_sum(float v) {
 
 constexpr int vocab_layout(int what) { return what == VOCAB_PLANES ? GG_NN : what == VOCAB_WEIGHT ? GG_TN : GG_NT; }
 
-// rows of bf16 in LDS -> rows of a matrix, whose columns below `cols` (a multiple of 8) are written
-template <typename Tile> __device__ __forceinline__ void store_rows(const char* smem, int wave, int lane, void* to, long long ld, long long m0, long long M, int n0, int cols) {
+// rows of bf16 in LDS -> rows of a matrix, whose columns below `cols` (a multiple of 8) are written.  In two parts (of up to BM / 2 rows): the second half's go behind the first's.
+template <typename Tile> __device__ __forceinline__ void store_rows(const char* smem, int wave, int lane, void* to, long long ld, long long m0, long long M, int n0, int cols, bool two = false) {
     constexpr int LPR = Tile::BN / 8, RPP = 64 / LPR, OWN = Tile::BM / RG_WAVES;  // lanes of a row, rows at a time, rows of a wave
     const int c = lane % LPR * 8;
     if (n0 + c >= cols) return;
 #pragma unroll 4
     for (int k = 0; k < OWN / RPP; ++k) {
         const int row = wave * OWN + k * RPP + lane / LPR;
-        if (m0 + row >= M) continue;
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(to) + (m0 + row) * ld + n0 + c) = *reinterpret_cast<const u32x4*>(smem + row * Tile::PITCH + c * 2);
+        long long m = m0 + (two ? row % (Tile::BM / 2) : row);
+        if (m >= M) continue;
+        if (two && row >= Tile::BM / 2) m += M;
+        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(to) + m * ld + n0 + c) = *reinterpret_cast<const u32x4*>(smem + row * Tile::PITCH + c * 2);
     }
 }
 
@@ -246,10 +249,12 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
     const float inv_cap = capped ? 1.f / p.rule.softcap : 0.f;
     cap_tile<Tile>(p.rule, acc);
     if constexpr (WHAT == VOCAB_PROBS) {
+        const bool two = UA == 1 && p.side.parts == 2;  // (host: up to half the rows of the smallest tile, whose other half holds what rounding has left)
+        constexpr int LEFT = Tile::BM / 2 * Tile::PITCH;
         if (p.side.rows) {
             if (tn == 0 && tid < Tile::BM && m0 + tid < p.M) vocab_list_row(p.rule, p.side, p.labels, p.idx, m0 + tid, p.M);
             if (p.side.zero_row && tm == p.tiles_m - 1 && tid < Tile::BN / 8 && n0 + tid * 8 < p.N)
-                *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.G) + p.M * p.ldg + n0 + tid * 8) = u32x4{0u, 0u, 0u, 0u};
+                *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.G) + p.side.parts * p.M * p.ldg + n0 + tid * 8) = u32x4{0u, 0u, 0u, 0u};
         }
         VocabRow rows[Tile::ROWS];
 #pragma unroll
@@ -260,6 +265,7 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
 #pragma unroll
         for (int i = 0; i < Tile::ROWS; ++i) {
             const int row = Tile::row(wave, lane, i);
+            if (two && row >= Tile::BM / 2) continue;
             const long long m = min(m0 + row, p.M - 1);
             const VocabRow of = rows[i];
             const uint32_t mask = of.counts ? ~0u : 0u;
@@ -278,7 +284,11 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
 #pragma unroll
                     for (int r = 0; r < 4; ++r) g[r] = n0 + c + r < p.N ? g[r] : 0.f;
                 }
-                *reinterpret_cast<uint2*>(to + c * 2) = make_uint2(pack_bf16x2_hw(g[0], g[1]) & mask, pack_bf16x2_hw(g[2], g[3]) & mask);
+                const uint2 v = make_uint2(pack_bf16x2_hw(g[0], g[1]), pack_bf16x2_hw(g[2], g[3]));
+                *reinterpret_cast<uint2*>(to + c * 2) = make_uint2(v.x & mask, v.y & mask);
+                if (two)
+                    *reinterpret_cast<uint2*>(to + LEFT + c * 2) = make_uint2(pack_bf16x2_hw(g[0] - bf16lo_to_f32(v.x), g[1] - bf16hi_to_f32(v.x)) & mask,
+                                                                              pack_bf16x2_hw(g[2] - bf16lo_to_f32(v.y), g[3] - bf16hi_to_f32(v.y)) & mask);
             }
             // the label's element, over what the lane has just written there: few tiles hold one
             const unsigned label = (unsigned)of.label - (unsigned)(p.v0 + n0);
@@ -290,13 +300,15 @@ __global__ __launch_bounds__(RG_THREADS, 1) void vocab_tile_kernel(VocabTilePara
                     const f32x4 v = Tile::at(acc, i, j);
                     const float g = vocab_grad(p.rule, of, at < 2 ? at ? v[1] : v[0] : at == 2 ? v[2] : v[3], true, inv_cap);
                     const uint32_t stored = pack_bf16x2_hw(g, 0.f);
+                    const float left = g - bf16lo_to_f32(stored);
                     *reinterpret_cast<uint16_t*>(to + label * 2) = (uint16_t)stored;
-                    p.rest[m] = g - bf16lo_to_f32(stored);
+                    if (two) *reinterpret_cast<uint16_t*>(to + LEFT + label * 2) = (uint16_t)pack_bf16x2_hw(left, 0.f);
+                    p.rest[m] = left;
                 }
             }
         }
         __syncthreads();
-        store_rows<Tile>(smem, wave, lane, p.G, p.ldg, m0, p.M, n0, (p.N + 7) & ~7);
+        store_rows<Tile>(smem, wave, lane, p.G, p.ldg, m0, p.M, n0, (p.N + 7) & ~7, two);
     }
 }
 

@@ -49,8 +49,9 @@ __device__ __forceinline__ float vocab_grad(const VocabRule& r, const VocabRow& 
 }
 __device__ __forceinline__ void vocab_list_row(const VocabRule& r, const VocabSide& side, const int* labels, const int* idx, long long m, long long M) {
     const int label = labels[m];
-    side.rows[m] = label >= 0 && label < r.V ? idx ? idx[m] : (int)m : side.past;
-    if (m == M - 1) side.rows[M] = side.past;
+    const int row = label >= 0 && label < r.V ? idx ? idx[m] : (int)m : side.past;
+    for (int part = 0; part < side.parts; ++part) side.rows[part * M + m] = row;
+    if (m == M - 1) side.rows[side.parts * M] = side.past;
 }
 
 }  // namespace lemo
