@@ -592,7 +592,8 @@ int lemo_dropout_add_grad(const void* dR, int64_t lddr, int64_t S, const int32_t
  *   once), or NULL for rows 0..M-1 (then M <= S);  labels [M] int32: a row whose label lies outside [0, V) does not count: its loss is 0.
  *   loss, lse [M] float (natural logarithm; lse is there for every row);  total [4] float or NULL: sum of the losses, number of rows that count, their
  *   mean, and 1 / number -- 0, 0, 0, 0 where none counts; the last is what the gradient of the mean takes.
- *   workspace: lemo_vocab_loss_workspace_bytes() bytes, 256-byte aligned.  M == 0: total is written, nothing else.
+ *   workspace: lemo_vocab_loss_workspace_bytes() bytes, 256-byte aligned: of up to 16384 rows 12 bytes for each 128 words, or in binary32 a piece of logits, up to 512 MiB.
+ *   M == 0: total is written, nothing else.
  *   One token: M = 1; -loss is its logarithm of probability.
  *
  * lemo_vocab_loss_grad: from dloss, the gradients of the losses (dloss_stride 1: [M]; 0: one value for all rows, e.g. total + 3), and lse as the forward
@@ -602,8 +603,10 @@ int lemo_dropout_add_grad(const void* dR, int64_t lddr, int64_t S, const int32_t
  *   dX [M, C] row stride lddx (row m is that of token kept_idx[m]: lemo_scatter_grad puts it back), dW [V, C] row stride lddw, both of dtype dt,
  *   overwritten; either may be NULL (a head that is not trained, a first layer).  Rows that do not count get zeros in dX and add nothing to dW, whatever
  *   their rows of X hold.
- *   The vocabulary is worked through `piece` columns at a time (0: this library's choice, about 256 MB of G; rounded up to 64).
- *   workspace: lemo_vocab_loss_grad_workspace_bytes() bytes for the same piece and ldw, 256-byte aligned: a piece of G, and binary32 sums of dX.
+ *   The vocabulary is worked through `piece` columns at a time, rounded up to 64.  0: this library's choice, the columns that 256 MiB of G hold, but no fewer than
+ *   8192 unless G would pass 2 GiB (from 131072 rows in bf16, half as many in fp32); fewer columns take less memory and more time, since dX's sums pass through memory with each piece.
+ *   workspace: lemo_vocab_loss_grad_workspace_bytes() bytes for the same piece and ldw, 256-byte aligned: a piece of G (bf16, up to 32 rows: twice); binary32 sums of dX, M C of
+ *   them or a few times that where the contraction is cut; in binary32 also a transposed copy of the piece of G or of its rows of W, whichever is smaller.
  *   M == 0 writes zeros to dW.
  *
  * Sums in binary32 (of the losses in 64 bits), over the whole vocabulary and all rows before they are rounded once; in bf16 G is rounded to bf16 for

@@ -1202,7 +1202,7 @@ def lemo_vocab_loss_grad(dloss: torch.Tensor, X: torch.Tensor, kept_idx: Optiona
                          softcap: float = 0.0, smoothing: float = 0.0, z_weight: float = 0.0, want_dX: bool = True, want_dW: bool = True,
                          dX: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None, piece: int = 0, workspace: Optional[torch.Tensor] = None):
     """Gradients of lemo_vocab_loss from dloss [M], or one value for all rows [1] (the mean's: total[3:]) -> (dX [M,C], dW [V,C]), either None if not
-    wanted.  piece: columns of the vocabulary at a time."""
+    wanted.  piece: columns of the vocabulary at a time (0: 256 MiB of G, or 8192 columns where that is more): fewer take less memory and more time."""
     done = _native.vocab_loss_grad(dloss, X, kept_idx, W, labels, lse, softcap, smoothing, z_weight, want_dX, want_dW, dX, dW, piece, workspace)
     if done is not None:
         _check(done[0], "lemo_vocab_loss_grad")
