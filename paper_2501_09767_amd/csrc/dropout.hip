@@ -44,19 +44,20 @@ __global__ __launch_bounds__(DO_THREADS) void dropout_kernel(DropoutParams p) {
     if (!GRAD && !there) return;
     const unsigned long long seed = p.rng[0], stream = p.rng[1] + p.site;
     const long long from = (GRAD ? row : m) * p.ldx, to = (GRAD ? m : row) * p.ldy;
-    for (int c = threadIdx.x % per_row * 8; c < p.C; c += per_row * 8) {
+    const unsigned C = (unsigned)p.C;
+    for (unsigned c = threadIdx.x % per_row * 8; c < C; c += per_row * 8) {  // (rows of up to 2^31 - 8 columns: a step past them is below 2^32)
         u32x4 in[NP], old[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             in[i] = old[i] = u32x4{0u, 0u, 0u, 0u};
-            if (c + i * E >= p.C) continue;
+            if (c + i * E >= C) continue;
             if (there) in[i] = row_load<T>(p.X, from + c + i * E);
             if (!GRAD) old[i] = row_load<T>(p.Y, to + c + i * E);
         }
-        const Philox bits = philox((unsigned)c / 8, (unsigned)row, stream, seed);
+        const Philox bits = philox(c / 8, (unsigned)row, stream, seed);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            if (c + i * E >= p.C) continue;
+            if (c + i * E >= C) continue;
             float x[E], y[E];
             RowPiece<T>::get(in[i], x);
             RowPiece<T>::get(old[i], y);
