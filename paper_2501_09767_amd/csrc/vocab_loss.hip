@@ -9,8 +9,8 @@
 // logits once more, turned into G, then its rows of dW (finished: every token is in them) and its part of dX, which is added up in
 // binary32 over the pieces and rounded once.  No atomics: the same bits on every run.
 //
-// What bounds it: the matrix cores, 2 M C V products forward and 6 in the gradients (8192 rows of 4096, 131072 words, bf16: loss 6.1 ms, 1.43 PFLOP/s; 777 rows
-// of 768, 50001 words, binary32: gradients 1.21 ms, 148 TFLOP/s of a library product's 154); with few rows the weight's bytes (16 rows of 4096,
+// What bounds it: the matrix cores, 2 M C V products forward and 6 in the gradients (8192 rows of 4096, 131072 words, bf16: loss 6.1 to 6.3 ms by
+// the card, 1.40 to 1.44 PFLOP/s; 777 rows of 768, 50001 words, binary32: gradients 1.21 to 1.28 ms, 140 to 148 TFLOP/s of a library product's 154); with few rows the weight's bytes (16 rows of 4096,
 // 32000 words, bf16: loss 61 us = 4.3 TB/s).  Keeping G of the whole vocabulary would save a piece's tail and the additions to dX, and is what
 // the operator is there to avoid.
 //

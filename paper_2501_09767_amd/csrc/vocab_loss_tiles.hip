@@ -14,7 +14,7 @@
 //   the weight's    dW = G^T X[idx], the piece's rows, times what was left out of G, rounded once.
 //
 // What bounds it: the matrix cores, as in gather_gemm_large.hip; the epilogues read no memory but a few bytes a row.  8192 rows, 4096 columns, 131072 words:
-// statistics 6.1 ms, 1.43 PFLOP/s, matrix cores busy for 75 % of the cycles; the gradients of 4096 rows 9.7 ms, 1.36 (probabilities 69 %, planes 73 %,
+// statistics 6.1 to 6.3 ms by the card, 1.40 to 1.44 PFLOP/s, matrix cores busy for 75 % of the cycles; the gradients of 4096 rows 9.6 to 10.0 ms, 1.32 to 1.37 (probabilities 69 %, planes 73 %,
 // the weight's 64 %).  Narrow rows are few slabs a tile, whose epilogue nothing overlaps: 256 columns take 1.75 times the products' time, the gradients 2.4.
 #include "gather_gemm_tiles.hpp"
 #include "vocab_softmax.hpp"
