@@ -10,8 +10,8 @@
 // a head is d / 2 channels' worth of lanes and nothing but the sums of the norm crosses lanes (by DPP).  cos and sin are formed once for a
 // token and stand in LDS, in the order in which the lanes want them.  Angles are taken in revolutions in binary64: the product of a position with a
 // frequency, and that with 1 / (2 pi), each in two parts, so that what is left after whole revolutions is off by 2^-53 whatever their number.  What binary32 leaves of that, as
-// much as sincospif's own error, turns the result on to first order.  cos and sin are off by 1.2 * 2^-24 at any position up to 2^32 (one product with a rounded frequency in
-// revolutions, then binary32: 1.7 near, 10.8 far; 32768 tokens, 32 + 8 heads, bf16: 1 to 2 % less time).
+// much as sincospif's own error, turns the result on to first order.  cos and sin are off by 1.4 * 2^-24 at any position up to 2^32 (one product with a rounded frequency in
+// revolutions, then binary32: 1.9 near, 10.8 far; 32768 tokens, 32 + 8 heads, bf16: up to 2 % less time).
 //
 // Measured: 32768 tokens, 32 + 8 heads of 128, bf16, 671 MB: 139 us = 4.8 TB/s; the gradient of 8192, 403 MB: 83 us; a single token's step: 5.6 us, its launch.
 #include <algorithm>
@@ -42,7 +42,9 @@ template <int E> __device__ __forceinline__ float2 turn_of(const float* inv_freq
     const int f = !pairs ? j * E + e : e < E / 2 ? j * (E / 2) + e : (rp + j) * (E / 2) + e - E / 2;
     const double x = (double)position, y = (double)inv_freq[f], angle = x * y, angle_left = fma(x, y, -angle);
     constexpr double PER = 0.15915494309189535, PER_LEFT = -9.839338337591243e-18;  // 1 / (2 pi)
-    const double half = 2.0 * (fma(angle, PER, -rint(angle * PER)) + fma(angle, PER_LEFT, angle_left * PER));  // half turns
+    double part = fma(angle, PER, -rint(angle * PER)) + fma(angle, PER_LEFT, angle_left * PER);
+    part -= rint(part);  // (more than half a revolution where their number passes 2^52)
+    const double half = 2.0 * part;  // half turns
     const float h = (float)half, left = (float)((half - (double)h) * 3.141592653589793);
     float s, c;
     sincospif(h, &s, &c);

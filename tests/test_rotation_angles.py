@@ -57,3 +57,21 @@ def test_far_positions_are_as_exact_as_near_ones(far, start, pairs):
     worst = [(x - want).abs().max().item() * 2 ** 24 for x, want in ((y[:, first], angle.cos()), (y[:, second], angle.sin()), (back[:, first], angle.cos()), (back[:, second], -angle.sin()))]
     print(f"positions to {far} + {start}: {worst} of 2^-24", flush=True)
     assert max(worst) <= BOUND * 2 ** 24
+
+
+@pytest.mark.gpu
+def test_numbers_of_turns_that_pass_binary64():
+    """Frequencies that no model has: exact up to 2^62 turns, beyond that still a rotation."""
+    pos = places(2 ** 31)
+    f = torch.tensor([1e7, 3e7, 1e9, 123456789.0, 8.5e8, 2.0 ** 30, 2.0 ** 30 + 64, 7e8], dtype=torch.float32)
+    angle = torch.tensor([[turns(p, x) for x in f.tolist()] for p in pos], dtype=torch.float64)
+    ones = torch.zeros(len(pos), 1, 64)
+    ones[:, 0, :8] = 1.0
+    at = torch.tensor(pos, dtype=torch.int32).cuda()
+    y = lemo.lemo_qk_rotate(ones.cuda(), None, f.cuda(), at, norm=lemo.NORM_NONE)[0].double().cpu()[:, 0]
+    worst = max((y[:, :8] - angle.cos()).abs().max().item(), (y[:, 8:16] - angle.sin()).abs().max().item())
+    print(f"{worst * 2 ** 24} of 2^-24", flush=True)
+    assert worst <= BOUND
+    far_off = torch.tensor([1e12, 1e20, 1e30, 3e38] * 2, dtype=torch.float32)
+    y = lemo.lemo_qk_rotate(ones.cuda(), None, far_off.cuda(), at, norm=lemo.NORM_NONE)[0].double().cpu()[:, 0]
+    assert ((y[:, :8] ** 2 + y[:, 8:16] ** 2 - 1).abs() <= 4 * BOUND).all()
